@@ -22,15 +22,20 @@
  * qf_decode_step_host (one step from host buffers; qf_host_pipe_* the same,
  * pipelined), qf_project_pair (the
  * cache side's W_o / W_q projections at a layer boundary, Section 4),
- * qf_enable_peer_access (a request's cache split over GPUs, Section 5).
+ * qf_enable_peer_access (a request's cache split over GPUs, Section 5).  Before
+ * decoding, and beside it: qf_rope_append (norms, rotary positions and the cache
+ * write of packed tokens), qf_prompt_attend (causal attention of whole prompts or
+ * chunks of them over the paged cache), qf_prefix_partial and qf_prefix_step (a
+ * prefix that several requests share, swept once for all of them).
  *
  * Readings fixed at this boundary where the paper is silent:
  *   - grouped-query attention: query head h reads KV head h / G, G = Hq/Hkv;
  *   - the sweep covers cached positions [0, seq_lens[b]) only; the current
  *     token's own key/value are merged elsewhere (Section 2, the accelerator's
  *     combine) and are not part of these calls;
- *   - no causal mask, rotary embedding or normalisation inside the kernels:
- *     q and the cached keys arrive ready to be multiplied;
+ *   - no causal mask, rotary embedding or normalisation inside the sweep:
+ *     q and the cached keys arrive ready to be multiplied (qf_rope_append makes
+ *     them so);
  *   - natural logarithm; the scale multiplies the finished fp32 dot product;
  *   - o_part is the shard-NORMALISED O(S); m_part is the running maximum
  *     score (auxiliary: W relative to m is o_part * e^{lse_part - m_part});
@@ -297,6 +302,120 @@ int qf_fold_append(const float *o_part, const float *lse_part, const int32_t *sh
                    int32_t *seq_lens, int advance_lengths,
                    const qf_params *p, void *cuda_stream);
 
+
+/*
+ * Rotary frequencies, on the host: inv_freq[i], i < rotary_dim / 2, for the pairs of a head's first rotary_dim
+ * channels, and the factor rot_scale that multiplies every sine and cosine (qf_rope_params.rot_scale):
+ *   QF_ROPE_PLAIN    theta^(-2i/rotary_dim)
+ *   QF_ROPE_LINEAR   the same, divided by `factor` (positions interpolated)
+ *   QF_ROPE_NTK      theta replaced by theta * factor^(d/(d-2)), d = rotary_dim
+ *   QF_ROPE_YARN     pairs that turn more than beta_fast times over original_len positions are left alone, pairs
+ *                    that turn less than beta_slow times are divided by `factor`, linearly between;
+ *                    rot_scale = 0.1 ln(factor) + 1 (Peng et al., "YaRN", 2023; 32 and 1 are its betas)
+ * Computed in double, rounded once to float.  original_len and the betas are read for QF_ROPE_YARN only.
+ * Touches no GPU.  rotary_dim: a positive multiple of 16, at most 128; theta > 1; factor >= 1.
+ */
+enum { QF_ROPE_PLAIN = 0, QF_ROPE_LINEAR = 1, QF_ROPE_NTK = 2, QF_ROPE_YARN = 3 };
+int qf_rope_frequencies(float *inv_freq_host, float *rot_scale, int rotary_dim, double theta, int scaling,
+                        double factor, double original_len, double beta_fast, double beta_slow);
+
+/*
+ * Placing packed tokens: one pass over the projections' output that makes queries and keys ready to be multiplied
+ * and writes keys and values into the cache.  Rows cu_tokens[b] .. cu_tokens[b+1]-1 belong to request b
+ * (int32 [B+1], non-decreasing; 1 row each = a decode step, thousands = prompts); its i-th row goes to cache
+ * position seq_lens[b] + i and has rotary position seq_lens[b] + i + pos_base[b] (pos_base NULL = 0; requests behind
+ * a shared prefix pass its length).  Per head row x of q and k:
+ *     y = x / sqrt(mean x^2 + eps) * gain        (bf16 [128] gains; NULL = no norm)
+ *     (y_a, y_b) -> rot_scale * (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = rotary position * inv_freq[j]
+ * for the pairs j < rotary_dim / 2 of the first rotary_dim channels: (j, j + rotary_dim/2), or (2j, 2j+1) with
+ * `interleaved`; the other channels pass.  The angle is formed and reduced in double; the rest is fp32 with ONE
+ * rounding to bf16 at the end; without norm and rotation a row passes bit for bit.
+ *   q, k, v  bf16, a token's rows *_stride elements apart (0 = packed; else a multiple of 8 of at least heads * 128):
+ *            slices of one fused projection can be passed as they are
+ *   q_out    bf16 [total_tokens, Hq, 128] (may be q itself when q is packed)
+ *   k_out    bf16 [total_tokens, Hkv, 128] or NULL: the finished keys too (what qf_combine_self, qf_fold_append take)
+ *   inv_freq fp32 [rotary_dim / 2] (device; see qf_rope_frequencies); rotary_dim a multiple of 16 up to 128, 0 = none
+ * q may be NULL (keys and values only) and so may k and v (queries only, Section 2: the query travels first).  The
+ * cache pointers are both given (then k and v are needed) or both NULL (then k needs k_out and v is ignored).  A
+ * position without a page (beyond the table row, or a table entry outside the pool) stores nothing in the cache;
+ * rows that belong to no request (before cu_tokens[0], from cu_tokens[B] on) are not touched.  seq_lens is not
+ * modified.  All other pointers are device pointers, 16-byte aligned where they are bf16.  One launch.
+ */
+typedef struct qf_rope_params {
+    int32_t total_tokens;      /* packed rows in q, k, v                                          */
+    int32_t rotary_dim;        /* channels that turn: 0 or a multiple of 16, at most 128          */
+    int32_t interleaved;       /* 0: pairs (j, j + rotary_dim/2); else pairs (2j, 2j+1)           */
+    float   eps;               /* of the norms                                                    */
+    float   rot_scale;         /* multiplies every sine and cosine (1 = plain)                    */
+    int32_t reserved;          /* 0                                                               */
+    int64_t q_stride, k_stride, v_stride;   /* elements between a token's rows; 0 = packed        */
+} qf_rope_params;
+int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, void *k_out,
+                   void *k_cache, void *v_cache, const int32_t *block_table,
+                   const int32_t *cu_tokens, const int32_t *seq_lens, const int32_t *pos_base,
+                   const void *q_gain, const void *k_gain, const float *inv_freq,
+                   const qf_params *p, const qf_rope_params *r, void *cuda_stream);
+
+/*
+ * Attention over whole prompts: the rows cu_tokens[b] .. cu_tokens[b+1]-1 of q (packed as for qf_rope_append, same
+ * seq_lens: positions cached BEFORE them) attend the paged cache, which already holds their own keys and values:
+ * row i of request b sees positions 0 .. seq_lens[b] + i.  An empty cache (seq_lens 0) is a whole prompt, a filled
+ * one a later chunk of it; one-row requests are decode steps riding along.
+ *     out bf16 [total_tokens, Hq, 128] (one rounding, of the fp32 result),  lse fp32 [total_tokens, Hq]
+ * The weights that multiply the values are rounded to bf16 (out is bf16: their errors average out below its own
+ * rounding); scores, maxima, sums and accumulators are fp32.  q: bf16, rows q_stride elements apart (0 = packed).
+ * Rows that belong to no request are left as they were.  A table entry outside [0, num_pages) contributes nothing
+ * (reported under QF_FLAG_CHECK_BOUNDS); positions beyond the table row are not attended.  Values at positions a
+ * row does not see never reach its result, NaN and infinities included.  p->max_shards is not used (pass 1).
+ * k_cache, v_cache 128-byte, q and out 16-byte aligned.  workspace: qf_prompt_workspace_bytes bytes, 256-byte
+ * aligned, contents need not be initialised; one call at a time.  Results do not depend on what ran before: the
+ * schedule, and so the order of every sum, follows from the lengths alone.
+ */
+size_t qf_prompt_workspace_bytes(const qf_params *p, int total_tokens);
+int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
+                     const int32_t *cu_tokens, const int32_t *seq_lens, void *out, float *lse,
+                     const qf_params *p, int total_tokens, int64_t q_stride,
+                     void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Status bits (QF_STATUS_*) raised by calls on this workspace since the last read; reads, clears and synchronises
+ * the stream.
+ */
+int qf_prompt_status(const void *workspace, int32_t *host_status, void *cuda_stream);
+
+/*
+ * A prefix that several requests share, swept ONCE for all of them (Section 5: states of disjoint token sets merge,
+ * so the prefix is one more shard of every request).  Requests group_offsets[g] .. group_offsets[g+1]-1 (int32
+ * [num_groups + 1], non-decreasing) share the pages prefix_table[g, :] (int32 [num_groups, max_prefix_pages], NULL =
+ * identity) holding prefix_lens[g] tokens.  Writes the state (O, running maximum, log Z) of every request and query
+ * head over its group's prefix into slot p->out_shard_offset of o_part [B, out_shards, Hq, 128], m_part, lse_part
+ * (out_shards = p->out_shards, or p->max_shards when that is 0), exactly as qf_decode_partial would write a shard;
+ * requests of no group and empty prefixes get (0, -inf, -inf).  Other slots are not touched.  num_groups <= B.
+ * fp32 throughout: the weights enter the value product as two bf16 terms (16 bits).
+ * prefix_lens beyond the table row are clamped to it.  Errors, bounds, alignment as for qf_decode_partial;
+ * workspace: qf_prefix_workspace_bytes bytes, one call at a time.
+ */
+size_t qf_prefix_workspace_bytes(const qf_params *p);
+int qf_prefix_partial(const void *q, const void *k_cache, const void *v_cache, const int32_t *prefix_table,
+                      const int32_t *prefix_lens, const int32_t *group_offsets,
+                      float *o_part, float *m_part, float *lse_part,
+                      const qf_params *p, int num_groups, int max_prefix_pages,
+                      void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * One decode step behind shared prefixes: qf_prefix_partial into slot 0, qf_decode_partial of every request's own
+ * pages (block_table, seq_lens, shard_ranges: p->max_shards shards, positions counted after the prefix) into slots
+ * 1 .. max_shards, and qf_combine over all of them.  o_part [B, max_shards + 1, Hq, 128], m_part, lse_part
+ * [B, max_shards + 1, Hq]; out [B, Hq, 128], lse [B, Hq] over prefix and own tokens.  p->out_shards must be 0.
+ * qf_prefix_status reads both sweeps' status (cleared, for the prefix, by reading) and synchronises the stream.
+ */
+int qf_prefix_step(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
+                   const int32_t *seq_lens, const int32_t *shard_ranges, const int32_t *prefix_table,
+                   const int32_t *prefix_lens, const int32_t *group_offsets,
+                   float *o_part, float *m_part, float *lse_part, float *out, float *lse,
+                   const qf_params *p, int num_groups, int max_prefix_pages,
+                   void *workspace, size_t workspace_bytes, void *cuda_stream);
+int qf_prefix_status(const void *workspace, const qf_params *p, int32_t *host_status, void *cuda_stream);
 
 /*
  * Section 4 (placement: W_q and W_o live with the cache) and the appendix

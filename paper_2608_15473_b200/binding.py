@@ -46,6 +46,8 @@ EXPORTS = (
     "qf_static_scratch_status", "qf_project_status_inject", "qf_enable_peer_access", "qf_decode_step",
     "qf_host_pipe_scratch_bytes", "qf_host_pipe_create", "qf_host_pipe_submit", "qf_host_pipe_wait",
     "qf_host_pipe_destroy",
+    "qf_rope_frequencies", "qf_rope_append", "qf_prompt_workspace_bytes", "qf_prompt_attend", "qf_prompt_status",
+    "qf_prefix_workspace_bytes", "qf_prefix_partial", "qf_prefix_step", "qf_prefix_status",
 )
 
 
@@ -65,6 +67,23 @@ class QFParams(ctypes.Structure):
         ("out_shard_offset", ctypes.c_int32),
         ("max_seq_len", ctypes.c_int32),
     ]
+
+
+class QFRopeParams(ctypes.Structure):
+    _fields_ = [
+        ("total_tokens", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("rot_scale", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+        ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
+    ]
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
 class QFError(RuntimeError):
@@ -143,6 +162,29 @@ def lib() -> ctypes.CDLL:
         L.qf_project_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32), vp]
         L.qf_plan_pieces.restype = ctypes.c_int
         L.qf_plan_pieces.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int, i32p, i32p, ctypes.c_int]
+        rp = ctypes.POINTER(QFRopeParams)
+        dbl = ctypes.c_double
+        L.qf_rope_frequencies.restype = ctypes.c_int
+        L.qf_rope_frequencies.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.c_int, dbl, ctypes.c_int, dbl, dbl, dbl, dbl]
+        L.qf_rope_append.restype = ctypes.c_int
+        L.qf_rope_append.argtypes = [vp] * 7 + [i32p] * 4 + [vp] * 3 + [pp, rp, vp]
+        L.qf_prompt_workspace_bytes.restype = ctypes.c_size_t
+        L.qf_prompt_workspace_bytes.argtypes = [pp, ctypes.c_int]
+        L.qf_prompt_attend.restype = ctypes.c_int
+        L.qf_prompt_attend.argtypes = [vp, vp, vp, i32p, i32p, i32p, vp, vp, pp, ctypes.c_int, ctypes.c_int64, vp,
+                                       ctypes.c_size_t, vp]
+        L.qf_prompt_status.restype = ctypes.c_int
+        L.qf_prompt_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32), vp]
+        L.qf_prefix_workspace_bytes.restype = ctypes.c_size_t
+        L.qf_prefix_workspace_bytes.argtypes = [pp]
+        L.qf_prefix_partial.restype = ctypes.c_int
+        L.qf_prefix_partial.argtypes = [vp, vp, vp, i32p, i32p, i32p, vp, vp, vp, pp, ctypes.c_int, ctypes.c_int, vp,
+                                        ctypes.c_size_t, vp]
+        L.qf_prefix_step.restype = ctypes.c_int
+        L.qf_prefix_step.argtypes = [vp, vp, vp, i32p, i32p, i32p, i32p, i32p, i32p, vp, vp, vp, vp, vp, pp,
+                                     ctypes.c_int, ctypes.c_int, vp, ctypes.c_size_t, vp]
+        L.qf_prefix_status.restype = ctypes.c_int
+        L.qf_prefix_status.argtypes = [vp, pp, ctypes.POINTER(ctypes.c_int32), vp]
         _lib = L
     return _lib
 
@@ -372,6 +414,115 @@ def project_status(workspace, stream=None) -> int:
     rc = lib().qf_project_status(_ptr(workspace), ctypes.byref(st), _stream(stream))
     if rc != QF_OK:
         raise QFError(rc, "qf_project_status")
+    return int(st.value)
+
+
+def _on_current_device(*tensors) -> None:
+    """The calls below launch on the current device: a tensor of another one is refused, not dereferenced there."""
+    import torch
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    for x in tensors:
+        dev = getattr(x, "device", None)
+        if dev is not None and (dev.type != "cuda" or (here is not None and dev.index != here)):
+            raise ValueError(f"expected a tensor on the current CUDA device ({here}), got one on {dev}")
+
+
+def rope_frequencies(rotary_dim: int = 128, theta: float = 1e6, scaling: str = "plain", factor: float = 1.0,
+                     original_len: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(inverse frequencies as a float32 array [rotary_dim / 2], factor of every sine and cosine).  Host arithmetic:
+    no GPU is touched."""
+    import numpy as np
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}, not {scaling!r}")
+    inv, scale = np.zeros(max(int(rotary_dim), 2) // 2, np.float32), ctypes.c_float(0)
+    rc = lib().qf_rope_frequencies(inv.ctypes.data, ctypes.byref(scale), int(rotary_dim), float(theta),
+                                   ROPE_SCALINGS[scaling], float(factor), float(original_len), float(beta_fast),
+                                   float(beta_slow))
+    if rc != QF_OK:
+        raise QFError(rc, "qf_rope_frequencies")
+    return inv, float(scale.value)
+
+
+def rope_params(total_tokens: int, rotary_dim: int = 128, interleaved: bool = False, eps: float = 1e-6,
+                rot_scale: float = 1.0, q_stride: int = 0, k_stride: int = 0, v_stride: int = 0) -> QFRopeParams:
+    return QFRopeParams(total_tokens, rotary_dim, 1 if interleaved else 0, eps, rot_scale, 0, q_stride, k_stride, v_stride)
+
+
+def rope_append(q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base, q_gain, k_gain,
+                inv_freq, p: QFParams, r: QFRopeParams, stream=None, check: bool = True) -> int:
+    """Norms, rotary positions and the cache write of packed tokens in one launch; any of q, (k, v), k_out, the
+    caches, pos_base and the gains may be None (see qf_rope_append)."""
+    _on_current_device(q, k, v, q_out, k_out, k_cache, v_cache)
+    rc = lib().qf_rope_append(_ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(k_out), _ptr(k_cache), _ptr(v_cache),
+                              _ptr(block_table), _ptr(cu_tokens), _ptr(seq_lens), _ptr(pos_base), _ptr(q_gain),
+                              _ptr(k_gain), _ptr(inv_freq), ctypes.byref(p), ctypes.byref(r), _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_rope_append")
+    return rc
+
+
+def prompt_workspace_bytes(p: QFParams, total_tokens: int) -> int:
+    return int(lib().qf_prompt_workspace_bytes(ctypes.byref(p), int(total_tokens)))
+
+
+def prompt_attend(q, k_cache, v_cache, block_table, cu_tokens, seq_lens, out, lse, p: QFParams, total_tokens: int,
+                  workspace, workspace_bytes: int, q_stride: int = 0, stream=None, check: bool = True) -> int:
+    """Causal attention of packed prompt rows over the paged cache that already holds their keys and values."""
+    _on_current_device(q, k_cache, v_cache, out, lse, workspace)
+    rc = lib().qf_prompt_attend(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(cu_tokens),
+                                _ptr(seq_lens), _ptr(out), _ptr(lse), ctypes.byref(p), int(total_tokens),
+                                int(q_stride), _ptr(workspace), int(workspace_bytes), _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_prompt_attend")
+    return rc
+
+
+def prompt_status(workspace, stream=None) -> int:
+    st = ctypes.c_int32(0)
+    rc = lib().qf_prompt_status(_ptr(workspace), ctypes.byref(st), _stream(stream))
+    if rc != QF_OK:
+        raise QFError(rc, "qf_prompt_status")
+    return int(st.value)
+
+
+def prefix_workspace_bytes(p: QFParams) -> int:
+    return int(lib().qf_prefix_workspace_bytes(ctypes.byref(p)))
+
+
+def prefix_partial(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, o_part, m_part, lse_part,
+                   p: QFParams, num_groups: int, max_prefix_pages: int, workspace, workspace_bytes: int, stream=None,
+                   check: bool = True) -> int:
+    """States of every request over its group's shared prefix, each prefix swept once."""
+    _on_current_device(q, k_cache, v_cache, o_part, m_part, lse_part, workspace)
+    rc = lib().qf_prefix_partial(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(prefix_table), _ptr(prefix_lens),
+                                 _ptr(group_offsets), _ptr(o_part), _ptr(m_part), _ptr(lse_part), ctypes.byref(p),
+                                 int(num_groups), int(max_prefix_pages), _ptr(workspace), int(workspace_bytes),
+                                 _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_prefix_partial")
+    return rc
+
+
+def prefix_step(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, prefix_table, prefix_lens, group_offsets,
+                o_part, m_part, lse_part, out, lse, p: QFParams, num_groups: int, max_prefix_pages: int, workspace,
+                workspace_bytes: int, stream=None, check: bool = True) -> int:
+    """One decode step behind shared prefixes: prefix sweep, own pages' sweep and the merge of both."""
+    _on_current_device(q, k_cache, v_cache, o_part, m_part, lse_part, out, lse, workspace)
+    rc = lib().qf_prefix_step(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens),
+                              _ptr(shard_ranges), _ptr(prefix_table), _ptr(prefix_lens), _ptr(group_offsets),
+                              _ptr(o_part), _ptr(m_part), _ptr(lse_part), _ptr(out), _ptr(lse), ctypes.byref(p),
+                              int(num_groups), int(max_prefix_pages), _ptr(workspace), int(workspace_bytes),
+                              _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_prefix_step")
+    return rc
+
+
+def prefix_status(workspace, p: QFParams, stream=None) -> int:
+    st = ctypes.c_int32(0)
+    rc = lib().qf_prefix_status(_ptr(workspace), ctypes.byref(p), ctypes.byref(st), _stream(stream))
+    if rc != QF_OK:
+        raise QFError(rc, "qf_prefix_status")
     return int(st.value)
 
 

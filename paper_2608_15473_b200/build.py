@@ -9,8 +9,8 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libqf.so"
-SOURCES = [CSRC / "qf_api.cu", CSRC / "qf_static_scratch.cu"]
-HEADERS = sorted(CSRC.glob("*.cuh")) + [PKG.parent / "include" / "qf.h"]
+SOURCES = [CSRC / "qf_api.cu", CSRC / "qf_static_scratch.cu", CSRC / "qf_prompt.cu"]
+HEADERS = sorted(CSRC.glob("*.cuh")) + sorted(CSRC.glob("*.h")) + sorted((PKG.parent / "include").glob("*.h"))
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -36,7 +36,7 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     if not force and not stale():
         return LIB
     tmp = LIB.with_suffix(f".so.tmp{os.getpid()}")
-    cmd = [_nvcc(), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []),
+    cmd = [_nvcc(), *NVCC_FLAGS, "--threads", str(len(SOURCES)), *(["-Xptxas", "-v"] if verbose else []),
            *[str(s) for s in SOURCES], "-o", str(tmp)]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or res.returncode:

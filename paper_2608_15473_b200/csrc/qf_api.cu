@@ -12,6 +12,7 @@
 #include "../../include/qf_testing.h"
 #include "qf_combine.cuh"
 #include "qf_common.cuh"
+#include "qf_host.h"
 #include "qf_proj.cuh"
 #include "qf_simple.cuh"
 #include "qf_sweep.cuh"
@@ -116,6 +117,16 @@ int launch_simple(const void *q, const void *k, const void *v, const int32_t *bt
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
+
+// The helpers above, for the boundary's other translation unit (qf_prompt.cu).
+namespace qf_host {
+int validate(const qf_params *p) { return ::validate(p); }
+qf::DevParams dev_params(const qf_params *p) { return ::dev_params(p); }
+int check_device(int *sm_count) { return ::check_device(sm_count); }
+int cuda_fail(cudaError_t e, const char *what) { return ::cuda_fail(e, what); }
+char *cuda_msg(size_t *len) { *len = sizeof g_cuda_msg; return g_cuda_msg; }
+void set_launches(int n) { g_last_launches = n; }
+}  // namespace qf_host
 
 extern "C" {
 
