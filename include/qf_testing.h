@@ -83,6 +83,17 @@ int qf_set_profile_events(void *start_event, void *stop_event);
  */
 int qf_project_status_inject(void *workspace, int32_t bits, void *cuda_stream);
 
+/*
+ * The schedule of qf_prompt_attend (causal != 0) and qf_prefix_partial for n_ctas CTAs, from host copies of the
+ * offsets and lengths: one record of 12 int32 per stretch of a block,
+ *     cta, sequence, KV head, first row, rows, first tile, end tile, slot (-1 = the whole block), narrow,
+ *     positions before the block's first row, positions in all, first tile's running number within the CTA
+ * in the order in which each CTA takes them.  Returns their number (records beyond `capacity` are counted, not
+ * stored) or a negative code.  Host arithmetic only: no GPU is touched.
+ */
+int qf_rows_schedule(int causal, const int32_t *offsets, const int32_t *lens, int n_seq, int group, int num_kv_heads,
+                     int max_tokens, int total_rows, int n_ctas, int32_t *records, int capacity);
+
 #ifdef __cplusplus
 }
 #endif

@@ -48,6 +48,7 @@ EXPORTS = (
     "qf_host_pipe_destroy",
     "qf_rope_frequencies", "qf_rope_append", "qf_prompt_workspace_bytes", "qf_prompt_attend", "qf_prompt_status",
     "qf_prefix_workspace_bytes", "qf_prefix_partial", "qf_prefix_step", "qf_prefix_status",
+    "qf_rows_schedule",
 )
 
 
@@ -185,6 +186,8 @@ def lib() -> ctypes.CDLL:
                                      ctypes.c_int, ctypes.c_int, vp, ctypes.c_size_t, vp]
         L.qf_prefix_status.restype = ctypes.c_int
         L.qf_prefix_status.argtypes = [vp, pp, ctypes.POINTER(ctypes.c_int32), vp]
+        L.qf_rows_schedule.restype = ctypes.c_int
+        L.qf_rows_schedule.argtypes = [ctypes.c_int, i32p, i32p] + [ctypes.c_int] * 6 + [i32p, ctypes.c_int]
         _lib = L
     return _lib
 
@@ -536,6 +539,24 @@ def plan_pieces(total_units: int, n_ctas: int, draw_always: bool = False):
     if n < 0:
         raise QFError(n, "qf_plan_pieces")
     return [(int(b[i]), int(e[i])) for i in range(n)]
+
+
+def rows_schedule(causal: bool, offsets, lens, group: int, num_kv_heads: int, max_tokens: int, n_ctas: int):
+    """The schedule of prompt_attend / prefix_partial as an int32 array [stretches, 12] (see qf_testing.h).  Host
+    arithmetic only: no GPU is touched."""
+    import numpy as np
+    off, ln = np.ascontiguousarray(offsets, np.int32), np.ascontiguousarray(lens, np.int32)
+    cap = 1 << 12
+    while True:
+        rec = np.zeros((cap, 12), np.int32)
+        n = lib().qf_rows_schedule(int(bool(causal)), off.ctypes.data, ln.ctypes.data, len(ln), int(group),
+                                   int(num_kv_heads), int(max_tokens), max(int(off.max()), 1), int(n_ctas),
+                                   rec.ctypes.data, cap)
+        if n < 0:
+            raise QFError(n, "qf_rows_schedule")
+        if n <= cap:
+            return rec[:n]
+        cap = n
 
 
 def read_status(workspace, stream=None) -> int:

@@ -12,7 +12,7 @@
 #include "qf_common.cuh"
 #include "qf_host.h"
 #include "qf_rope.cuh"
-#include "qf_rows_simple.cuh"
+#include "qf_rows.cuh"
 
 namespace {
 
@@ -22,23 +22,26 @@ bool misaligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0;
 // A token row stride in elements: 0 = the packed width; rows must start on 16 bytes and not overlap.
 bool bad_stride(int64_t stride, long long width) { return stride != 0 && (stride < width || (stride & 7)); }
 
-struct RowsLayout { size_t total; };
-RowsLayout rows_layout()
-{
-    RowsLayout L;
-    L.total = 256;
-    return L;
-}
-
 template <bool PREFIX>
-int launch_rows(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *p, cudaStream_t st)
+int launch_rows(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *p, char *ws, int sms, cudaStream_t st)
 {
-    const long long units = (long long)A.total_rows * P.num_q_heads;
-    const unsigned blocks = (unsigned)((units + qf::kRowsSimpleWarps - 1) / qf::kRowsSimpleWarps);
-    qf::rows_simple_kernel<PREFIX><<<blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return qf_host::cuda_fail(e, "rows_simple_kernel launch");
-    qf_host::set_launches(1);
+    if (p->flags & QF_FLAG_SIMPLE_KERNEL) {
+        const long long units = (long long)A.total_rows * P.num_q_heads;
+        const long long blocks = (units + qf::kRowsSimpleWarps - 1) / qf::kRowsSimpleWarps;
+        if (blocks > 0x7fffffffll) return QF_ERR_UNSUPPORTED;
+        qf::rows_simple_kernel<PREFIX><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return qf_host::cuda_fail(e, "rows_simple_kernel launch");
+        qf_host::set_launches(1);
+        return QF_OK;
+    }
+    qf::RowsMaps maps;
+    size_t len;
+    char *msg = qf_host::cuda_msg(&len);
+    if (qf::make_rows_maps(&maps, A, P, msg, len)) return QF_ERR_CUDA;
+    cudaError_t e = qf::launch_rows_kernels<PREFIX>(maps, A, P, ws, sms, st);
+    if (e != cudaSuccess) return qf_host::cuda_fail(e, "rows_kernel launch");
+    qf_host::set_launches(2);
     return QF_OK;
 }
 
@@ -135,7 +138,7 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
 size_t qf_prompt_workspace_bytes(const qf_params *p, int total_tokens)
 {
     if (qf_host::validate(p) != QF_OK || total_tokens <= 0) return 0;
-    return align256(rows_layout().total);
+    return align256(qf::rows_layout().total);
 }
 
 int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
@@ -151,7 +154,8 @@ int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, co
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < qf_prompt_workspace_bytes(p, total_tokens))
         return QF_ERR_WORKSPACE;
     if (misaligned(k_cache, 128) || misaligned(v_cache, 128) || misaligned(q, 16) || misaligned(out, 16)) return QF_ERR_BAD_SHAPE;
-    rc = qf_host::check_device(nullptr);
+    int sms = 0;
+    rc = qf_host::check_device(&sms);
     if (rc != QF_OK) return rc;
     const qf::DevParams P = qf_host::dev_params(p);
     qf::RowsArgs A = {};
@@ -160,13 +164,13 @@ int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, co
     A.out = (uint16_t *)out; A.lse = lse; A.status = (unsigned long long *)workspace;
     A.q_stride = q_stride ? q_stride : width;
     A.n_seq = p->batch; A.table_width = p->max_pages_per_req; A.max_tokens = P.max_tokens; A.total_rows = total_tokens;
-    return launch_rows<false>(A, P, p, (cudaStream_t)cuda_stream);
+    return launch_rows<false>(A, P, p, (char *)workspace, sms, (cudaStream_t)cuda_stream);
 }
 
 size_t qf_prefix_workspace_bytes(const qf_params *p)
 {
     if (qf_host::validate(p) != QF_OK) return 0;
-    return align256(rows_layout().total) + align256(qf_workspace_bytes(p));
+    return align256(qf::rows_layout().total) + align256(qf_workspace_bytes(p));
 }
 
 int qf_prefix_partial(const void *q, const void *k_cache, const void *v_cache, const int32_t *prefix_table,
@@ -180,9 +184,10 @@ int qf_prefix_partial(const void *q, const void *k_cache, const void *v_cache, c
     if (num_groups <= 0 || max_prefix_pages <= 0) return QF_ERR_BAD_SHAPE;
     if (num_groups > p->batch || (long long)max_prefix_pages * qf::kPageSize >= (1ll << 31)) return QF_ERR_UNSUPPORTED;
     if (!q || !k_cache || !v_cache || !prefix_lens || !group_offsets || !o_part || !m_part || !lse_part) return QF_ERR_NULL;
-    if (!workspace || misaligned(workspace, 256) || workspace_bytes < align256(rows_layout().total)) return QF_ERR_WORKSPACE;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < align256(qf::rows_layout().total)) return QF_ERR_WORKSPACE;
     if (misaligned(k_cache, 128) || misaligned(v_cache, 128) || misaligned(q, 16) || misaligned(o_part, 16)) return QF_ERR_BAD_SHAPE;
-    rc = qf_host::check_device(nullptr);
+    int sms = 0;
+    rc = qf_host::check_device(&sms);
     if (rc != QF_OK) return rc;
     const qf::DevParams P = qf_host::dev_params(p);
     qf::RowsArgs A = {};
@@ -193,7 +198,7 @@ int qf_prefix_partial(const void *q, const void *k_cache, const void *v_cache, c
     A.n_seq = num_groups; A.table_width = max_prefix_pages;
     A.max_tokens = qf::max_row_tokens(max_prefix_pages); A.total_rows = p->batch;
     A.out_shards = P.out_shards; A.slot = P.out_shard0;
-    return launch_rows<true>(A, P, p, (cudaStream_t)cuda_stream);
+    return launch_rows<true>(A, P, p, (char *)workspace, sms, (cudaStream_t)cuda_stream);
 }
 
 int qf_prefix_step(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
@@ -217,7 +222,7 @@ int qf_prefix_step(const void *q, const void *k_cache, const void *v_cache, cons
                            &wide, num_groups, max_prefix_pages, workspace, workspace_bytes, cuda_stream);
     if (rc != QF_OK) return rc;
     int launches = qf_last_launch_count();
-    const size_t own = align256(rows_layout().total);
+    const size_t own = align256(qf::rows_layout().total);
     wide.out_shard_offset = 1;
     rc = qf_decode_partial(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part, &wide,
                            (char *)workspace + own, workspace_bytes - own, cuda_stream);
@@ -251,9 +256,57 @@ int qf_prefix_status(const void *workspace, const qf_params *p, int32_t *host_st
     if (!workspace || !host_status) return QF_ERR_NULL;
     rc = qf_prompt_status(workspace, &own, cuda_stream);
     if (rc != QF_OK) return rc;
-    rc = qf_read_status((const char *)workspace + align256(rows_layout().total), &sweep, cuda_stream);
+    rc = qf_read_status((const char *)workspace + align256(qf::rows_layout().total), &sweep, cuda_stream);
     if (rc == QF_OK) *host_status = own | sweep;
     return rc;
+}
+
+int qf_rows_schedule(int causal, const int32_t *offsets, const int32_t *lens, int n_seq, int group, int num_kv_heads,
+                     int max_tokens, int total_rows, int n_ctas, int32_t *records, int capacity)
+{
+    if (!offsets || !lens || (capacity > 0 && !records)) return QF_ERR_NULL;
+    if (n_seq < 1 || group < 1 || group > 8 || num_kv_heads < 1 || max_tokens < 1 || total_rows < 1 || n_ctas < 1 ||
+        n_ctas > qf::kRowsMaxCtas || capacity < 0)
+        return QF_ERR_BAD_SHAPE;
+    auto first = [&](int s) { return std::min(std::max(offsets[s], 0), total_rows); };
+    auto plan = [&](int s) {
+        qf::SeqPlan q;
+        q.n = std::max(std::min(offsets[s + 1], total_rows) - first(s), 0);
+        q.off = std::min(std::max(lens[s], 0), max_tokens);
+        q.len = causal ? (int)std::min((long long)q.off + q.n, (long long)max_tokens) : q.off;
+        q.causal = causal != 0;
+        q.tile_rows = qf::kRowTile / group;
+        return q;
+    };
+    long long total = 0;
+    for (int s = 0; s < n_seq; ++s) { const qf::SeqPlan q = plan(s); if (q.n > 0 && q.len > 0) total += q.total() * num_kv_heads; }
+    const int n = qf::slices_of(total, n_ctas);
+    auto locate = [&](long long x) {
+        long long before = 0;
+        for (int s = 0; s < n_seq; ++s) {
+            const qf::SeqPlan q = plan(s);
+            const long long cost = q.n > 0 && q.len > 0 ? q.total() * num_kv_heads : 0;
+            if (x >= before && x < before + cost) return qf::locate_in_seq(q, s, group, x - before);
+            before += cost;
+        }
+        return qf::SlicePos{n_seq, 0, 0, 0};
+    };
+    int count = 0;
+    for (int c = 0; total > 0 && c < n; ++c) {
+        qf::SliceWalk<decltype(plan), decltype(first)> walk(plan, first, locate(qf::cut_at(total, n, c)),
+                                                            locate(qf::cut_at(total, n, c + 1)), n_seq, num_kv_heads, c);
+        qf::RowsBlock b;
+        int nt = 0, tiles = 0;
+        while (walk.next(b, nt)) {
+            if (count < capacity) {
+                const int32_t r[12] = {c, b.seq, b.head, b.row0, b.rows, b.t_lo, b.t_hi, b.slot, b.narrow, b.off + (causal ? b.i0 : 0), b.len, tiles};
+                std::copy(r, r + 12, records + (size_t)count * 12);
+            }
+            tiles += b.t_hi - b.t_lo;
+            ++count;
+        }
+    }
+    return count;
 }
 
 }  // extern "C"

@@ -1,0 +1,1118 @@
+// Attention of packed query rows over the paged cache on the tensor cores: whole prompts (causal) and prefixes that
+// requests share.  The problem and its two forms are described in qf_rows_simple.cuh.
+//
+//   S = Q K^T / sqrt(d),  P = e^{S - m},  O = P V / sum P,   per 128 query rows and 128 positions at a time.
+//
+// Both products are tcgen05.mma of 128 x 128 x 128 (bf16 in, fp32 in tensor memory).  A row tile holds the G query
+// heads of 128 / G tokens of one KV head, so one K and V tile serves all of them, whatever G is (rows past
+// G * (128 / G) are unused).  A CTA owns TWO row tiles ("wide") that share every K and V tile it streams: with one,
+// shared memory (A and B operands are both read from it) would bound the products.  While one tile's 128 softmax
+// threads (one per row, no shuffles) turn S into P, the tensor cores work on the other tile.  P goes back to tensor
+// memory over S and is the A operand of the second product from there.  A block with no more rows than one tile
+// ("narrow": a few decode tokens, a small group of requests) has the two softmax groups take alternate position
+// tiles of the same rows instead, each with an accumulator of its own, merged at the block's end: a lone tile's
+// chain product -> softmax -> product would leave the K/V stream waiting.
+//
+// Roles (352 threads, one CTA per SM): warps 0-3 and 4-7 softmax of the two tiles (and their epilogues), warp 8
+// issues every product, warp 9 loads (TMA, 5 tiles of 32 KB in flight or in use), warp 10 walks the schedule.
+//
+// Schedule: the work of all sequences, KV heads and row blocks is laid on one axis in units of half a wide tile
+// (plus a constant per block), and every CTA takes an equal slice, found in its prologue from the lengths alone
+// (closed-form sums, no plan kernel, no host copy of the lengths).  A slice end that falls close to a block's
+// border moves there; otherwise the block is cut along its positions and the pieces, (m, sum, unnormalised O) in
+// fp32, are merged by a second small kernel in slice order.  Long contexts with few rows are split over all SMs by
+// the same rule.  No atomics: the order of every sum follows from the lengths.
+//
+// Numbers: scores, maxima, sums and accumulators are fp32.  The running maximum used in the exponent moves only when
+// a row's maximum has grown by more than 2^8 (the factor cancels in O / sum; a power of two up to 2^8 changes no
+// rounding), so O is rescaled rarely.  Prompt form: P is rounded to bf16 (half a step is 2^-9..2^-8 of each weight;
+// the output itself is bf16).  Prefix form, whose states are fp32: P = hi + lo, two bf16 terms, 16 bits, and twice
+// the second product, which the stream of K and V hides up to about 200 rows.
+//
+// Bounds: a prompt is bound by the products and, equally, by the exponentials (16 per SM and cycle against 8,192
+// multiply-adds); a prefix by HBM while its rows are few, then by the products.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstdio>
+#include <mutex>
+
+#include "qf_common.cuh"
+#include "qf_page_math.cuh"
+#include "qf_proj.cuh"
+#include "qf_rows_simple.cuh"
+
+namespace qf {
+
+constexpr int kRowTile = 128;                    // query rows of a tile, and cached positions of a tile
+constexpr int kTilePages = kRowTile / kPageSize;
+constexpr int kRowsThreads = 11 * 32;
+constexpr int kRowsRing = 5;                     // K and V tiles in flight or in use
+constexpr int kTileBytes = kRowTile * kHeadDim * 2;
+constexpr int kHalfPageBytes = kPageBytes / 2;    // 16 rows x 64 channels
+constexpr int kInfoRing = 4;
+constexpr int kRowsMaxCtas = 160;                // one per SM
+constexpr int kBlockCost = 2;                    // units a block costs beside its tiles
+constexpr int kMinSlice = 3;                     // units: less per CTA is not worth a merge
+constexpr float kRescaleLog2 = 8.f;
+
+// One block's stretch of positions, as the schedule hands it to the other warps.
+struct __align__(16) RowsBlock {
+    int seq;        // -1: no more work
+    int head;       // KV head
+    int row0;       // first row of the block
+    int i0;         // its index within the sequence
+    int rows;       // tokens (prompt) or requests (prefix) in the block
+    int off, len;   // SeqRows of the sequence
+    int t_lo, t_hi; // position tiles
+    int slot;       // >= 0: a piece, its state goes to this slot; -1: the whole block
+    int narrow;
+    int pad;
+};
+// What a CTA leaves for the merge kernel: the block it began but did not finish, and whether its first piece ended one.
+struct __align__(16) RowsRecord { RowsBlock tail; int has_tail, head_state; int pad[2]; };   // head_state: 0 none, 1 goes on, 2 ends
+struct RowsLayout { size_t record_off, slot_off, total; };
+constexpr size_t kRowsSlotFloats = (size_t)2 * kRowTile * (kHeadDim + 4);   // O, then m (log2 units), sum, true maximum
+inline RowsLayout rows_layout()
+{
+    RowsLayout L;
+    L.record_off = 256;
+    L.slot_off = (L.record_off + kRowsMaxCtas * sizeof(RowsRecord) + 255) & ~(size_t)255;
+    L.total = (L.slot_off + 2 * kRowsMaxCtas * kRowsSlotFloats * sizeof(float) + 255) & ~(size_t)255;
+    return L;
+}
+
+// ------------------------------------------------------------------ schedule arithmetic (host and device)
+// sum over i < n of floor((a i + b) / m), by the Euclidean recursion (a, b >= 0).
+__host__ __device__ inline long long floor_sum(long long n, long long m, long long a, long long b)
+{
+    long long ans = 0;
+    while (n > 0) {
+        if (a >= m) { ans += n * (n - 1) / 2 * (a / m); a %= m; }
+        if (b >= m) { ans += n * (b / m); b %= m; }
+        const long long y = a * n + b;
+        if (y < m) break;
+        n = y / m;
+        b = y % m;
+        const long long t = m; m = a; a = t;
+    }
+    return ans;
+}
+struct SeqPlan {
+    int n, off, len, causal;     // rows, positions before row 0, positions in all
+    int tile_rows;               // tokens per row tile
+    __host__ __device__ int block_rows() const { return 2 * tile_rows; }
+    __host__ __device__ int blocks() const { return len > 0 ? (n + block_rows() - 1) / block_rows() : 0; }
+    __host__ __device__ int rows_of(int j) const { const int r = n - j * block_rows(); return r < block_rows() ? r : block_rows(); }
+    __host__ __device__ bool narrow(int j) const { return rows_of(j) <= tile_rows; }
+    __host__ __device__ int tiles(int j) const
+    {
+        long long lim = len;
+        if (causal) {
+            const long long last = (long long)off + (long long)j * block_rows() + rows_of(j);
+            if (last < lim) lim = last;
+        }
+        return (int)((lim + kRowTile - 1) / kRowTile);
+    }
+    __host__ __device__ int weight(int j) const { return narrow(j) ? 1 : 2; }
+    __host__ __device__ long long cost(int j) const { return (long long)weight(j) * tiles(j) + kBlockCost; }
+    // cost of the first j blocks; all but the last are full
+    __host__ __device__ long long cost_before(int j) const
+    {
+        const int full = j < blocks() - 1 ? j : (blocks() - 1 > 0 ? blocks() - 1 : 0);
+        long long t;
+        if (causal) {
+            const long long br = block_rows();
+            long long free = ((long long)len - off) / br;       // blocks that end at or before the last position
+            free = free < 0 ? 0 : free > full ? full : free;
+            if (free <= 8) {      // a few 32-bit shifts instead of 64-bit divisions
+                t = 0;
+                for (int i = 1; i <= (int)free; ++i) t += ((unsigned)off + (unsigned)(i * (int)br) + kRowTile - 1) / kRowTile;
+            } else {
+                t = floor_sum(free, kRowTile, br, (long long)off + br + kRowTile - 1);
+            }
+            t += (full - free) * (long long)((len + kRowTile - 1) / kRowTile);
+        } else {
+            t = (long long)full * ((len + kRowTile - 1) / kRowTile);
+        }
+        long long c = 2 * t + (long long)kBlockCost * full;
+        if (j > full) c += cost(full);
+        return c;
+    }
+    __host__ __device__ long long total() const { return cost_before(blocks()); }
+};
+struct SlicePos { int seq, head, block, tile; };   // a cut: this block's tiles below `tile` lie before it
+// Where position x of one sequence's stretch (heads in order, blocks of a head in order) falls.
+__host__ __device__ inline SlicePos locate_in_seq(const SeqPlan &q, int seq, int group, long long x)
+{
+    const long long per_head = q.total();
+    SlicePos p;
+    p.seq = seq;
+    p.head = (int)(x / per_head);
+    long long r = x - p.head * per_head;
+    int lo = 0, hi = q.blocks();
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (q.cost_before(mid) <= r) lo = mid; else hi = mid;
+    }
+    p.block = lo;
+    r -= q.cost_before(lo);
+    const long long cost = q.cost(lo);
+    // writing and merging a piece costs about as much as this many units of its rows' products
+    const int snap = q.rows_of(lo) * group / 32 + 1;
+    const int w = q.weight(lo), nt = q.tiles(lo);
+    if (r < snap) p.tile = 0;
+    else if (cost - r < snap) p.tile = nt;
+    else {
+        const long long t = (r - kBlockCost + w - 1) / w;
+        p.tile = t < 0 ? 0 : t > nt ? nt : (int)t;
+    }
+    return p;
+}
+
+// Cut c of n lies at total * c / n units; n is how many slices the work is worth.
+__host__ __device__ inline int slices_of(long long total, int n_ctas)
+{
+    const long long want = total / kMinSlice;
+    return want < 1 ? 1 : want < n_ctas ? (int)want : n_ctas;
+}
+__host__ __device__ inline long long cut_at(long long total, int n, int c)
+{
+    return (long long)(((unsigned long long)total * (unsigned)c) / (unsigned)n);
+}
+// The blocks between two cuts, in order.  `plan(s)` gives sequence s's SeqPlan, `first(s)` its first row.
+template <class Plan, class First>
+struct SliceWalk {
+    Plan plan;
+    First first;
+    SlicePos at, end;
+    int n_seq, heads, cta;
+    SeqPlan q;
+    int row0;
+    __host__ __device__ SliceWalk(Plan p, First f, SlicePos a, SlicePos z, int n_seq_, int heads_, int cta_)
+        : plan(p), first(f), at(a), end(z), n_seq(n_seq_), heads(heads_), cta(cta_), q(p(a.seq)), row0(f(a.seq)) {}
+    // false: no block is left.  nt: the whole block's tiles.
+    __host__ __device__ bool next(RowsBlock &b, int &nt)
+    {
+        while (at.seq < n_seq) {
+            const bool last = at.seq == end.seq && at.head == end.head && at.block == end.block;
+            const int lo = at.tile, hi = last ? end.tile : q.tiles(at.block), j = at.block;
+            const bool some = lo < hi;
+            if (some) {
+                nt = q.tiles(j);
+                b.seq = at.seq; b.head = at.head; b.i0 = j * q.block_rows(); b.row0 = row0 + b.i0;
+                b.rows = q.rows_of(j); b.off = q.off; b.len = q.len; b.t_lo = lo; b.t_hi = hi;
+                b.narrow = q.narrow(j) ? 1 : 0; b.pad = 0;
+                b.slot = (lo == 0 && hi == nt) ? -1 : lo > 0 ? 2 * cta : 2 * cta + 1;
+            }
+            if (last) at.seq = n_seq;
+            else {
+                at.tile = 0;
+                if (++at.block == q.blocks()) {
+                    at.block = 0;
+                    if (++at.head == heads) {
+                        at.head = 0;
+                        while (++at.seq < n_seq) {
+                            q = plan(at.seq);
+                            if (q.n > 0 && q.len > 0) { row0 = first(at.seq); break; }
+                        }
+                    }
+                }
+            }
+            if (some) return true;
+        }
+        return false;
+    }
+};
+
+// ------------------------------------------------------------------ PTX
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+// D[tmem] (+)= A[tmem] . B[smem], 128 x 128 x 16
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// A V page as the B operand (16 positions x 128 channels, channels contiguous): [2 channel halves][16 rows][128 B],
+// 128B swizzle.  Leading offset: the next 64 channels, 2,048 B; stride offset: the next 8 positions, 1,024 B.
+__device__ __forceinline__ uint64_t umma_desc_mn_page(uint32_t smem_addr)
+{
+    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(2048 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, float *v)
+{
+    float (&r)[32] = *reinterpret_cast<float (*)[32]>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+          "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
+          "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+          "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Ties 32 loaded registers to this point of the program: nothing that uses them moves above the wait before it.
+__device__ __forceinline__ void pin32(float *v)
+{
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7]));
+}
+// A bounded wait of a whole warp: every lane leaves with the same answer.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+// ------------------------------------------------------------------ the kernel
+struct RowsSmem {
+    alignas(1024) uint8_t q[2][kTileBytes];            // [row tile][channel half][128 rows][128 B]
+    alignas(1024) uint8_t kv[kRowsRing][kTileBytes];   // K: [half][128 positions][128 B]; V: [page][half][16][128 B]
+    alignas(16) RowsBlock info[kInfoRing];
+    alignas(8) unsigned long long kv_full[kRowsRing], kv_empty[kRowsRing], q_full, q_empty, s_full[2], p_full[2], o_full[2],
+        info_full[kInfoRing], info_empty[kInfoRing], pair[2], drain;
+    float2 ml[2][kRowTile];          // narrow blocks: each group's (maximum, sum) per row
+    unsigned bad_pages[8];           // per position tile (by its running number): pages without a valid table entry
+    int dirty[kInfoRing];            // a value the mask hides from some row of the block is not finite
+    SlicePos cut[2];
+    long long scan[kRowsThreads / 32];
+    long long cut_rest[2];
+    int cut_seq[2];
+    uint32_t tmem_base;
+    int abort_flag;
+};
+static_assert(sizeof(RowsSmem) <= 227 * 1024, "one CTA per SM");
+
+struct RowsMaps { CUtensorMap q, k, v; };
+
+template <bool PREFIX>
+__global__ void __launch_bounds__(kRowsThreads, 1)
+rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, RowsRecord *__restrict__ records,
+            float *__restrict__ slots)
+{
+    extern __shared__ __align__(1024) uint8_t rows_smem[];
+    RowsSmem &sm = *reinterpret_cast<RowsSmem *>(rows_smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int Hq = P.num_q_heads, Hkv = P.num_kv_heads, G = P.group;
+    const int tile_rows = kRowTile / G;               // tokens per row tile
+    volatile int *abort_flag = &sm.abort_flag;
+
+    if (tid == 0) {
+        for (int i = 0; i < kRowsRing; ++i) { mbar_init(smem_u32(&sm.kv_full[i]), 1); mbar_init(smem_u32(&sm.kv_empty[i]), 1); }
+        mbar_init(smem_u32(&sm.q_full), 1);
+        mbar_init(smem_u32(&sm.q_empty), 1);
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(smem_u32(&sm.s_full[w]), 1);
+            mbar_init(smem_u32(&sm.p_full[w]), 4);       // one arrival per softmax warp
+            mbar_init(smem_u32(&sm.o_full[w]), 1);
+            mbar_init(smem_u32(&sm.pair[w]), 8);
+        }
+        for (int i = 0; i < kInfoRing; ++i) { mbar_init(smem_u32(&sm.info_full[i]), 1); mbar_init(smem_u32(&sm.info_empty[i]), 10); }
+        mbar_init(smem_u32(&sm.drain), 1);
+        sm.abort_flag = 0;
+        sm.cut_seq[0] = sm.cut_seq[1] = -1;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) tmem_alloc(smem_u32(&sm.tmem_base), 512);
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    auto seq_plan = [&](int s) -> SeqPlan {
+        const SeqRows r = seq_rows<PREFIX>(A, s);
+        return SeqPlan{r.n, r.off, r.len, PREFIX ? 0 : 1, tile_rows};
+    };
+    auto give_up = [&]() {      // a bounded wait ran out (or another warp's did)
+        sm.abort_flag = 1;
+        rows_status_or(A.status, kStatusTimeout);
+    };
+
+    if (PREFIX) {
+        // empty states: requests of groups with an empty prefix, and of no group
+        auto empties = [&](int lo, int hi) {
+            const long long n4 = (long long)max(hi - lo, 0) * Hq * (kHeadDim / 4);
+            for (long long i = tid; i < n4; i += kRowsThreads) {
+                const long long row = lo + i / (Hq * (kHeadDim / 4));
+                const int rest = (int)(i % (Hq * (kHeadDim / 4)));
+                const size_t o = ((size_t)row * A.out_shards + A.slot) * Hq;
+                reinterpret_cast<float4 *>(A.o_part + o * kHeadDim)[rest] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (rest < Hq) { A.m_part[o + rest] = neg_inf(); A.lse_part[o + rest] = neg_inf(); }
+            }
+        };
+        for (int s = (int)blockIdx.x; s < A.n_seq + 2; s += (int)gridDim.x) {
+            if (s == A.n_seq) empties(0, min(max(A.cu[0], 0), A.total_rows));
+            else if (s == A.n_seq + 1) empties(min(max(A.cu[A.n_seq], 0), A.total_rows), A.total_rows);
+            else {
+                const SeqRows r = seq_rows<PREFIX>(A, s);
+                if (r.len == 0) empties(r.first, r.first + r.n);
+            }
+        }
+    }
+
+    // ---- this CTA's slice
+    const int n_ctas = (int)gridDim.x;
+    long long total = 0;
+    long long first_cost = 0, first_before = 0;       // of this thread's sequence in the first round
+    for (int base = 0; base < A.n_seq; base += kRowsThreads) {
+        const int s = base + tid;
+        long long cost = 0;
+        if (s < A.n_seq) {
+            const SeqPlan q = seq_plan(s);
+            if (q.n > 0 && q.len > 0) cost = q.total() * Hkv;
+        }
+        long long x = cost;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) sm.scan[warp] = x;
+        __syncthreads();
+        long long before = total;
+        for (int w = 0; w < kRowsThreads / 32; ++w) {
+            if (w < warp) before += sm.scan[w];
+            total += sm.scan[w];
+        }
+        if (base == 0) { first_cost = cost; first_before = before + x - cost; }
+        __syncthreads();
+    }
+    const int n_eff = slices_of(total, n_ctas);
+    const int me = (int)blockIdx.x;
+    const bool working = total > 0 && me < n_eff;
+    if (working) {
+        const long long xa = cut_at(total, n_eff, me), xb = cut_at(total, n_eff, me + 1);
+        auto offer = [&](int s, long long before, long long cost) {
+            if (cost > 0 && xa >= before && xa < before + cost) { sm.cut_seq[0] = s; sm.cut_rest[0] = xa - before; }
+            if (cost > 0 && xb >= before && xb < before + cost) { sm.cut_seq[1] = s; sm.cut_rest[1] = xb - before; }
+        };
+        if (A.n_seq <= kRowsThreads) {
+            if (tid < A.n_seq) offer(tid, first_before, first_cost);
+        } else {
+            long long run = 0;
+            for (int base = 0; base < A.n_seq; base += kRowsThreads) {
+                const int s = base + tid;
+                long long cost = 0;
+                if (s < A.n_seq) {
+                    const SeqPlan q = seq_plan(s);
+                    if (q.n > 0 && q.len > 0) cost = q.total() * Hkv;
+                }
+                long long x = cost;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+                    if (lane >= o) x += y;
+                }
+                if (lane == 31) sm.scan[warp] = x;
+                __syncthreads();
+                long long before = run;
+                for (int w = 0; w < kRowsThreads / 32; ++w) {
+                    if (w < warp) before += sm.scan[w];
+                    run += sm.scan[w];
+                }
+                offer(s, before + x - cost, cost);
+                __syncthreads();
+            }
+        }
+        __syncthreads();
+        if ((tid == 0 || tid == 32)) {
+            const int e = tid >> 5;
+            if (sm.cut_seq[e] >= 0) sm.cut[e] = locate_in_seq(seq_plan(sm.cut_seq[e]), sm.cut_seq[e], G, sm.cut_rest[e]);
+            else sm.cut[e] = SlicePos{A.n_seq, 0, 0, 0};    // the end of everything
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&sm.tmem_base);
+    const uint32_t t_s0 = tmem, t_o0 = tmem + 256;      // S (and P over it) of the two groups, then their O
+
+    if (!working) {
+        if (tid == 0) { records[me].has_tail = 0; records[me].head_state = 0; }
+    } else if (warp == 10) {
+        // ============================ schedule ============================
+        if (lane == 0) {
+            const SlicePos a = sm.cut[0], z = sm.cut[1];
+            RowsBlock tail = {};
+            int has_tail = 0, head_state = 0, idx = 0;
+            bool ok = true;
+            auto publish = [&](const RowsBlock &b) {
+                const int slot = idx % kInfoRing;
+                if (!mbar_wait(smem_u32(&sm.info_empty[slot]), (uint32_t)(((idx / kInfoRing) & 1) ^ 1), abort_flag)) { ok = false; return; }
+                sm.info[slot] = b;
+                mbar_arrive(smem_u32(&sm.info_full[slot]));
+                ++idx;
+            };
+            auto first = [&](int s) { return seq_rows<PREFIX>(A, s).first; };
+            SliceWalk<decltype(seq_plan), decltype(first)> walk(seq_plan, first, a, z, A.n_seq, Hkv, me);
+            RowsBlock b;
+            int nt = 0;
+            while (ok && walk.next(b, nt)) {
+                if (b.t_lo > 0) head_state = b.t_hi == nt ? 2 : 1;
+                else if (b.t_hi < nt) { has_tail = 1; tail = b; }
+                publish(b);
+            }
+            RowsBlock end = {};
+            end.seq = -1;
+            if (ok) publish(end);
+            if (!ok) give_up();
+            RowsRecord &rec = records[me];
+            rec.tail = tail;
+            rec.has_tail = ok ? has_tail : 0;
+            rec.head_state = head_state;
+        }
+    } else if (warp == 9) {
+        // ============================ loads ============================
+        int stage = 0, idx = 0, issued = 0, tile_no = 0;
+        uint32_t phase = 0;
+        int q_fill = -1;
+        bool ok = true;
+        const int none_row = (int)(P.kv_nhd ? P.num_pages * kPageSize : P.num_pages * Hkv * kPageSize);   // out of range: zeros
+        const uint32_t q_box = (uint32_t)(64 * 2) * G * tile_rows;
+        for (; ok; ++idx) {
+            const int slot = idx % kInfoRing;
+            if (!warp_wait(smem_u32(&sm.info_full[slot]), (uint32_t)((idx / kInfoRing) & 1), abort_flag)) { ok = false; break; }
+            const RowsBlock b = sm.info[slot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.info_empty[slot]));
+            if (b.seq < 0) break;
+            const int nt = b.t_hi - b.t_lo;
+            const int last_page = (b.len - 1) >> 4;
+            const long long row_base = (long long)b.seq * A.table_width;
+            auto entry = [&](int lp) -> int {
+                return lp <= last_page ? (A.table ? A.table[row_base + lp] : (int)(row_base + lp)) : -1;
+            };
+            // 64 table entries in registers; the second half is on its way while the first is used.  Values come last
+            // through a page, keys at most two tiles before them, so the window moves when values leave its first half.
+            int win = b.t_lo * kTilePages;
+            int tbl0 = entry(win + lane), tbl1 = entry(win + 32 + lane);
+            auto pages_of = [&](int page0, bool is_v) -> int {      // lane i: physical page page0 + i % 8, or -1
+                if (is_v && page0 - win >= 32) {
+                    win += 32;
+                    tbl0 = tbl1;
+                    tbl1 = entry(win + 32 + lane);
+                }
+                const int at = page0 - win;
+                return __shfl_sync(0xffffffffu, at < 32 ? tbl0 : tbl1, (at & 31) + (lane & 7));
+            };
+            // a tile's pages, K or V, into the ring's next slot
+            auto load_tile = [&](int t, bool is_v) {
+                const int page0 = t * kTilePages;
+                int phys = pages_of(page0, is_v);
+                const bool in = page0 + (lane & 7) <= last_page;
+                const bool bad = in && (phys < 0 || (long long)phys >= P.num_pages);
+                const unsigned bad_mask = __ballot_sync(0xffffffffu, bad) & 0xffu;
+                if (!warp_wait(smem_u32(&sm.kv_empty[stage]), phase ^ 1, abort_flag)) { ok = false; return; }
+                const uint32_t full = smem_u32(&sm.kv_full[stage]);
+                if (lane == 0) {
+                    if (!is_v) {
+                        sm.bad_pages[tile_no & 7] = bad_mask;
+                        if (bad_mask && P.check_bounds) rows_status_or(A.status, kStatusBadPage);
+                    }
+                    mbar_arrive_expect_tx(full, kTileBytes);
+                }
+                if (!is_v) ++tile_no;
+                __syncwarp();
+                const uint32_t dst = smem_u32(sm.kv[stage]);
+                const bool zero = !in || bad;
+                if (is_v) {
+                    if (lane < 8) {
+                        if (P.kv_nhd) tma_load_4d(dst + lane * kPageBytes, &maps.v, 0, b.head, zero ? none_row : phys * kPageSize, 0, full);
+                        else tma_load_3d(dst + lane * kPageBytes, &maps.v, 0, zero ? none_row : (phys * Hkv + b.head) * kPageSize, 0, full);
+                    }
+                } else if (lane < 16) {
+                    const int half = lane >> 3;
+                    const uint32_t at = dst + half * (kTileBytes / 2) + (lane & 7) * kHalfPageBytes;
+                    if (P.kv_nhd) tma_load_4d(at, &maps.k, 0, b.head, zero ? none_row : phys * kPageSize, half, full);
+                    else tma_load_3d(at, &maps.k, 0, zero ? none_row : (phys * Hkv + b.head) * kPageSize, half, full);
+                }
+                ++issued;
+                if (++stage == kRowsRing) { stage = 0; phase ^= 1; }
+            };
+            load_tile(b.t_lo, false);
+            if (!ok) break;
+            if (!warp_wait(smem_u32(&sm.q_empty), (uint32_t)((idx & 1) ^ 1), abort_flag)) { ok = false; break; }
+            if (lane == 0) {
+                const uint32_t full = smem_u32(&sm.q_full);
+                const int n_tiles = b.narrow ? 1 : 2;
+                mbar_arrive_expect_tx(full, q_box * 2u * n_tiles);
+                for (int w = 0; w < n_tiles; ++w)
+                    for (int half = 0; half < 2; ++half)
+                        tma_load_3d(smem_u32(sm.q[w]) + half * (kTileBytes / 2), &maps.q, half * 64, b.head * G,
+                                    b.row0 + w * tile_rows, full);
+            }
+            __syncwarp();
+            q_fill = idx;
+            // the order the products consume them in: K is one tile (wide) or two (narrow) ahead of V
+            const int ahead = b.narrow ? 2 : 1;
+            if (b.narrow && nt > 1) load_tile(b.t_lo + 1, false);
+            for (int t = 0; ok && t < nt; ++t) {
+                load_tile(b.t_lo + t, true);
+                if (ok && t + ahead < nt) load_tile(b.t_lo + t + ahead, false);
+            }
+        }
+        if (!ok) {
+            // flag it, then wait (bounded) for the copies still in flight
+            if (lane == 0) give_up();
+            __syncwarp();
+            int s2 = stage;
+            uint32_t ph2 = phase;
+            for (int k = 0; k < min(issued, kRowsRing); ++k) {
+                if (--s2 < 0) { s2 = kRowsRing - 1; ph2 ^= 1; }
+                for (unsigned it = 0; it < (1u << 20); ++it)
+                    if (mbar_try_wait(smem_u32(&sm.kv_full[s2]), ph2)) break;
+            }
+            if (q_fill >= 0)
+                for (unsigned it = 0; it < (1u << 20); ++it)
+                    if (mbar_try_wait(smem_u32(&sm.q_full), (uint32_t)(q_fill & 1))) break;
+        }
+    } else if (warp == 8) {
+        // ============================ products ============================
+        constexpr uint32_t idesc_qk = umma_idesc_bf16(kRowTile);
+        constexpr uint32_t idesc_pv = umma_idesc_bf16(kHeadDim) | (1u << 16);     // B (values) is channel-major
+        int stage = 0, idx = 0;
+        uint32_t phase = 0, p_phase[2] = {0, 0};
+        bool ok = true;
+        for (; ok; ++idx) {
+            const int slot = idx % kInfoRing;
+            if (!warp_wait(smem_u32(&sm.info_full[slot]), (uint32_t)((idx / kInfoRing) & 1), abort_flag)) { ok = false; break; }
+            const RowsBlock b = sm.info[slot];
+            if (lane == 0) sm.dirty[slot] = 0;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.info_empty[slot]));
+            if (b.seq < 0) break;
+            const int nt = b.t_hi - b.t_lo;
+            // positions every row of the block sees; tiles that reach beyond hold values hidden from some row
+            const int common = PREFIX ? b.len : min(b.off + b.i0 + 1, b.len);
+            auto take = [&]() -> bool {      // the ring's next tile has landed
+                if (!warp_wait(smem_u32(&sm.kv_full[stage]), phase, abort_flag)) { ok = false; return false; }
+                tc_fence_after();
+                return true;
+            };
+            auto release = [&]() {           // ... and is free again when the products issued so far are done
+                if (lane == 0) umma_commit(smem_u32(&sm.kv_empty[stage]));
+                if (++stage == kRowsRing) { stage = 0; phase ^= 1; }
+            };
+            auto qk = [&](int w, int qt) {
+                if (lane == 0) {
+                    const uint32_t a = smem_u32(sm.q[qt]), k = smem_u32(sm.kv[stage]);
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk) {
+                        const uint32_t o = (kk >> 2) * (kTileBytes / 2) + (kk & 3) * 32;
+                        umma_bf16(t_s0 + w * 128, umma_desc_k_sw128(a + o), umma_desc_k_sw128(k + o), idesc_qk, kk > 0);
+                    }
+                    umma_commit(smem_u32(&sm.s_full[w]));
+                }
+            };
+            auto pv = [&](int w, bool first) {
+                if (!warp_wait(smem_u32(&sm.p_full[w]), p_phase[w], abort_flag)) { ok = false; return; }
+                p_phase[w] ^= 1;
+                tc_fence_after();
+                if (lane == 0) {
+                    const uint32_t v = smem_u32(sm.kv[stage]);
+#pragma unroll
+                    for (int part = 0; part < (PREFIX ? 2 : 1); ++part)
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)
+                            umma_bf16_ts(t_o0 + w * 128, t_s0 + w * 128 + part * 64 + kk * 8, umma_desc_mn_page(v + kk * kPageBytes),
+                                         idesc_pv, !(first && part == 0 && kk == 0));
+                    umma_commit(smem_u32(&sm.o_full[w]));
+                }
+            };
+            // Values that no row, or not every row, may see.  Weights there are exactly 0, but 0 times a NaN or an
+            // infinity is not: rows of the last page beyond the context (never written) become 0, and so do non-finite
+            // values of a tile that is hidden from some row, which the epilogue then adds where they are seen.
+            auto clean_values = [&](int t) {
+                uint8_t *v = sm.kv[stage];
+                const int end = b.len - t * kRowTile;            // positions of the tile that exist
+                bool wrote = false;
+                if (end < kRowTile && (end & 15)) {
+                    uint8_t *page = v + (end >> 4) * kPageBytes;
+                    const int r0 = end & 15, n16 = (16 - r0) * 8;    // 16-byte words per half
+                    for (int i = lane; i < 2 * n16; i += 32) {
+                        const int half = i >= n16, w = i - half * n16;
+                        *reinterpret_cast<uint4 *>(page + half * kHalfPageBytes + r0 * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    wrote = true;
+                }
+                __syncwarp();
+                if (!PREFIX && (t + 1) * kRowTile > common) {
+                    unsigned seen = 0;
+#pragma unroll 8
+                    for (int i = lane; i < kTileBytes / 16; i += 32) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(v + i * 16);
+                        seen |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) |
+                                ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
+                    }
+                    if (__any_sync(0xffffffffu, (seen & 0x80008000u) != 0)) {
+                        for (int i = lane; i < kTileBytes / 2; i += 32) {
+                            uint16_t *x = reinterpret_cast<uint16_t *>(v) + i;
+                            if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
+                        }
+                        if (lane == 0) sm.dirty[slot] = 1;
+                        wrote = true;
+                    }
+                }
+                if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            };
+            auto needs_clean = [&](int t) {
+                return (!PREFIX && (t + 1) * kRowTile > common) || ((t + 1) * kRowTile > b.len && (b.len & 15));
+            };
+            if (!warp_wait(smem_u32(&sm.q_full), (uint32_t)(idx & 1), abort_flag)) { ok = false; break; }
+            auto q_done = [&]() { if (lane == 0) umma_commit(smem_u32(&sm.q_empty)); };
+            if (!b.narrow) {
+                if (!take()) break;
+                qk(0, 0);
+                qk(1, 1);
+                release();
+                if (nt == 1) q_done();
+                for (int t = 0; ok && t < nt; ++t) {
+                    // V of this tile is in `stage`; the next K lands in the slot after it
+                    if (!take()) break;
+                    if (needs_clean(b.t_lo + t)) clean_values(b.t_lo + t);
+                    const int v_stage = stage;
+                    const uint32_t v_phase = phase;
+                    auto to_k = [&]() { if (++stage == kRowsRing) { stage = 0; phase ^= 1; } };
+                    auto to_v = [&]() { stage = v_stage; phase = v_phase; };
+                    pv(0, t == 0);
+                    if (!ok) break;
+                    const bool more = t + 1 < nt;
+                    if (more) {
+                        to_k();
+                        if (!take()) break;
+                        qk(0, 0);
+                        to_v();
+                    }
+                    pv(1, t == 0);
+                    if (!ok) break;
+                    release();           // V
+                    if (more) {
+                        qk(1, 1);
+                        release();       // K
+                        if (t + 2 == nt) q_done();
+                    }
+                }
+            } else {
+                for (int t = 0; t < 2 && t < nt; ++t) {
+                    if (!take()) break;
+                    qk(t, 0);
+                    release();
+                }
+                if (!ok) break;
+                if (nt <= 2) q_done();
+                for (int t = 0; ok && t < nt; ++t) {
+                    const int w = t & 1;
+                    if (!take()) break;
+                    if (needs_clean(b.t_lo + t)) clean_values(b.t_lo + t);
+                    pv(w, t < 2);
+                    if (!ok) break;
+                    release();
+                    if (t + 2 < nt) {
+                        if (!take()) break;
+                        qk(w, 0);
+                        release();
+                        if (t + 3 == nt) q_done();
+                    }
+                }
+            }
+        }
+        if (!ok) {
+            if (lane == 0) {
+                give_up();
+                umma_commit(smem_u32(&sm.drain));      // products in flight still write tensor memory: wait (bounded)
+                for (unsigned it = 0; it < (1u << 20); ++it)
+                    if (mbar_try_wait(smem_u32(&sm.drain), 0)) break;
+            }
+            __syncwarp();
+        }
+    } else {
+        // ============================ softmax ============================
+        const int wg = warp >> 2, r = tid & 127;
+        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_s = t_s0 + wg * 128 + lane_base, t_o = t_o0 + wg * 128 + lane_base;
+        const float scale2 = P.sm_scale * 1.4426950408889634f;      // scores are kept in units of log 2
+        const float kLn2 = 0.6931471805599453f;
+        const int my_tok = r / G, my_g = r - my_tok * G;
+        uint32_t s_phase = 0, o_count = 0, pair_phase0 = 0, pair_phase1 = 0;
+        int tile_no = 0;
+        bool ok = true;
+        for (int idx = 0; ok; ++idx) {
+            const int slot = idx % kInfoRing;
+            if (!warp_wait(smem_u32(&sm.info_full[slot]), (uint32_t)((idx / kInfoRing) & 1), abort_flag)) { ok = false; break; }
+            const RowsBlock b = sm.info[slot];
+            if (b.seq < 0) break;
+            const int tok = (b.narrow ? 0 : wg * tile_rows) + my_tok;
+            const bool live = r < G * tile_rows && tok < b.rows;
+            const int lim = PREFIX ? b.len : min(b.off + b.i0 + tok + 1, b.len);
+            // positions that every row of this warp sees: tiles below need no mask
+            const int warp_lim = __shfl_sync(0xffffffffu, lim, 0);
+            const int step = b.narrow ? 2 : 1;
+            float m_ref = neg_inf(), m_true = neg_inf(), l = 0.f;
+            bool started = false;
+            for (int t = b.t_lo + (b.narrow ? wg : 0); t < b.t_hi; t += step) {
+                if (!warp_wait(smem_u32(&sm.s_full[wg]), s_phase, abort_flag)) { ok = false; break; }
+                s_phase ^= 1;
+                tc_fence_after();
+                float s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32_nowait(t_s + c * 32, s + c * 32);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) pin32(s + c * 32);
+                const unsigned bad = sm.bad_pages[(tile_no + t - b.t_lo) & 7];
+                if ((t + 1) * kRowTile > warp_lim || bad) {
+                    const int n = lim - t * kRowTile;
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i >= n || ((bad >> (i >> 4)) & 1)) s[i] = neg_inf();
+                }
+                float mx0 = fmaxf(s[0], s[1]), mx1 = fmaxf(s[2], s[3]), mx2 = fmaxf(s[4], s[5]), mx3 = fmaxf(s[6], s[7]);
+#pragma unroll
+                for (int i = 8; i < 128; i += 8) {
+                    mx0 = fmaxf(mx0, fmaxf(s[i], s[i + 1]));
+                    mx1 = fmaxf(mx1, fmaxf(s[i + 2], s[i + 3]));
+                    mx2 = fmaxf(mx2, fmaxf(s[i + 4], s[i + 5]));
+                    mx3 = fmaxf(mx3, fmaxf(s[i + 6], s[i + 7]));
+                }
+                const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+                m_true = fmaxf(m_true, mx);
+                if (!started) {
+                    m_ref = mx;
+                    started = true;
+                } else {
+                    const bool grow = mx > m_ref && (m_ref == neg_inf() || (mx - m_ref) * scale2 > kRescaleLog2);
+                    if (__any_sync(0xffffffffu, grow)) {
+                        // O of the tiles so far, once their products are done
+                        if (!warp_wait(smem_u32(&sm.o_full[wg]), (o_count + 1) & 1, abort_flag)) { ok = false; break; }
+                        tc_fence_after();
+                        const float f = grow ? fast_exp2((m_ref - mx) * scale2) : 1.f;
+                        if (grow) { l *= f; m_ref = mx; }
+#pragma unroll 1
+                        for (int c = 0; c < 8; ++c) {
+                            float o[16];
+                            tmem_ld16(t_o + c * 16, o);
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
+                            tmem_st16(t_o + c * 16, w);
+                        }
+                    }
+                }
+                const float m2 = m_ref == neg_inf() ? 0.f : m_ref * scale2;
+                float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t hi[16], lo[16];
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float p0 = fast_exp2(fmaf(s[c * 32 + i], scale2, -m2)), p1 = fast_exp2(fmaf(s[c * 32 + i + 1], scale2, -m2));
+                        const float p2 = fast_exp2(fmaf(s[c * 32 + i + 2], scale2, -m2)), p3 = fast_exp2(fmaf(s[c * 32 + i + 3], scale2, -m2));
+                        l0 += p0; l1 += p1; l2 += p2; l3 += p3;
+                        hi[i / 2] = pack_bf16(p0, p1);
+                        hi[i / 2 + 1] = pack_bf16(p2, p3);
+                        if (PREFIX) {
+                            lo[i / 2] = pack_bf16(p0 - bf16lo_to_f32(hi[i / 2]), p1 - bf16hi_to_f32(hi[i / 2]));
+                            lo[i / 2 + 1] = pack_bf16(p2 - bf16lo_to_f32(hi[i / 2 + 1]), p3 - bf16hi_to_f32(hi[i / 2 + 1]));
+                        }
+                    }
+                    tmem_st16(t_s + c * 16, hi);
+                    if (PREFIX) tmem_st16(t_s + 64 + c * 16, lo);
+                }
+                l += (l0 + l1) + (l2 + l3);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[wg]));
+                ++o_count;       // one product of this group's O per tile
+            }
+            if (!ok) break;
+            tile_no += b.t_hi - b.t_lo;
+
+            // ---- the block's (or piece's) result
+            if (started) {
+                if (!warp_wait(smem_u32(&sm.o_full[wg]), (o_count + 1) & 1, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+            }
+            float w_own = 1.f, w_other = 0.f;     // weights of this group's accumulator and, narrow, the other's
+            int c0 = 0, c1 = 8;                   // column chunks of 16 that this thread finishes
+            uint32_t t_x = t_o;                   // the other group's accumulator
+            if (b.narrow) {
+                sm.ml[wg][r] = make_float2(m_ref, l);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm.pair[0]));
+                if (!warp_wait(smem_u32(&sm.pair[0]), pair_phase0, abort_flag)) { ok = false; break; }
+                pair_phase0 ^= 1;
+                tc_fence_after();
+                const float2 other = sm.ml[wg ^ 1][r];
+                const float M = fmaxf(m_ref, other.x);
+                if (M != neg_inf()) {
+                    w_own = m_ref == neg_inf() ? 0.f : fast_exp2((m_ref - M) * scale2);
+                    w_other = other.x == neg_inf() ? 0.f : fast_exp2((other.x - M) * scale2);
+                }
+                l = l * w_own + other.y * w_other;
+                m_ref = M;
+                c0 = wg * 4;
+                c1 = c0 + 4;
+                t_x = t_o0 + (wg ^ 1) * 128 + lane_base;
+            }
+            const bool empty = m_ref == neg_inf();
+            const float inv = b.slot >= 0 ? 1.f : empty ? 0.f : 1.f / l;
+            const int row = b.row0 + tok, h = b.head * G + my_g;
+            const size_t out_row = PREFIX ? ((size_t)row * A.out_shards + A.slot) * Hq + h : (size_t)row * Hq + h;
+            float *slot_base = b.slot >= 0 ? slots + (size_t)b.slot * kRowsSlotFloats : nullptr;
+            const int slot_row = (b.narrow ? 0 : wg * kRowTile) + r;
+            const bool dirty = !PREFIX && *reinterpret_cast<volatile int *>(&sm.dirty[slot]) != 0;
+            for (int c = c0; c < c1; ++c) {
+                float o[16];
+                tmem_ld16(t_o + c * 16, o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = w_own == 0.f ? 0.f : o[i] * w_own;
+                if (b.narrow) {
+                    float x[16];
+                    tmem_ld16(t_x + c * 16, x);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] = w_other == 0.f ? o[i] : fmaf(x[i], w_other, o[i]);
+                }
+                if (!live) continue;
+                if (dirty) {
+                    // non-finite values of the tiles some rows do not see, for the rows that do
+                    const int common = min(b.off + b.i0 + 1, b.len);
+                    for (int pos = max(b.t_lo, common / kRowTile) * kRowTile; pos < min(lim, b.t_hi * kRowTile); ++pos) {
+                        const long long at = (long long)b.seq * A.table_width + (pos >> 4);
+                        const long long phys = A.table ? (long long)A.table[at] : at;
+                        if (phys < 0 || phys >= P.num_pages) continue;
+                        const uint16_t *v = A.v_cache + kv_row_offset(P, phys, b.head, pos & 15) + c * 16;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if ((v[i] & 0x7f80u) == 0x7f80u) o[i] += __uint_as_float((uint32_t)v[i] << 16);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] *= inv;
+                if (b.slot >= 0) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        __stcg(reinterpret_cast<float4 *>(slot_base) + (size_t)(c * 4 + i / 4) * (2 * kRowTile) + slot_row,
+                               make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+                } else if (PREFIX) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<float4 *>(A.o_part + out_row * kHeadDim + c * 16 + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 8)
+                        *reinterpret_cast<uint4 *>(A.out + out_row * kHeadDim + c * 16 + i) =
+                            make_uint4(pack_bf16(o[i], o[i + 1]), pack_bf16(o[i + 2], o[i + 3]), pack_bf16(o[i + 4], o[i + 5]), pack_bf16(o[i + 6], o[i + 7]));
+                }
+            }
+            if (b.narrow) {
+                // nobody may touch either accumulator, or ml, before both groups have read them
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm.pair[1]));
+                if (!warp_wait(smem_u32(&sm.pair[1]), pair_phase1, abort_flag)) { ok = false; break; }
+                pair_phase1 ^= 1;
+                if (PREFIX) {
+                    // the second group's true maximum, to the first, in a word that only the first overwrites later
+                    if (wg == 1) sm.ml[0][r].y = m_true;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sm.pair[0]));
+                    if (!warp_wait(smem_u32(&sm.pair[0]), pair_phase0, abort_flag)) { ok = false; break; }
+                    pair_phase0 ^= 1;
+                    if (wg == 0) m_true = fmaxf(m_true, sm.ml[0][r].y);
+                }
+            }
+            if (live && (!b.narrow || wg == 0)) {
+                if (b.slot >= 0) {
+                    float *ml = slot_base + (size_t)2 * kRowTile * kHeadDim;
+                    __stcg(ml + slot_row, empty ? neg_inf() : m_ref * scale2);
+                    __stcg(ml + 2 * kRowTile + slot_row, l);
+                    if (PREFIX) __stcg(ml + 4 * kRowTile + slot_row, m_true);
+                } else {
+                    const float lse = empty ? neg_inf() : fmaf(m_ref, P.sm_scale, log2f(l) * kLn2);
+                    if (PREFIX) { A.m_part[out_row] = m_true * P.sm_scale; A.lse_part[out_row] = lse; }
+                    else A.lse[out_row] = lse;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.info_empty[slot]));
+        }
+        if (!ok && lane == 0) give_up();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// ------------------------------------------------------------------ pieces of cut blocks
+// CTA (c, part): the block that slice c began and did not finish, channels [32 part, 32 part + 32); thread = row.
+constexpr int kRowsMergeParts = 4;
+template <bool PREFIX>
+__global__ void __launch_bounds__(2 * kRowTile)
+rows_merge_kernel(RowsArgs A, DevParams P, const RowsRecord *__restrict__ records, const float *__restrict__ slots, int n_slices)
+{
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int me = (int)blockIdx.x;
+    if (!__ldcg(&records[me].has_tail)) return;
+    const RowsBlock b = records[me].tail;
+    const int r = threadIdx.x, wg = r >> 7, G = P.group, Hq = P.num_q_heads, tile_rows = kRowTile / G;
+    if (b.narrow && wg) return;
+    const int rr = r & 127, tok = wg * tile_rows + rr / G, g = rr - rr / G * G;
+    if (rr >= G * tile_rows || tok >= b.rows) return;
+    const int part = (int)blockIdx.y;
+    auto piece = [&](int slot) { return slots + (size_t)slot * kRowsSlotFloats; };
+    constexpr size_t kMl = (size_t)2 * kRowTile * kHeadDim;
+    // the pieces in slice order: the owner's tail, then every later slice's first piece up to the one that ends the block
+    float M = __ldcg(piece(2 * me + 1) + kMl + r);
+    float top = PREFIX ? __ldcg(piece(2 * me + 1) + kMl + 4 * kRowTile + r) : 0.f;
+    int last = me;
+    for (int k = me + 1; k < n_slices; ++k) {
+        const int state = __ldcg(&records[k].head_state);
+        if (state == 0) continue;
+        M = fmaxf(M, __ldcg(piece(2 * k) + kMl + r));
+        if (PREFIX) top = fmaxf(top, __ldcg(piece(2 * k) + kMl + 4 * kRowTile + r));
+        last = k;
+        if (state == 2) break;
+    }
+    float z = 0.f;
+    float4 acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = me; k <= last; ++k) {
+        if (k > me && __ldcg(&records[k].head_state) == 0) continue;
+        const float *p = piece(k == me ? 2 * me + 1 : 2 * k);
+        const float mk = __ldcg(p + kMl + r);
+        if (mk == neg_inf()) continue;           // nothing visible in this piece
+        const float w = fast_exp2(mk - M);
+        z = fmaf(__ldcg(p + kMl + 2 * kRowTile + r), w, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 x = __ldcg(reinterpret_cast<const float4 *>(p) + (size_t)(part * 8 + i) * (2 * kRowTile) + r);
+            acc[i].x = fmaf(x.x, w, acc[i].x); acc[i].y = fmaf(x.y, w, acc[i].y);
+            acc[i].z = fmaf(x.z, w, acc[i].z); acc[i].w = fmaf(x.w, w, acc[i].w);
+        }
+    }
+    const bool empty = M == neg_inf();
+    const float inv = empty ? 0.f : 1.f / z;
+    const float kLn2 = 0.6931471805599453f;
+    const float lse = empty ? neg_inf() : (M + log2f(z)) * kLn2;
+    const int row = b.row0 + tok, h = b.head * G + g;
+    if (PREFIX) {
+        const size_t o = ((size_t)row * A.out_shards + A.slot) * Hq + h;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<float4 *>(A.o_part + o * kHeadDim + part * 32 + i * 4) =
+                make_float4(acc[i].x * inv, acc[i].y * inv, acc[i].z * inv, acc[i].w * inv);
+        if (part == 0) { A.m_part[o] = top * P.sm_scale; A.lse_part[o] = lse; }
+    } else {
+        const size_t o = (size_t)row * Hq + h;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2)
+            *reinterpret_cast<uint4 *>(A.out + o * kHeadDim + part * 32 + i * 4) =
+                make_uint4(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv),
+                           pack_bf16(acc[i + 1].x * inv, acc[i + 1].y * inv), pack_bf16(acc[i + 1].z * inv, acc[i + 1].w * inv));
+        if (part == 0) A.lse[o] = lse;
+    }
+}
+
+// ------------------------------------------------------------------ host side
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+inline EncodeTiledFn encode_tiled_fn()
+{
+    static std::mutex mu;
+    static EncodeTiledFn fn = nullptr;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!fn) {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
+            qres == cudaDriverEntryPointSuccess)
+            fn = (EncodeTiledFn)p;
+    }
+    return fn;
+}
+// Descriptors of one call (encoded every call: under a microsecond each).  q: [rows, Hq, 128] in boxes of 64 channels
+// x G heads x 128 / G rows; K pages in boxes of one channel half (so that a tile is two K-major operands of 128
+// positions), V pages whole (a page is one step of the second product).
+inline int make_rows_maps(RowsMaps *m, const RowsArgs &A, const DevParams &P, char *msg, size_t msg_len)
+{
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) { snprintf(msg, msg_len, "cuTensorMapEncodeTiled entry point not available"); return -1; }
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    auto make = [&](CUtensorMap *out, const void *base, int dims, const cuuint64_t *size, const cuuint64_t *stride, const cuuint32_t *box) {
+        return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dims, const_cast<void *>(base), size, stride, box, ones,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    const cuuint64_t q_size[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)P.num_q_heads, (cuuint64_t)A.total_rows};
+    const cuuint64_t q_stride[2] = {(cuuint64_t)kHeadDim * 2, (cuuint64_t)A.q_stride * 2};
+    const cuuint32_t q_box[3] = {64, (cuuint32_t)P.group, (cuuint32_t)(kRowTile / P.group)};
+    CUresult r = make(&m->q, A.q, 3, q_size, q_stride, q_box);
+    const cuuint64_t hkv = (cuuint64_t)P.num_kv_heads, rows = (cuuint64_t)P.num_pages * kPageSize;
+    const cuuint64_t size3[3] = {64, rows * hkv, 2}, stride3[2] = {(cuuint64_t)kHeadDim * 2, 128};
+    const cuuint64_t size4[4] = {64, hkv, rows, 2}, stride4[3] = {(cuuint64_t)kHeadDim * 2, hkv * kHeadDim * 2, 128};
+    const cuuint32_t k3[3] = {64, kPageSize, 1}, v3[3] = {64, kPageSize, 2}, k4[4] = {64, 1, kPageSize, 1}, v4[4] = {64, 1, kPageSize, 2};
+    const int dims = P.kv_nhd ? 4 : 3;
+    const cuuint64_t *size = P.kv_nhd ? size4 : size3, *stride = P.kv_nhd ? stride4 : stride3;
+    if (r == CUDA_SUCCESS) r = make(&m->k, A.k_cache, dims, size, stride, P.kv_nhd ? k4 : k3);
+    if (r == CUDA_SUCCESS) r = make(&m->v, A.v_cache, dims, size, stride, P.kv_nhd ? v4 : v3);
+    if (r != CUDA_SUCCESS) { snprintf(msg, msg_len, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r); return -1; }
+    return 0;
+}
+
+template <bool PREFIX>
+cudaError_t launch_rows_kernels(const RowsMaps &maps, const RowsArgs &A, const DevParams &P, char *ws, int sms, cudaStream_t st)
+{
+    {   // per-device kernel attribute, set once under a lock
+        static std::mutex mu;
+        static bool done[64];
+        int dev = 0;
+        cudaGetDevice(&dev);
+        std::lock_guard<std::mutex> lock(mu);
+        if (!done[dev & 63]) {
+            const cudaError_t e = cudaFuncSetAttribute(rows_kernel<PREFIX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowsSmem));
+            if (e != cudaSuccess) return e;
+            done[dev & 63] = true;
+        }
+    }
+    const RowsLayout L = rows_layout();
+    RowsRecord *records = reinterpret_cast<RowsRecord *>(ws + L.record_off);
+    float *slots = reinterpret_cast<float *>(ws + L.slot_off);
+    const int n = sms < kRowsMaxCtas ? sms : kRowsMaxCtas;
+    cudaError_t e = launch_pdl(rows_kernel<PREFIX>, dim3(n), dim3(kRowsThreads), sizeof(RowsSmem), st, maps, A, P, records, slots);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(rows_merge_kernel<PREFIX>, dim3(n, kRowsMergeParts), dim3(2 * kRowTile), 0, st, A, P,
+                      (const RowsRecord *)records, (const float *)slots, n);
+}
+
+}  // namespace qf

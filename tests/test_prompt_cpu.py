@@ -182,3 +182,57 @@ def test_workspace_sizes():
     assert qf.prompt_workspace_bytes(p, 0) == 0
     m = qf.prefix_workspace_bytes(p)
     assert m % 256 == 0 and m > qf.workspace_bytes(p)
+
+
+# ---- the schedule of the row kernels (host arithmetic)
+def brute_tiles(causal, n, off, length, rows, j):
+    last = min((j + 1) * rows, n)
+    lim = min(off + last, length) if causal else length
+    return -(-lim // 128)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("seed", range(40))
+def test_schedule_covers_every_tile_of_every_block_once(causal, seed):
+    rng = np.random.default_rng(seed)
+    group, heads = int(rng.integers(1, 9)), int(rng.choice([1, 2, 4, 8]))
+    n_seq = int(rng.integers(1, 40))
+    n = rng.integers(0, int(rng.choice([2, 70, 900])), n_seq)
+    lens = rng.integers(0, int(rng.choice([1, 130, 5000, 60000])), n_seq)
+    if seed % 4 == 0:
+        n, lens, n_seq = np.array([int(rng.integers(1, 20000))]), np.array([int(rng.integers(0, 100000))]), 1
+    max_tokens = int(rng.choice([1 << 30, 2000])) if seed % 3 == 0 else 1 << 30
+    off = np.concatenate([[0], np.cumsum(n)])
+    n_ctas = int(rng.choice([148, 132, 7, 1, 160]))
+    rec = qf.rows_schedule(causal, off, lens, group, heads, max_tokens, n_ctas)
+    tile_rows = 128 // group
+    seen, slots, per_cta = {}, set(), {}
+    for c, s, h, row0, rows, lo, hi, slot, narrow, before, length, first_no in rec.tolist():
+        assert 0 <= c < n_ctas and lo < hi and 1 <= rows <= 2 * tile_rows and narrow == (rows <= tile_rows)
+        j = (row0 - off[s]) // (2 * tile_rows)
+        want_len = min(lens[s], max_tokens) + (n[s] if causal else 0)
+        assert length == min(want_len, max_tokens) and rows == min(n[s] - j * 2 * tile_rows, 2 * tile_rows)
+        nt = brute_tiles(causal, n[s], min(lens[s], max_tokens), length, 2 * tile_rows, j)
+        assert hi <= nt and (slot == -1) == (lo == 0 and hi == nt)
+        if slot >= 0:
+            assert slot // 2 == c and slot % 2 == (0 if lo > 0 else 1) and slot not in slots
+            slots.add(slot)
+        got = seen.setdefault((s, h, j), [0, nt])
+        assert got[0] == lo            # stretches of a block come in order, without gap or overlap
+        got[0] = hi
+        per_cta.setdefault(c, []).append((hi - lo) * (1 if narrow else 2) + 2)
+    for (s, h, j), (end, nt) in seen.items():
+        assert end == nt
+    cap = lambda s: min(min(lens[s], max_tokens) + (n[s] if causal else 0), max_tokens)
+    want = sum(heads * -(-int(n[s]) // (2 * tile_rows)) for s in range(n_seq) if n[s] > 0 and cap(s) > 0)
+    assert len(seen) == want
+    assert [r[0] for r in rec.tolist()] == sorted(r[0] for r in rec.tolist())
+
+
+def test_schedule_balances_long_work():
+    for causal, n, lens, group in ((True, [16384], [0], 4), (True, [512], [30011], 4), (False, [256], [32768], 4), (True, [1], [100000], 1)):
+        rec = qf.rows_schedule(causal, [0, n[0]], lens, group, 8, 1 << 30, 148)
+        load = np.zeros(148)
+        for r in rec:
+            load[r[0]] += (r[6] - r[5]) * (1 if r[8] else 2) + 2
+        assert load.max() <= 1.15 * load.mean() + 12, (load.max(), load.mean())
