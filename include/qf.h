@@ -367,7 +367,7 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
  * Rows that belong to no request are left as they were.  A table entry outside [0, num_pages) contributes nothing
  * (reported under QF_FLAG_CHECK_BOUNDS); positions beyond the table row are not attended.  Values at positions a
  * row does not see never reach its result, NaN and infinities included.  p->max_shards is not used (pass 1).
- * k_cache, v_cache 128-byte, q and out 16-byte aligned.  workspace: qf_prompt_workspace_bytes bytes, 256-byte
+ * k_cache, v_cache 128-byte, q 16-byte, out 32-byte aligned.  workspace: qf_prompt_workspace_bytes bytes, 256-byte
  * aligned, contents need not be initialised; one call at a time.  Results do not depend on what ran before: the
  * schedule, and so the order of every sum, follows from the lengths alone.
  */
@@ -392,7 +392,8 @@ int qf_prompt_status(const void *workspace, int32_t *host_status, void *cuda_str
  * (out_shards = p->out_shards, or p->max_shards when that is 0), exactly as qf_decode_partial would write a shard;
  * requests of no group and empty prefixes get (0, -inf, -inf).  Other slots are not touched.  num_groups <= B.
  * fp32 throughout: the weights enter the value product as two bf16 terms (16 bits).
- * prefix_lens beyond the table row are clamped to it.  Errors, bounds, alignment as for qf_decode_partial;
+ * prefix_lens beyond the table row are clamped to it.  Errors, bounds, alignment as for qf_decode_partial, and o_part
+ * 32-byte aligned;
  * workspace: qf_prefix_workspace_bytes bytes, one call at a time.
  */
 size_t qf_prefix_workspace_bytes(const qf_params *p);

@@ -153,7 +153,7 @@ int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, co
     if (!q || !k_cache || !v_cache || !cu_tokens || !seq_lens || !out || !lse) return QF_ERR_NULL;
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < qf_prompt_workspace_bytes(p, total_tokens))
         return QF_ERR_WORKSPACE;
-    if (misaligned(k_cache, 128) || misaligned(v_cache, 128) || misaligned(q, 16) || misaligned(out, 16)) return QF_ERR_BAD_SHAPE;
+    if (misaligned(k_cache, 128) || misaligned(v_cache, 128) || misaligned(q, 16) || misaligned(out, 32)) return QF_ERR_BAD_SHAPE;
     int sms = 0;
     rc = qf_host::check_device(&sms);
     if (rc != QF_OK) return rc;
@@ -185,7 +185,7 @@ int qf_prefix_partial(const void *q, const void *k_cache, const void *v_cache, c
     if (num_groups > p->batch || (long long)max_prefix_pages * qf::kPageSize >= (1ll << 31)) return QF_ERR_UNSUPPORTED;
     if (!q || !k_cache || !v_cache || !prefix_lens || !group_offsets || !o_part || !m_part || !lse_part) return QF_ERR_NULL;
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < align256(qf::rows_layout().total)) return QF_ERR_WORKSPACE;
-    if (misaligned(k_cache, 128) || misaligned(v_cache, 128) || misaligned(q, 16) || misaligned(o_part, 16)) return QF_ERR_BAD_SHAPE;
+    if (misaligned(k_cache, 128) || misaligned(v_cache, 128) || misaligned(q, 16) || misaligned(o_part, 32)) return QF_ERR_BAD_SHAPE;
     int sms = 0;
     rc = qf_host::check_device(&sms);
     if (rc != QF_OK) return rc;

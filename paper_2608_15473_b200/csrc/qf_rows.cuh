@@ -13,8 +13,9 @@
 // tiles of the same rows instead, each with an accumulator of its own, merged at the block's end: a lone tile's
 // chain product -> softmax -> product would leave the K/V stream waiting.
 //
-// Roles (352 threads, one CTA per SM): warps 0-3 and 4-7 softmax of the two tiles (and their epilogues), warp 8
-// issues every product, warp 9 loads (TMA, 5 tiles of 32 KB in flight or in use), warp 10 walks the schedule.
+// Roles (384 threads, one CTA per SM): warps 0-3 and 4-7 softmax of the two tiles (and their epilogues), warps 8 and 9
+// issue the products of one tile each, warp 10 loads (TMA, 5 tiles of 32 KB in flight or in use), warp 11 walks the
+// schedule.
 //
 // Schedule: the work of all sequences, KV heads and row blocks is laid on one axis in units of half a wide tile
 // (plus a constant per block), and every CTA takes an equal slice, found in its prologue from the lengths alone
@@ -48,7 +49,8 @@ namespace qf {
 
 constexpr int kRowTile = 128;                    // query rows of a tile, and cached positions of a tile
 constexpr int kTilePages = kRowTile / kPageSize;
-constexpr int kRowsThreads = 11 * 32;
+constexpr int kUnit = 64;                        // positions of one product S = Q K^T and of one softmax pass
+constexpr int kRowsThreads = 12 * 32;
 constexpr int kRowsRing = 5;                     // K and V tiles in flight or in use
 constexpr int kTileBytes = kRowTile * kHeadDim * 2;
 constexpr int kHalfPageBytes = kPageBytes / 2;    // 16 rows x 64 channels
@@ -85,17 +87,22 @@ inline RowsLayout rows_layout()
 }
 
 // ------------------------------------------------------------------ schedule arithmetic (host and device)
+// 64-bit divisions of numbers that nearly always fit 32 bits (a 64-bit one is a subroutine of a hundred instructions).
+__host__ __device__ inline long long div_small(long long a, long long b)
+{
+    return (((unsigned long long)a | (unsigned long long)b) >> 32) ? a / b : (long long)((unsigned)a / (unsigned)b);
+}
 // sum over i < n of floor((a i + b) / m), by the Euclidean recursion (a, b >= 0).
 __host__ __device__ inline long long floor_sum(long long n, long long m, long long a, long long b)
 {
     long long ans = 0;
     while (n > 0) {
-        if (a >= m) { ans += n * (n - 1) / 2 * (a / m); a %= m; }
-        if (b >= m) { ans += n * (b / m); b %= m; }
+        if (a >= m) { const long long d = div_small(a, m); ans += n * (n - 1) / 2 * d; a -= d * m; }
+        if (b >= m) { const long long d = div_small(b, m); ans += n * d; b -= d * m; }
         const long long y = a * n + b;
         if (y < m) break;
-        n = y / m;
-        b = y % m;
+        n = div_small(y, m);
+        b = y - n * m;
         const long long t = m; m = a; a = t;
     }
     return ans;
@@ -125,8 +132,8 @@ struct SeqPlan {
         long long t;
         if (causal) {
             const long long br = block_rows();
-            long long free = ((long long)len - off) / br;       // blocks that end at or before the last position
-            free = free < 0 ? 0 : free > full ? full : free;
+            long long free = ((long long)len - off) < 0 ? 0 : (long long)((unsigned)(len - off) / (unsigned)br);       // blocks that end at or before the last position
+            free = free > full ? full : free;
             if (free <= 8) {      // a few 32-bit shifts instead of 64-bit divisions
                 t = 0;
                 for (int i = 1; i <= (int)free; ++i) t += ((unsigned)off + (unsigned)(i * (int)br) + kRowTile - 1) / kRowTile;
@@ -144,43 +151,56 @@ struct SeqPlan {
     __host__ __device__ long long total() const { return cost_before(blocks()); }
 };
 struct SlicePos { int seq, head, block, tile; };   // a cut: this block's tiles below `tile` lie before it
-// Where position x of one sequence's stretch (heads in order, blocks of a head in order) falls.
+// Where offset r of block j falls: the tile that a cut there precedes.
+__host__ __device__ inline int place_in_block(const SeqPlan &q, int j, int group, long long r)
+{
+    const long long cost = q.cost(j);
+    // writing and merging a piece costs about as much as this many units of its rows' products
+    const int snap = q.rows_of(j) * group / 32 + 1;
+    const int w = q.weight(j), nt = q.tiles(j);
+    if (r < snap) return 0;
+    if (cost - r < snap) return nt;
+    const long long t = w == 2 ? (r - kBlockCost + 1) >> 1 : r - kBlockCost;
+    return t < 0 ? 0 : t > nt ? nt : (int)t;
+}
+// Position x of one sequence's stretch (heads in order, blocks of a head in order).  On the device the lanes of a warp
+// search the blocks together, 32 prefix sums a round; on the host they are searched one by one.
 __host__ __device__ inline SlicePos locate_in_seq(const SeqPlan &q, int seq, int group, long long x)
 {
     const long long per_head = q.total();
     SlicePos p;
     p.seq = seq;
-    p.head = (int)(x / per_head);
+    p.head = (int)div_small(x, per_head);
     long long r = x - p.head * per_head;
-    int lo = 0, hi = q.blocks();
+    int lo = 0, hi = q.blocks();          // cost_before(lo) <= r < cost_before(hi)
+#ifdef __CUDA_ARCH__
+    const int lane = threadIdx.x & 31;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, mine = lo + lane * step;
+        const bool below = mine < hi && q.cost_before(mine) <= r;
+        const int n = __popc(__ballot_sync(0xffffffffu, below));
+        lo += (n - 1) * step;
+        hi = hi < lo + step ? hi : lo + step;
+    }
+#else
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (q.cost_before(mid) <= r) lo = mid; else hi = mid;
     }
+#endif
     p.block = lo;
-    r -= q.cost_before(lo);
-    const long long cost = q.cost(lo);
-    // writing and merging a piece costs about as much as this many units of its rows' products
-    const int snap = q.rows_of(lo) * group / 32 + 1;
-    const int w = q.weight(lo), nt = q.tiles(lo);
-    if (r < snap) p.tile = 0;
-    else if (cost - r < snap) p.tile = nt;
-    else {
-        const long long t = (r - kBlockCost + w - 1) / w;
-        p.tile = t < 0 ? 0 : t > nt ? nt : (int)t;
-    }
+    p.tile = place_in_block(q, lo, group, r - q.cost_before(lo));
     return p;
 }
-
 // Cut c of n lies at total * c / n units; n is how many slices the work is worth.
 __host__ __device__ inline int slices_of(long long total, int n_ctas)
 {
-    const long long want = total / kMinSlice;
+    const long long want = div_small(total, kMinSlice);
     return want < 1 ? 1 : want < n_ctas ? (int)want : n_ctas;
 }
 __host__ __device__ inline long long cut_at(long long total, int n, int c)
 {
-    return (long long)(((unsigned long long)total * (unsigned)c) / (unsigned)n);
+    return div_small(total * c, n);
 }
 // The blocks between two cuts, in order.  `plan(s)` gives sequence s's SeqPlan, `first(s)` its first row.
 template <class Plan, class First>
@@ -238,20 +258,35 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
 }
-// D[tmem] (+)= A[tmem] . B[smem], 128 x 128 x 16
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
-{
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
-}
+// Issuing a product costs its thread more than the product costs the tensor cores unless the operands are ready in
+// uniform registers: the descriptors' upper words are constants, the lower ones a warp-uniform base plus a constant.
+constexpr uint32_t kDescHi = (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);   // stride 1,024 B, version 1, 128B swizzle
+__device__ __forceinline__ uint32_t desc_lo_k(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | (1u << 16); }
 // A V page as the B operand (16 positions x 128 channels, channels contiguous): [2 channel halves][16 rows][128 B],
 // 128B swizzle.  Leading offset: the next 64 channels, 2,048 B; stride offset: the next 8 positions, 1,024 B.
-__device__ __forceinline__ uint64_t umma_desc_mn_page(uint32_t smem_addr)
+__device__ __forceinline__ uint32_t desc_lo_v(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | ((uint32_t)(2048 >> 4) << 16); }
+// D[tmem] (+)= A[smem] . B[smem]^T
+template <bool ACC>
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc)
 {
-    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(2048 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "n"(kDescHi), "r"(idesc), "n"(ACC ? 1 : 0) : "memory");
+}
+// D[tmem] (+)= A[tmem] . B[smem]
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "n"(kDescHi), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, float *v)
 {
@@ -288,12 +323,25 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 }
 
 // ------------------------------------------------------------------ the kernel
+__device__ __forceinline__ void st_global_32b(void *p, const uint32_t (&r)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+// Units of 64 positions that row group w of a block takes: [2 t_lo, this).
+template <bool PREFIX>
+__device__ __forceinline__ int unit_end(const RowsBlock &b, int w, int tile_rows)
+{
+    const int last = b.narrow || w ? b.rows : min(b.rows, tile_rows);
+    const int lim = PREFIX ? b.len : min(b.off + b.i0 + last, b.len);
+    return min(2 * b.t_hi, (lim + kUnit - 1) / kUnit);
+}
 struct RowsSmem {
     alignas(1024) uint8_t q[2][kTileBytes];            // [row tile][channel half][128 rows][128 B]
     alignas(1024) uint8_t kv[kRowsRing][kTileBytes];   // K: [half][128 positions][128 B]; V: [page][half][16][128 B]
     alignas(16) RowsBlock info[kInfoRing];
-    alignas(8) unsigned long long kv_full[kRowsRing], kv_empty[kRowsRing], q_full, q_empty, s_full[2], p_full[2], o_full[2],
-        info_full[kInfoRing], info_empty[kInfoRing], pair[2], drain;
+    alignas(8) unsigned long long kv_full[kRowsRing], kv_empty[kRowsRing], q_full, q_empty, s_full[2][2], p_full[2][2], o_full[2], o_last[2],
+        info_full[kInfoRing], info_empty[kInfoRing], pair[2], drain[2];
     float2 ml[2][kRowTile];          // narrow blocks: each group's (maximum, sum) per row
     unsigned bad_pages[8];           // per position tile (by its running number): pages without a valid table entry
     int dirty[kInfoRing];            // a value the mask hides from some row of the block is not finite
@@ -321,17 +369,21 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
     volatile int *abort_flag = &sm.abort_flag;
 
     if (tid == 0) {
-        for (int i = 0; i < kRowsRing; ++i) { mbar_init(smem_u32(&sm.kv_full[i]), 1); mbar_init(smem_u32(&sm.kv_empty[i]), 1); }
+        for (int i = 0; i < kRowsRing; ++i) { mbar_init(smem_u32(&sm.kv_full[i]), 1); mbar_init(smem_u32(&sm.kv_empty[i]), 2); }
         mbar_init(smem_u32(&sm.q_full), 1);
-        mbar_init(smem_u32(&sm.q_empty), 1);
+        mbar_init(smem_u32(&sm.q_empty), 2);         // one per product warp
         for (int w = 0; w < 2; ++w) {
-            mbar_init(smem_u32(&sm.s_full[w]), 1);
-            mbar_init(smem_u32(&sm.p_full[w]), 4);       // one arrival per softmax warp
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(smem_u32(&sm.s_full[w][i]), 1);
+                mbar_init(smem_u32(&sm.p_full[w][i]), 4);    // one arrival per softmax warp
+            }
+            mbar_init(smem_u32(&sm.o_last[w]), 1);
             mbar_init(smem_u32(&sm.o_full[w]), 1);
             mbar_init(smem_u32(&sm.pair[w]), 8);
         }
-        for (int i = 0; i < kInfoRing; ++i) { mbar_init(smem_u32(&sm.info_full[i]), 1); mbar_init(smem_u32(&sm.info_empty[i]), 10); }
-        mbar_init(smem_u32(&sm.drain), 1);
+        for (int i = 0; i < kInfoRing; ++i) { mbar_init(smem_u32(&sm.info_full[i]), 1); mbar_init(smem_u32(&sm.info_empty[i]), 11); }
+        mbar_init(smem_u32(&sm.drain[0]), 1);
+        mbar_init(smem_u32(&sm.drain[1]), 1);
         sm.abort_flag = 0;
         sm.cut_seq[0] = sm.cut_seq[1] = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -436,10 +488,10 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
             }
         }
         __syncthreads();
-        if ((tid == 0 || tid == 32)) {
-            const int e = tid >> 5;
-            if (sm.cut_seq[e] >= 0) sm.cut[e] = locate_in_seq(seq_plan(sm.cut_seq[e]), sm.cut_seq[e], G, sm.cut_rest[e]);
-            else sm.cut[e] = SlicePos{A.n_seq, 0, 0, 0};    // the end of everything
+        if (warp < 2) {
+            SlicePos at{A.n_seq, 0, 0, 0};                  // the end of everything
+            if (sm.cut_seq[warp] >= 0) at = locate_in_seq(seq_plan(sm.cut_seq[warp]), sm.cut_seq[warp], G, sm.cut_rest[warp]);
+            if (lane == 0) sm.cut[warp] = at;
         }
     }
     tc_fence_before();
@@ -450,7 +502,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
 
     if (!working) {
         if (tid == 0) { records[me].has_tail = 0; records[me].head_state = 0; }
-    } else if (warp == 10) {
+    } else if (warp == 11) {
         // ============================ schedule ============================
         if (lane == 0) {
             const SlicePos a = sm.cut[0], z = sm.cut[1];
@@ -461,6 +513,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 const int slot = idx % kInfoRing;
                 if (!mbar_wait(smem_u32(&sm.info_empty[slot]), (uint32_t)(((idx / kInfoRing) & 1) ^ 1), abort_flag)) { ok = false; return; }
                 sm.info[slot] = b;
+                sm.dirty[slot] = 0;
                 mbar_arrive(smem_u32(&sm.info_full[slot]));
                 ++idx;
             };
@@ -482,7 +535,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
             rec.has_tail = ok ? has_tail : 0;
             rec.head_state = head_state;
         }
-    } else if (warp == 9) {
+    } else if (warp == 10) {
         // ============================ loads ============================
         int stage = 0, idx = 0, issued = 0, tile_no = 0;
         uint32_t phase = 0;
@@ -587,72 +640,88 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 for (unsigned it = 0; it < (1u << 20); ++it)
                     if (mbar_try_wait(smem_u32(&sm.q_full), (uint32_t)(q_fill & 1))) break;
         }
-    } else if (warp == 8) {
+    } else if (warp >= 8) {
         // ============================ products ============================
-        constexpr uint32_t idesc_qk = umma_idesc_bf16(kRowTile);
+        // One warp per softmax group, so that neither group waits for the other's turn and the few dozen instructions
+        // between two products of a group overlap the other group's.
+        const int w = warp - 8;
+        constexpr uint32_t idesc_qk = umma_idesc_bf16(kUnit);
         constexpr uint32_t idesc_pv = umma_idesc_bf16(kHeadDim) | (1u << 16);     // B (values) is channel-major
+        const uint32_t q_lo = desc_lo_k(smem_u32(sm.q[0])), k_lo = desc_lo_k(smem_u32(sm.kv[0])), v_lo = desc_lo_v(smem_u32(sm.kv[0]));
+        const uint32_t t_s = t_s0 + w * 128, t_o = t_o0 + w * 128;
+        const uint32_t bar_full = smem_u32(sm.kv_full), bar_empty = smem_u32(sm.kv_empty), bar_s = smem_u32(sm.s_full[w]),
+                       bar_p = smem_u32(sm.p_full[w]), bar_o = smem_u32(&sm.o_full[w]), bar_last = smem_u32(&sm.o_last[w]);
         int stage = 0, idx = 0;
-        uint32_t phase = 0, p_phase[2] = {0, 0};
+        uint32_t phase = 0, p_phase = 0;       // p_phase: bit h is p_full[w][h]'s
         bool ok = true;
         for (; ok; ++idx) {
             const int slot = idx % kInfoRing;
             if (!warp_wait(smem_u32(&sm.info_full[slot]), (uint32_t)((idx / kInfoRing) & 1), abort_flag)) { ok = false; break; }
             const RowsBlock b = sm.info[slot];
-            if (lane == 0) sm.dirty[slot] = 0;
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm.info_empty[slot]));
             if (b.seq < 0) break;
-            const int nt = b.t_hi - b.t_lo;
             // positions every row of the block sees; tiles that reach beyond hold values hidden from some row
             const int common = PREFIX ? b.len : min(b.off + b.i0 + 1, b.len);
-            auto take = [&]() -> bool {      // the ring's next tile has landed
-                if (!warp_wait(smem_u32(&sm.kv_full[stage]), phase, abort_flag)) { ok = false; return false; }
+            const int end = unit_end<PREFIX>(b, w, tile_rows);
+            const uint32_t q_at = q_lo + (b.narrow ? 0 : w) * (kTileBytes >> 4);
+            auto take = [&](int at, uint32_t ph) -> bool {      // a tile of the ring has landed
+                if (!warp_wait(bar_full + at * 8, ph, abort_flag)) { ok = false; return false; }
                 tc_fence_after();
                 return true;
             };
-            auto release = [&]() {           // ... and is free again when the products issued so far are done
-                if (lane == 0) umma_commit(smem_u32(&sm.kv_empty[stage]));
+            // This warp is done with the ring's next tile: when its products so far are (or at once, if it is the other's).
+            auto release = [&](bool own) {
+                if (elect_one()) {
+                    if (own) umma_commit(bar_empty + stage * 8);
+                    else mbar_arrive(bar_empty + stage * 8);
+                }
                 if (++stage == kRowsRing) { stage = 0; phase ^= 1; }
             };
-            auto qk = [&](int w, int qt) {
-                if (lane == 0) {
-                    const uint32_t a = smem_u32(sm.q[qt]), k = smem_u32(sm.kv[stage]);
+            // S[h] = Q (K half h)^T: the unit's slot is its half
+            auto qk = [&](int h, int at) {
+                const uint32_t k = k_lo + at * (kTileBytes >> 4) + h * (kUnit * 128 >> 4), d = t_s + h * kUnit;
+                if (elect_one()) {
+                    umma_ss<false>(d, q_at, k, idesc_qk);
 #pragma unroll
-                    for (int kk = 0; kk < 8; ++kk) {
-                        const uint32_t o = (kk >> 2) * (kTileBytes / 2) + (kk & 3) * 32;
-                        umma_bf16(t_s0 + w * 128, umma_desc_k_sw128(a + o), umma_desc_k_sw128(k + o), idesc_qk, kk > 0);
+                    for (int kk = 1; kk < 8; ++kk) {
+                        const uint32_t o = ((kk >> 2) * (kTileBytes / 2) + (kk & 3) * 32) >> 4;
+                        umma_ss<true>(d, q_at + o, k + o, idesc_qk);
                     }
-                    umma_commit(smem_u32(&sm.s_full[w]));
+                    umma_commit(bar_s + h * 8);
                 }
             };
-            auto pv = [&](int w, bool first) {
-                if (!warp_wait(smem_u32(&sm.p_full[w]), p_phase[w], abort_flag)) { ok = false; return; }
-                p_phase[w] ^= 1;
+            // O += P[h] (V half h)
+            auto pv = [&](int h, int at, bool first, bool last) {
+                if (!warp_wait(bar_p + h * 8, (p_phase >> h) & 1, abort_flag)) { ok = false; return; }
+                p_phase ^= 1u << h;
                 tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t v = smem_u32(sm.kv[stage]);
+                const uint32_t v = v_lo + at * (kTileBytes >> 4) + h * ((kUnit / kPageSize) * kPageBytes >> 4), pa = t_s + h * kUnit;
+                const uint32_t acc = first ? 0u : 1u;
+                if (elect_one()) {
 #pragma unroll
                     for (int part = 0; part < (PREFIX ? 2 : 1); ++part)
 #pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)
-                            umma_bf16_ts(t_o0 + w * 128, t_s0 + w * 128 + part * 64 + kk * 8, umma_desc_mn_page(v + kk * kPageBytes),
-                                         idesc_pv, !(first && part == 0 && kk == 0));
-                    umma_commit(smem_u32(&sm.o_full[w]));
+                        for (int kk = 0; kk < 4; ++kk)
+                            umma_ts(t_o, pa + part * 32 + kk * 8, v + kk * (kPageBytes >> 4), idesc_pv, part == 0 && kk == 0 ? acc : 1u);
+                    umma_commit(bar_o);
+                    if (last) umma_commit(bar_last);
                 }
             };
             // Values that no row, or not every row, may see.  Weights there are exactly 0, but 0 times a NaN or an
             // infinity is not: rows of the last page beyond the context (never written) become 0, and so do non-finite
-            // values of a tile that is hidden from some row, which the epilogue then adds where they are seen.
-            auto clean_values = [&](int t) {
-                uint8_t *v = sm.kv[stage];
-                const int end = b.len - t * kRowTile;            // positions of the tile that exist
+            // values of a tile that is hidden from some row, which the epilogue then adds where they are seen.  Both
+            // product warps do it, each before its own products: what the second one writes is what is there.
+            auto clean_values = [&](int t, int at) {
+                uint8_t *v = sm.kv[at];
+                const int exist = b.len - t * kRowTile;          // positions of the tile that exist
                 bool wrote = false;
-                if (end < kRowTile && (end & 15)) {
-                    uint8_t *page = v + (end >> 4) * kPageBytes;
-                    const int r0 = end & 15, n16 = (16 - r0) * 8;    // 16-byte words per half
+                if (exist < kRowTile && (exist & 15)) {
+                    uint8_t *page = v + (exist >> 4) * kPageBytes;
+                    const int r0 = exist & 15, n16 = (16 - r0) * 8;    // 16-byte words per half
                     for (int i = lane; i < 2 * n16; i += 32) {
-                        const int half = i >= n16, w = i - half * n16;
-                        *reinterpret_cast<uint4 *>(page + half * kHalfPageBytes + r0 * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        const int half = i >= n16, x = i - half * n16;
+                        *reinterpret_cast<uint4 *>(page + half * kHalfPageBytes + r0 * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
                     }
                     wrote = true;
                 }
@@ -666,11 +735,13 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                                 ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
                     }
                     if (__any_sync(0xffffffffu, (seen & 0x80008000u) != 0)) {
+                        if (lane == 0) *reinterpret_cast<volatile int *>(&sm.dirty[slot]) = 1;
+                        __threadfence_block();      // said before the first value is gone: the other warp may find none left
+                        __syncwarp();
                         for (int i = lane; i < kTileBytes / 2; i += 32) {
                             uint16_t *x = reinterpret_cast<uint16_t *>(v) + i;
                             if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
                         }
-                        if (lane == 0) sm.dirty[slot] = 1;
                         wrote = true;
                     }
                 }
@@ -681,69 +752,50 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 return (!PREFIX && (t + 1) * kRowTile > common) || ((t + 1) * kRowTile > b.len && (b.len & 15));
             };
             if (!warp_wait(smem_u32(&sm.q_full), (uint32_t)(idx & 1), abort_flag)) { ok = false; break; }
-            auto q_done = [&]() { if (lane == 0) umma_commit(smem_u32(&sm.q_empty)); };
-            if (!b.narrow) {
-                if (!take()) break;
-                qk(0, 0);
-                qk(1, 1);
-                release();
-                if (nt == 1) q_done();
-                for (int t = 0; ok && t < nt; ++t) {
-                    // V of this tile is in `stage`; the next K lands in the slot after it
-                    if (!take()) break;
-                    if (needs_clean(b.t_lo + t)) clean_values(b.t_lo + t);
-                    const int v_stage = stage;
-                    const uint32_t v_phase = phase;
-                    auto to_k = [&]() { if (++stage == kRowsRing) { stage = 0; phase ^= 1; } };
-                    auto to_v = [&]() { stage = v_stage; phase = v_phase; };
-                    pv(0, t == 0);
-                    if (!ok) break;
-                    const bool more = t + 1 < nt;
-                    if (more) {
-                        to_k();
-                        if (!take()) break;
-                        qk(0, 0);
-                        to_v();
-                    }
-                    pv(1, t == 0);
-                    if (!ok) break;
-                    release();           // V
-                    if (more) {
-                        qk(1, 1);
-                        release();       // K
-                        if (t + 2 == nt) q_done();
-                    }
-                }
-            } else {
-                for (int t = 0; t < 2 && t < nt; ++t) {
-                    if (!take()) break;
-                    qk(t, 0);
-                    release();
+            auto q_done = [&]() { if (elect_one()) umma_commit(smem_u32(&sm.q_empty)); };
+            // The order: S of a tile's two units, then for every unit P V of this tile and, into the slot that P V has
+            // just freed (a thread's products run in the order of issue), S of the tile this group takes next.
+            const int ahead = b.narrow ? 2 : 1;      // tiles between the values in use and the keys
+            for (int t = b.t_lo; t < b.t_hi && t < b.t_lo + ahead; ++t) {
+                if (!take(stage, phase)) break;
+                const bool own = !b.narrow || ((t - b.t_lo) & 1) == w;
+                if (own && 2 * t < end) qk(0, stage);
+                if (own && 2 * t + 1 < end) qk(1, stage);
+                release(own);
+            }
+            if (ok && b.t_hi - b.t_lo <= ahead) q_done();
+            for (int t = b.t_lo; ok && t < b.t_hi; ++t) {
+                const bool more = t + ahead < b.t_hi, own = !b.narrow || ((t - b.t_lo) & 1) == w;
+                const int v_at = stage, k_at = stage + 1 == kRowsRing ? 0 : stage + 1;
+                const uint32_t v_phase = phase, k_phase = k_at ? phase : phase ^ 1;
+                if (!take(v_at, v_phase)) break;
+                if (own && needs_clean(t)) clean_values(t, v_at);
+                if (more && !take(k_at, k_phase)) break;
+                if (own) {
+                    const int left = end - 2 * t;      // units of this group from this tile on
+                    const int next = left - 2 * ahead;
+                    const bool tail = t + ahead >= b.t_hi;      // its last tile (narrow: every second one is its own)
+                    const bool fresh = t < b.t_lo + ahead;
+                    if (left > 0) pv(0, v_at, fresh, left == 1);
+                    if (ok && more && next > 0) qk(0, k_at);
+                    if (ok && left > 1) pv(1, v_at, false, b.narrow ? tail : left == 2);
+                    if (ok && more && next > 1) qk(1, k_at);
                 }
                 if (!ok) break;
-                if (nt <= 2) q_done();
-                for (int t = 0; ok && t < nt; ++t) {
-                    const int w = t & 1;
-                    if (!take()) break;
-                    if (needs_clean(b.t_lo + t)) clean_values(b.t_lo + t);
-                    pv(w, t < 2);
-                    if (!ok) break;
-                    release();
-                    if (t + 2 < nt) {
-                        if (!take()) break;
-                        qk(w, 0);
-                        release();
-                        if (t + 3 == nt) q_done();
-                    }
+                release(own);
+                if (more) {
+                    release(own);
+                    if (t + ahead + 1 == b.t_hi) q_done();
                 }
             }
         }
         if (!ok) {
-            if (lane == 0) {
-                give_up();
-                umma_commit(smem_u32(&sm.drain));      // products in flight still write tensor memory: wait (bounded)
+            if (lane == 0) give_up();
+            __syncwarp();
+            if (elect_one()) {
+                umma_commit(smem_u32(&sm.drain[w]));      // products in flight still write tensor memory: wait (bounded)
                 for (unsigned it = 0; it < (1u << 20); ++it)
-                    if (mbar_try_wait(smem_u32(&sm.drain), 0)) break;
+                    if (mbar_try_wait(smem_u32(&sm.drain[w]), 0)) break;
             }
             __syncwarp();
         }
@@ -755,7 +807,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
         const float scale2 = P.sm_scale * 1.4426950408889634f;      // scores are kept in units of log 2
         const float kLn2 = 0.6931471805599453f;
         const int my_tok = r / G, my_g = r - my_tok * G;
-        uint32_t s_phase = 0, o_count = 0, pair_phase0 = 0, pair_phase1 = 0;
+        uint32_t s_phase = 0, o_count = 0, last_phase = 0, pair_phase0 = 0, pair_phase1 = 0;   // s_phase: bit i is s_full[wg][i]'s
         int tile_no = 0;
         bool ok = true;
         for (int idx = 0; ok; ++idx) {
@@ -766,31 +818,33 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
             const int tok = (b.narrow ? 0 : wg * tile_rows) + my_tok;
             const bool live = r < G * tile_rows && tok < b.rows;
             const int lim = PREFIX ? b.len : min(b.off + b.i0 + tok + 1, b.len);
-            // positions that every row of this warp sees: tiles below need no mask
+            // positions that every row of this warp sees: units below need no mask
             const int warp_lim = __shfl_sync(0xffffffffu, lim, 0);
-            const int step = b.narrow ? 2 : 1;
+            const int u_end = unit_end<PREFIX>(b, wg, tile_rows);
             float m_ref = neg_inf(), m_true = neg_inf(), l = 0.f;
             bool started = false;
-            for (int t = b.t_lo + (b.narrow ? wg : 0); t < b.t_hi; t += step) {
-                if (!warp_wait(smem_u32(&sm.s_full[wg]), s_phase, abort_flag)) { ok = false; break; }
-                s_phase ^= 1;
+            for (int u = 2 * (b.t_lo + (b.narrow ? wg : 0)); u < u_end; u += (b.narrow && (u & 1)) ? 3 : 1) {
+                const int h = u & 1;
+                const uint32_t t_u = t_s + h * kUnit;
+                if (!warp_wait(smem_u32(&sm.s_full[wg][h]), (s_phase >> h) & 1, abort_flag)) { ok = false; break; }
+                s_phase ^= 1u << h;
                 tc_fence_after();
-                float s[128];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32_nowait(t_s + c * 32, s + c * 32);
+                float s[kUnit];
+                tmem_ld32_nowait(t_u, s);
+                tmem_ld32_nowait(t_u + 32, s + 32);
+                const unsigned bad = (sm.bad_pages[(tile_no + (u >> 1) - b.t_lo) & 7] >> (4 * h)) & 15u;
                 tmem_wait_ld();
+                pin32(s);
+                pin32(s + 32);
+                if ((u + 1) * kUnit > warp_lim || bad) {
+                    const int n = lim - u * kUnit;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) pin32(s + c * 32);
-                const unsigned bad = sm.bad_pages[(tile_no + t - b.t_lo) & 7];
-                if ((t + 1) * kRowTile > warp_lim || bad) {
-                    const int n = lim - t * kRowTile;
-#pragma unroll
-                    for (int i = 0; i < 128; ++i)
+                    for (int i = 0; i < kUnit; ++i)
                         if (i >= n || ((bad >> (i >> 4)) & 1)) s[i] = neg_inf();
                 }
                 float mx0 = fmaxf(s[0], s[1]), mx1 = fmaxf(s[2], s[3]), mx2 = fmaxf(s[4], s[5]), mx3 = fmaxf(s[6], s[7]);
 #pragma unroll
-                for (int i = 8; i < 128; i += 8) {
+                for (int i = 8; i < kUnit; i += 8) {
                     mx0 = fmaxf(mx0, fmaxf(s[i], s[i + 1]));
                     mx1 = fmaxf(mx1, fmaxf(s[i + 2], s[i + 3]));
                     mx2 = fmaxf(mx2, fmaxf(s[i + 4], s[i + 5]));
@@ -804,7 +858,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 } else {
                     const bool grow = mx > m_ref && (m_ref == neg_inf() || (mx - m_ref) * scale2 > kRescaleLog2);
                     if (__any_sync(0xffffffffu, grow)) {
-                        // O of the tiles so far, once their products are done
+                        // O of the units so far, once their products are done (all but the last are: S came after them)
                         if (!warp_wait(smem_u32(&sm.o_full[wg]), (o_count + 1) & 1, abort_flag)) { ok = false; break; }
                         tc_fence_after();
                         const float f = grow ? fast_exp2((m_ref - mx) * scale2) : 1.f;
@@ -823,7 +877,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 const float m2 = m_ref == neg_inf() ? 0.f : m_ref * scale2;
                 float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     uint32_t hi[16], lo[16];
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
@@ -837,26 +891,27 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                             lo[i / 2 + 1] = pack_bf16(p2 - bf16lo_to_f32(hi[i / 2 + 1]), p3 - bf16hi_to_f32(hi[i / 2 + 1]));
                         }
                     }
-                    tmem_st16(t_s + c * 16, hi);
-                    if (PREFIX) tmem_st16(t_s + 64 + c * 16, lo);
+                    tmem_st16(t_u + c * 16, hi);
+                    if (PREFIX) tmem_st16(t_u + 32 + c * 16, lo);
                 }
                 l += (l0 + l1) + (l2 + l3);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[wg]));
-                ++o_count;       // one product of this group's O per tile
+                if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[wg][h]));
+                ++o_count;       // one product of this group's O per unit
             }
             if (!ok) break;
             tile_no += b.t_hi - b.t_lo;
 
             // ---- the block's (or piece's) result
             if (started) {
-                if (!warp_wait(smem_u32(&sm.o_full[wg]), (o_count + 1) & 1, abort_flag)) { ok = false; break; }
+                if (!warp_wait(smem_u32(&sm.o_last[wg]), last_phase, abort_flag)) { ok = false; break; }
+                last_phase ^= 1;
                 tc_fence_after();
             }
-            float w_own = 1.f, w_other = 0.f;     // weights of this group's accumulator and, narrow, the other's
-            int c0 = 0, c1 = 8;                   // column chunks of 16 that this thread finishes
+            float w_own = started ? 1.f : 0.f, w_other = 0.f;     // weights of this group's accumulator and, narrow, the other's
+            int c0 = 0, c1 = 4;                   // column chunks of 32 that this thread finishes
             uint32_t t_x = t_o;                   // the other group's accumulator
             if (b.narrow) {
                 sm.ml[wg][r] = make_float2(m_ref, l);
@@ -874,8 +929,8 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 }
                 l = l * w_own + other.y * w_other;
                 m_ref = M;
-                c0 = wg * 4;
-                c1 = c0 + 4;
+                c0 = wg * 2;
+                c1 = c0 + 2;
                 t_x = t_o0 + (wg ^ 1) * 128 + lane_base;
             }
             const bool empty = m_ref == neg_inf();
@@ -885,16 +940,28 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
             float *slot_base = b.slot >= 0 ? slots + (size_t)b.slot * kRowsSlotFloats : nullptr;
             const int slot_row = (b.narrow ? 0 : wg * kRowTile) + r;
             const bool dirty = !PREFIX && *reinterpret_cast<volatile int *>(&sm.dirty[slot]) != 0;
+#pragma unroll 1
             for (int c = c0; c < c1; ++c) {
-                float o[16];
-                tmem_ld16(t_o + c * 16, o);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] = w_own == 0.f ? 0.f : o[i] * w_own;
+                float o[32];
+                tmem_ld32_nowait(t_o + c * 32, o);
                 if (b.narrow) {
-                    float x[16];
-                    tmem_ld16(t_x + c * 16, x);
+                    float x[32];
+                    tmem_ld32_nowait(t_x + c * 32, x);
+                    tmem_wait_ld();
+                    pin32(o);
+                    pin32(x);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[i] = w_other == 0.f ? o[i] : fmaf(x[i], w_other, o[i]);
+                    for (int i = 0; i < 32; ++i) {
+                        o[i] = w_own == 0.f ? 0.f : o[i] * w_own;
+                        o[i] = w_other == 0.f ? o[i] : fmaf(x[i], w_other, o[i]);
+                    }
+                } else {
+                    tmem_wait_ld();
+                    pin32(o);
+                    if (!started) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0.f;
+                    }
                 }
                 if (!live) continue;
                 if (dirty) {
@@ -904,28 +971,29 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                         const long long at = (long long)b.seq * A.table_width + (pos >> 4);
                         const long long phys = A.table ? (long long)A.table[at] : at;
                         if (phys < 0 || phys >= P.num_pages) continue;
-                        const uint16_t *v = A.v_cache + kv_row_offset(P, phys, b.head, pos & 15) + c * 16;
+                        const uint16_t *v = A.v_cache + kv_row_offset(P, phys, b.head, pos & 15) + c * 32;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
+                        for (int i = 0; i < 32; ++i)
                             if ((v[i] & 0x7f80u) == 0x7f80u) o[i] += __uint_as_float((uint32_t)v[i] << 16);
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] *= inv;
                 if (b.slot >= 0) {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        __stcg(reinterpret_cast<float4 *>(slot_base) + (size_t)(c * 4 + i / 4) * (2 * kRowTile) + slot_row,
+                    for (int i = 0; i < 32; i += 4)
+                        __stcg(reinterpret_cast<float4 *>(slot_base) + (size_t)(c * 8 + i / 4) * (2 * kRowTile) + slot_row,
                                make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
-                } else if (PREFIX) {
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        *reinterpret_cast<float4 *>(A.o_part + out_row * kHeadDim + c * 16 + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                 } else {
+                    // whole 32-byte sectors: each thread's row is its own, so nothing else is coalesced
+                    constexpr int kPer = PREFIX ? 8 : 16;
 #pragma unroll
-                    for (int i = 0; i < 16; i += 8)
-                        *reinterpret_cast<uint4 *>(A.out + out_row * kHeadDim + c * 16 + i) =
-                            make_uint4(pack_bf16(o[i], o[i + 1]), pack_bf16(o[i + 2], o[i + 3]), pack_bf16(o[i + 4], o[i + 5]), pack_bf16(o[i + 6], o[i + 7]));
+                    for (int i = 0; i < 32; i += kPer) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            w[e] = PREFIX ? __float_as_uint(o[i + e] * inv) : pack_bf16(o[i + 2 * e % kPer] * inv, o[i + (2 * e + 1) % kPer] * inv);
+                        if (PREFIX) st_global_32b(A.o_part + out_row * kHeadDim + c * 32 + i, w);
+                        else st_global_32b(A.out + out_row * kHeadDim + c * 32 + i, w);
+                    }
                 }
             }
             if (b.narrow) {
