@@ -59,6 +59,11 @@ constexpr int kRowsMaxCtas = 160;                // one per SM
 constexpr int kBlockCost = 2;                    // units a block costs beside its tiles
 constexpr int kMinSlice = 3;                     // units: less per CTA is not worth a merge
 constexpr float kRescaleLog2 = 8.f;
+// Of every 8 pairs of scores, how many take their exponentials from the multiply-add units.
+#ifndef QF_ROWS_POLY
+#define QF_ROWS_POLY 2
+#endif
+constexpr int kPolyPairs = QF_ROWS_POLY;
 
 // One block's stretch of positions, as the schedule hands it to the other warps.
 struct __align__(16) RowsBlock {
@@ -87,13 +92,16 @@ inline RowsLayout rows_layout()
 }
 
 // ------------------------------------------------------------------ schedule arithmetic (host and device)
+// The schedule's arithmetic runs a few times per CTA: as functions it stays out of the way of the loops that the
+// instruction cache has to hold.
+#define QF_COLD __noinline__
 // 64-bit divisions of numbers that nearly always fit 32 bits (a 64-bit one is a subroutine of a hundred instructions).
-__host__ __device__ inline long long div_small(long long a, long long b)
+QF_COLD __host__ __device__ inline long long div_small(long long a, long long b)
 {
     return (((unsigned long long)a | (unsigned long long)b) >> 32) ? a / b : (long long)((unsigned)a / (unsigned)b);
 }
 // sum over i < n of floor((a i + b) / m), by the Euclidean recursion (a, b >= 0).
-__host__ __device__ inline long long floor_sum(long long n, long long m, long long a, long long b)
+QF_COLD __host__ __device__ inline long long floor_sum(long long n, long long m, long long a, long long b)
 {
     long long ans = 0;
     while (n > 0) {
@@ -126,7 +134,7 @@ struct SeqPlan {
     __host__ __device__ int weight(int j) const { return narrow(j) ? 1 : 2; }
     __host__ __device__ long long cost(int j) const { return (long long)weight(j) * tiles(j) + kBlockCost; }
     // cost of the first j blocks; all but the last are full
-    __host__ __device__ long long cost_before(int j) const
+    QF_COLD __host__ __device__ long long cost_before(int j) const
     {
         const int full = j < blocks() - 1 ? j : (blocks() - 1 > 0 ? blocks() - 1 : 0);
         long long t;
@@ -152,7 +160,7 @@ struct SeqPlan {
 };
 struct SlicePos { int seq, head, block, tile; };   // a cut: this block's tiles below `tile` lie before it
 // Where offset r of block j falls: the tile that a cut there precedes.
-__host__ __device__ inline int place_in_block(const SeqPlan &q, int j, int group, long long r)
+QF_COLD __host__ __device__ inline int place_in_block(const SeqPlan &q, int j, int group, long long r)
 {
     const long long cost = q.cost(j);
     // writing and merging a piece costs about as much as this many units of its rows' products
@@ -165,7 +173,7 @@ __host__ __device__ inline int place_in_block(const SeqPlan &q, int j, int group
 }
 // Position x of one sequence's stretch (heads in order, blocks of a head in order).  On the device the lanes of a warp
 // search the blocks together, 32 prefix sums a round; on the host they are searched one by one.
-__host__ __device__ inline SlicePos locate_in_seq(const SeqPlan &q, int seq, int group, long long x)
+QF_COLD __host__ __device__ inline SlicePos locate_in_seq(const SeqPlan &q, int seq, int group, long long x)
 {
     const long long per_head = q.total();
     SlicePos p;
@@ -214,7 +222,7 @@ struct SliceWalk {
     __host__ __device__ SliceWalk(Plan p, First f, SlicePos a, SlicePos z, int n_seq_, int heads_, int cta_)
         : plan(p), first(f), at(a), end(z), n_seq(n_seq_), heads(heads_), cta(cta_), q(p(a.seq)), row0(f(a.seq)) {}
     // false: no block is left.  nt: the whole block's tiles.
-    __host__ __device__ bool next(RowsBlock &b, int &nt)
+    QF_COLD __host__ __device__ bool next(RowsBlock &b, int &nt)
     {
         while (at.seq < n_seq) {
             const bool last = at.seq == end.seq && at.head == end.head && at.block == end.block;
@@ -308,10 +316,15 @@ __device__ __forceinline__ void pin32(float *v)
     for (int i = 0; i < 32; i += 8)
         asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7]));
 }
-// A bounded wait of a whole warp: every lane leaves with the same answer.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+// A bounded wait of a whole warp: every lane leaves with the same answer.  The loop is a function of its own.
+__device__ QF_COLD bool warp_wait_loop(uint32_t bar, uint32_t parity, volatile int *abort_flag)
 {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+{
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return warp_wait_loop(bar, parity, abort_flag);
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
@@ -323,6 +336,74 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 }
 
 // ------------------------------------------------------------------ the kernel
+// Pairs of fp32 in one 64-bit register: add, multiply and multiply-add issue once for both.
+__device__ __forceinline__ unsigned long long pack2(float lo, float hi)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(unsigned long long v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c)
+{
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+#if QF_MAX3
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+#else
+    return max_nan(a, max_nan(b, c));
+#endif
+}
+// 2^x for a pair, on the multiply-add units (the special-function unit makes 16 exponentials per SM and cycle, which
+// is what bounds a softmax): x = n + f with n the nearest integer (added into the low mantissa bits of 1.5 * 2^23),
+// 2^f on [-1/2, 1/2] by a polynomial whose largest relative error is least among those with p(0) = 1 (linear program
+// over Chebyshev points: 2.9e-6 in degree 4, 1.7e-7 in degree 5, in fp32), n added to its exponent.  Below -127 the result
+// is exactly 0: p(0) = 1 and the exponent field becomes 0.  x <= 127; a NaN does not come through.
+template <int DEGREE>
+__device__ __forceinline__ void exp2_pair(unsigned long long x, float &p0, float &p1)
+{
+    float a, b;
+    unpack2(x, a, b);
+    x = pack2(fmaxf(a, -127.f), fmaxf(b, -127.f));
+    const unsigned long long magic = pack2(12582912.f, 12582912.f), n_magic = pack2(-12582912.f, -12582912.f);
+    const unsigned long long n = add2(x, magic), minus = pack2(-1.f, -1.f);
+    const unsigned long long f = fma2(add2(n, n_magic), minus, x);
+    unsigned long long p;
+    if (DEGREE == 4) {
+        p = fma2(pack2(0.009581047110259533f, 0.009581047110259533f), f, pack2(0.05590597167611122f, 0.05590597167611122f));
+        p = fma2(p, f, pack2(0.24024145305156708f, 0.24024145305156708f));
+        p = fma2(p, f, pack2(0.6931243538856506f, 0.6931243538856506f));
+    } else {
+        p = fma2(pack2(0.00132546026725322f, 0.00132546026725322f), f, pack2(0.009671999141573906f, 0.009671999141573906f));
+        p = fma2(p, f, pack2(0.05550779402256012f, 0.05550779402256012f));
+        p = fma2(p, f, pack2(0.24022231996059418f, 0.24022231996059418f));
+        p = fma2(p, f, pack2(0.6931469440460205f, 0.6931469440460205f));
+    }
+    p = fma2(p, f, pack2(1.f, 1.f));
+    float n0, n1;
+    unpack2(n, n0, n1);
+    unpack2(p, p0, p1);
+    p0 = __int_as_float(__float_as_int(p0) + (__float_as_int(n0) << 23));
+    p1 = __int_as_float(__float_as_int(p1) + (__float_as_int(n1) << 23));
+}
 __device__ __forceinline__ void st_global_32b(void *p, const uint32_t (&r)[8])
 {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
@@ -353,6 +434,33 @@ struct RowsSmem {
     int abort_flag;
 };
 static_assert(sizeof(RowsSmem) <= 227 * 1024, "one CTA per SM");
+
+// The rare end of a block whose last tiles hold non-finite values (see clean_values): this thread's row, already
+// written, gets those it sees.  A weight is positive, so an infinity stays one and two of opposite signs make a NaN.
+__device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const RowsBlock &b, int lim, int c0, int c1,
+                                   float *slot_base, int slot_row, size_t out_row)
+{
+    const int common = min(b.off + b.i0 + 1, b.len);
+#pragma unroll 1
+    for (int pos = max(b.t_lo, common / kRowTile) * kRowTile; pos < min(lim, b.t_hi * kRowTile); ++pos) {
+        const long long at = (long long)b.seq * A.table_width + (pos >> 4);
+        const long long phys = A.table ? (long long)A.table[at] : at;
+        if (phys < 0 || phys >= P.num_pages) continue;
+        const uint16_t *v = A.v_cache + kv_row_offset(P, phys, b.head, pos & 15);
+#pragma unroll 1
+        for (int d = c0 * 32; d < c1 * 32; ++d) {
+            if ((v[d] & 0x7f80u) != 0x7f80u) continue;
+            const float x = __uint_as_float((uint32_t)v[d] << 16);
+            if (b.slot >= 0) {
+                float *o = slot_base + ((size_t)(d >> 2) * (2 * kRowTile) + slot_row) * 4 + (d & 3);
+                __stcg(o, __ldcg(o) + x);
+            } else {
+                uint16_t *o = A.out + out_row * kHeadDim + d;
+                *o = (uint16_t)(pack_bf16(__uint_as_float((uint32_t)*reinterpret_cast<volatile uint16_t *>(o) << 16) + x, 0.f) & 0xffffu);
+            }
+        }
+    }
+}
 
 struct RowsMaps { CUtensorMap q, k, v; };
 
@@ -837,21 +945,25 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 pin32(s);
                 pin32(s + 32);
                 if ((u + 1) * kUnit > warp_lim || bad) {
-                    const int n = lim - u * kUnit;
 #pragma unroll
-                    for (int i = 0; i < kUnit; ++i)
-                        if (i >= n || ((bad >> (i >> 4)) & 1)) s[i] = neg_inf();
+                    for (int g = 0; g < kUnit / kPageSize; ++g) {
+                        const int n = ((bad >> g) & 1) ? 0 : lim - u * kUnit - g * kPageSize;
+#pragma unroll
+                        for (int i = 0; i < kPageSize; ++i)
+                            if (i >= n) s[g * kPageSize + i] = neg_inf();
+                    }
                 }
-                float mx0 = fmaxf(s[0], s[1]), mx1 = fmaxf(s[2], s[3]), mx2 = fmaxf(s[4], s[5]), mx3 = fmaxf(s[6], s[7]);
+                // NaN wins every maximum here: a NaN score must make its row NaN, and the polynomial would lose it
+                float mx0 = max_nan(s[0], s[1]), mx1 = max_nan(s[2], s[3]), mx2 = max_nan(s[4], s[5]), mx3 = max_nan(s[6], s[7]);
 #pragma unroll
                 for (int i = 8; i < kUnit; i += 8) {
-                    mx0 = fmaxf(mx0, fmaxf(s[i], s[i + 1]));
-                    mx1 = fmaxf(mx1, fmaxf(s[i + 2], s[i + 3]));
-                    mx2 = fmaxf(mx2, fmaxf(s[i + 4], s[i + 5]));
-                    mx3 = fmaxf(mx3, fmaxf(s[i + 6], s[i + 7]));
+                    mx0 = max3_nan(mx0, s[i], s[i + 1]);
+                    mx1 = max3_nan(mx1, s[i + 2], s[i + 3]);
+                    mx2 = max3_nan(mx2, s[i + 4], s[i + 5]);
+                    mx3 = max3_nan(mx3, s[i + 6], s[i + 7]);
                 }
-                const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-                m_true = fmaxf(m_true, mx);
+                const float mx = max_nan(max_nan(mx0, mx1), max_nan(mx2, mx3));
+                m_true = max_nan(m_true, mx);
                 if (!started) {
                     m_ref = mx;
                     started = true;
@@ -875,26 +987,42 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                     }
                 }
                 const float m2 = m_ref == neg_inf() ? 0.f : m_ref * scale2;
-                float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+                const unsigned long long scale22 = pack2(scale2, scale2), m22 = pack2(-m2, -m2);
+                unsigned long long la = pack2(0.f, 0.f), lb = la;
+                float ls[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     uint32_t hi[16], lo[16];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float p0 = fast_exp2(fmaf(s[c * 32 + i], scale2, -m2)), p1 = fast_exp2(fmaf(s[c * 32 + i + 1], scale2, -m2));
-                        const float p2 = fast_exp2(fmaf(s[c * 32 + i + 2], scale2, -m2)), p3 = fast_exp2(fmaf(s[c * 32 + i + 3], scale2, -m2));
-                        l0 += p0; l1 += p1; l2 += p2; l3 += p3;
-                        hi[i / 2] = pack_bf16(p0, p1);
-                        hi[i / 2 + 1] = pack_bf16(p2, p3);
-                        if (PREFIX) {
-                            lo[i / 2] = pack_bf16(p0 - bf16lo_to_f32(hi[i / 2]), p1 - bf16hi_to_f32(hi[i / 2]));
-                            lo[i / 2 + 1] = pack_bf16(p2 - bf16lo_to_f32(hi[i / 2 + 1]), p3 - bf16hi_to_f32(hi[i / 2 + 1]));
+                    for (int i = 0; i < 16; ++i) {
+                        float p0, p1;
+                        if ((i & 7) >= 8 - kPolyPairs) {
+                            exp2_pair<PREFIX ? 5 : 4>(fma2(pack2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale22, m22), p0, p1);
+                        } else {
+#if QF_X2 & 1
+                            unpack2(fma2(pack2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale22, m22), p0, p1);
+#else
+                            p0 = fmaf(s[c * 32 + 2 * i], scale2, -m2);
+                            p1 = fmaf(s[c * 32 + 2 * i + 1], scale2, -m2);
+#endif
+                            p0 = fast_exp2(p0);
+                            p1 = fast_exp2(p1);
                         }
+#if QF_X2 & 2
+                        if (i & 1) la = add2(la, pack2(p0, p1)); else lb = add2(lb, pack2(p0, p1));
+#else
+                        ls[(2 * i) & 3] += p0;
+                        ls[(2 * i + 1) & 3] += p1;
+#endif
+                        hi[i] = pack_bf16(p0, p1);
+                        if (PREFIX) lo[i] = pack_bf16(p0 - bf16lo_to_f32(hi[i]), p1 - bf16hi_to_f32(hi[i]));
                     }
                     tmem_st16(t_u + c * 16, hi);
                     if (PREFIX) tmem_st16(t_u + 32 + c * 16, lo);
                 }
-                l += (l0 + l1) + (l2 + l3);
+                float l0, l1;
+                unpack2(add2(la, lb), l0, l1);
+                l += (l0 + l1) + (ls[0] + ls[1]) + (ls[2] + ls[3]);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -910,6 +1038,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 last_phase ^= 1;
                 tc_fence_after();
             }
+            if (!(m_true < __int_as_float(0x7f800000))) l = __int_as_float(0x7fc00000);   // a score was NaN or +infinity
             float w_own = started ? 1.f : 0.f, w_other = 0.f;     // weights of this group's accumulator and, narrow, the other's
             int c0 = 0, c1 = 4;                   // column chunks of 32 that this thread finishes
             uint32_t t_x = t_o;                   // the other group's accumulator
@@ -964,19 +1093,6 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                     }
                 }
                 if (!live) continue;
-                if (dirty) {
-                    // non-finite values of the tiles some rows do not see, for the rows that do
-                    const int common = min(b.off + b.i0 + 1, b.len);
-                    for (int pos = max(b.t_lo, common / kRowTile) * kRowTile; pos < min(lim, b.t_hi * kRowTile); ++pos) {
-                        const long long at = (long long)b.seq * A.table_width + (pos >> 4);
-                        const long long phys = A.table ? (long long)A.table[at] : at;
-                        if (phys < 0 || phys >= P.num_pages) continue;
-                        const uint16_t *v = A.v_cache + kv_row_offset(P, phys, b.head, pos & 15) + c * 32;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if ((v[i] & 0x7f80u) == 0x7f80u) o[i] += __uint_as_float((uint32_t)v[i] << 16);
-                    }
-                }
                 if (b.slot >= 0) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
@@ -996,6 +1112,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                     }
                 }
             }
+            if (dirty && live) add_hidden(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
             if (b.narrow) {
                 // nobody may touch either accumulator, or ml, before both groups have read them
                 tc_fence_before();
