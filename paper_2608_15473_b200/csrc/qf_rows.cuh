@@ -47,6 +47,9 @@
 
 namespace qf {
 
+#ifndef QF_BC
+#define QF_BC 5
+#endif
 constexpr int kRowTile = 128;                    // query rows of a tile, and cached positions of a tile
 constexpr int kTilePages = kRowTile / kPageSize;
 constexpr int kUnit = 64;                        // positions of one product S = Q K^T and of one softmax pass
@@ -56,7 +59,7 @@ constexpr int kTileBytes = kRowTile * kHeadDim * 2;
 constexpr int kHalfPageBytes = kPageBytes / 2;    // 16 rows x 64 channels
 constexpr int kInfoRing = 4;
 constexpr int kRowsMaxCtas = 160;                // one per SM
-constexpr int kBlockCost = 2;                    // units a block costs beside its tiles
+constexpr int kBlockCost = QF_BC;                    // units a block costs beside its tiles
 constexpr int kMinSlice = 3;                     // units: less per CTA is not worth a merge
 constexpr float kRescaleLog2 = 8.f;
 // Of every 8 pairs of scores, how many take their exponentials from the multiply-add units.
@@ -321,6 +324,8 @@ __device__ QF_COLD bool warp_wait_loop(uint32_t bar, uint32_t parity, volatile i
 {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
+// The same for one thread.
+__device__ QF_COLD bool wait_loop(uint32_t bar, uint32_t parity, volatile int *abort_flag) { return mbar_wait(bar, parity, abort_flag); }
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
 {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
@@ -364,13 +369,9 @@ __device__ __forceinline__ float max_nan(float a, float b)
 }
 __device__ __forceinline__ float max3_nan(float a, float b, float c)
 {
-#if QF_MAX3
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
-#else
-    return max_nan(a, max_nan(b, c));
-#endif
 }
 // 2^x for a pair, on the multiply-add units (the special-function unit makes 16 exponentials per SM and cycle, which
 // is what bounds a softmax): x = n + f with n the nearest integer (added into the low mantissa bits of 1.5 * 2^23),
@@ -466,7 +467,7 @@ struct RowsMaps { CUtensorMap q, k, v; };
 
 template <bool PREFIX>
 __global__ void __launch_bounds__(kRowsThreads, 1)
-rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, RowsRecord *__restrict__ records,
+rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsArgs A, const __grid_constant__ DevParams P, RowsRecord *__restrict__ records,
             float *__restrict__ slots)
 {
     extern __shared__ __align__(1024) uint8_t rows_smem[];
@@ -872,7 +873,74 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 release(own);
             }
             if (ok && b.t_hi - b.t_lo <= ahead) q_done();
-            for (int t = b.t_lo; ok && t < b.t_hi; ++t) {
+            // The tiles with nothing special about them (every unit there, nothing to clean, keys to come): one thread, no
+            // votes, constants where the operands allow it.
+            int t_plain = min(b.t_hi - ahead, (end - 2 * ahead) / 2);
+            if (!PREFIX) t_plain = min(t_plain, common / kRowTile);
+            else if (b.len & 15) t_plain = min(t_plain, b.len / kRowTile);
+            t_plain = max(t_plain, b.t_lo);
+            if (ok && t_plain > b.t_lo) {
+                bool fine = true;
+                if (elect_one()) {
+                    int at = stage;
+                    uint32_t ph = phase, pp = p_phase;
+                    auto wait = [&](uint32_t bar, uint32_t parity) {
+                        if (!mbar_try_wait(bar, parity) && !wait_loop(bar, parity, abort_flag)) fine = false;
+                    };
+#pragma unroll 1
+                    for (int t = b.t_lo; t < t_plain; ++t) {
+                        const int v_at = at;
+                        const uint32_t v_ph = ph;
+                        if (++at == kRowsRing) { at = 0; ph ^= 1; }
+                        wait(bar_full + v_at * 8, v_ph);
+                        wait(bar_full + at * 8, ph);
+                        if (!fine) break;
+                        tc_fence_after();
+                        if (!b.narrow || ((t - b.t_lo) & 1) == w) {
+                            const uint32_t v = v_lo + v_at * (kTileBytes >> 4), k = k_lo + at * (kTileBytes >> 4);
+                            const uint32_t acc = t >= b.t_lo + ahead ? 1u : 0u;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                wait(bar_p + h * 8, (pp >> h) & 1);
+                                if (!fine) break;
+                                tc_fence_after();
+#pragma unroll
+                                for (int part = 0; part < (PREFIX ? 2 : 1); ++part)
+#pragma unroll
+                                    for (int kk = 0; kk < 4; ++kk)
+                                        umma_ts(t_o, t_s + h * kUnit + part * 32 + kk * 8, v + (h * 4 + kk) * (kPageBytes >> 4), idesc_pv,
+                                                h == 0 && part == 0 && kk == 0 ? acc : 1u);
+                                umma_commit(bar_o);
+#pragma unroll
+                                for (int kk = 0; kk < 8; ++kk) {
+                                    const uint32_t o = ((kk >> 2) * (kTileBytes / 2) + (kk & 3) * 32) >> 4;
+                                    if (kk == 0) umma_ss<false>(t_s + h * kUnit, q_at + o, k + h * (kUnit * 128 >> 4) + o, idesc_qk);
+                                    else umma_ss<true>(t_s + h * kUnit, q_at + o, k + h * (kUnit * 128 >> 4) + o, idesc_qk);
+                                }
+                                umma_commit(bar_s + h * 8);
+                            }
+                            if (!fine) break;
+                            pp ^= 3;
+                            umma_commit(bar_empty + v_at * 8);
+                            umma_commit(bar_empty + at * 8);
+                        } else {
+                            mbar_arrive(bar_empty + v_at * 8);
+                            mbar_arrive(bar_empty + at * 8);
+                        }
+                        if (++at == kRowsRing) { at = 0; ph ^= 1; }
+                    }
+                }
+                if (!__all_sync(0xffffffffu, fine)) { ok = false; break; }
+                // where that thread has got to
+                const int n = t_plain - b.t_lo;
+                const int mine = b.narrow ? (w == 0 ? (n + 1) / 2 : n / 2) : n;
+                if (mine & 1) p_phase ^= 3;
+                const int moved = stage + 2 * n;
+                phase ^= (uint32_t)((moved / kRowsRing) & 1);
+                stage = moved % kRowsRing;
+            }
+            if (ok && t_plain > b.t_lo && t_plain + ahead == b.t_hi) q_done();
+            for (int t = t_plain; ok && t < b.t_hi; ++t) {
                 const bool more = t + ahead < b.t_hi, own = !b.narrow || ((t - b.t_lo) & 1) == w;
                 const int v_at = stage, k_at = stage + 1 == kRowsRing ? 0 : stage + 1;
                 const uint32_t v_phase = phase, k_phase = k_at ? phase : phase ^ 1;
@@ -989,31 +1057,21 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 const float m2 = m_ref == neg_inf() ? 0.f : m_ref * scale2;
                 const unsigned long long scale22 = pack2(scale2, scale2), m22 = pack2(-m2, -m2);
                 unsigned long long la = pack2(0.f, 0.f), lb = la;
-                float ls[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     uint32_t hi[16], lo[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
+                        const unsigned long long x = fma2(pack2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale22, m22);
                         float p0, p1;
                         if ((i & 7) >= 8 - kPolyPairs) {
-                            exp2_pair<PREFIX ? 5 : 4>(fma2(pack2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale22, m22), p0, p1);
+                            exp2_pair<PREFIX ? 5 : 4>(x, p0, p1);
                         } else {
-#if QF_X2 & 1
-                            unpack2(fma2(pack2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale22, m22), p0, p1);
-#else
-                            p0 = fmaf(s[c * 32 + 2 * i], scale2, -m2);
-                            p1 = fmaf(s[c * 32 + 2 * i + 1], scale2, -m2);
-#endif
+                            unpack2(x, p0, p1);
                             p0 = fast_exp2(p0);
                             p1 = fast_exp2(p1);
                         }
-#if QF_X2 & 2
                         if (i & 1) la = add2(la, pack2(p0, p1)); else lb = add2(lb, pack2(p0, p1));
-#else
-                        ls[(2 * i) & 3] += p0;
-                        ls[(2 * i + 1) & 3] += p1;
-#endif
                         hi[i] = pack_bf16(p0, p1);
                         if (PREFIX) lo[i] = pack_bf16(p0 - bf16lo_to_f32(hi[i]), p1 - bf16hi_to_f32(hi[i]));
                     }
@@ -1022,7 +1080,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, RowsArgs A, DevParams P, Rows
                 }
                 float l0, l1;
                 unpack2(add2(la, lb), l0, l1);
-                l += (l0 + l1) + (ls[0] + ls[1]) + (ls[2] + ls[3]);
+                l += l0 + l1;
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
