@@ -274,27 +274,27 @@ int qf_rows_schedule(int causal, const int32_t *offsets, const int32_t *lens, in
         q.n = std::max(std::min(offsets[s + 1], total_rows) - first(s), 0);
         q.off = std::min(std::max(lens[s], 0), max_tokens);
         q.len = causal ? (int)std::min((long long)q.off + q.n, (long long)max_tokens) : q.off;
-        q.causal = causal != 0;
-        q.tile_rows = qf::kRowTile / group;
         return q;
     };
-    long long total = 0;
-    for (int s = 0; s < n_seq; ++s) { const qf::SeqPlan q = plan(s); if (q.n > 0 && q.len > 0) total += q.total() * num_kv_heads; }
+    const qf::RowShape shape{causal != 0, qf::kRowTile / group, group};
+    long long per_head = 0;
+    for (int s = 0; s < n_seq; ++s) per_head += qf::seq_cost(plan(s), shape);
+    const long long total = per_head * num_kv_heads;
     const int n = qf::slices_of(total, n_ctas);
-    auto locate = [&](long long x) {
-        long long before = 0;
+    auto locate = [&](int c) {
+        if (c == n) return qf::SlicePos{0, num_kv_heads, 0, 0};
+        long long rest, before = 0;
+        const int h = qf::head_of(qf::cut_at(total, n, c), per_head, rest);
         for (int s = 0; s < n_seq; ++s) {
-            const qf::SeqPlan q = plan(s);
-            const long long cost = q.n > 0 && q.len > 0 ? q.total() * num_kv_heads : 0;
-            if (x >= before && x < before + cost) return qf::locate_in_seq(q, s, group, x - before);
+            const long long cost = qf::seq_cost(plan(s), shape);
+            if (rest >= before && rest < before + cost) return qf::locate_in_seq(plan(s), shape, s, h, rest - before);
             before += cost;
         }
-        return qf::SlicePos{n_seq, 0, 0, 0};
+        return qf::SlicePos{0, num_kv_heads, 0, 0};
     };
     int count = 0;
     for (int c = 0; total > 0 && c < n; ++c) {
-        qf::SliceWalk<decltype(plan), decltype(first)> walk(plan, first, locate(qf::cut_at(total, n, c)),
-                                                            locate(qf::cut_at(total, n, c + 1)), n_seq, num_kv_heads, c);
+        qf::SliceWalk<decltype(plan), decltype(first)> walk(plan, first, shape, locate(c), locate(c + 1), n_seq, num_kv_heads, c);
         qf::RowsBlock b;
         int nt = 0, tiles = 0;
         while (walk.next(b, nt)) {

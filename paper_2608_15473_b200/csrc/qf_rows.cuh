@@ -95,123 +95,99 @@ inline RowsLayout rows_layout()
 }
 
 // ------------------------------------------------------------------ schedule arithmetic (host and device)
-// The schedule's arithmetic runs a few times per CTA: as functions it stays out of the way of the loops that the
-// instruction cache has to hold.
-#define QF_COLD __noinline__
-// 64-bit divisions of numbers that nearly always fit 32 bits (a 64-bit one is a subroutine of a hundred instructions).
-QF_COLD __host__ __device__ inline long long div_small(long long a, long long b)
+// One axis of units: KV heads in order, for each the sequences in order, for each its row blocks in order.
+#define QF_COLD __noinline__      // rare paths: as functions they leave the instruction cache to the loops
+struct SeqPlan { int n, off, len; };     // rows, positions before row 0, positions in all
+struct RowShape { int causal, tile_rows, group; };   // tile_rows: tokens of a row tile
+__host__ __device__ inline int min_int(int a, int b) { return a < b ? a : b; }
+__host__ __device__ inline int seq_blocks(SeqPlan q, RowShape f)
 {
-    return (((unsigned long long)a | (unsigned long long)b) >> 32) ? a / b : (long long)((unsigned)a / (unsigned)b);
+    return q.n > 0 && q.len > 0 ? (int)(((unsigned)q.n + 2u * f.tile_rows - 1) / (2u * f.tile_rows)) : 0;
 }
-// sum over i < n of floor((a i + b) / m), by the Euclidean recursion (a, b >= 0).
-QF_COLD __host__ __device__ inline long long floor_sum(long long n, long long m, long long a, long long b)
+__host__ __device__ inline int block_rows(SeqPlan q, RowShape f, int j) { return min_int(q.n - j * 2 * f.tile_rows, 2 * f.tile_rows); }
+__host__ __device__ inline int block_tiles(SeqPlan q, RowShape f, int j)
 {
-    long long ans = 0;
-    while (n > 0) {
-        if (a >= m) { const long long d = div_small(a, m); ans += n * (n - 1) / 2 * d; a -= d * m; }
-        if (b >= m) { const long long d = div_small(b, m); ans += n * d; b -= d * m; }
-        const long long y = a * n + b;
-        if (y < m) break;
-        n = div_small(y, m);
-        b = y - n * m;
-        const long long t = m; m = a; a = t;
+    unsigned lim = (unsigned)q.len;
+    if (f.causal) {
+        const unsigned last = (unsigned)q.off + (unsigned)(j * 2 * f.tile_rows + block_rows(q, f, j));
+        if (last < lim) lim = last;
     }
-    return ans;
+    return (int)((lim + kRowTile - 1) / kRowTile);
 }
-struct SeqPlan {
-    int n, off, len, causal;     // rows, positions before row 0, positions in all
-    int tile_rows;               // tokens per row tile
-    __host__ __device__ int block_rows() const { return 2 * tile_rows; }
-    __host__ __device__ int blocks() const { return len > 0 ? (n + block_rows() - 1) / block_rows() : 0; }
-    __host__ __device__ int rows_of(int j) const { const int r = n - j * block_rows(); return r < block_rows() ? r : block_rows(); }
-    __host__ __device__ bool narrow(int j) const { return rows_of(j) <= tile_rows; }
-    __host__ __device__ int tiles(int j) const
-    {
-        long long lim = len;
-        if (causal) {
-            const long long last = (long long)off + (long long)j * block_rows() + rows_of(j);
-            if (last < lim) lim = last;
-        }
-        return (int)((lim + kRowTile - 1) / kRowTile);
-    }
-    __host__ __device__ int weight(int j) const { return narrow(j) ? 1 : 2; }
-    __host__ __device__ long long cost(int j) const { return (long long)weight(j) * tiles(j) + kBlockCost; }
-    // cost of the first j blocks; all but the last are full
-    QF_COLD __host__ __device__ long long cost_before(int j) const
-    {
-        const int full = j < blocks() - 1 ? j : (blocks() - 1 > 0 ? blocks() - 1 : 0);
-        long long t;
-        if (causal) {
-            const long long br = block_rows();
-            long long free = ((long long)len - off) < 0 ? 0 : (long long)((unsigned)(len - off) / (unsigned)br);       // blocks that end at or before the last position
-            free = free > full ? full : free;
-            if (free <= 8) {      // a few 32-bit shifts instead of 64-bit divisions
-                t = 0;
-                for (int i = 1; i <= (int)free; ++i) t += ((unsigned)off + (unsigned)(i * (int)br) + kRowTile - 1) / kRowTile;
-            } else {
-                t = floor_sum(free, kRowTile, br, (long long)off + br + kRowTile - 1);
-            }
-            t += (full - free) * (long long)((len + kRowTile - 1) / kRowTile);
-        } else {
-            t = (long long)full * ((len + kRowTile - 1) / kRowTile);
-        }
-        long long c = 2 * t + (long long)kBlockCost * full;
-        if (j > full) c += cost(full);
-        return c;
-    }
-    __host__ __device__ long long total() const { return cost_before(blocks()); }
-};
-struct SlicePos { int seq, head, block, tile; };   // a cut: this block's tiles below `tile` lie before it
-// Where offset r of block j falls: the tile that a cut there precedes.
-QF_COLD __host__ __device__ inline int place_in_block(const SeqPlan &q, int j, int group, long long r)
+__host__ __device__ inline int block_weight(SeqPlan q, RowShape f, int j) { return block_rows(q, f, j) <= f.tile_rows ? 1 : 2; }
+__host__ __device__ inline int block_cost(SeqPlan q, RowShape f, int j) { return block_weight(q, f, j) * block_tiles(q, f, j) + kBlockCost; }
+__host__ __device__ inline long long seq_cost(SeqPlan q, RowShape f)
 {
-    const long long cost = q.cost(j);
-    // writing and merging a piece costs about as much as this many units of its rows' products
-    const int snap = q.rows_of(j) * group / 32 + 1;
-    const int w = q.weight(j), nt = q.tiles(j);
-    if (r < snap) return 0;
-    if (cost - r < snap) return nt;
-    const long long t = w == 2 ? (r - kBlockCost + 1) >> 1 : r - kBlockCost;
-    return t < 0 ? 0 : t > nt ? nt : (int)t;
+    long long c = 0;
+    const int n = seq_blocks(q, f);
+    for (int j = 0; j < n; ++j) c += block_cost(q, f, j);
+    return c;
 }
-// Position x of one sequence's stretch (heads in order, blocks of a head in order).  On the device the lanes of a warp
-// search the blocks together, 32 prefix sums a round; on the host they are searched one by one.
-QF_COLD __host__ __device__ inline SlicePos locate_in_seq(const SeqPlan &q, int seq, int group, long long x)
-{
-    const long long per_head = q.total();
-    SlicePos p;
-    p.seq = seq;
-    p.head = (int)div_small(x, per_head);
-    long long r = x - p.head * per_head;
-    int lo = 0, hi = q.blocks();          // cost_before(lo) <= r < cost_before(hi)
-#ifdef __CUDA_ARCH__
-    const int lane = threadIdx.x & 31;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 31) / 32, mine = lo + lane * step;
-        const bool below = mine < hi && q.cost_before(mine) <= r;
-        const int n = __popc(__ballot_sync(0xffffffffu, below));
-        lo += (n - 1) * step;
-        hi = hi < lo + step ? hi : lo + step;
-    }
-#else
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (q.cost_before(mid) <= r) lo = mid; else hi = mid;
-    }
-#endif
-    p.block = lo;
-    p.tile = place_in_block(q, lo, group, r - q.cost_before(lo));
-    return p;
-}
-// Cut c of n lies at total * c / n units; n is how many slices the work is worth.
+// How many slices the work is worth, and where cut c of them lies.
 __host__ __device__ inline int slices_of(long long total, int n_ctas)
 {
-    const long long want = div_small(total, kMinSlice);
-    return want < 1 ? 1 : want < n_ctas ? (int)want : n_ctas;
+    return total >= (long long)kMinSlice * n_ctas ? n_ctas : total < kMinSlice ? 1 : (int)((unsigned)total / kMinSlice);
 }
-__host__ __device__ inline long long cut_at(long long total, int n, int c)
+__host__ __device__ inline long long cut_at(long long total, int n, int c) { return (long long)((double)total / n * c); }
+// Position x of the axis: its KV head, and the rest within the head.
+__host__ __device__ inline int head_of(long long x, long long per_head, long long &rest)
 {
-    return div_small(total * c, n);
+    int h = (int)((double)x / (double)per_head);
+    rest = x - h * per_head;
+    if (rest < 0) { --h; rest += per_head; }
+    if (rest >= per_head) { ++h; rest -= per_head; }
+    return h;
+}
+struct SlicePos { int seq, head, block, tile; };   // a cut: this block's tiles below `tile` lie before it
+// Where offset r of block j falls: the tile that a cut there precedes.
+__host__ __device__ inline int place_in_block(SeqPlan q, RowShape f, int j, int r)
+{
+    // writing and merging a piece costs about as much as this many units of its rows' products
+    const int snap = block_rows(q, f, j) * f.group / 32 + 1;
+    const int w = block_weight(q, f, j), nt = block_tiles(q, f, j);
+    if (r < snap) return 0;
+    if (w * nt + kBlockCost - r < snap) return nt;
+    const int t = w == 2 ? (r - kBlockCost + 1) >> 1 : r - kBlockCost;
+    return t < 0 ? 0 : t > nt ? nt : t;
+}
+// Offset r of sequence seq.  On the device the lanes of a warp add up 32 blocks at a time.
+__host__ __device__ inline SlicePos locate_in_seq(SeqPlan q, RowShape f, int seq, int head, long long r)
+{
+    SlicePos p{seq, head, 0, 0};
+    const int n = seq_blocks(q, f);
+#ifdef __CUDA_ARCH__
+    const int lane = threadIdx.x & 31;
+    for (int j0 = 0; j0 < n; j0 += 32) {
+        const int c = j0 + lane < n ? block_cost(q, f, j0 + lane) : 0;
+        int x = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, (long long)x > r);
+        if (past) {
+            const int l = __ffs((int)past) - 1;
+            p.block = j0 + l;
+            p.tile = place_in_block(q, f, p.block, (int)r - __shfl_sync(0xffffffffu, x - c, l));
+            return p;
+        }
+        r -= __shfl_sync(0xffffffffu, x, 31);
+    }
+#else
+    for (int j = 0; j < n; ++j) {
+        const int c = block_cost(q, f, j);
+        if (r < c) {
+            p.block = j;
+            p.tile = place_in_block(q, f, j, (int)r);
+            return p;
+        }
+        r -= c;
+    }
+#endif
+    p.block = n - 1;      // not reached: r lies within the sequence
+    p.tile = block_tiles(q, f, n - 1);
+    return p;
 }
 // The blocks between two cuts, in order.  `plan(s)` gives sequence s's SeqPlan, `first(s)` its first row.
 template <class Plan, class First>
@@ -219,36 +195,45 @@ struct SliceWalk {
     Plan plan;
     First first;
     SlicePos at, end;
-    int n_seq, heads, cta;
+    int n_seq, heads, cta, n_blocks, row0;
+    RowShape f;
     SeqPlan q;
-    int row0;
-    __host__ __device__ SliceWalk(Plan p, First f, SlicePos a, SlicePos z, int n_seq_, int heads_, int cta_)
-        : plan(p), first(f), at(a), end(z), n_seq(n_seq_), heads(heads_), cta(cta_), q(p(a.seq)), row0(f(a.seq)) {}
-    // false: no block is left.  nt: the whole block's tiles.
-    QF_COLD __host__ __device__ bool next(RowsBlock &b, int &nt)
+    __host__ __device__ SliceWalk(Plan p, First fi, RowShape f_, SlicePos a, SlicePos z, int n_seq_, int heads_, int cta_)
+        : plan(p), first(fi), at(a), end(z), n_seq(n_seq_), heads(heads_), cta(cta_), f(f_)
     {
-        while (at.seq < n_seq) {
-            const bool last = at.seq == end.seq && at.head == end.head && at.block == end.block;
-            const int lo = at.tile, hi = last ? end.tile : q.tiles(at.block), j = at.block;
+        q = plan(at.seq);
+        row0 = first(at.seq);
+        n_blocks = seq_blocks(q, f);
+    }
+    // false: no block is left.  nt: the whole block's tiles.
+    __host__ __device__ bool next(RowsBlock &b, int &nt)
+    {
+        while (at.head < heads) {
+            const int j = at.block;
+            const bool last = at.head == end.head && at.seq == end.seq && j == end.block;
+            nt = block_tiles(q, f, j);
+            const int lo = at.tile, hi = last ? end.tile : nt;
             const bool some = lo < hi;
             if (some) {
-                nt = q.tiles(j);
-                b.seq = at.seq; b.head = at.head; b.i0 = j * q.block_rows(); b.row0 = row0 + b.i0;
-                b.rows = q.rows_of(j); b.off = q.off; b.len = q.len; b.t_lo = lo; b.t_hi = hi;
-                b.narrow = q.narrow(j) ? 1 : 0; b.pad = 0;
+                b.seq = at.seq; b.head = at.head; b.i0 = j * 2 * f.tile_rows; b.row0 = row0 + b.i0;
+                b.rows = block_rows(q, f, j); b.off = q.off; b.len = q.len; b.t_lo = lo; b.t_hi = hi;
+                b.narrow = b.rows <= f.tile_rows ? 1 : 0; b.pad = 0;
                 b.slot = (lo == 0 && hi == nt) ? -1 : lo > 0 ? 2 * cta : 2 * cta + 1;
             }
-            if (last) at.seq = n_seq;
+            if (last) at.head = heads;
             else {
                 at.tile = 0;
-                if (++at.block == q.blocks()) {
+                if (++at.block == n_blocks) {
                     at.block = 0;
-                    if (++at.head == heads) {
-                        at.head = 0;
-                        while (++at.seq < n_seq) {
+                    if (n_seq > 1) {      // the next sequence with work, in the next head after the last
+                        do {
+                            if (++at.seq == n_seq) { at.seq = 0; ++at.head; }
                             q = plan(at.seq);
-                            if (q.n > 0 && q.len > 0) { row0 = first(at.seq); break; }
-                        }
+                            n_blocks = seq_blocks(q, f);
+                        } while (n_blocks == 0 && at.head < heads);
+                        row0 = first(at.seq);
+                    } else {
+                        ++at.head;
                     }
                 }
             }
@@ -276,6 +261,7 @@ __device__ __forceinline__ uint32_t desc_lo_k(uint32_t smem_addr) { return ((sme
 // A V page as the B operand (16 positions x 128 channels, channels contiguous): [2 channel halves][16 rows][128 B],
 // 128B swizzle.  Leading offset: the next 64 channels, 2,048 B; stride offset: the next 8 positions, 1,024 B.
 __device__ __forceinline__ uint32_t desc_lo_v(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | ((uint32_t)(2048 >> 4) << 16); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // D[tmem] (+)= A[smem] . B[smem]^T
 template <bool ACC>
 __device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc)
@@ -498,12 +484,18 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8) tmem_alloc(smem_u32(&sm.tmem_base), 512);
+    if (tid == 0) {
+        prefetch_map(&maps.q);
+        prefetch_map(&maps.k);
+        prefetch_map(&maps.v);
+    }
     grid_dependency_wait();
     grid_launch_dependents();
 
+    const RowShape shape{PREFIX ? 0 : 1, tile_rows, G};
     auto seq_plan = [&](int s) -> SeqPlan {
         const SeqRows r = seq_rows<PREFIX>(A, s);
-        return SeqPlan{r.n, r.off, r.len, PREFIX ? 0 : 1, tile_rows};
+        return SeqPlan{r.n, r.off, r.len};
     };
     auto give_up = [&]() {      // a bounded wait ran out (or another warp's did)
         sm.abort_flag = 1;
@@ -532,17 +524,26 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         }
     }
 
-    // ---- this CTA's slice
+    // ---- this CTA's slice.  A thread adds up a sequence's blocks, or a warp does while there are no more sequences
+    // than warps.
     const int n_ctas = (int)gridDim.x;
-    long long total = 0;
-    long long first_cost = 0, first_before = 0;       // of this thread's sequence in the first round
-    for (int base = 0; base < A.n_seq; base += kRowsThreads) {
-        const int s = base + tid;
-        long long cost = 0;
-        if (s < A.n_seq) {
-            const SeqPlan q = seq_plan(s);
-            if (q.n > 0 && q.len > 0) cost = q.total() * Hkv;
+    constexpr int kWarps = kRowsThreads / 32;
+    if (A.n_seq <= kWarps) {
+        if (warp < A.n_seq) {
+            const SeqPlan q = seq_plan(warp);
+            const int n = seq_blocks(q, shape);
+            long long c = 0;
+            for (int j = lane; j < n; j += 32) c += block_cost(q, shape, j);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+            if (lane == 0) sm.scan[warp] = c;
         }
+        __syncthreads();
+    }
+    long long per_head = 0;      // units of one KV head
+    // (units before sequence base + tid, its own units); adds the round's total to per_head
+    auto scan_round = [&](int base, long long &before, long long &cost) {
+        cost = base + tid < A.n_seq ? seq_cost(seq_plan(base + tid), shape) : 0;
         long long x = cost;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -551,55 +552,53 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         }
         if (lane == 31) sm.scan[warp] = x;
         __syncthreads();
-        long long before = total;
-        for (int w = 0; w < kRowsThreads / 32; ++w) {
+        before = per_head + x - cost;
+        for (int w = 0; w < kWarps; ++w) {
             if (w < warp) before += sm.scan[w];
-            total += sm.scan[w];
+            per_head += sm.scan[w];
         }
-        if (base == 0) { first_cost = cost; first_before = before + x - cost; }
         __syncthreads();
+    };
+    long long before0 = 0, cost0 = 0;       // of the first round
+    if (A.n_seq <= kWarps) {
+        for (int s = 0; s < A.n_seq; ++s) {
+            if (s == tid) { before0 = per_head; cost0 = sm.scan[s]; }
+            per_head += sm.scan[s];
+        }
+    } else {
+        for (int base = 0; base < A.n_seq; base += kRowsThreads) {
+            long long before, cost;
+            scan_round(base, before, cost);
+            if (base == 0) { before0 = before; cost0 = cost; }
+        }
     }
+    const long long total = per_head * Hkv;
     const int n_eff = slices_of(total, n_ctas);
     const int me = (int)blockIdx.x;
     const bool working = total > 0 && me < n_eff;
     if (working) {
-        const long long xa = cut_at(total, n_eff, me), xb = cut_at(total, n_eff, me + 1);
+        long long ra, rb;
+        const int ha = head_of(cut_at(total, n_eff, me), per_head, ra);
+        const int hb = me + 1 < n_eff ? head_of(cut_at(total, n_eff, me + 1), per_head, rb) : (rb = -1, Hkv);
         auto offer = [&](int s, long long before, long long cost) {
-            if (cost > 0 && xa >= before && xa < before + cost) { sm.cut_seq[0] = s; sm.cut_rest[0] = xa - before; }
-            if (cost > 0 && xb >= before && xb < before + cost) { sm.cut_seq[1] = s; sm.cut_rest[1] = xb - before; }
+            if (ra >= before && ra < before + cost) { sm.cut_seq[0] = s; sm.cut_rest[0] = ra - before; }
+            if (rb >= before && rb < before + cost) { sm.cut_seq[1] = s; sm.cut_rest[1] = rb - before; }
         };
         if (A.n_seq <= kRowsThreads) {
-            if (tid < A.n_seq) offer(tid, first_before, first_cost);
+            offer(tid, before0, cost0);
         } else {
-            long long run = 0;
+            per_head = 0;
             for (int base = 0; base < A.n_seq; base += kRowsThreads) {
-                const int s = base + tid;
-                long long cost = 0;
-                if (s < A.n_seq) {
-                    const SeqPlan q = seq_plan(s);
-                    if (q.n > 0 && q.len > 0) cost = q.total() * Hkv;
-                }
-                long long x = cost;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const long long y = __shfl_up_sync(0xffffffffu, x, o);
-                    if (lane >= o) x += y;
-                }
-                if (lane == 31) sm.scan[warp] = x;
-                __syncthreads();
-                long long before = run;
-                for (int w = 0; w < kRowsThreads / 32; ++w) {
-                    if (w < warp) before += sm.scan[w];
-                    run += sm.scan[w];
-                }
-                offer(s, before + x - cost, cost);
-                __syncthreads();
+                long long before, cost;
+                scan_round(base, before, cost);
+                offer(base + tid, before, cost);
             }
         }
         __syncthreads();
         if (warp < 2) {
-            SlicePos at{A.n_seq, 0, 0, 0};                  // the end of everything
-            if (sm.cut_seq[warp] >= 0) at = locate_in_seq(seq_plan(sm.cut_seq[warp]), sm.cut_seq[warp], G, sm.cut_rest[warp]);
+            SlicePos at{0, Hkv, 0, 0};                      // the end of everything
+            if (sm.cut_seq[warp] >= 0)
+                at = locate_in_seq(seq_plan(sm.cut_seq[warp]), shape, sm.cut_seq[warp], warp ? hb : ha, sm.cut_rest[warp]);
             if (lane == 0) sm.cut[warp] = at;
         }
     }
@@ -627,7 +626,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 ++idx;
             };
             auto first = [&](int s) { return seq_rows<PREFIX>(A, s).first; };
-            SliceWalk<decltype(seq_plan), decltype(first)> walk(seq_plan, first, a, z, A.n_seq, Hkv, me);
+            SliceWalk<decltype(seq_plan), decltype(first)> walk(seq_plan, first, shape, a, z, A.n_seq, Hkv, me);
             RowsBlock b;
             int nt = 0;
             while (ok && walk.next(b, nt)) {
@@ -652,6 +651,10 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         bool ok = true;
         const int none_row = (int)(P.kv_nhd ? P.num_pages * kPageSize : P.num_pages * Hkv * kPageSize);   // out of range: zeros
         const uint32_t q_box = (uint32_t)(64 * 2) * G * tile_rows;
+        if (A.table) {      // the first block's table entries, while the schedule names it
+            const int at = sm.cut[0].tile * kTilePages + lane;
+            if (at < A.table_width) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.table + (size_t)sm.cut[0].seq * A.table_width + at));
+        }
         for (; ok; ++idx) {
             const int slot = idx % kInfoRing;
             if (!warp_wait(smem_u32(&sm.info_full[slot]), (uint32_t)((idx / kInfoRing) & 1), abort_flag)) { ok = false; break; }
