@@ -420,14 +420,23 @@ def project_status(workspace, stream=None) -> int:
     return int(st.value)
 
 
+_many_gpus: Optional[bool] = None
+
+
 def _on_current_device(*tensors) -> None:
     """The calls below launch on the current device: a tensor of another one is refused, not dereferenced there."""
-    import torch
-    here = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    global _many_gpus
+    if _many_gpus is None:
+        import torch
+        _many_gpus = torch.cuda.device_count() > 1
     for x in tensors:
-        dev = getattr(x, "device", None)
-        if dev is not None and (dev.type != "cuda" or (here is not None and dev.index != here)):
-            raise ValueError(f"expected a tensor on the current CUDA device ({here}), got one on {dev}")
+        if hasattr(x, "is_cuda"):
+            if not x.is_cuda:
+                raise ValueError(f"expected a CUDA tensor, got one on {x.device}")
+            if _many_gpus:
+                import torch
+                if x.get_device() != torch.cuda.current_device():
+                    raise ValueError(f"expected a tensor on the current device (cuda:{torch.cuda.current_device()}), got one on {x.device}")
 
 
 def rope_frequencies(rotary_dim: int = 128, theta: float = 1e6, scaling: str = "plain", factor: float = 1.0,

@@ -119,17 +119,12 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
     A.n_q = q ? (int)Hq : 0; A.n_k = k ? (int)Hkv : 0;
     A.rows = A.n_q + A.n_k + (cache ? (int)Hkv : 0);
     A.eps = r->eps; A.rot_scale = r->rot_scale;
-    // rows per item: a token's angles are computed once per item, so many rows when there is work for every SM and
-    // one when there is not
-    A.rows_per_item = 16;
-    while (A.rows_per_item > 1 &&
-           (long long)A.total_tokens * ((A.rows + A.rows_per_item - 1) / A.rows_per_item) < 64ll * sms) A.rows_per_item /= 2;
-    A.items_per_token = (A.rows + A.rows_per_item - 1) / A.rows_per_item;
-    const long long items = (long long)A.total_tokens * A.items_per_token;
-    const long long blocks = (items + qf::kRopeItemsPerCta - 1) / qf::kRopeItemsPerCta;
-    if (blocks > 0x7fffffffll) return QF_ERR_UNSUPPORTED;
-    cudaError_t e = qf::launch_pdl(qf::rope_append_kernel, dim3((unsigned)blocks), dim3(qf::kRopeThreads), 0,
-                                   (cudaStream_t)cuda_stream, A, qf_host::dev_params(p));
+    // one token per CTA until there are several for every SM, then steps of more: fewer, longer row lists per group
+    A.tokens_per_cta = 1;
+    while (A.tokens_per_cta < qf::kRopeMaxTokens && A.total_tokens >= 8 * A.tokens_per_cta * sms) A.tokens_per_cta *= 2;
+    const long long steps = ((long long)A.total_tokens + A.tokens_per_cta - 1) / A.tokens_per_cta;
+    const long long blocks = std::min<long long>(steps, (long long)qf::kRopeCtasPerSm * sms);
+    cudaError_t e = qf::launch_rope(A, qf_host::dev_params(p), (unsigned)blocks, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) return qf_host::cuda_fail(e, "rope_append_kernel launch");
     qf_host::set_launches(1);
     return QF_OK;
