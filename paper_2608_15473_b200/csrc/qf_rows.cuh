@@ -48,7 +48,7 @@
 namespace qf {
 
 #ifndef QF_BC
-#define QF_BC 5
+#define QF_BC 7
 #endif
 constexpr int kRowTile = 128;                    // query rows of a tile, and cached positions of a tile
 constexpr int kTilePages = kRowTile / kPageSize;
@@ -429,7 +429,7 @@ __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const 
 {
     const int common = min(b.off + b.i0 + 1, b.len);
 #pragma unroll 1
-    for (int pos = max(b.t_lo, common / kRowTile) * kRowTile; pos < min(lim, b.t_hi * kRowTile); ++pos) {
+    for (int pos = max(b.t_lo * kRowTile, common / kPageSize * kPageSize); pos < min(lim, b.t_hi * kRowTile); ++pos) {
         const long long at = (long long)b.seq * A.table_width + (pos >> 4);
         const long long phys = A.table ? (long long)A.table[at] : at;
         if (phys < 0 || phys >= P.num_pages) continue;
@@ -840,8 +840,9 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 __syncwarp();
                 if (!PREFIX && (t + 1) * kRowTile > common) {
                     unsigned seen = 0;
-#pragma unroll 8
-                    for (int i = lane; i < kTileBytes / 16; i += 32) {
+                    const int from = max(common - t * kRowTile, 0) / kPageSize * (kPageBytes / 16);   // pages with a hidden row
+#pragma unroll 4
+                    for (int i = from + lane; i < kTileBytes / 16; i += 32) {
                         const uint4 x = *reinterpret_cast<const uint4 *>(v + i * 16);
                         seen |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) |
                                 ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
@@ -850,7 +851,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                         if (lane == 0) *reinterpret_cast<volatile int *>(&sm.dirty[slot]) = 1;
                         __threadfence_block();      // said before the first value is gone: the other warp may find none left
                         __syncwarp();
-                        for (int i = lane; i < kTileBytes / 2; i += 32) {
+                        for (int i = from * 8 + lane; i < kTileBytes / 2; i += 32) {
                             uint16_t *x = reinterpret_cast<uint16_t *>(v) + i;
                             if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
                         }
@@ -1130,30 +1131,8 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             float *slot_base = b.slot >= 0 ? slots + (size_t)b.slot * kRowsSlotFloats : nullptr;
             const int slot_row = (b.narrow ? 0 : wg * kRowTile) + r;
             const bool dirty = !PREFIX && *reinterpret_cast<volatile int *>(&sm.dirty[slot]) != 0;
-#pragma unroll 1
-            for (int c = c0; c < c1; ++c) {
-                float o[32];
-                tmem_ld32_nowait(t_o + c * 32, o);
-                if (b.narrow) {
-                    float x[32];
-                    tmem_ld32_nowait(t_x + c * 32, x);
-                    tmem_wait_ld();
-                    pin32(o);
-                    pin32(x);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        o[i] = w_own == 0.f ? 0.f : o[i] * w_own;
-                        o[i] = w_other == 0.f ? o[i] : fmaf(x[i], w_other, o[i]);
-                    }
-                } else {
-                    tmem_wait_ld();
-                    pin32(o);
-                    if (!started) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = 0.f;
-                    }
-                }
-                if (!live) continue;
+            auto finish = [&](int c, const float (&o)[32]) {
+                if (!live) return;
                 if (b.slot >= 0) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
@@ -1171,6 +1150,39 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                         if (PREFIX) st_global_32b(A.o_part + out_row * kHeadDim + c * 32 + i, w);
                         else st_global_32b(A.out + out_row * kHeadDim + c * 32 + i, w);
                     }
+                }
+            };
+            if (!b.narrow) {
+#pragma unroll
+                for (int c = 0; c < 4; c += 2) {
+                    float o[2][32];
+                    tmem_ld32_nowait(t_o + c * 32, o[0]);
+                    tmem_ld32_nowait(t_o + c * 32 + 32, o[1]);
+                    tmem_wait_ld();
+                    pin32(o[0]);
+                    pin32(o[1]);
+                    if (!started) {      // nothing visible: the accumulator may hold anything
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) o[i >> 5][i & 31] = 0.f;
+                    }
+                    finish(c, o[0]);
+                    finish(c + 1, o[1]);
+                }
+            } else {
+#pragma unroll 1
+                for (int c = c0; c < c1; ++c) {
+                    float o[32], x[32];
+                    tmem_ld32_nowait(t_o + c * 32, o);
+                    tmem_ld32_nowait(t_x + c * 32, x);
+                    tmem_wait_ld();
+                    pin32(o);
+                    pin32(x);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        o[i] = w_own == 0.f ? 0.f : o[i] * w_own;
+                        o[i] = w_other == 0.f ? o[i] : fmaf(x[i], w_other, o[i]);
+                    }
+                    finish(c, o);
                 }
             }
             if (dirty && live) add_hidden(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
