@@ -9,9 +9,10 @@
 // shared memory (A and B operands are both read from it) would bound the products.  While one tile's 128 softmax
 // threads (one per row, no shuffles) turn S into P, the tensor cores work on the other tile.  P goes back to tensor
 // memory over S and is the A operand of the second product from there.  A block with no more rows than one tile
-// ("narrow": a few decode tokens, a small group of requests) has the two softmax groups take alternate position
-// tiles of the same rows instead, each with an accumulator of its own, merged at the block's end: a lone tile's
-// chain product -> softmax -> product would leave the K/V stream waiting.
+// ("narrow": a few decode tokens, a small group of requests) has the two softmax groups take the two halves of every
+// position tile for the same rows instead, each with an accumulator of its own, merged at the block's end: a lone
+// tile's chain product -> softmax -> product would leave the K/V stream waiting.  (Whole tiles in turn held four of the
+// five tiles of the ring at a time: 2,600 cycles per tile against 1,600.)
 //
 // Roles (384 threads, one CTA per SM): warps 0-3 and 4-7 softmax of the two tiles (and their epilogues), warps 8 and 9
 // issue the products of one tile each, warp 10 loads (TMA, 5 tiles of 32 KB in flight or in use), warp 11 walks the
@@ -47,9 +48,6 @@
 
 namespace qf {
 
-#ifndef QF_BC
-#define QF_BC 7
-#endif
 constexpr int kRowTile = 128;                    // query rows of a tile, and cached positions of a tile
 constexpr int kTilePages = kRowTile / kPageSize;
 constexpr int kUnit = 64;                        // positions of one product S = Q K^T and of one softmax pass
@@ -59,8 +57,12 @@ constexpr int kTileBytes = kRowTile * kHeadDim * 2;
 constexpr int kHalfPageBytes = kPageBytes / 2;    // 16 rows x 64 channels
 constexpr int kInfoRing = 4;
 constexpr int kRowsMaxCtas = 160;                // one per SM
-constexpr int kBlockCost = QF_BC;                    // units a block costs beside its tiles
-constexpr int kMinSlice = 3;                     // units: less per CTA is not worth a merge
+// What things cost, in units of about 400 cycles (fitted to the cycles of some 7,000 slices of random batches, to 4 %):
+// a position tile of two row tiles 3,150 cycles and of one 2,560 (it reads as much K and V: HBM is what it waits for),
+// and what a block costs beside its tiles 7,500 and 5,000.
+constexpr int kWideTileCost = 8, kNarrowTileCost = 6, kWideBlockCost = 18, kNarrowBlockCost = 12;
+constexpr int kMinSlice = 12;                    // less per CTA is not worth a merge
+constexpr int kWideSnap = 18, kNarrowSnap = 6;   // a cut this close to a block's border moves there
 constexpr float kRescaleLog2 = 8.f;
 // Of every 8 pairs of scores, how many take their exponentials from the multiply-add units.
 #ifndef QF_ROWS_POLY
@@ -114,8 +116,12 @@ __host__ __device__ inline int block_tiles(SeqPlan q, RowShape f, int j)
     }
     return (int)((lim + kRowTile - 1) / kRowTile);
 }
-__host__ __device__ inline int block_weight(SeqPlan q, RowShape f, int j) { return block_rows(q, f, j) <= f.tile_rows ? 1 : 2; }
-__host__ __device__ inline int block_cost(SeqPlan q, RowShape f, int j) { return block_weight(q, f, j) * block_tiles(q, f, j) + kBlockCost; }
+__host__ __device__ inline bool block_is_wide(SeqPlan q, RowShape f, int j) { return block_rows(q, f, j) > f.tile_rows; }
+__host__ __device__ inline int block_cost(SeqPlan q, RowShape f, int j)
+{
+    const int nt = block_tiles(q, f, j);
+    return block_is_wide(q, f, j) ? kWideTileCost * nt + kWideBlockCost : kNarrowTileCost * nt + kNarrowBlockCost;
+}
 __host__ __device__ inline long long seq_cost(SeqPlan q, RowShape f)
 {
     long long c = 0;
@@ -142,12 +148,12 @@ struct SlicePos { int seq, head, block, tile; };   // a cut: this block's tiles 
 // Where offset r of block j falls: the tile that a cut there precedes.
 __host__ __device__ inline int place_in_block(SeqPlan q, RowShape f, int j, int r)
 {
-    // writing and merging a piece costs about as much as this many units of its rows' products
-    const int snap = block_rows(q, f, j) * f.group / 32 + 1;
-    const int w = block_weight(q, f, j), nt = block_tiles(q, f, j);
+    const bool wide = block_is_wide(q, f, j);
+    const int snap = wide ? kWideSnap : kNarrowSnap, each = wide ? kWideTileCost : kNarrowTileCost, fixed = wide ? kWideBlockCost : kNarrowBlockCost;
+    const int nt = block_tiles(q, f, j);
     if (r < snap) return 0;
-    if (w * nt + kBlockCost - r < snap) return nt;
-    const int t = w == 2 ? (r - kBlockCost + 1) >> 1 : r - kBlockCost;
+    if (each * nt + fixed - r < snap) return nt;
+    const int t = (r - fixed + each - 1) / each;
     return t < 0 ? 0 : t > nt ? nt : t;
 }
 // Offset r of sequence seq.  On the device the lanes of a warp add up 32 blocks at a time.
@@ -782,17 +788,15 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 tc_fence_after();
                 return true;
             };
-            // This warp is done with the ring's next tile: when its products so far are (or at once, if it is the other's).
-            auto release = [&](bool own) {
-                if (elect_one()) {
-                    if (own) umma_commit(bar_empty + stage * 8);
-                    else mbar_arrive(bar_empty + stage * 8);
-                }
+            // This warp is done with the ring's next tile when its products so far are.
+            auto release = [&]() {
+                if (elect_one()) umma_commit(bar_empty + stage * 8);
                 if (++stage == kRowsRing) { stage = 0; phase ^= 1; }
             };
-            // S[h] = Q (K half h)^T: the unit's slot is its half
-            auto qk = [&](int h, int at) {
-                const uint32_t k = k_lo + at * (kTileBytes >> 4) + h * (kUnit * 128 >> 4), d = t_s + h * kUnit;
+            // A unit's slot: its half of the tile, or, narrow, where a group has one half of every tile, the tile's parity.
+            // S[slot] = Q (K half h)^T
+            auto qk = [&](int h, int sl, int at) {
+                const uint32_t k = k_lo + at * (kTileBytes >> 4) + h * (kUnit * 128 >> 4), d = t_s + sl * kUnit;
                 if (elect_one()) {
                     umma_ss<false>(d, q_at, k, idesc_qk);
 #pragma unroll
@@ -800,15 +804,15 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                         const uint32_t o = ((kk >> 2) * (kTileBytes / 2) + (kk & 3) * 32) >> 4;
                         umma_ss<true>(d, q_at + o, k + o, idesc_qk);
                     }
-                    umma_commit(bar_s + h * 8);
+                    umma_commit(bar_s + sl * 8);
                 }
             };
-            // O += P[h] (V half h)
-            auto pv = [&](int h, int at, bool first, bool last) {
-                if (!warp_wait(bar_p + h * 8, (p_phase >> h) & 1, abort_flag)) { ok = false; return; }
-                p_phase ^= 1u << h;
+            // O += P[slot] (V half h)
+            auto pv = [&](int h, int sl, int at, bool first, bool last) {
+                if (!warp_wait(bar_p + sl * 8, (p_phase >> sl) & 1, abort_flag)) { ok = false; return; }
+                p_phase ^= 1u << sl;
                 tc_fence_after();
-                const uint32_t v = v_lo + at * (kTileBytes >> 4) + h * ((kUnit / kPageSize) * kPageBytes >> 4), pa = t_s + h * kUnit;
+                const uint32_t v = v_lo + at * (kTileBytes >> 4) + h * ((kUnit / kPageSize) * kPageBytes >> 4), pa = t_s + sl * kUnit;
                 const uint32_t acc = first ? 0u : 1u;
                 if (elect_one()) {
 #pragma unroll
@@ -871,15 +875,18 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             const int ahead = b.narrow ? 2 : 1;      // tiles between the values in use and the keys
             for (int t = b.t_lo; t < b.t_hi && t < b.t_lo + ahead; ++t) {
                 if (!take(stage, phase)) break;
-                const bool own = !b.narrow || ((t - b.t_lo) & 1) == w;
-                if (own && 2 * t < end) qk(0, stage);
-                if (own && 2 * t + 1 < end) qk(1, stage);
-                release(own);
+                if (b.narrow) {
+                    if (2 * t + w < end) qk(w, t & 1, stage);
+                } else {
+                    if (2 * t < end) qk(0, 0, stage);
+                    if (2 * t + 1 < end) qk(1, 1, stage);
+                }
+                release();
             }
             if (ok && b.t_hi - b.t_lo <= ahead) q_done();
             // The tiles with nothing special about them (every unit there, nothing to clean, keys to come): one thread, no
             // votes, constants where the operands allow it.
-            int t_plain = min(b.t_hi - ahead, (end - 2 * ahead) / 2);
+            int t_plain = min(b.t_hi - ahead, b.narrow ? (end - w - 3) >> 1 : (end - 2) >> 1);
             if (!PREFIX) t_plain = min(t_plain, common / kRowTile);
             else if (b.len & 15) t_plain = min(t_plain, b.len / kRowTile);
             t_plain = max(t_plain, b.t_lo);
@@ -900,71 +907,76 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                         wait(bar_full + at * 8, ph);
                         if (!fine) break;
                         tc_fence_after();
-                        if (!b.narrow || ((t - b.t_lo) & 1) == w) {
-                            const uint32_t v = v_lo + v_at * (kTileBytes >> 4), k = k_lo + at * (kTileBytes >> 4);
-                            const uint32_t acc = t >= b.t_lo + ahead ? 1u : 0u;
+                        const uint32_t v = v_lo + v_at * (kTileBytes >> 4), k = k_lo + at * (kTileBytes >> 4);
+                        const uint32_t acc = t > b.t_lo ? 1u : 0u;
+                        auto unit = [&](int h, int sl, uint32_t first_acc) {
+                            wait(bar_p + sl * 8, (pp >> sl) & 1);
+                            if (!fine) return;
+                            tc_fence_after();
+                            const uint32_t v_h = v + h * (4 * kPageBytes >> 4), k_h = k + h * (kUnit * 128 >> 4), slot_at = t_s + sl * kUnit;
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                wait(bar_p + h * 8, (pp >> h) & 1);
-                                if (!fine) break;
-                                tc_fence_after();
+                            for (int part = 0; part < (PREFIX ? 2 : 1); ++part)
 #pragma unroll
-                                for (int part = 0; part < (PREFIX ? 2 : 1); ++part)
+                                for (int kk = 0; kk < 4; ++kk)
+                                    umma_ts(t_o, slot_at + part * 32 + kk * 8, v_h + kk * (kPageBytes >> 4), idesc_pv, part == 0 && kk == 0 ? first_acc : 1u);
+                            umma_commit(bar_o);
 #pragma unroll
-                                    for (int kk = 0; kk < 4; ++kk)
-                                        umma_ts(t_o, t_s + h * kUnit + part * 32 + kk * 8, v + (h * 4 + kk) * (kPageBytes >> 4), idesc_pv,
-                                                h == 0 && part == 0 && kk == 0 ? acc : 1u);
-                                umma_commit(bar_o);
-#pragma unroll
-                                for (int kk = 0; kk < 8; ++kk) {
-                                    const uint32_t o = ((kk >> 2) * (kTileBytes / 2) + (kk & 3) * 32) >> 4;
-                                    if (kk == 0) umma_ss<false>(t_s + h * kUnit, q_at + o, k + h * (kUnit * 128 >> 4) + o, idesc_qk);
-                                    else umma_ss<true>(t_s + h * kUnit, q_at + o, k + h * (kUnit * 128 >> 4) + o, idesc_qk);
-                                }
-                                umma_commit(bar_s + h * 8);
+                            for (int kk = 0; kk < 8; ++kk) {
+                                const uint32_t o = ((kk >> 2) * (kTileBytes / 2) + (kk & 3) * 32) >> 4;
+                                if (kk == 0) umma_ss<false>(slot_at, q_at + o, k_h + o, idesc_qk);
+                                else umma_ss<true>(slot_at, q_at + o, k_h + o, idesc_qk);
                             }
-                            if (!fine) break;
-                            pp ^= 3;
-                            umma_commit(bar_empty + v_at * 8);
-                            umma_commit(bar_empty + at * 8);
+                            umma_commit(bar_s + sl * 8);
+                            pp ^= 1u << sl;
+                        };
+                        if (b.narrow) {
+                            unit(w, t & 1, acc);
                         } else {
-                            mbar_arrive(bar_empty + v_at * 8);
-                            mbar_arrive(bar_empty + at * 8);
+                            unit(0, 0, acc);
+                            if (fine) unit(1, 1, 1u);
                         }
+                        if (!fine) break;
+                        umma_commit(bar_empty + v_at * 8);
+                        umma_commit(bar_empty + at * 8);
                         if (++at == kRowsRing) { at = 0; ph ^= 1; }
                     }
                 }
                 if (!__all_sync(0xffffffffu, fine)) { ok = false; break; }
                 // where that thread has got to
                 const int n = t_plain - b.t_lo;
-                const int mine = b.narrow ? (w == 0 ? (n + 1) / 2 : n / 2) : n;
-                if (mine & 1) p_phase ^= 3;
+                if (!b.narrow) {
+                    if (n & 1) p_phase ^= 3;
+                } else {
+                    if (((n + 1) >> 1) & 1) p_phase ^= 1u << (b.t_lo & 1);
+                    if ((n >> 1) & 1) p_phase ^= 2u >> (b.t_lo & 1);
+                }
                 const int moved = stage + 2 * n;
                 phase ^= (uint32_t)((moved / kRowsRing) & 1);
                 stage = moved % kRowsRing;
             }
             if (ok && t_plain > b.t_lo && t_plain + ahead == b.t_hi) q_done();
             for (int t = t_plain; ok && t < b.t_hi; ++t) {
-                const bool more = t + ahead < b.t_hi, own = !b.narrow || ((t - b.t_lo) & 1) == w;
+                const bool more = t + ahead < b.t_hi;
                 const int v_at = stage, k_at = stage + 1 == kRowsRing ? 0 : stage + 1;
                 const uint32_t v_phase = phase, k_phase = k_at ? phase : phase ^ 1;
                 if (!take(v_at, v_phase)) break;
-                if (own && needs_clean(t)) clean_values(t, v_at);
+                if (needs_clean(t)) clean_values(t, v_at);
                 if (more && !take(k_at, k_phase)) break;
-                if (own) {
+                if (b.narrow) {
+                    const int u = 2 * t + w, sl = t & 1;
+                    if (u < end) pv(w, sl, v_at, t == b.t_lo, u + 2 >= end);
+                    if (ok && more && u + 4 < end) qk(w, sl, k_at);
+                } else {
                     const int left = end - 2 * t;      // units of this group from this tile on
-                    const int next = left - 2 * ahead;
-                    const bool tail = t + ahead >= b.t_hi;      // its last tile (narrow: every second one is its own)
-                    const bool fresh = t < b.t_lo + ahead;
-                    if (left > 0) pv(0, v_at, fresh, left == 1);
-                    if (ok && more && next > 0) qk(0, k_at);
-                    if (ok && left > 1) pv(1, v_at, false, b.narrow ? tail : left == 2);
-                    if (ok && more && next > 1) qk(1, k_at);
+                    if (left > 0) pv(0, 0, v_at, t == b.t_lo, left == 1);
+                    if (ok && more && left > 2) qk(0, 0, k_at);
+                    if (ok && left > 1) pv(1, 1, v_at, false, left == 2);
+                    if (ok && more && left > 3) qk(1, 1, k_at);
                 }
                 if (!ok) break;
-                release(own);
+                release();
                 if (more) {
-                    release(own);
+                    release();
                     if (t + ahead + 1 == b.t_hi) q_done();
                 }
             }
@@ -1003,11 +1015,11 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             const int u_end = unit_end<PREFIX>(b, wg, tile_rows);
             float m_ref = neg_inf(), m_true = neg_inf(), l = 0.f;
             bool started = false;
-            for (int u = 2 * (b.t_lo + (b.narrow ? wg : 0)); u < u_end; u += (b.narrow && (u & 1)) ? 3 : 1) {
-                const int h = u & 1;
-                const uint32_t t_u = t_s + h * kUnit;
-                if (!warp_wait(smem_u32(&sm.s_full[wg][h]), (s_phase >> h) & 1, abort_flag)) { ok = false; break; }
-                s_phase ^= 1u << h;
+            for (int u = 2 * b.t_lo + (b.narrow ? wg : 0); u < u_end; u += b.narrow ? 2 : 1) {
+                const int h = u & 1, sl = b.narrow ? (u >> 1) & 1 : h;      // half of the tile, slot of the scores
+                const uint32_t t_u = t_s + sl * kUnit;
+                if (!warp_wait(smem_u32(&sm.s_full[wg][sl]), (s_phase >> sl) & 1, abort_flag)) { ok = false; break; }
+                s_phase ^= 1u << sl;
                 tc_fence_after();
                 float s[kUnit];
                 tmem_ld32_nowait(t_u, s);
@@ -1088,7 +1100,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[wg][h]));
+                if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[wg][sl]));
                 ++o_count;       // one product of this group's O per unit
             }
             if (!ok) break;
