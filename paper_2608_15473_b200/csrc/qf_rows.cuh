@@ -64,6 +64,11 @@ constexpr int kWideTileCost = 8, kNarrowTileCost = 6, kWideBlockCost = 18, kNarr
 constexpr int kMinSlice = 12;                    // less per CTA is not worth a merge
 constexpr int kWideSnap = 18, kNarrowSnap = 6;   // a cut this close to a block's border moves there
 constexpr float kRescaleLog2 = 8.f;
+// Units after which a group's accumulator is set aside and begun anew.  The tensor cores cut off what does not fit when
+// they add a product to an accumulator, so a long chain drifts towards zero: 1.6e-8 of the value per 16-position step
+// (measured: -1.4e-5 after 55 tiles of a prefix).  Prefix states are fp32, and an addition every 2,048 positions, in
+// fp32 and rounded, keeps the drift at 4e-6 for 5 % of the time; prompts' bf16 results want it only after 65,536.
+template <bool PREFIX> constexpr int kChainUnits = PREFIX ? 32 : 1024;
 // Of every 8 pairs of scores, how many take their exponentials from the multiply-add units.
 #ifndef QF_ROWS_POLY
 #define QF_ROWS_POLY 2
@@ -84,14 +89,17 @@ struct __align__(16) RowsBlock {
     int pad;
 };
 // What a CTA leaves for the merge kernel: the block it began but did not finish, and whether its first piece ended one.
-struct __align__(16) RowsRecord { RowsBlock tail; int has_tail, head_state; int pad[2]; };   // head_state: 0 none, 1 goes on, 2 ends
-struct RowsLayout { size_t record_off, slot_off, total; };
+struct __align__(16) RowsRecord { RowsBlock tail; int has_tail, head_state; int pad[2]; };
+static_assert(sizeof(RowsRecord) == 64 && sizeof(RowsBlock) == 48, "the merge kernel reads records as four 16-byte words");   // head_state: 0 none, 1 goes on, 2 ends
+struct RowsLayout { size_t record_off, aside_off, slot_off, total; };
+constexpr size_t kRowsAsideFloats = (size_t)2 * kRowTile * kHeadDim;         // per CTA: both groups' accumulators set aside
 constexpr size_t kRowsSlotFloats = (size_t)2 * kRowTile * (kHeadDim + 4);   // O, then m (log2 units), sum, true maximum
 inline RowsLayout rows_layout()
 {
     RowsLayout L;
     L.record_off = 256;
-    L.slot_off = (L.record_off + kRowsMaxCtas * sizeof(RowsRecord) + 255) & ~(size_t)255;
+    L.aside_off = (L.record_off + kRowsMaxCtas * sizeof(RowsRecord) + 255) & ~(size_t)255;
+    L.slot_off = L.aside_off + kRowsMaxCtas * kRowsAsideFloats * sizeof(float);
     L.total = (L.slot_off + 2 * kRowsMaxCtas * kRowsSlotFloats * sizeof(float) + 255) & ~(size_t)255;
     return L;
 }
@@ -428,6 +436,42 @@ struct RowsSmem {
 };
 static_assert(sizeof(RowsSmem) <= 227 * 1024, "one CTA per SM");
 
+// A thread's row of an accumulator plus f times the part set aside (if any), into memory or back into tensor memory.
+// All 32 lanes call it together.
+__device__ QF_COLD void exchange_aside(uint32_t t_o, float *aside, bool has_aside, bool to_memory, float f)
+{
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        float4 *at = reinterpret_cast<float4 *>(aside + (size_t)c * 8 * kRowTile * 4);      // [channels / 4][row]
+        float4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = has_aside ? __ldcg(at + i * kRowTile) : make_float4(0.f, 0.f, 0.f, 0.f);
+        float o[32];
+        tmem_ld32_nowait(t_o + c * 32, o);
+        tmem_wait_ld();
+        pin32(o);
+        if (has_aside) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                o[4 * i] = fmaf(x[i].x, f, o[4 * i]); o[4 * i + 1] = fmaf(x[i].y, f, o[4 * i + 1]);
+                o[4 * i + 2] = fmaf(x[i].z, f, o[4 * i + 2]); o[4 * i + 3] = fmaf(x[i].w, f, o[4 * i + 3]);
+            }
+        }
+        if (to_memory) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) __stcg(at + i * kRowTile, make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[16 * h + i]);
+                tmem_st16(t_o + c * 32 + 16 * h, w);
+            }
+        }
+    }
+}
+
 // The rare end of a block whose last tiles hold non-finite values (see clean_values): this thread's row, already
 // written, gets those it sees.  A weight is positive, so an infinity stays one and two of opposite signs make a NaN.
 __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const RowsBlock &b, int lim, int c0, int c1,
@@ -460,7 +504,7 @@ struct RowsMaps { CUtensorMap q, k, v; };
 template <bool PREFIX>
 __global__ void __launch_bounds__(kRowsThreads, 1)
 rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsArgs A, const __grid_constant__ DevParams P, RowsRecord *__restrict__ records,
-            float *__restrict__ slots)
+            float *__restrict__ asides, float *__restrict__ slots)
 {
     extern __shared__ __align__(1024) uint8_t rows_smem[];
     RowsSmem &sm = *reinterpret_cast<RowsSmem *>(rows_smem);
@@ -908,7 +952,8 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                         if (!fine) break;
                         tc_fence_after();
                         const uint32_t v = v_lo + v_at * (kTileBytes >> 4), k = k_lo + at * (kTileBytes >> 4);
-                        const uint32_t acc = t > b.t_lo ? 1u : 0u;
+                        // a group's first unit, and every kChainUnits-th, begins its accumulator anew
+                        const uint32_t acc = ((t - b.t_lo) * (b.narrow ? 1 : 2) & (kChainUnits<PREFIX> - 1)) ? 1u : 0u;
                         auto unit = [&](int h, int sl, uint32_t first_acc) {
                             wait(bar_p + sl * 8, (pp >> sl) & 1);
                             if (!fine) return;
@@ -964,11 +1009,11 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 if (more && !take(k_at, k_phase)) break;
                 if (b.narrow) {
                     const int u = 2 * t + w, sl = t & 1;
-                    if (u < end) pv(w, sl, v_at, t == b.t_lo, u + 2 >= end);
+                    if (u < end) pv(w, sl, v_at, !((t - b.t_lo) & (kChainUnits<PREFIX> - 1)), u + 2 >= end);
                     if (ok && more && u + 4 < end) qk(w, sl, k_at);
                 } else {
                     const int left = end - 2 * t;      // units of this group from this tile on
-                    if (left > 0) pv(0, 0, v_at, t == b.t_lo, left == 1);
+                    if (left > 0) pv(0, 0, v_at, !((t - b.t_lo) * 2 & (kChainUnits<PREFIX> - 1)), left == 1);
                     if (ok && more && left > 2) qk(0, 0, k_at);
                     if (ok && left > 1) pv(1, 1, v_at, false, left == 2);
                     if (ok && more && left > 3) qk(1, 1, k_at);
@@ -1015,93 +1060,111 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             const int u_end = unit_end<PREFIX>(b, wg, tile_rows);
             float m_ref = neg_inf(), m_true = neg_inf(), l = 0.f;
             bool started = false;
-            for (int u = 2 * b.t_lo + (b.narrow ? wg : 0); u < u_end; u += b.narrow ? 2 : 1) {
-                const int h = u & 1, sl = b.narrow ? (u >> 1) & 1 : h;      // half of the tile, slot of the scores
-                const uint32_t t_u = t_s + sl * kUnit;
-                if (!warp_wait(smem_u32(&sm.s_full[wg][sl]), (s_phase >> sl) & 1, abort_flag)) { ok = false; break; }
-                s_phase ^= 1u << sl;
-                tc_fence_after();
-                float s[kUnit];
-                tmem_ld32_nowait(t_u, s);
-                tmem_ld32_nowait(t_u + 32, s + 32);
-                const unsigned bad = (sm.bad_pages[(tile_no + (u >> 1) - b.t_lo) & 7] >> (4 * h)) & 15u;
-                tmem_wait_ld();
-                pin32(s);
-                pin32(s + 32);
-                if ((u + 1) * kUnit > warp_lim || bad) {
+            // accumulators set aside: their own reference, and how many units the present one holds
+            float *aside = asides + ((size_t)me * 2 + wg) * kRowTile * kHeadDim + r * 4;      // [channels / 4][row]
+            float m_aside = neg_inf();
+            bool has_aside = false;
+            auto aside_weight = [&]() { return m_aside == neg_inf() ? 0.f : fast_exp2((m_aside - m_ref) * scale2); };
+            int u = 2 * b.t_lo + (b.narrow ? wg : 0);
+            const int step = b.narrow ? 2 : 1;
+            for (;;) {
+                const int chain_end = min(u_end, u + kChainUnits<PREFIX> * step);
+                for (; u < chain_end; u += step) {
+                    const int h = u & 1, sl = b.narrow ? (u >> 1) & 1 : h;      // half of the tile, slot of the scores
+                    const uint32_t t_u = t_s + sl * kUnit;
+                    if (!warp_wait(smem_u32(&sm.s_full[wg][sl]), (s_phase >> sl) & 1, abort_flag)) { ok = false; break; }
+                    s_phase ^= 1u << sl;
+                    tc_fence_after();
+                    float s[kUnit];
+                    tmem_ld32_nowait(t_u, s);
+                    tmem_ld32_nowait(t_u + 32, s + 32);
+                    const unsigned bad = (sm.bad_pages[(tile_no + (u >> 1) - b.t_lo) & 7] >> (4 * h)) & 15u;
+                    tmem_wait_ld();
+                    pin32(s);
+                    pin32(s + 32);
+                    if ((u + 1) * kUnit > warp_lim || bad) {
 #pragma unroll
-                    for (int g = 0; g < kUnit / kPageSize; ++g) {
-                        const int n = ((bad >> g) & 1) ? 0 : lim - u * kUnit - g * kPageSize;
+                        for (int g = 0; g < kUnit / kPageSize; ++g) {
+                            const int n = ((bad >> g) & 1) ? 0 : lim - u * kUnit - g * kPageSize;
 #pragma unroll
-                        for (int i = 0; i < kPageSize; ++i)
-                            if (i >= n) s[g * kPageSize + i] = neg_inf();
+                            for (int i = 0; i < kPageSize; ++i)
+                                if (i >= n) s[g * kPageSize + i] = neg_inf();
+                        }
                     }
-                }
-                // NaN wins every maximum here: a NaN score must make its row NaN, and the polynomial would lose it
-                float mx0 = max_nan(s[0], s[1]), mx1 = max_nan(s[2], s[3]), mx2 = max_nan(s[4], s[5]), mx3 = max_nan(s[6], s[7]);
+                    // NaN wins every maximum here: a NaN score must make its row NaN, and the polynomial would lose it
+                    float mx0 = max_nan(s[0], s[1]), mx1 = max_nan(s[2], s[3]), mx2 = max_nan(s[4], s[5]), mx3 = max_nan(s[6], s[7]);
 #pragma unroll
-                for (int i = 8; i < kUnit; i += 8) {
-                    mx0 = max3_nan(mx0, s[i], s[i + 1]);
-                    mx1 = max3_nan(mx1, s[i + 2], s[i + 3]);
-                    mx2 = max3_nan(mx2, s[i + 4], s[i + 5]);
-                    mx3 = max3_nan(mx3, s[i + 6], s[i + 7]);
-                }
-                const float mx = max_nan(max_nan(mx0, mx1), max_nan(mx2, mx3));
-                m_true = max_nan(m_true, mx);
-                if (!started) {
-                    m_ref = mx;
-                    started = true;
-                } else {
-                    const bool grow = mx > m_ref && (m_ref == neg_inf() || (mx - m_ref) * scale2 > kRescaleLog2);
-                    if (__any_sync(0xffffffffu, grow)) {
-                        // O of the units so far, once their products are done (all but the last are: S came after them)
-                        if (!warp_wait(smem_u32(&sm.o_full[wg]), (o_count + 1) & 1, abort_flag)) { ok = false; break; }
-                        tc_fence_after();
-                        const float f = grow ? fast_exp2((m_ref - mx) * scale2) : 1.f;
-                        if (grow) { l *= f; m_ref = mx; }
+                    for (int i = 8; i < kUnit; i += 8) {
+                        mx0 = max3_nan(mx0, s[i], s[i + 1]);
+                        mx1 = max3_nan(mx1, s[i + 2], s[i + 3]);
+                        mx2 = max3_nan(mx2, s[i + 4], s[i + 5]);
+                        mx3 = max3_nan(mx3, s[i + 6], s[i + 7]);
+                    }
+                    const float mx = max_nan(max_nan(mx0, mx1), max_nan(mx2, mx3));
+                    m_true = max_nan(m_true, mx);
+                    if (!started) {
+                        m_ref = mx;
+                        started = true;
+                    } else {
+                        const bool grow = mx > m_ref && (m_ref == neg_inf() || (mx - m_ref) * scale2 > kRescaleLog2);
+                        if (__any_sync(0xffffffffu, grow)) {
+                            // O of the units so far, once their products are done (all but the last are: S came after them)
+                            if (!warp_wait(smem_u32(&sm.o_full[wg]), (o_count + 1) & 1, abort_flag)) { ok = false; break; }
+                            tc_fence_after();
+                            const float f = grow ? fast_exp2((m_ref - mx) * scale2) : 1.f;
+                            if (grow) { l *= f; m_ref = mx; }
 #pragma unroll 1
-                        for (int c = 0; c < 8; ++c) {
-                            float o[16];
-                            tmem_ld16(t_o + c * 16, o);
-                            uint32_t w[16];
+                            for (int c = 0; c < 8; ++c) {
+                                float o[16];
+                                tmem_ld16(t_o + c * 16, o);
+                                uint32_t w[16];
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
-                            tmem_st16(t_o + c * 16, w);
+                                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
+                                tmem_st16(t_o + c * 16, w);
+                            }
                         }
                     }
-                }
-                const float m2 = m_ref == neg_inf() ? 0.f : m_ref * scale2;
-                const unsigned long long scale22 = pack2(scale2, scale2), m22 = pack2(-m2, -m2);
-                unsigned long long la = pack2(0.f, 0.f), lb = la;
+                    const float m2 = m_ref == neg_inf() ? 0.f : m_ref * scale2;
+                    const unsigned long long scale22 = pack2(scale2, scale2), m22 = pack2(-m2, -m2);
+                    unsigned long long la = pack2(0.f, 0.f), lb = la;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t hi[16], lo[16];
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t hi[16], lo[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const unsigned long long x = fma2(pack2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale22, m22);
-                        float p0, p1;
-                        if ((i & 7) >= 8 - kPolyPairs) {
-                            exp2_pair<PREFIX ? 5 : 4>(x, p0, p1);
-                        } else {
-                            unpack2(x, p0, p1);
-                            p0 = fast_exp2(p0);
-                            p1 = fast_exp2(p1);
+                        for (int i = 0; i < 16; ++i) {
+                            const unsigned long long x = fma2(pack2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale22, m22);
+                            float p0, p1;
+                            if ((i & 7) >= 8 - kPolyPairs) {
+                                exp2_pair<PREFIX ? 5 : 4>(x, p0, p1);
+                            } else {
+                                unpack2(x, p0, p1);
+                                p0 = fast_exp2(p0);
+                                p1 = fast_exp2(p1);
+                            }
+                            if (i & 1) la = add2(la, pack2(p0, p1)); else lb = add2(lb, pack2(p0, p1));
+                            hi[i] = pack_bf16(p0, p1);
+                            if (PREFIX) lo[i] = pack_bf16(p0 - bf16lo_to_f32(hi[i]), p1 - bf16hi_to_f32(hi[i]));
                         }
-                        if (i & 1) la = add2(la, pack2(p0, p1)); else lb = add2(lb, pack2(p0, p1));
-                        hi[i] = pack_bf16(p0, p1);
-                        if (PREFIX) lo[i] = pack_bf16(p0 - bf16lo_to_f32(hi[i]), p1 - bf16hi_to_f32(hi[i]));
+                        tmem_st16(t_u + c * 16, hi);
+                        if (PREFIX) tmem_st16(t_u + 32 + c * 16, lo);
                     }
-                    tmem_st16(t_u + c * 16, hi);
-                    if (PREFIX) tmem_st16(t_u + 32 + c * 16, lo);
+                    float l0, l1;
+                    unpack2(add2(la, lb), l0, l1);
+                    l += l0 + l1;
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[wg][sl]));
+                    ++o_count;       // one product of this group's O per unit
                 }
-                float l0, l1;
-                unpack2(add2(la, lb), l0, l1);
-                l += l0 + l1;
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[wg][sl]));
-                ++o_count;       // one product of this group's O per unit
+                if (!ok || u >= u_end) break;
+                // a chain is full: its products (the last one's accumulator is the next to be begun anew), then a new chain
+                if (!warp_wait(smem_u32(&sm.s_full[wg][b.narrow ? (u >> 1) & 1 : u & 1]), (s_phase >> (b.narrow ? (u >> 1) & 1 : u & 1)) & 1, abort_flag) ||
+                    !warp_wait(smem_u32(&sm.o_full[wg]), (o_count + 1) & 1, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                exchange_aside(t_o, aside, has_aside, true, aside_weight());
+                has_aside = true;
+                m_aside = m_ref;
             }
             if (!ok) break;
             tile_no += b.t_hi - b.t_lo;
@@ -1111,6 +1174,10 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 if (!warp_wait(smem_u32(&sm.o_last[wg]), last_phase, abort_flag)) { ok = false; break; }
                 last_phase ^= 1;
                 tc_fence_after();
+                if (has_aside) {
+                    exchange_aside(t_o, aside, true, false, aside_weight());
+                    tmem_wait_st();
+                }
             }
             if (!(m_true < __int_as_float(0x7f800000))) l = __int_as_float(0x7fc00000);   // a score was NaN or +infinity
             float w_own = started ? 1.f : 0.f, w_other = 0.f;     // weights of this group's accumulator and, narrow, the other's
@@ -1242,58 +1309,104 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
 
 // ------------------------------------------------------------------ pieces of cut blocks
 // CTA (c, part): the block that slice c began and did not finish, channels [32 part, 32 part + 32); thread = row.
-constexpr int kRowsMergeParts = 4;
+// Bound by the latency of dependent loads, so whatever does not depend on another load is requested with it: the
+// record and every slice's state first, then all maxima, then sums and channels of two pieces at a time.
+constexpr int kRowsMergeParts = 4, kRowsMergeBatch = 2;
 template <bool PREFIX>
-__global__ void __launch_bounds__(2 * kRowTile)
-rows_merge_kernel(RowsArgs A, DevParams P, const RowsRecord *__restrict__ records, const float *__restrict__ slots, int n_slices)
+__global__ void __launch_bounds__(2 * kRowTile, 2)
+rows_merge_kernel(const __grid_constant__ RowsArgs A, const __grid_constant__ DevParams P, const RowsRecord *__restrict__ records,
+                  const float *__restrict__ slots, int n_slices)
 {
+    __shared__ int slot_of[kRowsMaxCtas];      // the pieces' slots, in slice order
+    __shared__ int n_pieces;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int me = (int)blockIdx.x;
-    if (!__ldcg(&records[me].has_tail)) return;
-    const RowsBlock b = records[me].tail;
-    const int r = threadIdx.x, wg = r >> 7, G = P.group, Hq = P.num_q_heads, tile_rows = kRowTile / G;
-    if (b.narrow && wg) return;
+    const int me = (int)blockIdx.x, r = threadIdx.x;
+    const int state = r > me && r < n_slices ? __ldcg(&records[r].head_state) : 0;
+    const int4 *rec = reinterpret_cast<const int4 *>(records + me);
+    const int4 r0 = __ldcg(rec), r1 = __ldcg(rec + 1), r2 = __ldcg(rec + 2), r3 = __ldcg(rec + 3);
+    if (!r3.x) return;                          // has_tail; the same for every thread
+    // the owner's tail, then every later slice's first piece up to the one that ends the block
+    const int row0 = r0.z, rows = r1.x, narrow = r2.z, head = r0.y;
+    __shared__ unsigned some[kRowsMaxCtas / 32], ends[kRowsMaxCtas / 32];
+    if (r < kRowsMaxCtas) {
+        const unsigned x = __ballot_sync(0xffffffffu, state != 0), y = __ballot_sync(0xffffffffu, state == 2);
+        if ((r & 31) == 0) { some[r >> 5] = x; ends[r >> 5] = y; }
+    }
+    __syncthreads();
+    if (r < 32) {
+        // lane w holds word w; `past`: the block has ended in an earlier word
+        unsigned x = r < kRowsMaxCtas / 32 ? some[r] : 0, y = r < kRowsMaxCtas / 32 ? ends[r] : 0;
+        const unsigned has_end = __ballot_sync(0xffffffffu, y != 0);
+        const int end_word = has_end ? __ffs((int)has_end) - 1 : 31;
+        if (r > end_word) x = 0;
+        else if (r == end_word && y) x &= (2u << (__ffs((int)y) - 1)) - 1u;
+        int before = __popc(x), mine = before;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, before, o);
+            if (r >= o) before += v;
+        }
+        if (r == 31) n_pieces = before + 1;
+        int at = before - mine + 1;
+        for (; x; x &= x - 1) slot_of[at++] = 2 * (r * 32 + __ffs((int)x) - 1);
+        if (r == 0) slot_of[0] = 2 * me + 1;
+    }
+    __syncthreads();
+    const int n = n_pieces;
+    const int wg = r >> 7, G = P.group, Hq = P.num_q_heads, tile_rows = kRowTile / G;
+    if (narrow && wg) return;
     const int rr = r & 127, tok = wg * tile_rows + rr / G, g = rr - rr / G * G;
-    if (rr >= G * tile_rows || tok >= b.rows) return;
+    if (rr >= G * tile_rows || tok >= rows) return;
     const int part = (int)blockIdx.y;
-    auto piece = [&](int slot) { return slots + (size_t)slot * kRowsSlotFloats; };
+    auto piece = [&](int i) { return slots + (size_t)slot_of[i] * kRowsSlotFloats; };
     constexpr size_t kMl = (size_t)2 * kRowTile * kHeadDim;
-    // the pieces in slice order: the owner's tail, then every later slice's first piece up to the one that ends the block
-    float M = __ldcg(piece(2 * me + 1) + kMl + r);
-    float top = PREFIX ? __ldcg(piece(2 * me + 1) + kMl + 4 * kRowTile + r) : 0.f;
-    int last = me;
-    for (int k = me + 1; k < n_slices; ++k) {
-        const int state = __ldcg(&records[k].head_state);
-        if (state == 0) continue;
-        M = fmaxf(M, __ldcg(piece(2 * k) + kMl + r));
-        if (PREFIX) top = fmaxf(top, __ldcg(piece(2 * k) + kMl + 4 * kRowTile + r));
-        last = k;
-        if (state == 2) break;
+    float M = neg_inf(), top = neg_inf();
+    for (int i0 = 0; i0 < n; i0 += 2 * kRowsMergeBatch) {
+        float m[2 * kRowsMergeBatch], x[2 * kRowsMergeBatch];
+#pragma unroll
+        for (int i = 0; i < 2 * kRowsMergeBatch; ++i) {
+            m[i] = i0 + i < n ? __ldcg(piece(i0 + i) + kMl + r) : neg_inf();
+            x[i] = PREFIX && i0 + i < n ? __ldcg(piece(i0 + i) + kMl + 4 * kRowTile + r) : neg_inf();
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * kRowsMergeBatch; ++i) { M = fmaxf(M, m[i]); top = fmaxf(top, x[i]); }
     }
     float z = 0.f;
     float4 acc[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = me; k <= last; ++k) {
-        if (k > me && __ldcg(&records[k].head_state) == 0) continue;
-        const float *p = piece(k == me ? 2 * me + 1 : 2 * k);
-        const float mk = __ldcg(p + kMl + r);
-        if (mk == neg_inf()) continue;           // nothing visible in this piece
-        const float w = fast_exp2(mk - M);
-        z = fmaf(__ldcg(p + kMl + 2 * kRowTile + r), w, z);
+    for (int i0 = 0; i0 < n; i0 += kRowsMergeBatch) {
+        float m[kRowsMergeBatch], l[kRowsMergeBatch];
+        float4 x[kRowsMergeBatch][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 x = __ldcg(reinterpret_cast<const float4 *>(p) + (size_t)(part * 8 + i) * (2 * kRowTile) + r);
-            acc[i].x = fmaf(x.x, w, acc[i].x); acc[i].y = fmaf(x.y, w, acc[i].y);
-            acc[i].z = fmaf(x.z, w, acc[i].z); acc[i].w = fmaf(x.w, w, acc[i].w);
+        for (int i = 0; i < kRowsMergeBatch; ++i) {
+            if (i0 + i < n) {
+                const float *p = piece(i0 + i);
+                m[i] = __ldcg(p + kMl + r);
+                l[i] = __ldcg(p + kMl + 2 * kRowTile + r);
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    x[i][c] = __ldcg(reinterpret_cast<const float4 *>(p) + (size_t)(part * 8 + c) * (2 * kRowTile) + r);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kRowsMergeBatch; ++i) {
+            if (i0 + i >= n || m[i] == neg_inf()) continue;      // nothing visible in this piece
+            const float w = fast_exp2(m[i] - M);
+            z = fmaf(l[i], w, z);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                acc[c].x = fmaf(x[i][c].x, w, acc[c].x); acc[c].y = fmaf(x[i][c].y, w, acc[c].y);
+                acc[c].z = fmaf(x[i][c].z, w, acc[c].z); acc[c].w = fmaf(x[i][c].w, w, acc[c].w);
+            }
         }
     }
-    const bool empty = M == neg_inf();
+    const bool empty = M == neg_inf() && z == 0.f;      // not so if a row's reference is NaN
     const float inv = empty ? 0.f : 1.f / z;
     const float kLn2 = 0.6931471805599453f;
     const float lse = empty ? neg_inf() : (M + log2f(z)) * kLn2;
-    const int row = b.row0 + tok, h = b.head * G + g;
+    const int row = row0 + tok, h = head * G + g;
     if (PREFIX) {
         const size_t o = ((size_t)row * A.out_shards + A.slot) * Hq + h;
 #pragma unroll
@@ -1377,9 +1490,9 @@ cudaError_t launch_rows_kernels(const RowsMaps &maps, const RowsArgs &A, const D
     }
     const RowsLayout L = rows_layout();
     RowsRecord *records = reinterpret_cast<RowsRecord *>(ws + L.record_off);
-    float *slots = reinterpret_cast<float *>(ws + L.slot_off);
+    float *asides = reinterpret_cast<float *>(ws + L.aside_off), *slots = reinterpret_cast<float *>(ws + L.slot_off);
     const int n = sms < kRowsMaxCtas ? sms : kRowsMaxCtas;
-    cudaError_t e = launch_pdl(rows_kernel<PREFIX>, dim3(n), dim3(kRowsThreads), sizeof(RowsSmem), st, maps, A, P, records, slots);
+    cudaError_t e = launch_pdl(rows_kernel<PREFIX>, dim3(n), dim3(kRowsThreads), sizeof(RowsSmem), st, maps, A, P, records, asides, slots);
     if (e != cudaSuccess) return e;
     return launch_pdl(rows_merge_kernel<PREFIX>, dim3(n, kRowsMergeParts), dim3(2 * kRowTile), 0, st, A, P,
                       (const RowsRecord *)records, (const float *)slots, n);

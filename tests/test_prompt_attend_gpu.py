@@ -253,3 +253,20 @@ def test_two_streams_and_a_replayed_graph():
     torch.cuda.synchronize()
     a.cached = [50, 1500]
     compare(w[6], w[7], prompt64(a, w[0]))
+
+
+@pytest.mark.parametrize("rows", [2, 40])
+def test_very_long_chains_of_tiles(rows):
+    """Enough requests over the same 77,000 positions that every slice runs through hundreds of tiles of one block."""
+    n_req = 160 if rows == 2 else 80
+    pg = Paged([rows], [76_800], 1, seed=21)
+    pg.table, pg.new, pg.cached = pg.table.repeat(n_req, 1), [rows] * n_req, [76_800] * n_req
+    pg.B, pg.total = n_req, rows * n_req
+    pg.cu, pg.lens = torch.arange(n_req + 1, dtype=torch.int32) * rows, torch.full((n_req,), 76_800, dtype=torch.int32)
+    q = queries(pg, 4)
+    out, lse, _ = attend(pg, q)
+    from prompt_testlib import attend64
+    pick = torch.arange(0, pg.total, 37)
+    k, v = (pg.rows(0, 76_800 + rows, w).cuda() for w in "kv")
+    ref = attend64(q[pick.cuda()].double(), k, v, (76_801 + pick % rows).cuda())
+    compare(out[pick.cuda()], lse[pick.cuda()], {n: t.cpu() for n, t in ref.items()})
