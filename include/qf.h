@@ -339,7 +339,8 @@ int qf_rope_frequencies(float *inv_freq_host, float *rot_scale, int rotary_dim, 
  * cache pointers are both given (then k and v are needed) or both NULL (then k needs k_out and v is ignored).  A
  * position without a page (beyond the table row, or a table entry outside the pool) stores nothing in the cache;
  * rows that belong to no request (before cu_tokens[0], from cu_tokens[B] on) are not touched.  seq_lens is not
- * modified.  All other pointers are device pointers, 16-byte aligned where they are bf16.  One launch.
+ * modified.  A row behind the table's end or a position placed twice by one call is the caller's error: the former
+ * stores nothing, of the latter one of the two rows stays.  At most 2^30 rows.  All other pointers are device pointers, 16-byte aligned where they are bf16.  One launch.
  */
 typedef struct qf_rope_params {
     int32_t total_tokens;      /* packed rows in q, k, v                                          */
@@ -369,7 +370,8 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
  * row does not see never reach its result, NaN and infinities included.  p->max_shards is not used (pass 1).
  * k_cache, v_cache 128-byte, q 16-byte, out 32-byte aligned.  workspace: qf_prompt_workspace_bytes bytes, 256-byte
  * aligned, contents need not be initialised; one call at a time.  Results do not depend on what ran before: the
- * schedule, and so the order of every sum, follows from the lengths alone.
+ * schedule, and so the order of every sum, follows from the lengths alone.  At most 2^30 rows; positions from 2^30 on
+ * are not attended.  Enqueues two kernels; capturable (make one call per device before capturing).
  */
 size_t qf_prompt_workspace_bytes(const qf_params *p, int total_tokens);
 int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
@@ -391,7 +393,8 @@ int qf_prompt_status(const void *workspace, int32_t *host_status, void *cuda_str
  * head over its group's prefix into slot p->out_shard_offset of o_part [B, out_shards, Hq, 128], m_part, lse_part
  * (out_shards = p->out_shards, or p->max_shards when that is 0), exactly as qf_decode_partial would write a shard;
  * requests of no group and empty prefixes get (0, -inf, -inf).  Other slots are not touched.  num_groups <= B.
- * fp32 throughout: the weights enter the value product as two bf16 terms (16 bits).
+ * The weights enter the value product as two bf16 terms (16 bits), everything else is fp32; against 64 bits the states
+ * are off by 2e-6 to 6e-6 of their norm, like qf_decode_partial's.
  * prefix_lens beyond the table row are clamped to it.  Errors, bounds, alignment as for qf_decode_partial, and o_part
  * 32-byte aligned;
  * workspace: qf_prefix_workspace_bytes bytes, one call at a time.

@@ -19,6 +19,9 @@ namespace {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
+// Positions and rows of the row kernels stay below this, so that their 32-bit arithmetic has room.
+constexpr int kMostPositions = 1 << 30;
+
 // A token row stride in elements: 0 = the packed width; rows must start on 16 bytes and not overlap.
 bool bad_stride(int64_t stride, long long width) { return stride != 0 && (stride < width || (stride & 7)); }
 
@@ -90,6 +93,7 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
     int rc = qf_host::validate(p);
     if (rc != QF_OK) return rc;
     if (!r) return QF_ERR_NULL;
+    if (r->total_tokens > kMostPositions) return QF_ERR_UNSUPPORTED;
     if (r->total_tokens <= 0 || r->rotary_dim < 0 || !(r->eps >= 0.f) || !std::isfinite(r->rot_scale)) return QF_ERR_BAD_SHAPE;
     if (r->rotary_dim > qf::kHeadDim || (r->rotary_dim & 15)) return QF_ERR_UNSUPPORTED;
     const long long D = qf::kHeadDim, Hq = p->num_q_heads, Hkv = p->num_kv_heads;
@@ -145,6 +149,7 @@ int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, co
     if (rc != QF_OK) return rc;
     const long long width = (long long)p->num_q_heads * qf::kHeadDim;
     if (total_tokens <= 0 || bad_stride(q_stride, width)) return QF_ERR_BAD_SHAPE;
+    if (total_tokens > kMostPositions) return QF_ERR_UNSUPPORTED;
     if (!q || !k_cache || !v_cache || !cu_tokens || !seq_lens || !out || !lse) return QF_ERR_NULL;
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < qf_prompt_workspace_bytes(p, total_tokens))
         return QF_ERR_WORKSPACE;
@@ -158,7 +163,7 @@ int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, co
     A.cu = cu_tokens; A.lens = seq_lens; A.table = block_table;
     A.out = (uint16_t *)out; A.lse = lse; A.status = (unsigned long long *)workspace;
     A.q_stride = q_stride ? q_stride : width;
-    A.n_seq = p->batch; A.table_width = p->max_pages_per_req; A.max_tokens = P.max_tokens; A.total_rows = total_tokens;
+    A.n_seq = p->batch; A.table_width = p->max_pages_per_req; A.max_tokens = std::min(P.max_tokens, kMostPositions); A.total_rows = total_tokens;
     return launch_rows<false>(A, P, p, (char *)workspace, sms, (cudaStream_t)cuda_stream);
 }
 
@@ -191,7 +196,7 @@ int qf_prefix_partial(const void *q, const void *k_cache, const void *v_cache, c
     A.o_part = o_part; A.m_part = m_part; A.lse_part = lse_part; A.status = (unsigned long long *)workspace;
     A.q_stride = (long long)p->num_q_heads * qf::kHeadDim;
     A.n_seq = num_groups; A.table_width = max_prefix_pages;
-    A.max_tokens = qf::max_row_tokens(max_prefix_pages); A.total_rows = p->batch;
+    A.max_tokens = std::min(qf::max_row_tokens(max_prefix_pages), kMostPositions); A.total_rows = p->batch;
     A.out_shards = P.out_shards; A.slot = P.out_shard0;
     return launch_rows<true>(A, P, p, (char *)workspace, sms, (cudaStream_t)cuda_stream);
 }

@@ -89,8 +89,8 @@ struct __align__(16) RowsBlock {
     int pad;
 };
 // What a CTA leaves for the merge kernel: the block it began but did not finish, and whether its first piece ended one.
-struct __align__(16) RowsRecord { RowsBlock tail; int has_tail, head_state; int pad[2]; };
-static_assert(sizeof(RowsRecord) == 64 && sizeof(RowsBlock) == 48, "the merge kernel reads records as four 16-byte words");   // head_state: 0 none, 1 goes on, 2 ends
+struct __align__(16) RowsRecord { RowsBlock tail; int has_tail, head_state; int pad[2]; };   // head_state: 0 none, 1 goes on, 2 ends
+static_assert(sizeof(RowsRecord) == 64 && sizeof(RowsBlock) == 48, "the merge kernel reads records as four 16-byte words");
 struct RowsLayout { size_t record_off, aside_off, slot_off, total; };
 constexpr size_t kRowsAsideFloats = (size_t)2 * kRowTile * kHeadDim;         // per CTA: both groups' accumulators set aside
 constexpr size_t kRowsSlotFloats = (size_t)2 * kRowTile * (kHeadDim + 4);   // O, then m (log2 units), sum, true maximum
@@ -172,18 +172,18 @@ __host__ __device__ inline SlicePos locate_in_seq(SeqPlan q, RowShape f, int seq
 #ifdef __CUDA_ARCH__
     const int lane = threadIdx.x & 31;
     for (int j0 = 0; j0 < n; j0 += 32) {
-        const int c = j0 + lane < n ? block_cost(q, f, j0 + lane) : 0;
-        int x = c;
+        const long long c = j0 + lane < n ? block_cost(q, f, j0 + lane) : 0;
+        long long x = c;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            const long long y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
-        const unsigned past = __ballot_sync(0xffffffffu, (long long)x > r);
+        const unsigned past = __ballot_sync(0xffffffffu, x > r);
         if (past) {
             const int l = __ffs((int)past) - 1;
             p.block = j0 + l;
-            p.tile = place_in_block(q, f, p.block, (int)r - __shfl_sync(0xffffffffu, x - c, l));
+            p.tile = place_in_block(q, f, p.block, (int)(r - __shfl_sync(0xffffffffu, x - c, l)));
             return p;
         }
         r -= __shfl_sync(0xffffffffu, x, 31);
@@ -1158,8 +1158,9 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     ++o_count;       // one product of this group's O per unit
                 }
                 if (!ok || u >= u_end) break;
-                // a chain is full: its products (the last one's accumulator is the next to be begun anew), then a new chain
-                if (!warp_wait(smem_u32(&sm.s_full[wg][b.narrow ? (u >> 1) & 1 : u & 1]), (s_phase >> (b.narrow ? (u >> 1) & 1 : u & 1)) & 1, abort_flag) ||
+                // a chain is full: its products are waited for and set aside
+                const int sl = b.narrow ? (u >> 1) & 1 : u & 1;      // the next scores came after all products but the last
+                if (!warp_wait(smem_u32(&sm.s_full[wg][sl]), (s_phase >> sl) & 1, abort_flag) ||
                     !warp_wait(smem_u32(&sm.o_full[wg]), (o_count + 1) & 1, abort_flag)) { ok = false; break; }
                 tc_fence_after();
                 exchange_aside(t_o, aside, has_aside, true, aside_weight());
