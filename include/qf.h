@@ -339,8 +339,8 @@ int qf_rope_frequencies(float *inv_freq_host, float *rot_scale, int rotary_dim, 
  * cache pointers are both given (then k and v are needed) or both NULL (then k needs k_out and v is ignored).  A
  * position without a page (beyond the table row, or a table entry outside the pool) stores nothing in the cache;
  * rows that belong to no request (before cu_tokens[0], from cu_tokens[B] on) are not touched.  seq_lens is not
- * modified.  A row behind the table's end or a position placed twice by one call is the caller's error: the former
- * stores nothing, of the latter one of the two rows stays.  At most 2^30 rows.  All other pointers are device pointers, 16-byte aligned where they are bf16.  One launch.
+ * modified.  If one call places two rows at the same slot of the pool (requests with a common page), one of the two
+ * stays.  At most 2^30 rows.  All pointers are device pointers, 16-byte aligned where they are bf16.  One launch.
  */
 typedef struct qf_rope_params {
     int32_t total_tokens;      /* packed rows in q, k, v                                          */
@@ -394,10 +394,10 @@ int qf_prompt_status(const void *workspace, int32_t *host_status, void *cuda_str
  * (out_shards = p->out_shards, or p->max_shards when that is 0), exactly as qf_decode_partial would write a shard;
  * requests of no group and empty prefixes get (0, -inf, -inf).  Other slots are not touched.  num_groups <= B.
  * The weights enter the value product as two bf16 terms (16 bits), everything else is fp32; against 64 bits the states
- * are off by 2e-6 to 6e-6 of their norm, like qf_decode_partial's.
- * prefix_lens beyond the table row are clamped to it.  Errors, bounds, alignment as for qf_decode_partial, and o_part
- * 32-byte aligned;
- * workspace: qf_prefix_workspace_bytes bytes, one call at a time.
+ * are off by 2e-6 to 6e-6 of their norm, like qf_decode_partial's.  prefix_lens beyond the table row are clamped to
+ * it.  Errors, bounds and alignment as for qf_decode_partial, and o_part 32-byte aligned; workspace:
+ * qf_prefix_workspace_bytes bytes, 256-byte aligned, one call at a time.  Enqueues two kernels; capturable (make one
+ * call per device before capturing).
  */
 size_t qf_prefix_workspace_bytes(const qf_params *p);
 int qf_prefix_partial(const void *q, const void *k_cache, const void *v_cache, const int32_t *prefix_table,

@@ -1,38 +1,45 @@
 // Attention of packed query rows over the paged cache on the tensor cores: whole prompts (causal) and prefixes that
 // requests share.  The problem and its two forms are described in qf_rows_simple.cuh.
 //
-//   S = Q K^T / sqrt(d),  P = e^{S - m},  O = P V / sum P,   per 128 query rows and 128 positions at a time.
+//   S = Q K^T / sqrt(d),  P = e^{S - m},  O = P V / sum P,   per 128 query rows, K and V in tiles of 128 positions.
 //
-// Both products are tcgen05.mma of 128 x 128 x 128 (bf16 in, fp32 in tensor memory).  A row tile holds the G query
-// heads of 128 / G tokens of one KV head, so one K and V tile serves all of them, whatever G is (rows past
-// G * (128 / G) are unused).  A CTA owns TWO row tiles ("wide") that share every K and V tile it streams: with one,
-// shared memory (A and B operands are both read from it) would bound the products.  While one tile's 128 softmax
-// threads (one per row, no shuffles) turn S into P, the tensor cores work on the other tile.  P goes back to tensor
-// memory over S and is the A operand of the second product from there.  A block with no more rows than one tile
-// ("narrow": a few decode tokens, a small group of requests) has the two softmax groups take the two halves of every
-// position tile for the same rows instead, each with an accumulator of its own, merged at the block's end: a lone
-// tile's chain product -> softmax -> product would leave the K/V stream waiting.  (Whole tiles in turn held four of the
-// five tiles of the ring at a time: 2,600 cycles per tile against 1,600.)
+// Both products are tcgen05.mma (bf16 in, fp32 in tensor memory), 64 positions at a time: S 128 x 64 x 128, O 128 x 128
+// x 64.  A row tile holds the G query heads of 128 / G tokens of one KV head, so one K and V tile serves all of them,
+// whatever G is (rows past G * (128 / G) are unused).  A CTA owns TWO row tiles ("wide") that share every K and V tile
+// it streams: with one, shared memory (A and B operands are both read from it) would bound the products.  Every group
+// of 128 softmax threads (one per row, no shuffles) has two slots of scores, so that the tensor cores work on one while
+// the threads turn the other into P; P goes back to tensor memory over S and is the A operand of the second product
+// from there.  Tensor memory is then full: 2 groups x (2 x 64 columns of scores + 128 of O).
+// A block with no more rows than one tile ("narrow": a few decode tokens, a small group of requests) has the two
+// softmax groups take the two halves of every position tile for the same rows instead, each with an accumulator of its
+// own, merged at the block's end: a lone tile's chain product -> softmax -> product would leave the K/V stream waiting.
+// (Whole tiles in turn held four of the five tiles of the ring at a time: 2,600 cycles per tile against 1,600.)
 //
 // Roles (384 threads, one CTA per SM): warps 0-3 and 4-7 softmax of the two tiles (and their epilogues), warps 8 and 9
-// issue the products of one tile each, warp 10 loads (TMA, 5 tiles of 32 KB in flight or in use), warp 11 walks the
+// issue the products of one group each, warp 10 loads (TMA, 5 tiles of 32 KB in flight or in use), warp 11 walks the
 // schedule.
 //
-// Schedule: the work of all sequences, KV heads and row blocks is laid on one axis in units of half a wide tile
-// (plus a constant per block), and every CTA takes an equal slice, found in its prologue from the lengths alone
-// (closed-form sums, no plan kernel, no host copy of the lengths).  A slice end that falls close to a block's
-// border moves there; otherwise the block is cut along its positions and the pieces, (m, sum, unnormalised O) in
-// fp32, are merged by a second small kernel in slice order.  Long contexts with few rows are split over all SMs by
-// the same rule.  No atomics: the order of every sum follows from the lengths.
+// Schedule: all row blocks lie on one axis (KV heads, then sequences, then blocks) with the cost that a block and its
+// tiles were measured to have, and every CTA takes an equal slice of it, found in its prologue from the lengths alone
+// (no plan kernel, no host copy of the lengths).  A slice end that falls close to a block's border moves there;
+// otherwise the block is cut along its positions and the pieces, (m, sum, unnormalised O) in fp32, are merged by a
+// second small kernel in slice order.  Long contexts with few rows are split over all SMs by the same rule.  Heads are
+// outermost so that CTAs that run together share a prefix's or a long prompt's pages in L2 (8 packed prompts: 159 us
+// against 204 with sequences outermost).  No atomics: the order of every sum follows from the lengths.
 //
-// Numbers: scores, maxima, sums and accumulators are fp32.  The running maximum used in the exponent moves only when
-// a row's maximum has grown by more than 2^8 (the factor cancels in O / sum; a power of two up to 2^8 changes no
-// rounding), so O is rescaled rarely.  Prompt form: P is rounded to bf16 (half a step is 2^-9..2^-8 of each weight;
-// the output itself is bf16).  Prefix form, whose states are fp32: P = hi + lo, two bf16 terms, 16 bits, and twice
-// the second product, which the stream of K and V hides up to about 200 rows.
+// Numbers: scores, maxima, sums and accumulators are fp32.  The reference that the exponents subtract moves only when a
+// row's maximum has grown by more than 2^8; until then it is the same factor in O and in the sum, and cancels.  So O is
+// rescaled rarely.  Prompt form: P is rounded to bf16 (at most 2^-8 of each weight; the output itself is bf16).  Prefix
+// form, whose states are fp32: P = hi + lo, two bf16 terms, 16 bits, and twice the second product, which the stream of
+// K and V hides up to about 200 rows.  How accumulators drift, and what is done about it: kChainUnits.
 //
-// Bounds: a prompt is bound by the products and, equally, by the exponentials (16 per SM and cycle against 8,192
-// multiply-adds); a prefix by HBM while its rows are few, then by the products.
+// Measured (32 query heads on 8 KV heads; 6.54 TB/s and 1.67 PFLOP/s are what a copy and a library product reach).  One
+// prompt of 16,384 tokens: 1.80 ms, 1.22 PFLOP/s, 2.1 ms and 1.04 when the card is held at its power limit.  A unit of
+// two row tiles takes about 1,600 cycles, of which the products alone would take 1,140: the rest is the chain wait for
+// S -> read tensor memory -> 64 exponentials -> write P -> wait, which two slots per group do not quite cover, and there
+// is no tensor memory for a third.  A thread's exponentials are the chain's longest part (16 per SM and cycle), so a
+// quarter of them goes to the multiply-add units; a half gave nothing more, and neither did twice the softmax threads.
+// Narrow blocks stream at 5.9 TB/s.
 #pragma once
 
 #include <cuda.h>
@@ -66,14 +73,12 @@ constexpr int kWideSnap = 18, kNarrowSnap = 6;   // a cut this close to a block'
 constexpr float kRescaleLog2 = 8.f;
 // Units after which a group's accumulator is set aside and begun anew.  The tensor cores cut off what does not fit when
 // they add a product to an accumulator, so a long chain drifts towards zero: 1.6e-8 of the value per 16-position step
-// (measured: -1.4e-5 after 55 tiles of a prefix).  Prefix states are fp32, and an addition every 2,048 positions, in
-// fp32 and rounded, keeps the drift at 4e-6 for 5 % of the time; prompts' bf16 results want it only after 65,536.
+// (measured: -1.4e-5 after 55 tiles of a prefix).  Prefix states are fp32, and an addition every 32 units (2,048
+// positions, 4,096 when two groups share them), in fp32 and rounded, keeps the drift at 4e-6 for 5 % of the time;
+// prompts' bf16 results want it only after 1,024 units.
 template <bool PREFIX> constexpr int kChainUnits = PREFIX ? 32 : 1024;
 // Of every 8 pairs of scores, how many take their exponentials from the multiply-add units.
-#ifndef QF_ROWS_POLY
-#define QF_ROWS_POLY 2
-#endif
-constexpr int kPolyPairs = QF_ROWS_POLY;
+constexpr int kPolyPairs = 2;
 
 // One block's stretch of positions, as the schedule hands it to the other warps.
 struct __align__(16) RowsBlock {
@@ -106,7 +111,6 @@ inline RowsLayout rows_layout()
 
 // ------------------------------------------------------------------ schedule arithmetic (host and device)
 // One axis of units: KV heads in order, for each the sequences in order, for each its row blocks in order.
-#define QF_COLD __noinline__      // rare paths: as functions they leave the instruction cache to the loops
 struct SeqPlan { int n, off, len; };     // rows, positions before row 0, positions in all
 struct RowShape { int causal, tile_rows, group; };   // tile_rows: tokens of a row tile
 __host__ __device__ inline int min_int(int a, int b) { return a < b ? a : b; }
@@ -256,6 +260,8 @@ struct SliceWalk {
         return false;
     }
 };
+
+#define QF_COLD __noinline__      // rare paths: as functions they leave the instruction cache to the loops
 
 // ------------------------------------------------------------------ PTX
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
