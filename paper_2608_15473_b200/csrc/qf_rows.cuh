@@ -45,6 +45,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdio>
 #include <mutex>
 
@@ -138,6 +139,7 @@ __host__ __device__ inline long long seq_cost(SeqPlan q, RowShape f)
 {
     long long c = 0;
     const int n = seq_blocks(q, f);
+#pragma unroll 1
     for (int j = 0; j < n; ++j) c += block_cost(q, f, j);
     return c;
 }
@@ -175,6 +177,7 @@ __host__ __device__ inline SlicePos locate_in_seq(SeqPlan q, RowShape f, int seq
     const int n = seq_blocks(q, f);
 #ifdef __CUDA_ARCH__
     const int lane = threadIdx.x & 31;
+#pragma unroll 1
     for (int j0 = 0; j0 < n; j0 += 32) {
         const long long c = j0 + lane < n ? block_cost(q, f, j0 + lane) : 0;
         long long x = c;
@@ -505,6 +508,50 @@ __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const 
     }
 }
 
+// A tile of values in shared memory, by one warp: rows from `exist` on, as far as their page goes, become 0, and so do
+// non-finite values among rows seen_by_all .. used - 1 (from the page's start), which `dirty` then reports.
+__device__ QF_COLD void clean_tile(uint8_t *v, int exist, int seen_by_all, int used, volatile int *dirty)
+{
+    const int lane = threadIdx.x & 31;
+    if (exist & 15) {
+        uint8_t *page = v + (exist >> 4) * kPageBytes;
+        const int r0 = exist & 15, n16 = (16 - r0) * 8;    // 16-byte words per half
+#pragma unroll 1
+        for (int i = lane; i < 2 * n16; i += 32) {
+            const int half = i >= n16, x = i - half * n16;
+            *reinterpret_cast<uint4 *>(page + half * kHalfPageBytes + r0 * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        __syncwarp();
+    }
+    const int from = seen_by_all / kPageSize * (kPageBytes / 16), to = (used + kPageSize - 1) / kPageSize * (kPageBytes / 16);
+    if (seen_by_all < used) {
+        // a product with 0 keeps only what is not finite: one instruction for two values
+        uint32_t bad[4] = {0u, 0u, 0u, 0u};
+#pragma unroll 1
+        for (int i = from + lane; i < to; i += 256)          // a page is 256 words
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(v + (i + 32 * e) * 16);
+                asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(bad[0]) : "r"(x.x), "r"(0u));
+                asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(bad[1]) : "r"(x.y), "r"(0u));
+                asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(bad[2]) : "r"(x.z), "r"(0u));
+                asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(bad[3]) : "r"(x.w), "r"(0u));
+            }
+        if (__any_sync(0xffffffffu, ((bad[0] | bad[1] | bad[2] | bad[3]) & 0x7fff7fffu) != 0)) {
+            if (lane == 0) *dirty = 1;
+            __threadfence_block();      // said before the first value is gone: the other warp may find none left
+            __syncwarp();
+#pragma unroll 1
+            for (int i = from * 8 + lane; i < to * 8; i += 32) {
+                uint16_t *x = reinterpret_cast<uint16_t *>(v) + i;
+                if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
+            }
+        }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the products read what is there now
+    __syncwarp();
+}
+
 struct RowsMaps { CUtensorMap q, k, v; };
 
 template <bool PREFIX>
@@ -562,6 +609,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         // empty states: requests of groups with an empty prefix, and of no group
         auto empties = [&](int lo, int hi) {
             const long long n4 = (long long)max(hi - lo, 0) * Hq * (kHeadDim / 4);
+#pragma unroll 1
             for (long long i = tid; i < n4; i += kRowsThreads) {
                 const long long row = lo + i / (Hq * (kHeadDim / 4));
                 const int rest = (int)(i % (Hq * (kHeadDim / 4)));
@@ -589,6 +637,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             const SeqPlan q = seq_plan(warp);
             const int n = seq_blocks(q, shape);
             long long c = 0;
+#pragma unroll 1
             for (int j = lane; j < n; j += 32) c += block_cost(q, shape, j);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
@@ -596,8 +645,8 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         }
         __syncthreads();
     }
-    long long per_head = 0;      // units of one KV head
-    // (units before sequence base + tid, its own units); adds the round's total to per_head
+    long long running = 0;       // units of the sequences so far
+    // (units before sequence base + tid, its own units); adds the round's total to `running`
     auto scan_round = [&](int base, long long &before, long long &cost) {
         cost = base + tid < A.n_seq ? seq_cost(seq_plan(base + tid), shape) : 0;
         long long x = cost;
@@ -608,48 +657,54 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         }
         if (lane == 31) sm.scan[warp] = x;
         __syncthreads();
-        before = per_head + x - cost;
+        before = running + x - cost;
+#pragma unroll 1
         for (int w = 0; w < kWarps; ++w) {
             if (w < warp) before += sm.scan[w];
-            per_head += sm.scan[w];
+            running += sm.scan[w];
         }
         __syncthreads();
     };
-    long long before0 = 0, cost0 = 0;       // of the first round
-    if (A.n_seq <= kWarps) {
-        for (int s = 0; s < A.n_seq; ++s) {
-            if (s == tid) { before0 = per_head; cost0 = sm.scan[s]; }
-            per_head += sm.scan[s];
-        }
-    } else {
-        for (int base = 0; base < A.n_seq; base += kRowsThreads) {
-            long long before, cost;
-            scan_round(base, before, cost);
-            if (base == 0) { before0 = before; cost0 = cost; }
-        }
-    }
-    const long long total = per_head * Hkv;
-    const int n_eff = slices_of(total, n_ctas);
     const int me = (int)blockIdx.x;
-    const bool working = total > 0 && me < n_eff;
-    if (working) {
-        long long ra, rb;
-        const int ha = head_of(cut_at(total, n_eff, me), per_head, ra);
-        const int hb = me + 1 < n_eff ? head_of(cut_at(total, n_eff, me + 1), per_head, rb) : (rb = -1, Hkv);
-        auto offer = [&](int s, long long before, long long cost) {
+    bool working = false;
+    long long ra = -1, rb = -1;          // where this CTA's cuts fall within their heads ha and hb
+    int ha = 0, hb = 0;
+    // the first pass finds the total, the second, for more sequences than threads, the cuts' sequences
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        long long before = 0, cost = 0;
+        auto offer = [&](int s) {
             if (ra >= before && ra < before + cost) { sm.cut_seq[0] = s; sm.cut_rest[0] = ra - before; }
             if (rb >= before && rb < before + cost) { sm.cut_seq[1] = s; sm.cut_rest[1] = rb - before; }
         };
-        if (A.n_seq <= kRowsThreads) {
-            offer(tid, before0, cost0);
+        running = 0;
+        if (A.n_seq <= kWarps) {
+#pragma unroll 1
+            for (int s = 0; s < A.n_seq; ++s) {
+                if (s == tid) { before = running; cost = sm.scan[s]; }
+                running += sm.scan[s];
+            }
         } else {
-            per_head = 0;
+#pragma unroll 1
             for (int base = 0; base < A.n_seq; base += kRowsThreads) {
-                long long before, cost;
                 scan_round(base, before, cost);
-                offer(base + tid, before, cost);
+                if (pass) offer(base + tid);
             }
         }
+        if (pass) break;
+        const long long total = running * Hkv;
+        const int n_eff = slices_of(total, n_ctas);
+        working = total > 0 && me < n_eff;
+        if (!working) break;
+        ha = head_of(cut_at(total, n_eff, me), running, ra);
+        hb = Hkv;
+        if (me + 1 < n_eff) hb = head_of(cut_at(total, n_eff, me + 1), running, rb);
+        if (A.n_seq <= kRowsThreads) {
+            offer(tid);
+            break;
+        }
+    }
+    if (working) {
         __syncthreads();
         if (warp < 2) {
             SlicePos at{0, Hkv, 0, 0};                      // the end of everything
@@ -675,7 +730,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             bool ok = true;
             auto publish = [&](const RowsBlock &b) {
                 const int slot = idx % kInfoRing;
-                if (!mbar_wait(smem_u32(&sm.info_empty[slot]), (uint32_t)(((idx / kInfoRing) & 1) ^ 1), abort_flag)) { ok = false; return; }
+                if (!wait_loop(smem_u32(&sm.info_empty[slot]), (uint32_t)(((idx / kInfoRing) & 1) ^ 1), abort_flag)) { ok = false; return; }
                 sm.info[slot] = b;
                 sm.dirty[slot] = 0;
                 mbar_arrive(smem_u32(&sm.info_full[slot]));
@@ -705,7 +760,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         uint32_t phase = 0;
         int q_fill = -1;
         bool ok = true;
-        const int none_row = (int)(P.kv_nhd ? P.num_pages * kPageSize : P.num_pages * Hkv * kPageSize);   // out of range: zeros
+        const int none_c2 = (int)(P.kv_nhd ? P.num_pages * kPageSize : P.num_pages * Hkv);   // out of range: zeros
         const uint32_t q_box = (uint32_t)(64 * 2) * G * tile_rows;
         if (A.table) {      // the first block's table entries, while the schedule names it
             const int at = sm.cut[0].tile * kTilePages + lane;
@@ -718,8 +773,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm.info_empty[slot]));
             if (b.seq < 0) break;
-            const int nt = b.t_hi - b.t_lo;
-            const int last_page = (b.len - 1) >> 4;
+            const int last_page = (b.len - 1) >> 4, c1 = P.kv_nhd ? b.head : 0;
             const long long row_base = (long long)b.seq * A.table_width;
             auto entry = [&](int lp) -> int {
                 return lp <= last_page ? (A.table ? A.table[row_base + lp] : (int)(row_base + lp)) : -1;
@@ -745,52 +799,53 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 const bool bad = in && (phys < 0 || (long long)phys >= P.num_pages);
                 const unsigned bad_mask = __ballot_sync(0xffffffffu, bad) & 0xffu;
                 if (!warp_wait(smem_u32(&sm.kv_empty[stage]), phase ^ 1, abort_flag)) { ok = false; return; }
-                const uint32_t full = smem_u32(&sm.kv_full[stage]);
-                if (lane == 0) {
-                    if (!is_v) {
+                // One thread issues every copy, with operands that are the same for the warp: a lane per page made each copy
+                // a turn of a loop over lanes, 1,500 cycles per tile and the bound of the whole kernel.
+                const int c2 = !in || bad ? none_c2 : P.kv_nhd ? phys * kPageSize : phys * Hkv + b.head;
+                int at[kTilePages];
+#pragma unroll
+                for (int i = 0; i < kTilePages; ++i) at[i] = __shfl_sync(0xffffffffu, c2, i);
+                if (elect_one()) {
+                    const uint32_t full = smem_u32(&sm.kv_full[stage]), dst = smem_u32(sm.kv[stage]);
+                    mbar_arrive_expect_tx(full, kTileBytes);
+                    if (is_v) {
+#pragma unroll
+                        for (int i = 0; i < kTilePages; ++i) tma_load_4d(dst + i * kPageBytes, &maps.v, 0, c1, at[i], 0, full);
+                    } else {
                         sm.bad_pages[tile_no & 7] = bad_mask;
                         if (bad_mask && P.check_bounds) rows_status_or(A.status, kStatusBadPage);
+#pragma unroll
+                        for (int i = 0; i < 2 * kTilePages; ++i)
+                            tma_load_4d(dst + i * kHalfPageBytes, &maps.k, 0, c1, at[i & 7], i >> 3, full);
                     }
-                    mbar_arrive_expect_tx(full, kTileBytes);
                 }
-                if (!is_v) ++tile_no;
                 __syncwarp();
-                const uint32_t dst = smem_u32(sm.kv[stage]);
-                const bool zero = !in || bad;
-                if (is_v) {
-                    if (lane < 8) {
-                        if (P.kv_nhd) tma_load_4d(dst + lane * kPageBytes, &maps.v, 0, b.head, zero ? none_row : phys * kPageSize, 0, full);
-                        else tma_load_3d(dst + lane * kPageBytes, &maps.v, 0, zero ? none_row : (phys * Hkv + b.head) * kPageSize, 0, full);
-                    }
-                } else if (lane < 16) {
-                    const int half = lane >> 3;
-                    const uint32_t at = dst + half * (kTileBytes / 2) + (lane & 7) * kHalfPageBytes;
-                    if (P.kv_nhd) tma_load_4d(at, &maps.k, 0, b.head, zero ? none_row : phys * kPageSize, half, full);
-                    else tma_load_3d(at, &maps.k, 0, zero ? none_row : (phys * Hkv + b.head) * kPageSize, half, full);
-                }
+                if (!is_v) ++tile_no;
                 ++issued;
                 if (++stage == kRowsRing) { stage = 0; phase ^= 1; }
             };
-            load_tile(b.t_lo, false);
-            if (!ok) break;
-            if (!warp_wait(smem_u32(&sm.q_empty), (uint32_t)((idx & 1) ^ 1), abort_flag)) { ok = false; break; }
-            if (lane == 0) {
-                const uint32_t full = smem_u32(&sm.q_full);
-                const int n_tiles = b.narrow ? 1 : 2;
-                mbar_arrive_expect_tx(full, q_box * 2u * n_tiles);
-                for (int w = 0; w < n_tiles; ++w)
-                    for (int half = 0; half < 2; ++half)
-                        tma_load_3d(smem_u32(sm.q[w]) + half * (kTileBytes / 2), &maps.q, half * 64, b.head * G,
-                                    b.row0 + w * tile_rows, full);
-            }
-            __syncwarp();
-            q_fill = idx;
-            // the order the products consume them in: K is one tile (wide) or two (narrow) ahead of V
+            // The order the products consume them in: K is one tile (wide) or two (narrow) ahead of V.  Q after the first.
             const int ahead = b.narrow ? 2 : 1;
-            if (b.narrow && nt > 1) load_tile(b.t_lo + 1, false);
-            for (int t = 0; ok && t < nt; ++t) {
-                load_tile(b.t_lo + t, true);
-                if (ok && t + ahead < nt) load_tile(b.t_lo + t + ahead, false);
+            int k_next = b.t_lo, v_next = b.t_lo;
+#pragma unroll 1
+            while (v_next < b.t_hi) {
+                const bool is_v = k_next == b.t_hi || k_next - v_next >= ahead;
+                load_tile(is_v ? v_next++ : k_next++, is_v);
+                if (!ok) break;
+                if (is_v || k_next != b.t_lo + 1) continue;
+                if (!warp_wait(smem_u32(&sm.q_empty), (uint32_t)((idx & 1) ^ 1), abort_flag)) { ok = false; break; }
+                if (lane == 0) {
+                    const uint32_t full = smem_u32(&sm.q_full);
+                    const int n_tiles = b.narrow ? 1 : 2;
+                    mbar_arrive_expect_tx(full, q_box * 2u * n_tiles);
+#pragma unroll 1
+                    for (int i = 0; i < 2 * n_tiles; ++i) {
+                        const int w = i >> 1, half = i & 1;
+                        tma_load_3d(smem_u32(sm.q[w]) + half * (kTileBytes / 2), &maps.q, half * 64, b.head * G, b.row0 + w * tile_rows, full);
+                    }
+                }
+                __syncwarp();
+                q_fill = idx;
             }
         }
         if (!ok) {
@@ -879,41 +934,10 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             // values of a tile that is hidden from some row, which the epilogue then adds where they are seen.  Both
             // product warps do it, each before its own products: what the second one writes is what is there.
             auto clean_values = [&](int t, int at) {
-                uint8_t *v = sm.kv[at];
-                const int exist = b.len - t * kRowTile;          // positions of the tile that exist
-                bool wrote = false;
-                if (exist < kRowTile && (exist & 15)) {
-                    uint8_t *page = v + (exist >> 4) * kPageBytes;
-                    const int r0 = exist & 15, n16 = (16 - r0) * 8;    // 16-byte words per half
-                    for (int i = lane; i < 2 * n16; i += 32) {
-                        const int half = i >= n16, x = i - half * n16;
-                        *reinterpret_cast<uint4 *>(page + half * kHalfPageBytes + r0 * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    wrote = true;
-                }
-                __syncwarp();
-                if (!PREFIX && (t + 1) * kRowTile > common) {
-                    unsigned seen = 0;
-                    const int from = max(common - t * kRowTile, 0) / kPageSize * (kPageBytes / 16);   // pages with a hidden row
-#pragma unroll 4
-                    for (int i = from + lane; i < kTileBytes / 16; i += 32) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(v + i * 16);
-                        seen |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) |
-                                ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
-                    }
-                    if (__any_sync(0xffffffffu, (seen & 0x80008000u) != 0)) {
-                        if (lane == 0) *reinterpret_cast<volatile int *>(&sm.dirty[slot]) = 1;
-                        __threadfence_block();      // said before the first value is gone: the other warp may find none left
-                        __syncwarp();
-                        for (int i = from * 8 + lane; i < kTileBytes / 2; i += 32) {
-                            uint16_t *x = reinterpret_cast<uint16_t *>(v) + i;
-                            if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
-                        }
-                        wrote = true;
-                    }
-                }
-                if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
+                const int exist = min(b.len - t * kRowTile, kRowTile);          // positions of the tile that exist
+                const int seen_by_all = PREFIX ? exist : max(common - t * kRowTile, 0);
+                const int used = min(end * kUnit - t * kRowTile, exist);        // this group's products use these (and their pages' rest)
+                clean_tile(sm.kv[at], exist, seen_by_all, used, &sm.dirty[slot]);
             };
             auto needs_clean = [&](int t) {
                 return (!PREFIX && (t + 1) * kRowTile > common) || ((t + 1) * kRowTile > b.len && (b.len & 15));
@@ -923,14 +947,12 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             // The order: S of a tile's two units, then for every unit P V of this tile and, into the slot that P V has
             // just freed (a thread's products run in the order of issue), S of the tile this group takes next.
             const int ahead = b.narrow ? 2 : 1;      // tiles between the values in use and the keys
+            const int step = ahead, first = b.narrow ? w : 0;      // this group's units of a tile: first, first + step
             for (int t = b.t_lo; t < b.t_hi && t < b.t_lo + ahead; ++t) {
                 if (!take(stage, phase)) break;
-                if (b.narrow) {
-                    if (2 * t + w < end) qk(w, t & 1, stage);
-                } else {
-                    if (2 * t < end) qk(0, 0, stage);
-                    if (2 * t + 1 < end) qk(1, 1, stage);
-                }
+#pragma unroll 1
+                for (int i = 0; i < 2 / step; ++i)
+                    if (2 * t + first + i < end) qk(first + i, b.narrow ? t & 1 : i, stage);
                 release();
             }
             if (ok && b.t_hi - b.t_lo <= ahead) q_done();
@@ -1013,16 +1035,11 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 if (!take(v_at, v_phase)) break;
                 if (needs_clean(t)) clean_values(t, v_at);
                 if (more && !take(k_at, k_phase)) break;
-                if (b.narrow) {
-                    const int u = 2 * t + w, sl = t & 1;
-                    if (u < end) pv(w, sl, v_at, !((t - b.t_lo) & (kChainUnits<PREFIX> - 1)), u + 2 >= end);
-                    if (ok && more && u + 4 < end) qk(w, sl, k_at);
-                } else {
-                    const int left = end - 2 * t;      // units of this group from this tile on
-                    if (left > 0) pv(0, 0, v_at, !((t - b.t_lo) * 2 & (kChainUnits<PREFIX> - 1)), left == 1);
-                    if (ok && more && left > 2) qk(0, 0, k_at);
-                    if (ok && left > 1) pv(1, 1, v_at, false, left == 2);
-                    if (ok && more && left > 3) qk(1, 1, k_at);
+#pragma unroll 1
+                for (int i = 0; ok && i < 2 / step; ++i) {
+                    const int h = first + i, u = 2 * t + h, sl = b.narrow ? t & 1 : i;
+                    if (u < end) pv(h, sl, v_at, i == 0 && !((t - b.t_lo) * (2 / step) & (kChainUnits<PREFIX> - 1)), u + step >= end);
+                    if (ok && more && u + 2 * ahead < end) qk(h, sl, k_at);
                 }
                 if (!ok) break;
                 release();
@@ -1238,38 +1255,26 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     }
                 }
             };
-            if (!b.narrow) {
-#pragma unroll
-                for (int c = 0; c < 4; c += 2) {
-                    float o[2][32];
-                    tmem_ld32_nowait(t_o + c * 32, o[0]);
-                    tmem_ld32_nowait(t_o + c * 32 + 32, o[1]);
-                    tmem_wait_ld();
-                    pin32(o[0]);
-                    pin32(o[1]);
-                    if (!started) {      // nothing visible: the accumulator may hold anything
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) o[i >> 5][i & 31] = 0.f;
-                    }
-                    finish(c, o[0]);
-                    finish(c + 1, o[1]);
-                }
-            } else {
+            // one chunk at a time, in one loop for both kinds of block: this code runs cold, once per block, and unrolled it
+            // took longer to fetch than to run
 #pragma unroll 1
-                for (int c = c0; c < c1; ++c) {
-                    float o[32], x[32];
-                    tmem_ld32_nowait(t_o + c * 32, o);
+            for (int c = c0; c < c1; ++c) {
+                float o[32];
+                tmem_ld32_nowait(t_o + c * 32, o);
+                tmem_wait_ld();
+                pin32(o);
+                if (b.narrow || !started) {      // nothing visible: the accumulator may hold anything
+                    float x[32];
                     tmem_ld32_nowait(t_x + c * 32, x);
                     tmem_wait_ld();
-                    pin32(o);
                     pin32(x);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         o[i] = w_own == 0.f ? 0.f : o[i] * w_own;
                         o[i] = w_other == 0.f ? o[i] : fmaf(x[i], w_other, o[i]);
                     }
-                    finish(c, o);
                 }
+                finish(c, o);
             }
             if (dirty && live) add_hidden(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
             if (b.narrow) {
@@ -1469,13 +1474,16 @@ inline int make_rows_maps(RowsMaps *m, const RowsArgs &A, const DevParams &P, ch
     const cuuint32_t q_box[3] = {64, (cuuint32_t)P.group, (cuuint32_t)(kRowTile / P.group)};
     CUresult r = make(&m->q, A.q, 3, q_size, q_stride, q_box);
     const cuuint64_t hkv = (cuuint64_t)P.num_kv_heads, rows = (cuuint64_t)P.num_pages * kPageSize;
-    const cuuint64_t size3[3] = {64, rows * hkv, 2}, stride3[2] = {(cuuint64_t)kHeadDim * 2, 128};
-    const cuuint64_t size4[4] = {64, hkv, rows, 2}, stride4[3] = {(cuuint64_t)kHeadDim * 2, hkv * kHeadDim * 2, 128};
-    const cuuint32_t k3[3] = {64, kPageSize, 1}, v3[3] = {64, kPageSize, 2}, k4[4] = {64, 1, kPageSize, 1}, v4[4] = {64, 1, kPageSize, 2};
-    const int dims = P.kv_nhd ? 4 : 3;
-    const cuuint64_t *size = P.kv_nhd ? size4 : size3, *stride = P.kv_nhd ? stride4 : stride3;
-    if (r == CUDA_SUCCESS) r = make(&m->k, A.k_cache, dims, size, stride, P.kv_nhd ? k4 : k3);
-    if (r == CUDA_SUCCESS) r = make(&m->v, A.v_cache, dims, size, stride, P.kv_nhd ? v4 : v3);
+    // both layouts as [half][.][.][64 channels]: a page of a head is 16 rows of one plane, or one head of 16 planes
+    const cuuint64_t hnd[4] = {64, kPageSize, (cuuint64_t)P.num_pages * hkv, 2}, hnd_stride[3] = {(cuuint64_t)kHeadDim * 2, kPageBytes, 128};
+    const cuuint64_t nhd[4] = {64, hkv, rows, 2}, nhd_stride[3] = {(cuuint64_t)kHeadDim * 2, hkv * kHeadDim * 2, 128};
+    const cuuint32_t hnd_box[4] = {64, kPageSize, 1, 1}, nhd_box[4] = {64, 1, kPageSize, 1};
+    cuuint32_t box[4];
+    std::copy(P.kv_nhd ? nhd_box : hnd_box, (P.kv_nhd ? nhd_box : hnd_box) + 4, box);
+    const cuuint64_t *size = P.kv_nhd ? nhd : hnd, *stride = P.kv_nhd ? nhd_stride : hnd_stride;
+    if (r == CUDA_SUCCESS) r = make(&m->k, A.k_cache, 4, size, stride, box);
+    box[3] = 2;
+    if (r == CUDA_SUCCESS) r = make(&m->v, A.v_cache, 4, size, stride, box);
     if (r != CUDA_SUCCESS) { snprintf(msg, msg_len, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r); return -1; }
     return 0;
 }
