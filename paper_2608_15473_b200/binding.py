@@ -193,21 +193,35 @@ def lib() -> ctypes.CDLL:
 
 
 def _ptr(x) -> Optional[int]:
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return int(x.data_ptr())
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        pass
     if hasattr(x, "ctypes"):  # numpy (host buffers of decode_step_host)
         return int(x.ctypes.data)
     raise TypeError(f"cannot take the address of {type(x)}")
 
 
+_raw_stream = None      # () -> the current device's current stream, once CUDA is up
+
+
+def _current_stream() -> int:
+    """torch.cuda.current_stream().cuda_stream without the object around it (3.4 us of a 12 us call)."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        stream_of, device = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+        if stream_of is None or device is None or not torch.cuda.is_initialized():
+            return int(torch.cuda.current_stream().cuda_stream)
+        _raw_stream = lambda: int(stream_of(device()))      # noqa: E731
+    return _raw_stream()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return int(stream.cuda_stream)
