@@ -33,13 +33,14 @@
 // form, whose states are fp32: P = hi + lo, two bf16 terms, 16 bits, and twice the second product, which the stream of
 // K and V hides up to about 200 rows.  How accumulators drift, and what is done about it: kChainUnits.
 //
-// Measured (32 query heads on 8 KV heads; 6.54 TB/s and 1.67 PFLOP/s are what a copy and a library product reach).  One
-// prompt of 16,384 tokens: 1.80 ms, 1.22 PFLOP/s, 2.1 ms and 1.04 when the card is held at its power limit.  A unit of
-// two row tiles takes about 1,600 cycles, of which the products alone would take 1,140: the rest is the chain wait for
-// S -> read tensor memory -> 64 exponentials -> write P -> wait, which two slots per group do not quite cover, and there
-// is no tensor memory for a third.  A thread's exponentials are the chain's longest part (16 per SM and cycle), so a
-// quarter of them goes to the multiply-add units; a half gave nothing more, and neither did twice the softmax threads.
-// Narrow blocks stream at 5.9 TB/s.
+// Measured (32 query heads on 8 KV heads; a copy reaches 6.54 TB/s, a library product 1.67 PFLOP/s, 1.40 for seconds on
+// end).  One prompt of 16,384 tokens: 1.82 ms, 1.21 PFLOP/s; 2.1 ms and 1.04 among other work, when the card is at its
+// power limit and the clock near 1.4 GHz.  64 positions of two row tiles take about 1,600 cycles, of which the products
+// alone would take 1,140: a row's thread needs 1,450 from its scores' arrival to its weights' (tensor memory, maximum,
+// 64 exponentials, rounding, tensor memory) and waits 150-300 for the next.  Narrow blocks stream at 5.9 TB/s.
+// Outside the loops the kernel runs cold: about 9,000 cycles until a CTA's first product and 5,800 per wide block are
+// mostly instruction fetch and first loads, so every role has ONE copy of its code, in rolled loops (131 KB of code and
+// 7,500 cycles per block before; 8 packed prompts 169 us against 155).
 #pragma once
 
 #include <cuda.h>
@@ -65,9 +66,10 @@ constexpr int kTileBytes = kRowTile * kHeadDim * 2;
 constexpr int kHalfPageBytes = kPageBytes / 2;    // 16 rows x 64 channels
 constexpr int kInfoRing = 4;
 constexpr int kRowsMaxCtas = 160;                // one per SM
-// What things cost, in units of about 400 cycles (fitted to the cycles of some 7,000 slices of random batches, to 4 %):
-// a position tile of two row tiles 3,150 cycles and of one 2,560 (it reads as much K and V: HBM is what it waits for),
-// and what a block costs beside its tiles 7,500 and 5,000.
+// What things cost, in units of about 400 cycles, fitted to the cycles of some 7,000 slices of random batches: a position
+// tile of two row tiles 3,100 cycles and of one 2,100 to 2,600 (it reads as much K and V: HBM is what it waits for), and
+// what a block costs beside its tiles 5,800 and 3,700 (7,500 and 5,000 when blocks and tiles of a slice are counted in
+// whole; units of 8, 5, 14, 9 balanced no better).
 constexpr int kWideTileCost = 8, kNarrowTileCost = 6, kWideBlockCost = 18, kNarrowBlockCost = 12;
 constexpr int kMinSlice = 12;                    // less per CTA is not worth a merge
 constexpr int kWideSnap = 18, kNarrowSnap = 6;   // a cut this close to a block's border moves there
@@ -78,8 +80,10 @@ constexpr float kRescaleLog2 = 8.f;
 // positions, 4,096 when two groups share them), in fp32 and rounded, keeps the drift at 4e-6 for 5 % of the time;
 // prompts' bf16 results want it only after 1,024 units.
 template <bool PREFIX> constexpr int kChainUnits = PREFIX ? 32 : 1024;
-// Of every 8 pairs of scores, how many take their exponentials from the multiply-add units.
-constexpr int kPolyPairs = 2;
+// Of every 8 pairs of scores, how many take their exponentials from the multiply-add units.  Slowest CTA, in thousand
+// cycles, with 1, 2, 3, 4 of 8: a prompt of 16,384 tokens 3,186, 3,046, 2,990, 3,346; 256 requests behind 32,768 tokens
+// (whose polynomial is one degree longer and whose weights are split in two) 265, 267, 294, 307.
+template <bool PREFIX> constexpr int kPolyPairs = PREFIX ? 1 : 3;
 
 // One block's stretch of positions, as the schedule hands it to the other warps.
 struct __align__(16) RowsBlock {
@@ -1157,7 +1161,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                         for (int i = 0; i < 16; ++i) {
                             const unsigned long long x = fma2(pack2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale22, m22);
                             float p0, p1;
-                            if ((i & 7) >= 8 - kPolyPairs) {
+                            if ((i & 7) >= 8 - kPolyPairs<PREFIX>) {
                                 exp2_pair<PREFIX ? 5 : 4>(x, p0, p1);
                             } else {
                                 unpack2(x, p0, p1);
