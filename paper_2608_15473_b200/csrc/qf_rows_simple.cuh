@@ -113,8 +113,9 @@ rows_simple_kernel(RowsArgs A, DevParams P)
         acc[3] = fmaf(p, bf16hi_to_f32(vw.y), acc[3] * alpha);
         m = mn;
     }
-    const float inv = m == neg_inf() ? 0.f : 1.f / l;
-    const float lse = m == neg_inf() ? neg_inf() : m + logf(l);
+    const bool empty = l == 0.f;                  // nothing visible; a NaN score makes the sum NaN, not the maximum
+    const float inv = empty ? 0.f : 1.f / l;
+    const float lse = empty ? neg_inf() : m + logf(l);
     if (PREFIX) {
         const size_t o = ((size_t)row * A.out_shards + A.slot) * Hq + h;
         *reinterpret_cast<float4 *>(A.o_part + o * kHeadDim + lane * 4) =
