@@ -368,8 +368,8 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
  * Rows that belong to no request are left as they were.  A table entry outside [0, num_pages) contributes nothing
  * (reported under QF_FLAG_CHECK_BOUNDS); positions beyond the table row are not attended.  Values at positions a
  * row does not see never reach its result, NaN and infinities included.  p->max_shards is not used (pass 1).
- * k_cache, v_cache 128-byte, q 16-byte, out 32-byte aligned.  workspace: qf_prompt_workspace_bytes bytes, 256-byte
- * aligned, contents need not be initialised; one call at a time.  Results do not depend on what ran before: the
+ * k_cache, v_cache 128-byte, q 16-byte, out 32-byte aligned.  workspace: qf_prompt_workspace_bytes bytes (64 MB,
+ * whatever the sizes), 256-byte aligned, contents need not be initialised; one call at a time.  Results do not depend on what ran before: the
  * schedule, and so the order of every sum, follows from the lengths alone.  At most 2^30 rows; positions from 2^30 on
  * are not attended.  Enqueues two kernels; capturable (make one call per device before capturing).
  */
