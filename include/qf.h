@@ -369,9 +369,10 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
  * (reported under QF_FLAG_CHECK_BOUNDS); positions beyond the table row are not attended.  Values at positions a
  * row does not see never reach its result, NaN and infinities included.  p->max_shards is not used (pass 1).
  * k_cache, v_cache 128-byte, q 16-byte, out 32-byte aligned.  workspace: qf_prompt_workspace_bytes bytes (64 MB,
- * whatever the sizes), 256-byte aligned, contents need not be initialised; one call at a time.  Results do not depend on what ran before: the
- * schedule, and so the order of every sum, follows from the lengths alone.  At most 2^30 rows; positions from 2^30 on
- * are not attended.  Enqueues two kernels; capturable (make one call per device before capturing).
+ * whatever the sizes), 256-byte aligned, contents need not be initialised; one call at a time.  Results do not depend
+ * on what ran before: the schedule, and so the order of every sum, follows from the lengths alone.  At most 2^30 rows;
+ * positions from 2^30 on are not attended.  Enqueues two kernels; capturable (make one call per device before
+ * capturing).
  */
 size_t qf_prompt_workspace_bytes(const qf_params *p, int total_tokens);
 int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,

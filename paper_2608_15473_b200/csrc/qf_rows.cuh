@@ -38,9 +38,10 @@
 // power limit and the clock near 1.4 GHz.  64 positions of two row tiles take about 1,600 cycles, of which the products
 // alone would take 1,140: a row's thread needs 1,450 from its scores' arrival to its weights' (tensor memory, maximum,
 // 64 exponentials, rounding, tensor memory) and waits 150-300 for the next.  Narrow blocks stream at 5.9 TB/s.
-// Outside the loops the kernel runs cold: about 9,000 cycles until a CTA's first product and 5,800 per wide block are
-// mostly instruction fetch and first loads, so every role has ONE copy of its code, in rolled loops (131 KB of code and
-// 7,500 cycles per block before; 8 packed prompts 169 us against 155).
+// Outside the loops latency rules: about 9,000 cycles until a CTA's first product (lengths -> cuts -> block -> table ->
+// copies, chains of dependent scalar steps; running that code once beforehand on made-up lengths, to have it fetched,
+// changed nothing) and 5,800 per wide block.  Every role has ONE copy of its code, in rolled loops: with 131 KB of
+// unrolled code a block cost 7,500 (8 packed prompts 169 us against 155).
 #pragma once
 
 #include <cuda.h>
@@ -167,7 +168,8 @@ struct SlicePos { int seq, head, block, tile; };   // a cut: this block's tiles 
 __host__ __device__ inline int place_in_block(SeqPlan q, RowShape f, int j, int r)
 {
     const bool wide = block_is_wide(q, f, j);
-    const int snap = wide ? kWideSnap : kNarrowSnap, each = wide ? kWideTileCost : kNarrowTileCost, fixed = wide ? kWideBlockCost : kNarrowBlockCost;
+    const int snap = wide ? kWideSnap : kNarrowSnap, each = wide ? kWideTileCost : kNarrowTileCost;
+    const int fixed = wide ? kWideBlockCost : kNarrowBlockCost;
     const int nt = block_tiles(q, f, j);
     if (r < snap) return 0;
     if (each * nt + fixed - r < snap) return nt;
@@ -560,8 +562,8 @@ struct RowsMaps { CUtensorMap q, k, v; };
 
 template <bool PREFIX>
 __global__ void __launch_bounds__(kRowsThreads, 1)
-rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsArgs A, const __grid_constant__ DevParams P, RowsRecord *__restrict__ records,
-            float *__restrict__ asides, float *__restrict__ slots)
+rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsArgs A, const __grid_constant__ DevParams P,
+            RowsRecord *__restrict__ records, float *__restrict__ asides, float *__restrict__ slots)
 {
     extern __shared__ __align__(1024) uint8_t rows_smem[];
     RowsSmem &sm = *reinterpret_cast<RowsSmem *>(rows_smem);
@@ -1259,8 +1261,8 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     }
                 }
             };
-            // one chunk at a time, in one loop for both kinds of block: this code runs cold, once per block, and unrolled it
-            // took longer to fetch than to run
+            // one chunk at a time, in one rolled loop for both kinds of block: this code runs once per block, between loops
+            // that it would push out of the instruction cache
 #pragma unroll 1
             for (int c = c0; c < c1; ++c) {
                 float o[32];
