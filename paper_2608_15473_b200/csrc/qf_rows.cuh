@@ -69,8 +69,8 @@ constexpr int kInfoRing = 4;
 constexpr int kRowsMaxCtas = 160;                // one per SM
 // What things cost, in units of about 400 cycles, fitted to the cycles of some 7,000 slices of random batches: a position
 // tile of two row tiles 3,100 cycles and of one 2,100 to 2,600 (it reads as much K and V: HBM is what it waits for), and
-// what a block costs beside its tiles 5,800 and 3,700 (7,500 and 5,000 when blocks and tiles of a slice are counted in
-// whole; units of 8, 5, 14, 9 balanced no better).
+// what a block costs beside its tiles 5,800 and 3,700.  (7,500 and 5,000 when the units were chosen; 8, 5, 14 and 9, which
+// would fit better now, balance no better.)
 constexpr int kWideTileCost = 8, kNarrowTileCost = 6, kWideBlockCost = 18, kNarrowBlockCost = 12;
 constexpr int kMinSlice = 12;                    // less per CTA is not worth a merge
 constexpr int kWideSnap = 18, kNarrowSnap = 6;   // a cut this close to a block's border moves there
