@@ -70,6 +70,13 @@ __device__ __forceinline__ int4 ld_sync_int4(const int4 *p)
     return v;
 }
 
+// The larger of two, NaN if one of them is.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000u); }
 
 // bf16 pair packed in a 32-bit word -> two fp32 (exact).

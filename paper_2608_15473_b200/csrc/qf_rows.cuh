@@ -376,12 +376,6 @@ __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigne
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
 __device__ __forceinline__ float max3_nan(float a, float b, float c)
 {
     float r;
@@ -1209,7 +1203,8 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     tmem_wait_st();
                 }
             }
-            if (!(m_true < __int_as_float(0x7f800000))) l = __int_as_float(0x7fc00000);   // a score was NaN or +infinity
+            // A score was NaN or +infinity: the row is NaN, and not empty, whatever its reference was when the score came.
+            if (!(m_true < __int_as_float(0x7f800000))) l = m_ref = __int_as_float(0x7fc00000);
             float w_own = started ? 1.f : 0.f, w_other = 0.f;     // weights of this group's accumulator and, narrow, the other's
             int c0 = 0, c1 = 4;                   // column chunks of 32 that this thread finishes
             uint32_t t_x = t_o;                   // the other group's accumulator
@@ -1222,7 +1217,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 pair_phase0 ^= 1;
                 tc_fence_after();
                 const float2 other = sm.ml[wg ^ 1][r];
-                const float M = fmaxf(m_ref, other.x);
+                const float M = max_nan(m_ref, other.x);
                 if (M != neg_inf()) {
                     w_own = m_ref == neg_inf() ? 0.f : fast_exp2((m_ref - M) * scale2);
                     w_other = other.x == neg_inf() ? 0.f : fast_exp2((other.x - M) * scale2);
@@ -1297,7 +1292,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     if (lane == 0) mbar_arrive(smem_u32(&sm.pair[0]));
                     if (!warp_wait(smem_u32(&sm.pair[0]), pair_phase0, abort_flag)) { ok = false; break; }
                     pair_phase0 ^= 1;
-                    if (wg == 0) m_true = fmaxf(m_true, sm.ml[0][r].y);
+                    if (wg == 0) m_true = max_nan(m_true, sm.ml[0][r].y);
                 }
             }
             if (live && (!b.narrow || wg == 0)) {
@@ -1388,7 +1383,7 @@ rows_merge_kernel(const __grid_constant__ RowsArgs A, const __grid_constant__ De
             x[i] = PREFIX && i0 + i < n ? __ldcg(piece(i0 + i) + kMl + 4 * kRowTile + r) : neg_inf();
         }
 #pragma unroll
-        for (int i = 0; i < 2 * kRowsMergeBatch; ++i) { M = fmaxf(M, m[i]); top = fmaxf(top, x[i]); }
+        for (int i = 0; i < 2 * kRowsMergeBatch; ++i) { M = fmaxf(M, m[i]); top = max_nan(top, x[i]); }
     }
     float z = 0.f;
     float4 acc[8];
@@ -1420,7 +1415,7 @@ rows_merge_kernel(const __grid_constant__ RowsArgs A, const __grid_constant__ De
             }
         }
     }
-    const bool empty = M == neg_inf() && z == 0.f;      // not so if a row's reference is NaN
+    const bool empty = M == neg_inf() && z == 0.f;      // not so if a piece's reference is NaN: its weight is NaN too
     const float inv = empty ? 0.f : 1.f / z;
     const float kLn2 = 0.6931471805599453f;
     const float lse = empty ? neg_inf() : (M + log2f(z)) * kLn2;

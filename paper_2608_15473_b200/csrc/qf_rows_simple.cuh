@@ -104,7 +104,7 @@ rows_simple_kernel(RowsArgs A, DevParams P)
         for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
         const float sc = d * P.sm_scale;
         if (sc == neg_inf()) continue;            // weight 0 against any other score
-        const float mn = fmaxf(m, sc);
+        const float mn = max_nan(m, sc);          // NaN from the first NaN score on
         const float alpha = __expf(m - mn), p = __expf(sc - mn);
         l = l * alpha + p;
         acc[0] = fmaf(p, bf16lo_to_f32(vw.x), acc[0] * alpha);
@@ -113,7 +113,7 @@ rows_simple_kernel(RowsArgs A, DevParams P)
         acc[3] = fmaf(p, bf16hi_to_f32(vw.y), acc[3] * alpha);
         m = mn;
     }
-    const bool empty = l == 0.f;                  // nothing visible; a NaN score makes the sum NaN, not the maximum
+    const bool empty = l == 0.f;                  // nothing visible; a NaN score makes maximum and sum NaN
     const float inv = empty ? 0.f : 1.f / l;
     const float lse = empty ? neg_inf() : m + logf(l);
     if (PREFIX) {
