@@ -65,12 +65,12 @@ combine_warp(long long bh, const float *__restrict__ o_part, const float *__rest
     int ns = shard_counts ? shard_counts[b] : max_shards;
     ns = min(max(ns, 0), max_shards);
 
-    // M = max over operands of log Z; lanes stride over shards
+    // M = max over operands of log Z; lanes stride over shards.  NaN wins: a NaN state beside empty ones is not empty.
     float M = s_self;
-    if (lane < ns) M = fmaxf(M, ls_first);
-    for (int s = lane + 32; s < ns; s += 32) M = fmaxf(M, lrow[(size_t)s * num_q_heads]);
+    if (lane < ns) M = max_nan(M, ls_first);
+    for (int s = lane + 32; s < ns; s += 32) M = max_nan(M, lrow[(size_t)s * num_q_heads]);
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    for (int off = 16; off > 0; off >>= 1) M = max_nan(M, __shfl_xor_sync(0xffffffffu, M, off));
 
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float wsum = 0.f;

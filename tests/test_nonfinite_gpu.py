@@ -197,3 +197,32 @@ def test_a_step_behind_a_prefix_with_a_bad_key(flags, n):
     ro, rl = step64(sh, q)
     assert torch.isnan(rl[:3]).all() and torch.isfinite(rl[3:]).all()
     check_state(out, None, lse, (ro, None, rl))
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+@pytest.mark.parametrize("n", [1, 40, 300])
+def test_a_step_with_nothing_but_a_prefix_with_a_bad_key(flags, n):
+    """Requests without own positions: the merge sees one state, and it is NaN."""
+    sh = Shared([3, 2], [n, n], [0, 7, 0, 0, 5], 2, seed=n)
+    put_key(sh.pg, sh.ptab[0], n // 2, NAN)
+    q = queries_of(sh, 8)
+    out, lse, _ = step(sh, q, 2, flags)
+    ro, rl = step64(sh, q)
+    assert torch.isnan(rl[:3]).all() and torch.isfinite(rl[3:]).all()
+    check_state(out, None, lse, (ro, None, rl))
+
+
+@pytest.mark.parametrize("shards", [1, 3, 40])
+def test_merge_of_states_of_which_only_a_nan_is_not_empty(shards):
+    """qf_combine over log-sum-exps that are -inf but for a NaN, a finite one, or nothing at all."""
+    hq = 4
+    p = qf.params(3, hq, 2, 1, shards, 1)
+    o = torch.zeros((3, shards, hq, 128), device="cuda")
+    l = torch.full((3, shards, hq), -INF, device="cuda")
+    o[0, shards - 1], l[0, shards - 1] = NAN, NAN
+    o[1, 0], l[1, 0] = 2.0, 1.5
+    out, lse = torch.full((3, hq, 128), 7.0, device="cuda"), torch.full((3, hq), 7.0, device="cuda")
+    qf.combine(o, l, None, out, lse, p)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
+    assert (out[1] == 2).all() and (lse[1] == 1.5).all() and (out[2] == 0).all() and torch.isneginf(lse[2]).all()
