@@ -109,7 +109,7 @@ finish_kernel(const int4 *__restrict__ piece_info, const unsigned long long *__r
     auto write_final = [&]() {
 #pragma unroll
         for (int o = 0; o < G; ++o) {
-            const bool empty = (M[o] == neg_inf());
+            const bool empty = M[o] == neg_inf() && z[o] == 0.f;   // scores that are all NaN leave M, not z
             o_part[(out_row + o) * kHeadDim + d] = empty ? 0.f : acc[o] / z[o];
             if (d == 0) {
                 m_part[out_row + o] = empty ? neg_inf() : M[o] * kLn2;

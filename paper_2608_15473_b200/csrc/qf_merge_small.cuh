@@ -199,7 +199,7 @@ merge_small_kernel(const int *__restrict__ seq_lens, const int *__restrict__ sha
     const size_t unit_row = out_entry(P, b * S + min(role, S - 1)) * Hq + (size_t)c * G;
 #pragma unroll
     for (int o = 0; o < G; ++o) {
-        const bool empty = (M[o] == neg_inf());
+        const bool empty = M[o] == neg_inf() && z[o] == 0.f;   // scores that are all NaN leave M, not z
         const float val = empty ? 0.f : acc[o] / z[o];
         const float l = empty ? neg_inf() : (M[o] + log2f(z[o])) * kLn2;
         if (role == S) {

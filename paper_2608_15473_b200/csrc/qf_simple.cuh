@@ -70,7 +70,7 @@ sweep_simple_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
             const float sc = d * P.sm_scale;
-            const float mn = fmaxf(m[g], sc);
+            const float mn = max_nan(m[g], sc);      // NaN from the first NaN score on
             const float alpha = __expf(m[g] - mn);   // m = -inf on the first token: e^{-inf} = 0
             const float p = __expf(sc - mn);
             l[g] = l[g] * alpha + p;
@@ -98,7 +98,7 @@ sweep_simple_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__
         const int g = idx / kHeadDim, d = idx % kHeadDim;
         float M = neg_inf();
 #pragma unroll
-        for (int w = 0; w < kSimpleWarps; ++w) M = fmaxf(M, sm_m[w][g]);
+        for (int w = 0; w < kSimpleWarps; ++w) M = max_nan(M, sm_m[w][g]);
         const size_t slot = out_entry(P, b * S + s) * Hq + c * G + g;
         if (M == neg_inf()) {  // empty shard
             o_part[slot * kHeadDim + d] = 0.f;

@@ -613,8 +613,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                     float M = neg_inf();
 #pragma unroll
                     for (int w = 0; w < kConsumerWarps; ++w) M = fmaxf(M, sm.red_ml[w][head][0]);
-                    const bool empty = (M == neg_inf());
-                    const float Ms = empty ? 0.f : M;
+                    const float Ms = (M == neg_inf()) ? 0.f : M;
                     float ew[kConsumerWarps];
                     float z = 0.f;
 #pragma unroll
@@ -622,6 +621,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                         ew[w] = fast_exp2(sm.red_ml[w][head][0] - Ms);
                         z = fmaf(sm.red_ml[w][head][1], ew[w], z);
                     }
+                    const bool empty = M == neg_inf() && z == 0.f;   // scores that are all NaN leave M, not z
                     const float inv = empty ? 0.f : 1.f / z;
                     for (int d = d0; d < kHeadDim; d += kThreadsPerHead) {
                         float wsum = 0.f;

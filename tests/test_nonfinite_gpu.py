@@ -226,3 +226,77 @@ def test_merge_of_states_of_which_only_a_nan_is_not_empty(shards):
     torch.cuda.synchronize()
     assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
     assert (out[1] == 2).all() and (lse[1] == 1.5).all() and (out[2] == 0).all() and torch.isneginf(lse[2]).all()
+
+
+def own_pages(sh, q, bad, flags, S):
+    for b, spots in bad.items():
+        for i in spots:
+            put_key(sh.pg, sh.stab[b], i, NAN)
+    out, lse, _ = step(sh, q, S, flags)
+    ro, rl = step64(sh, q)
+    assert torch.isnan(rl[list(bad)]).all() and int(torch.isnan(rl).sum()) == len(bad) * q.shape[1]
+    check_state(out, None, lse, (ro, None, rl))
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+@pytest.mark.parametrize("S", [1, 3])
+def test_a_step_whose_own_positions_are_all_bad(flags, S):
+    """A request whose own keys are all NaN is NaN, not what its prefix alone gives."""
+    sh = Shared([4, 2], [100, 30], [1, 20, 300, 9, 0, 3], 2)
+    own_pages(sh, queries_of(sh, 8), {0: [0], 2: range(300), 3: range(9), 5: [0, 1, 2]}, flags, S)
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+def test_a_step_with_one_bad_key_among_own_positions(flags):
+    sh = Shared([5], [100], [1, 20, 300, 9, 2000], 2)
+    own_pages(sh, queries_of(sh, 8), {1: [19], 2: [0], 4: [1999]}, flags, 1)
+
+
+@pytest.mark.parametrize("flags", KERNELS + [pytest.param(qf.QF_FLAG_DRAW_ALWAYS, id="drawn")])
+def test_sweep_states_whose_scores_are_all_nan(flags):
+    """Shards of one to many tokens, one of them cut into pieces: (NaN, ., NaN), and the step's merge of them."""
+    lens = [1, 16, 100, 30_000, 40]
+    pg = Paged([0] * 5, lens, 2)
+    for b in (0, 2, 3):
+        for i in range(lens[b]):
+            put_key(pg, pg.table[b], i, NAN)
+    q = torch.randn((5, 8, 128), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    p = qf.params(5, 8, 2, pg.width, 1, pg.num_pages, flags=flags)
+    kc, vc = pg.pools()
+    ranges = torch.stack([torch.zeros_like(pg.lens), pg.lens], -1).reshape(5, 1, 2).cuda()
+    o, m, l = (torch.full(s, 7.0, device="cuda") for s in ((5, 1, 8, 128), (5, 1, 8), (5, 1, 8)))
+    out, lse = torch.full((5, 8, 128), 7.0, device="cuda"), torch.full((5, 8), 7.0, device="cuda")
+    n = qf.workspace_bytes(p)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    head = (q, kc, vc, pg.table.cuda(), pg.lens.cuda(), ranges)
+    qf.decode_partial(*head, o, m, l, p, ws, n)
+    qf.decode_step(*head, None, o.clone(), m.clone(), l.clone(), out, lse, p, ws, n)
+    torch.cuda.synchronize()
+    bad = torch.tensor([True, False, True, True, False])
+    for x in (o[:, 0], l[:, 0], out, lse):
+        assert torch.isnan(x[bad.cuda()]).all() and torch.isfinite(x[~bad.cuda()]).all()
+
+
+def test_small_step_whose_scores_are_all_nan():
+    """The same through the merge of small sweeps."""
+    lens = [1, 40, 500]
+    pg = Paged([0] * 3, lens, 1)
+    for b in (0, 2):
+        for i in range(lens[b]):
+            put_key(pg, pg.table[b], i, NAN)
+    q = torch.randn((3, 4, 128), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    for S in (1, 4):
+        p = qf.params(3, 4, 1, pg.width, S, pg.num_pages)
+        kc, vc = pg.pools()
+        cut = -(-pg.lens // S)
+        lo = torch.minimum(torch.arange(S)[None] * cut[:, None], pg.lens[:, None])
+        ranges = torch.stack([lo, torch.minimum(lo + cut[:, None], pg.lens[:, None])], -1).to(torch.int32).cuda()
+        o, m, l = (torch.empty(s, device="cuda") for s in ((3, S, 4, 128), (3, S, 4), (3, S, 4)))
+        out, lse = torch.empty((3, 4, 128), device="cuda"), torch.empty((3, 4), device="cuda")
+        n = qf.workspace_bytes(p)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        qf.decode_step(q, kc, vc, pg.table.cuda(), pg.lens.cuda(), ranges, None, o, m, l, out, lse, p, ws, n)
+        assert qf.last_launch_count() == 2
+        torch.cuda.synchronize()
+        for x in (out, lse):
+            assert torch.isnan(x[0]).all() and torch.isnan(x[2]).all() and torch.isfinite(x[1]).all()
