@@ -435,28 +435,50 @@ def project_status(workspace, stream=None) -> int:
 
 
 _many_gpus: Optional[bool] = None
+_kinds = {}      # a call's letters -> the element types of its arrays
 
 
-def _on_current_device(*args) -> None:
-    """The calls below launch on the current device: whatever is not None, an address or a tensor of that device (host
-    tensors, NumPy arrays such as rope_frequencies', tensors of another device) is refused, not dereferenced there."""
+def _kinds_of(letters):
+    """The element types of every array: b bf16 (or 16-bit integers that hold its bits), i int32, f fp32, * any."""
     global _many_gpus
-    if _many_gpus is None:
+    import torch
+    _many_gpus = torch.cuda.device_count() > 1
+    anything = (torch.uint8, *{x for x in vars(torch).values() if isinstance(x, torch.dtype)})
+    types = {"b": (torch.bfloat16, torch.int16, torch.uint16), "i": (torch.int32,), "f": (torch.float32,), "*": anything}
+    _kinds[letters] = tuple(types[x] for x in letters)
+    return _kinds[letters]
+
+
+def _address(x, kinds) -> Optional[int]:
+    """_arrays for one array, with the reason of a refusal."""
+    if x is None or isinstance(x, int):
+        return x
+    if not hasattr(x, "is_cuda"):
+        raise ValueError(f"expected a CUDA tensor, got {type(x).__module__}.{type(x).__qualname__}")
+    if not x.is_cuda:
+        raise ValueError(f"expected a CUDA tensor, got one on {x.device}")
+    if _many_gpus:
         import torch
-        _many_gpus = torch.cuda.device_count() > 1
-    for x in args:
-        if x is None or isinstance(x, int):
-            continue
+        if x.get_device() != torch.cuda.current_device():
+            raise ValueError(f"expected a tensor on the current device (cuda:{torch.cuda.current_device()}), got one on {x.device}")
+    if x.dtype not in kinds:
+        raise ValueError(f"expected elements of {kinds[0]}, got {x.dtype}")
+    return x.data_ptr()
+
+
+def _arrays(letters, *args):
+    """The arrays' addresses.  The calls below launch on the current device and read each array as what the library
+    expects: whatever is not None, an address or a tensor of that device (host tensors, NumPy arrays such as
+    rope_frequencies', tensors of another device) is refused, not dereferenced there, and so is a tensor of other elements,
+    which would be misread.  (One pass in one expression: a dozen calls of _address would be a third of a small call.)"""
+    kinds = _kinds.get(letters) or _kinds_of(letters)
+    if not _many_gpus:
         try:
-            where = x.get_device()
+            return [x if x is None or type(x) is int else x.data_ptr() if x.is_cuda and x.dtype in kind else _address(x, kind)
+                    for x, kind in zip(args, kinds)]
         except AttributeError:
-            raise ValueError(f"expected a CUDA tensor, got {type(x).__module__}.{type(x).__qualname__}") from None
-        if where < 0:
-            raise ValueError(f"expected a CUDA tensor, got one on {x.device}")
-        if _many_gpus:
-            import torch
-            if where != torch.cuda.current_device():
-                raise ValueError(f"expected a tensor on the current device (cuda:{torch.cuda.current_device()}), got one on {x.device}")
+            pass
+    return [_address(x, kind) for x, kind in zip(args, kinds)]
 
 
 def rope_frequencies(rotary_dim: int = 128, theta: float = 1e6, scaling: str = "plain", factor: float = 1.0,
@@ -484,10 +506,9 @@ def rope_append(q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens,
                 inv_freq, p: QFParams, r: QFRopeParams, stream=None, check: bool = True) -> int:
     """Norms, rotary positions and the cache write of packed tokens in one launch; any of q, (k, v), k_out, the
     caches, pos_base and the gains may be None (see qf_rope_append)."""
-    _on_current_device(q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base, q_gain, k_gain, inv_freq)
-    rc = lib().qf_rope_append(_ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(k_out), _ptr(k_cache), _ptr(v_cache),
-                              _ptr(block_table), _ptr(cu_tokens), _ptr(seq_lens), _ptr(pos_base), _ptr(q_gain),
-                              _ptr(k_gain), _ptr(inv_freq), ctypes.byref(p), ctypes.byref(r), _stream(stream))
+    at = _arrays("bbbbbbbiiiibbf", q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base, q_gain,
+                 k_gain, inv_freq)
+    rc = lib().qf_rope_append(*at, ctypes.byref(p), ctypes.byref(r), _stream(stream))
     if check and rc != QF_OK:
         raise QFError(rc, "qf_rope_append")
     return rc
@@ -500,10 +521,8 @@ def prompt_workspace_bytes(p: QFParams, total_tokens: int) -> int:
 def prompt_attend(q, k_cache, v_cache, block_table, cu_tokens, seq_lens, out, lse, p: QFParams, total_tokens: int,
                   workspace, workspace_bytes: int, q_stride: int = 0, stream=None, check: bool = True) -> int:
     """Causal attention of packed prompt rows over the paged cache that already holds their keys and values."""
-    _on_current_device(q, k_cache, v_cache, block_table, cu_tokens, seq_lens, out, lse, workspace)
-    rc = lib().qf_prompt_attend(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(cu_tokens),
-                                _ptr(seq_lens), _ptr(out), _ptr(lse), ctypes.byref(p), int(total_tokens),
-                                int(q_stride), _ptr(workspace), int(workspace_bytes), _stream(stream))
+    *at, ws = _arrays("bbbiiibf*", q, k_cache, v_cache, block_table, cu_tokens, seq_lens, out, lse, workspace)
+    rc = lib().qf_prompt_attend(*at, ctypes.byref(p), int(total_tokens), int(q_stride), ws, int(workspace_bytes), _stream(stream))
     if check and rc != QF_OK:
         raise QFError(rc, "qf_prompt_attend")
     return rc
@@ -525,10 +544,8 @@ def prefix_partial(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets
                    p: QFParams, num_groups: int, max_prefix_pages: int, workspace, workspace_bytes: int, stream=None,
                    check: bool = True) -> int:
     """States of every request over its group's shared prefix, each prefix swept once."""
-    _on_current_device(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, o_part, m_part, lse_part, workspace)
-    rc = lib().qf_prefix_partial(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(prefix_table), _ptr(prefix_lens),
-                                 _ptr(group_offsets), _ptr(o_part), _ptr(m_part), _ptr(lse_part), ctypes.byref(p),
-                                 int(num_groups), int(max_prefix_pages), _ptr(workspace), int(workspace_bytes),
+    *at, ws = _arrays("bbbiiifff*", q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, o_part, m_part, lse_part, workspace)
+    rc = lib().qf_prefix_partial(*at, ctypes.byref(p), int(num_groups), int(max_prefix_pages), ws, int(workspace_bytes),
                                  _stream(stream))
     if check and rc != QF_OK:
         raise QFError(rc, "qf_prefix_partial")
@@ -539,13 +556,9 @@ def prefix_step(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, prefix
                 o_part, m_part, lse_part, out, lse, p: QFParams, num_groups: int, max_prefix_pages: int, workspace,
                 workspace_bytes: int, stream=None, check: bool = True) -> int:
     """One decode step behind shared prefixes: prefix sweep, own pages' sweep and the merge of both."""
-    _on_current_device(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, prefix_table, prefix_lens, group_offsets, o_part,
-                       m_part, lse_part, out, lse, workspace)
-    rc = lib().qf_prefix_step(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens),
-                              _ptr(shard_ranges), _ptr(prefix_table), _ptr(prefix_lens), _ptr(group_offsets),
-                              _ptr(o_part), _ptr(m_part), _ptr(lse_part), _ptr(out), _ptr(lse), ctypes.byref(p),
-                              int(num_groups), int(max_prefix_pages), _ptr(workspace), int(workspace_bytes),
-                              _stream(stream))
+    *at, ws = _arrays("bbbiiiiiifffff*", q, k_cache, v_cache, block_table, seq_lens, shard_ranges, prefix_table, prefix_lens,
+                      group_offsets, o_part, m_part, lse_part, out, lse, workspace)
+    rc = lib().qf_prefix_step(*at, ctypes.byref(p), int(num_groups), int(max_prefix_pages), ws, int(workspace_bytes), _stream(stream))
     if check and rc != QF_OK:
         raise QFError(rc, "qf_prefix_step")
     return rc

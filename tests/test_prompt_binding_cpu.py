@@ -67,7 +67,7 @@ class OnDevice:
     """Stands in for a CUDA tensor of a machine with several GPUs."""
 
     def __init__(self, index, dtype=torch.bfloat16):
-        self.index, self.dtype, self.device = index, dtype, f"cuda:{index}"
+        self.index, self.dtype, self.device, self.is_cuda = index, dtype, f"cuda:{index}", True
 
     def get_device(self):
         return self.index
@@ -78,7 +78,32 @@ class OnDevice:
 
 @pytest.mark.parametrize("call,name", ARGS)
 def test_a_tensor_of_another_gpu_is_refused_whatever_the_argument(call, name, monkeypatch):
+    assert go(call) == qf.QF_ERR_UNSUPPORTED           # the number of GPUs has been looked up
     monkeypatch.setattr(qf, "_many_gpus", True)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     with pytest.raises(ValueError, match="current device"):
-        go(call, **{name: OnDevice(1)})
+        go(call, **{name: OnDevice(1, types(call, name)[0][0])})
+
+
+def types(call, name):
+    """Element types that an argument may have, and some that it may not."""
+    if name in INTS:
+        return [torch.int32], [torch.int64, torch.int16, torch.float32]
+    if name in FLOATS or (call == "prefix_step" and name == "out"):
+        return [torch.float32], [torch.float64, torch.bfloat16, torch.int32]
+    return [torch.bfloat16, torch.int16, torch.uint16], [torch.float16, torch.float32, torch.float8_e4m3fn, torch.int32]
+
+
+INTS = {"block_table", "cu_tokens", "seq_lens", "pos_base", "shard_ranges", "prefix_table", "prefix_lens", "group_offsets"}
+FLOATS = {"inv_freq", "lse", "o_part", "m_part", "lse_part"}
+
+
+@pytest.mark.parametrize("call,name", ARGS)
+def test_other_element_types_are_refused_whatever_the_argument(call, name):
+    """Offsets from torch.cumsum are 64 bits wide, gains of a model may be fp32, fp16 is not bf16: all would be misread."""
+    fine, wrong = types(call, name)
+    for t in wrong:
+        with pytest.raises(ValueError, match="expected elements"):
+            go(call, **{name: OnDevice(0, t)})
+    for t in fine:
+        assert go(call, **{name: OnDevice(0, t)}) == qf.QF_ERR_UNSUPPORTED
