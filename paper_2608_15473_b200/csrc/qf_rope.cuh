@@ -25,6 +25,7 @@
 #pragma once
 
 #include <mutex>
+#include <stddef.h>
 
 #include "qf_common.cuh"
 #include "qf_page_math.cuh"
@@ -102,11 +103,12 @@ __device__ __forceinline__ unsigned long long swap_pair(unsigned long long v)
 }
 
 // Place and angles of the tokens t0 .. t0 + tokens - 1, by one warp.
-struct RopeStep {
+struct __align__(16) RopeStep {
     float2 turn[kRopeMaxTokens][64];     // (cos, sin) of every pair
     long long page[kRopeMaxTokens];      // physical page of the token's position, -1 = none
     int slot[kRopeMaxTokens];            // slot within the page; -1: a token of no request
 };
+static_assert(alignof(RopeStep) >= 16 && offsetof(RopeStep, turn) % 16 == 0, "two pairs of a turn are read as one float4");
 __device__ __forceinline__ void rope_prepare(RopeStep &st, const RopeArgs &A, const DevParams &P, int t0, int tokens)
 {
     const int lane = threadIdx.x & 31;
