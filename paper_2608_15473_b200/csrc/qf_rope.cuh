@@ -118,7 +118,7 @@ __device__ __forceinline__ void rope_prepare(RopeStep &st, const RopeArgs &A, co
     if (lane < tokens && t0 + lane < A.total_tokens) {
         b = request_of(A.cu, P.batch, t0 + lane);
         if (b >= 0) {
-            pos = (long long)max(A.seq_lens[b], 0) + (t0 + lane - A.cu[b]);
+            pos = (long long)max(A.seq_lens[b], 0) + ((long long)(t0 + lane) - A.cu[b]);   // not below 0, whatever the offset
             base = A.pos_base ? A.pos_base[b] : 0;
             long long phys = -1;      // nothing is stored where the position has no page
             if (A.k_cache && (pos >> 4) < P.max_pages_per_req) {

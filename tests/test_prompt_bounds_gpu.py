@@ -1,0 +1,39 @@
+"""Offsets and table entries that are far out of range: nothing outside the arrays is read or written, and what is in range
+stays right."""
+import pytest
+import torch
+
+from paper_2608_15473_b200 import binding as qf
+from paper_2608_15473_b200 import build as qf_build
+from prompt_testlib import D, Paged
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    qf_build.build()
+
+
+@pytest.mark.parametrize("first", [-1, -2 ** 30, -2 ** 31])
+def test_rows_of_a_request_that_begins_far_below_zero(first):
+    """The caller's error, but one whose rows lie 2^31 positions into the context: beyond every table row, so that nothing
+    is stored.  (At -1 the rows' places are one further on.)"""
+    hq, n = 4, 40
+    pg = Paged([n], [3], 2, extra_pages=2, max_pages=4)
+    pg.table[0, :4] = torch.arange(4, dtype=torch.int32)
+    g = torch.Generator().manual_seed(2)
+    q, k, v = (torch.randn((n, h * D), generator=g).to(torch.bfloat16).cuda() for h in (hq, 2, 2))
+    kc, vc = pg.pools()
+    k0, v0, qo = kc.clone(), vc.clone(), torch.empty_like(q)
+    p, r = qf.params(1, hq, 2, 4, 1, pg.num_pages), qf.rope_params(n, 0)
+    cu = torch.tensor([first, n], dtype=torch.int32).cuda()
+    qf.rope_append(q, k, v, qo, None, kc, vc, pg.table.cuda(), cu, pg.lens.cuda(), None, None, None, None, p, r)
+    torch.cuda.synchronize()
+    assert torch.equal(qo, q)
+    if first != -1:
+        assert torch.equal(kc, k0) and torch.equal(vc, v0)
+    else:
+        for pool, x in ((kc, k), (vc, v)):
+            rows = pool[:4].permute(0, 2, 1, 3).reshape(64, 2, D)
+            assert torch.equal(rows[4:4 + n], x.reshape(n, 2, D))
