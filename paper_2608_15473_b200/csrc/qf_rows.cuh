@@ -807,12 +807,13 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 for (int i = 0; i < kTilePages; ++i) at[i] = __shfl_sync(0xffffffffu, c2, i);
                 if (elect_one()) {
                     const uint32_t full = smem_u32(&sm.kv_full[stage]), dst = smem_u32(sm.kv[stage]);
+                    // before the arrival, which releases it to whoever works on this tile
+                    if (!is_v) sm.bad_pages[tile_no & 7] = bad_mask;
                     mbar_arrive_expect_tx(full, kTileBytes);
                     if (is_v) {
 #pragma unroll
                         for (int i = 0; i < kTilePages; ++i) tma_load_4d(dst + i * kPageBytes, &maps.v, 0, c1, at[i], 0, full);
                     } else {
-                        sm.bad_pages[tile_no & 7] = bad_mask;
                         if (bad_mask && P.check_bounds) rows_status_or(A.status, kStatusBadPage);
 #pragma unroll
                         for (int i = 0; i < 2 * kTilePages; ++i)

@@ -5,7 +5,8 @@ import torch
 
 from paper_2608_15473_b200 import binding as qf
 from paper_2608_15473_b200 import build as qf_build
-from prompt_testlib import D, Paged
+from prompt_testlib import D, PAGE, Paged, attend64
+from test_prompt_attend_gpu import attend, compare, queries
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +38,30 @@ def test_rows_of_a_request_that_begins_far_below_zero(first):
         for pool, x in ((kc, k), (vc, v)):
             rows = pool[:4].permute(0, 2, 1, 3).reshape(64, 2, D)
             assert torch.equal(rows[4:4 + n], x.reshape(n, 2, D))
+
+
+@pytest.mark.parametrize("rows", [[1], [200], [3, 90, 1, 40]])
+def test_bad_entries_that_differ_from_tile_to_tile(rows):
+    """Random entries are bad, other ones in every tile of 8 pages, over many turns of the ring of tiles: each tile's
+    positions are hidden by its own entries, time after time."""
+    cached = [6_000 + 130 * i for i in range(len(rows))]
+    pg = Paged(rows, cached, 2, seed=len(rows))
+    good = pg.table.clone()
+    g = torch.Generator().manual_seed(3)
+    gone = torch.rand(pg.table.shape, generator=g) < 0.3
+    pg.table[gone] = torch.tensor([-1, pg.num_pages, 2 ** 31 - 1, -2 ** 31])[torch.randint(4, (int(gone.sum()),), generator=g)].to(torch.int32)
+    q = queries(pg, 8)
+    parts = []
+    for b, n in enumerate(rows):
+        keep = torch.tensor([i for i in range(cached[b] + n) if not gone[b, i // PAGE]])
+        k, v = ((pg.k if w == "k" else pg.v)[good[b][keep // PAGE].long(), :, keep % PAGE].permute(1, 0, 2).double() for w in "kv")
+        seen = (keep[None, :] <= cached[b] + torch.arange(n)[:, None]).sum(1)
+        parts.append(attend64(q[int(pg.cu[b]):int(pg.cu[b]) + n].double(), k.cuda(), v.cuda(), seen.cuda()))
+    ref = {n: torch.cat([d[n] for d in parts]).cpu() for n in parts[0]}
+    first = None
+    for _ in range(20):
+        out, lse, status = attend(pg, q, qf.QF_FLAG_CHECK_BOUNDS)
+        assert status == qf.QF_STATUS_BAD_PAGE
+        first = first or (out, lse)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    compare(out, lse, ref)
