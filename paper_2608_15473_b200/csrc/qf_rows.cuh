@@ -508,6 +508,51 @@ __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const 
     }
 }
 
+// The rare end of a prefix block whose values are not all finite.  Weights are positive, but the second term of a weight may
+// be 0 or negative, and an infinity times that, or an accumulator's infinity times a factor that underflows, is NaN.  So the
+// warp searches the values of the stretch, and every row that is not NaN or empty itself gets what it sees, over what it
+// has written: NaN, or both infinities, make NaN, infinities of one sign make that infinity.
+__device__ QF_COLD void mend_infinite(const RowsArgs &A, const DevParams &P, const RowsBlock &b, bool mine, int c0, int c1,
+                                      float *slot_base, int slot_row, size_t out_row)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int c = c0; c < c1; ++c) {
+        unsigned nan = 0, pos = 0, neg = 0;      // bit i: channel 32 c + i
+#pragma unroll 1
+        for (int i = b.t_lo * kRowTile + lane; i < min(b.len, b.t_hi * kRowTile); i += 32) {
+            const long long at = (long long)b.seq * A.table_width + (i >> 4);
+            const long long phys = A.table ? (long long)A.table[at] : at;
+            if (phys < 0 || phys >= P.num_pages) continue;
+            const uint4 *v = reinterpret_cast<const uint4 *>(A.v_cache + kv_row_offset(P, phys, b.head, i & 15) + c * 32);
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+                const uint4 x = v[k];
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t u = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu, bit = 1u << (8 * k + e);
+                    if ((u & 0x7f80u) != 0x7f80u) continue;
+                    if (u & 0x7fu) nan |= bit;
+                    else if (u >> 15) neg |= bit;
+                    else pos |= bit;
+                }
+            }
+        }
+        nan = __reduce_or_sync(0xffffffffu, nan);
+        pos = __reduce_or_sync(0xffffffffu, pos);
+        neg = __reduce_or_sync(0xffffffffu, neg);
+        nan |= pos & neg;
+        if (!mine) continue;
+        for (unsigned left = nan | pos | neg; left; left &= left - 1) {
+            const int i = __ffs((int)left) - 1, d = c * 32 + i;
+            const float x = __uint_as_float((nan >> i) & 1 ? 0x7fc00000u : (pos >> i) & 1 ? 0x7f800000u : 0xff800000u);
+            if (b.slot >= 0) __stcg(slot_base + ((size_t)(d >> 2) * (2 * kRowTile) + slot_row) * 4 + (d & 3), x);
+            else A.o_part[out_row * kHeadDim + d] = x;
+        }
+    }
+}
+
 // A tile of values in shared memory, by one warp: rows from `exist` on, as far as their page goes, become 0, and so do
 // non-finite values among rows seen_by_all .. used - 1 (from the page's start), which `dirty` then reports.
 __device__ QF_COLD void clean_tile(uint8_t *v, int exist, int seen_by_all, int used, volatile int *dirty)
@@ -1236,8 +1281,13 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             float *slot_base = b.slot >= 0 ? slots + (size_t)b.slot * kRowsSlotFloats : nullptr;
             const int slot_row = (b.narrow ? 0 : wg * kRowTile) + r;
             const bool dirty = !PREFIX && *reinterpret_cast<volatile int *>(&sm.dirty[slot]) != 0;
+            float odd = 0.f;      // prefix: NaN once a result is not finite
             auto finish = [&](int c, const float (&o)[32]) {
                 if (!live) return;
+                if (PREFIX) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) odd = fmaf(o[i], 0.f, odd);
+                }
                 if (b.slot >= 0) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
@@ -1279,6 +1329,10 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 finish(c, o);
             }
             if (dirty && live) add_hidden(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
+            if (PREFIX) {
+                const bool mine = live && !empty && l == l;
+                if (__any_sync(0xffffffffu, mine && odd != odd)) mend_infinite(A, P, sm.info[slot], mine, c0, c1, slot_base, slot_row, out_row);
+            }
             if (b.narrow) {
                 // nobody may touch either accumulator, or ml, before both groups have read them
                 tc_fence_before();

@@ -300,3 +300,51 @@ def test_small_step_whose_scores_are_all_nan():
         torch.cuda.synchronize()
         for x in (out, lse):
             assert torch.isnan(x[0]).all() and torch.isnan(x[2]).all() and torch.isfinite(x[1]).all()
+
+
+# ---- values
+def plant_values(sh, g, n):
+    """Channel 3: +infinity; 40: -infinity; 77: both; 90: NaN; 127: +infinity twice; 64: the last position's."""
+    def put(i, ch, x):
+        sh.pg.v[int(sh.ptab[g, i // PAGE]), :, i % PAGE, ch] = x
+    put(n // 2, 3, INF), put(n // 3, 40, -INF), put(n - 1, 64, INF), put(n // 2, 90, NAN), put(0, 127, INF), put(n // 2, 127, INF)
+    if n > 1:
+        put(0, 77, INF), put(n - 1, 77, -INF)
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+@pytest.mark.parametrize("sizes,n", [([1, 2], 1), ([3, 2], 50), ([3, 1], 100), ([40, 3], 128), ([90, 2], 700), ([2, 1], 20_000), ([40, 5], 9_000)])
+def test_infinite_values_of_a_prefix(flags, sizes, n):
+    """Every request of the group sees them with a positive weight: infinities of one sign are the result, not NaN."""
+    sh = Shared(sizes, [n, 70], [1] * sum(sizes), 2, seed=n)
+    plant_values(sh, 0, n)
+    q = queries_of(sh, 8)
+    ref = partial64(sh, q)
+    assert torch.isposinf(ref[0][:sizes[0], :, 3]).all() and torch.isfinite(ref[0][sizes[0]:]).all()
+    o, m, l, _ = partial(sh, q, flags)
+    check_state(o, m, l, ref)
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+def test_infinite_values_in_a_step(flags):
+    sh = Shared([5, 3], [1000, 30], [1 + 9 * i for i in range(8)], 2)
+    plant_values(sh, 0, 1000)
+    q = queries_of(sh, 8)
+    out, lse, _ = step(sh, q, 2, flags)
+    ro, rl = step64(sh, q)
+    check_state(out, None, lse, (ro, None, rl))
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+def test_infinite_values_and_a_bad_key(flags):
+    """A row whose scores are NaN stays NaN; positions behind bad entries hold nothing, whatever the pool holds."""
+    sh = Shared([3, 3], [200, 200], [1] * 6, 2)
+    plant_values(sh, 0, 200), plant_values(sh, 1, 200)
+    put_key(sh.pg, sh.ptab[0], 150, NAN)
+    whole = Shared([3, 3], [200, 192], [1] * 6, 2)
+    whole.pg, whole.ptab = sh.pg, sh.ptab.clone()
+    q = queries_of(sh, 8)
+    ref = partial64(whole, q)
+    sh.ptab[1, 12] = -5
+    o, m, l, _ = partial(sh, q, flags)
+    check_state(o, m, l, ref)
