@@ -9,14 +9,15 @@ ragged contexts in [1,024, 36,480], 16-token pages in a shuffled block table,
 4,096-token shards), the configuration the headline metric is quoted on.
 
   python bench.py [--gpus N] [--steps K] [--warmup W] [--workload 3] [--impl reference]
-                  [--split-request] [--no-also]
+                  [--split-request] [--no-also] [--record FILE]
 
-Prints ONE JSON line (rank 0).  The K steps are timed R >= 7 times (enough repeats for about 0.4 s of
-load); `ms_per_step` is the median repeat, and the line carries the spread and every repeat's median SM
-clock, so that a reader can tell the kernel from the clock.  At N = 1 the line also carries, under
+Prints ONE JSON line (rank 0), short enough for a reader that keeps the end of an output; --record FILE stores
+the whole record.  The K steps are timed R >= 7 times (enough repeats for about 0.4 s of
+load); `ms_per_step` is the median repeat, the line carries the spread, and the record every repeat's time and
+median SM clock, so that a reader can tell the kernel from the clock.  At N = 1 the line also carries, under
 `also`, the other configurations (the one-million-token split-KV workload with its identity table and
 with a shuffled one, the two other batched workloads, the single short request cold and warm), each
-with its own roofline, clocks and whole-workload parity against the CPU oracle.
+in the record with its own roofline, clocks and whole-workload parity against the CPU oracle.
 
 With N > 1 (launched by torch.distributed.run) every rank sweeps its own batch of requests; requests are
 independent, so there is no data-path collective and scaling is weak.  With --split-request the N ranks
@@ -255,6 +256,39 @@ def run_reference(args):
         "kv_tokens_per_s": ntok * args.steps / total,
     }
     print(json.dumps(line), flush=True)
+
+
+# ----------------------------------------------------------------------------------------------- the line
+LINE_CHARS = 2700      # what a reader of the last 3,000 characters of the output still sees whole
+
+
+def short_line(rec):
+    """The record without what only explains its numbers: notes, lists of repeats, the other configurations' details;
+    numbers other than the contract's to six digits."""
+    explains = ("note", "what", "tolerance", "against", "single_thread", "source", "per_repeat", "ms_x_mhz", "inf_pattern", "corr_",
+                "fastest_", "slowest_", "min_ms_per_", "max_ms_per_", "synchronous_min", "p10", "p90")
+
+    def brief(x):
+        if isinstance(x, dict):
+            return {k: brief(v) for k, v in x.items() if not k.startswith(explains)}
+        return float(f"{x:.6g}") if isinstance(x, float) else x
+
+    line = {k: v if k in ("value", "ms_per_step") else brief(v) for k, v in rec.items() if k not in ("also", "sweep_kernel_pct_of_hbm_peak")}
+    if "e2e" in rec:
+        line["e2e"]["value"] = rec["e2e"]["value"]
+    if "also" in rec:
+        line["also"] = []
+        for a in rec["also"]:
+            name = a["workload"].split()[0] + next((" " + x for x in ("shuffled table", "token-major") if "(" + x in a["workload"]), "")
+            line["also"].append({"workload": name, "error": a["error"][:60]} if "error" in a else
+                                {"workload": name, **brief({k: a[k] for k in ("ms_per_step", "GB/s")}), "parity_ok": a.get("parity", {}).get("ok")})
+    return line
+
+
+def emit(rec, path=None):
+    if path:
+        Path(path).write_text(json.dumps(rec) + "\n")
+    print(json.dumps(short_line(rec)), flush=True)
 
 
 # ----------------------------------------------------------------------------------------------- timing
@@ -549,7 +583,7 @@ def run_split_request(args, dist, rank, world, local_rank, device):
                               "against": "the CPU oracle's unsharded sweep of the whole request"}
             line["cpu_baseline"] = {"value": total_bytes / dt / 1e9, "unit": "GB/s", "cores": orc.num_threads(),
                                     "kind": "oracle", "seconds": dt, "sample": "the whole request once, unsharded"}
-        print(json.dumps(line), flush=True)
+        emit(line, args.record)
     if dist is not None:
         dist.barrier()
         dist.destroy_process_group()
@@ -732,7 +766,7 @@ def run_cuda(args):
             except Exception as ex:
                 also.append({"workload": workload_name(1), "error": f"{type(ex).__name__}: {ex}"})
             line["also"] = also
-        print(json.dumps(line), flush=True)
+        emit(line, args.record)
     if dist is not None:
         dist.barrier()
         dist.destroy_process_group()
@@ -754,6 +788,8 @@ def main():
     ap.add_argument("--split-transport", default="parked", choices=["parked", "gather"],
                     help="with --split-request: shard states stored straight into the owner's arrays (default) or all-gathered")
     ap.add_argument("--no-cpu-baseline", action="store_true")
+    ap.add_argument("--record", default=None, metavar="FILE",
+                    help="store the whole record: every repeat's time and clock, notes, the other configurations in full")
     ap.add_argument("--no-also", action="store_true", help="time the headline configuration only")
     ap.add_argument("--profile-mode", action="store_true",
                     help="for runs under a profiler: one repeat, one end-to-end step, no CPU baseline, no other configurations")
