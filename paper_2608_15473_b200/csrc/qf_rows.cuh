@@ -1251,7 +1251,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             }
             // A score was NaN or +infinity: the row is NaN, and not empty, whatever its reference was when the score came.
             if (!(m_true < __int_as_float(0x7f800000))) l = m_ref = __int_as_float(0x7fc00000);
-            float w_own = started ? 1.f : 0.f, w_other = 0.f;     // weights of this group's accumulator and, narrow, the other's
+            float w_own = 1.f, w_other = 0.f;     // weights of this group's accumulator and, narrow, the other's
             int c0 = 0, c1 = 4;                   // column chunks of 32 that this thread finishes
             uint32_t t_x = t_o;                   // the other group's accumulator
             if (b.narrow) {
@@ -1274,7 +1274,10 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 c1 = c0 + 2;
                 t_x = t_o0 + (wg ^ 1) * 128 + lane_base;
             }
+            // Nothing visible, or weights that are all 0: the result is 0, whatever the values (and the accumulator) hold.
             const bool empty = m_ref == neg_inf();
+            if (empty) w_own = w_other = 0.f;
+            const bool any_empty = __any_sync(0xffffffffu, empty);
             const float inv = b.slot >= 0 ? 1.f : empty ? 0.f : 1.f / l;
             const int row = b.row0 + tok, h = b.head * G + my_g;
             const size_t out_row = PREFIX ? ((size_t)row * A.out_shards + A.slot) * Hq + h : (size_t)row * Hq + h;
@@ -1315,7 +1318,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 tmem_ld32_nowait(t_o + c * 32, o);
                 tmem_wait_ld();
                 pin32(o);
-                if (b.narrow || !started) {      // nothing visible: the accumulator may hold anything
+                if (b.narrow || any_empty) {
                     float x[32];
                     tmem_ld32_nowait(t_x + c * 32, x);
                     tmem_wait_ld();
@@ -1328,7 +1331,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 }
                 finish(c, o);
             }
-            if (dirty && live) add_hidden(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
+            if (dirty && live && !empty) add_hidden(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
             if (PREFIX) {
                 const bool mine = live && !empty && l == l;
                 if (__any_sync(0xffffffffu, mine && odd != odd)) mend_infinite(A, P, sm.info[slot], mine, c0, c1, slot_base, slot_row, out_row);

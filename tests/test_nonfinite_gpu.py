@@ -348,3 +348,35 @@ def test_infinite_values_and_a_bad_key(flags):
     sh.ptab[1, 12] = -5
     o, m, l, _ = partial(sh, q, flags)
     check_state(o, m, l, ref)
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+@pytest.mark.parametrize("n", [1, 30, 64, 100, 150, 300])
+def test_rows_whose_every_weight_is_zero(flags, n):
+    """All visible scores are -infinity: such a row is an empty set (0, -infinity), whatever the values hold."""
+    pg = Paged([n, 1, n], [0, 20, 0], 2, seed=n)
+    for b, last in ((0, n), (1, 21), (2, 1 + n // 2)):      # the third request: rows from 1 + n / 2 on see a finite key
+        for i in range(last):
+            put_key(pg, pg.table[b], i, -INF)
+    for b in range(2):
+        for ch, x in ((3, INF), (40, NAN), (90, -INF), (127, INF)):
+            pg.v[int(pg.table[b, 0]), :, 0, ch] = x
+    q = positive_first(queries(pg, 8))
+    out, lse, _ = attend(pg, q, flags)
+    empty = torch.tensor([True] * n + [True] + [i < 1 + n // 2 for i in range(n)]).cuda()
+    assert (out[empty] == 0).all() and torch.isneginf(lse[empty]).all()
+    assert torch.isfinite(out[~empty]).all() and torch.isfinite(lse[~empty]).all()
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+@pytest.mark.parametrize("sizes,n", [([2, 1], 1), ([2, 1], 50), ([3, 2], 130), ([90, 2], 700), ([1, 1], 9_000)])
+def test_prefixes_whose_every_weight_is_zero(flags, sizes, n):
+    sh = Shared(sizes, [n, 70], [1] * sum(sizes), 2, seed=n)
+    for i in range(n):
+        put_key(sh.pg, sh.ptab[0], i, -INF)
+    plant_values(sh, 0, n)
+    q = positive_first(queries_of(sh, 8))
+    o, m, l, _ = partial(sh, q, flags)
+    a = sizes[0]
+    assert (o[:a] == 0).all() and torch.isneginf(m[:a]).all() and torch.isneginf(l[:a]).all()
+    assert torch.isfinite(o[a:]).all() and torch.isfinite(l[a:]).all()
