@@ -673,6 +673,10 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         }
     }
 
+    if (P.check_bounds)
+        for (int s = (int)blockIdx.x * kRowsThreads + tid; s < A.n_seq; s += (int)gridDim.x * kRowsThreads)
+            if (seq_overruns<PREFIX>(A, s)) rows_status_or(A.status, kStatusBadPage);
+
     // ---- this CTA's slice.  A thread adds up a sequence's blocks, or a warp does while there are no more sequences
     // than warps.
     const int n_ctas = (int)gridDim.x;

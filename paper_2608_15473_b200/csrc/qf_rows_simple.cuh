@@ -57,6 +57,14 @@ __device__ __forceinline__ int row_limit(const SeqRows &r, int i)
     return PREFIX ? r.len : (int)min((long long)r.off + i + 1, (long long)r.len);
 }
 
+// Rows of the sequence would see positions beyond the table row (or the caller's bound): clamped, and reported if asked for.
+template <bool PREFIX>
+__device__ __forceinline__ bool seq_overruns(const RowsArgs &A, int s)
+{
+    const SeqRows r = seq_rows<PREFIX>(A, s);
+    return r.n > 0 && (long long)max(A.lens[s], 0) + (PREFIX ? 0 : r.n) > A.max_tokens;
+}
+
 constexpr int kRowsSimpleWarps = 8;
 
 // One warp per (row, query head), lane owns four channels, fp32 online softmax over the positions in order.
@@ -83,6 +91,7 @@ rows_simple_kernel(RowsArgs A, DevParams P)
     if (s >= 0) {
         const SeqRows sr = seq_rows<PREFIX>(A, s);
         limit = row_limit<PREFIX>(sr, row - sr.first);
+        if (P.check_bounds && row == sr.first && h == 0 && lane == 0 && seq_overruns<PREFIX>(A, s)) rows_status_or(A.status, kStatusBadPage);
     }
     const uint2 qw = *reinterpret_cast<const uint2 *>(A.q + (long long)row * A.q_stride + h * kHeadDim + lane * 4);
     float m = neg_inf(), l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};

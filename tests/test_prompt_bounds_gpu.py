@@ -6,7 +6,8 @@ import torch
 from paper_2608_15473_b200 import binding as qf
 from paper_2608_15473_b200 import build as qf_build
 from prompt_testlib import D, PAGE, Paged, attend64
-from test_prompt_attend_gpu import attend, compare, queries
+from test_prefix_gpu import Shared, partial
+from test_prompt_attend_gpu import KERNELS, attend, compare, queries
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +66,23 @@ def test_bad_entries_that_differ_from_tile_to_tile(rows):
         first = first or (out, lse)
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
     compare(out, lse, ref)
+
+
+@pytest.mark.parametrize("flags", KERNELS)
+def test_lengths_beyond_the_table_row_are_reported(flags):
+    """As the sweep reports them: under QF_FLAG_CHECK_BOUNDS, and only where rows would see positions beyond it."""
+    check = flags | qf.QF_FLAG_CHECK_BOUNDS
+    for new, cached, want in ((20, 44, 0), (20, 45, 1), (1, 64, 1), (0, 1000, 0), (70, 0, 1), (64, 0, 0)):
+        pg = Paged([new, 3], [cached, 2], 2, max_pages=4, extra_pages=80)
+        q = queries(pg, 4)
+        assert attend(pg, q, flags)[2] == 0
+        assert attend(pg, q, check)[2] == (qf.QF_STATUS_BAD_PAGE if want else 0), (new, cached)
+    pg = Paged([20, 20], [0, 18], 2, max_pages=4)
+    assert attend(pg, queries(pg, 4), check, max_seq_len=38)[2] == 0
+    assert attend(pg, queries(pg, 4), check, max_seq_len=37)[2] == qf.QF_STATUS_BAD_PAGE
+    for more, want in ((0, 0), (1, 1), (2 ** 31 - 1 - 64, 1)):
+        sh = Shared([4, 2], [64, 30], [1] * 6, 2)
+        sh.plen[0] += more
+        q = torch.randn((6, 4, D), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+        assert partial(sh, q, flags)[3] == 0
+        assert partial(sh, q, check)[3] == (qf.QF_STATUS_BAD_PAGE if want else 0), more
