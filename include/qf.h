@@ -37,6 +37,9 @@
  *     q and the cached keys arrive ready to be multiplied (qf_rope_append makes
  *     them so);
  *   - natural logarithm; the scale multiplies the finished fp32 dot product;
+ *   - a score that is NaN or +infinity (a key or a query that is not finite)
+ *     makes the state it belongs to NaN, vector and log Z, and every merge of
+ *     that state; a set whose every score is -infinity is an empty one;
  *   - o_part is the shard-NORMALISED O(S); m_part is the running maximum
  *     score (auxiliary: W relative to m is o_part * e^{lse_part - m_part});
  *   - outputs are fp32; K, V, q are bf16.
@@ -363,10 +366,12 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
  * row i of request b sees positions 0 .. seq_lens[b] + i.  An empty cache (seq_lens 0) is a whole prompt, a filled
  * one a later chunk of it; one-row requests are decode steps riding along.
  *     out bf16 [total_tokens, Hq, 128] (one rounding, of the fp32 result),  lse fp32 [total_tokens, Hq]
- * The weights that multiply the values are rounded to bf16 (out is bf16: their errors average out below its own
- * rounding); scores, maxima, sums and accumulators are fp32.  q: bf16, rows q_stride elements apart (0 = packed).
- * Rows that belong to no request are left as they were.  A table entry outside [0, num_pages) contributes nothing
- * (reported under QF_FLAG_CHECK_BOUNDS); positions beyond the table row are not attended.  Values at positions a
+ * The weights that multiply the values are rounded to bf16 (out is bf16: out is off by 1.2 to 1.4 times what its own
+ * rounding alone would give); scores, maxima, sums and accumulators are fp32, and three of eight exponentials come
+ * from a polynomial with a relative error of 2.9e-6.  q: bf16, rows q_stride elements apart (0 = packed).
+ * Rows that belong to no request are left as they were.  A table entry outside [0, num_pages) contributes nothing;
+ * positions beyond the table row, or from p->max_seq_len on if that is set (here it bounds cached and new positions
+ * together), are not attended; both are reported under QF_FLAG_CHECK_BOUNDS.  Values at positions a
  * row does not see never reach its result, NaN and infinities included.  p->max_shards is not used (pass 1).
  * k_cache, v_cache 128-byte, q 16-byte, out 32-byte aligned.  workspace: qf_prompt_workspace_bytes bytes (64 MB,
  * whatever the sizes), 256-byte aligned, contents need not be initialised; one call at a time.  Results do not depend
@@ -394,9 +399,11 @@ int qf_prompt_status(const void *workspace, int32_t *host_status, void *cuda_str
  * head over its group's prefix into slot p->out_shard_offset of o_part [B, out_shards, Hq, 128], m_part, lse_part
  * (out_shards = p->out_shards, or p->max_shards when that is 0), exactly as qf_decode_partial would write a shard;
  * requests of no group and empty prefixes get (0, -inf, -inf).  Other slots are not touched.  num_groups <= B.
- * The weights enter the value product as two bf16 terms (16 bits), everything else is fp32; against 64 bits the states
- * are off by 2e-6 to 6e-6 of their norm, like qf_decode_partial's.  prefix_lens beyond the table row are clamped to
- * it.  Errors, bounds and alignment as for qf_decode_partial, and o_part 32-byte aligned; workspace:
+ * The weights enter the value product as two bf16 terms (16 bits), one of eight exponentials comes from a polynomial
+ * with a relative error of 1.7e-7, everything else is fp32; against 64 bits the states are off by 2e-6 to 6e-6 of their
+ * norm, like qf_decode_partial's (all in fp32: 0.5e-6 to 3e-6).  A value that is infinite makes its channel infinite
+ * (NaN where both infinities or a NaN are seen); qf_decode_partial makes it NaN.  prefix_lens beyond the table row are
+ * clamped to it (reported under QF_FLAG_CHECK_BOUNDS).  Errors, bounds and alignment as for qf_decode_partial, and o_part 32-byte aligned; workspace:
  * qf_prefix_workspace_bytes bytes, 256-byte aligned, one call at a time.  Enqueues two kernels; capturable (make one
  * call per device before capturing).
  */

@@ -505,7 +505,8 @@ def rope_params(total_tokens: int, rotary_dim: int = 128, interleaved: bool = Fa
 def rope_append(q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base, q_gain, k_gain,
                 inv_freq, p: QFParams, r: QFRopeParams, stream=None, check: bool = True) -> int:
     """Norms, rotary positions and the cache write of packed tokens in one launch; any of q, (k, v), k_out, the
-    caches, pos_base and the gains may be None (see qf_rope_append)."""
+    caches, pos_base and the gains may be None (see qf_rope_append).  Arrays: CUDA tensors of the current device with the
+    library's element types, or addresses."""
     at = _arrays("bbbbbbbiiiibbf", q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base, q_gain,
                  k_gain, inv_freq)
     rc = lib().qf_rope_append(*at, ctypes.byref(p), ctypes.byref(r), _stream(stream))

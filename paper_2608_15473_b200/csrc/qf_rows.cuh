@@ -31,7 +31,8 @@
 // row's maximum has grown by more than 2^8; until then it is the same factor in O and in the sum, and cancels.  So O is
 // rescaled rarely.  Prompt form: P is rounded to bf16 (at most 2^-8 of each weight; the output itself is bf16).  Prefix
 // form, whose states are fp32: P = hi + lo, two bf16 terms, 16 bits, and twice the second product, which the stream of
-// K and V hides up to about 200 rows.  How accumulators drift, and what is done about it: kChainUnits.
+// K and V hides up to about 200 rows.  How accumulators drift, and what is done about it: kChainUnits.  A row with a score
+// that is NaN or +infinity is NaN; a row whose every score is -infinity is empty.
 //
 // Measured (32 query heads on 8 KV heads; a copy reaches 6.54 TB/s, a library product 1.67 PFLOP/s, 1.40 for seconds on
 // end).  One prompt of 16,384 tokens: 1.82 ms, 1.21 PFLOP/s; 2.1 ms and 1.04 among other work, when the card is at its
@@ -70,7 +71,7 @@ constexpr int kRowsMaxCtas = 160;                // one per SM
 // What things cost, in units of about 400 cycles, fitted to the cycles of some 7,000 slices of random batches: a position
 // tile of two row tiles 3,100 cycles and of one 2,100 to 2,600 (it reads as much K and V: HBM is what it waits for), and
 // what a block costs beside its tiles 5,800 and 3,700.  (7,500 and 5,000 when the units were chosen; 8, 5, 14 and 9, which
-// would fit better now, balance no better.)
+// would fit better now, balance no better.)  A cut is not charged the second prologue and end that it causes.
 constexpr int kWideTileCost = 8, kNarrowTileCost = 6, kWideBlockCost = 18, kNarrowBlockCost = 12;
 constexpr int kMinSlice = 12;                    // less per CTA is not worth a merge
 constexpr int kWideSnap = 18, kNarrowSnap = 6;   // a cut this close to a block's border moves there
