@@ -361,6 +361,79 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
                    const qf_params *p, const qf_rope_params *r, void *cuda_stream);
 
 /*
+ * Rotary positions with several axes (time, height and width of images and video): the same pass, but pair j turns by
+ *     t = positions[pair_axis[j], row] * inv_freq[j]
+ * instead of by the row's place in its sequence.  positions: int32 [num_axes, total_tokens], any values (tokens of no
+ * request are not read as far as their results go); pair_axis: int32 [rotary_dim / 2] (device; see qf_rope_pair_axes),
+ * entries outside [0, num_axes) count as the nearest axis; num_axes 1 to 8.  The row's place in the CACHE still follows
+ * from seq_lens.  With every axis equal to that place the results are qf_rope_append's.  Everything else as there.
+ */
+int qf_rope_append_axes(const void *q, const void *k, const void *v, void *q_out, void *k_out,
+                        void *k_cache, void *v_cache, const int32_t *block_table,
+                        const int32_t *cu_tokens, const int32_t *seq_lens,
+                        const int32_t *positions, const int32_t *pair_axis, int num_axes,
+                        const void *q_gain, const void *k_gain, const float *inv_freq,
+                        const qf_params *p, const qf_rope_params *r, void *cuda_stream);
+
+/*
+ * On the host: which axis turns each of the rotary_dim / 2 pairs, from the number of pairs that each axis has
+ * (sections[num_axes], which add up to rotary_dim / 2): in stretches, axis 0 first, or, with `interleaved`, in turn
+ * (axis a > 0 has the pairs a, a + num_axes, ..., sections[a] of them; axis 0 the others).  Touches no GPU.
+ */
+int qf_rope_pair_axes(int32_t *pair_axis_host, int rotary_dim, const int32_t *sections, int num_axes, int interleaved);
+
+/*
+ * A SCALED CACHE holds keys and values in one byte each: the number at (page, KV head, slot, channel) is
+ *     code[page, head, slot, channel] * scale[page, head]
+ * with a scale per page and KV head, one array for keys and one for values.  The pools have the shapes of the bf16 pools
+ * (head-major, or token-major with QF_FLAG_KV_NHD) with one byte per element, 128-byte aligned; k_scale, v_scale are fp32
+ * [num_pages, Hkv].  Block tables, lengths, shards, states and statuses are what they are for the bf16 cache.
+ *   QF_KV_E4M3   a code is an 8-bit float: 4 exponent bits, 3 mantissa bits, magnitudes up to 448, 0x7f and 0xff NaN
+ *   QF_KV_INT8   a code is an integer, -128 to 127
+ * The calls that read take any scale.  A NaN scale (or code) makes what it stands for NaN.  Pages with a table entry
+ * outside [0, num_pages) are always skipped (their scales could not be read); QF_FLAG_CHECK_BOUNDS reports them.
+ */
+enum { QF_KV_E4M3 = 1, QF_KV_INT8 = 2 };
+
+/*
+ * qf_rope_append (or, with positions, qf_rope_append_axes) into a scaled cache.  Norms, rotation, q_out and k_out are
+ * theirs; keys and values go from the fp32 result straight to codes.  With M = 448 or 127, the scale of a block (page, head)
+ * becomes the smallest power of two, 2^-100 at least, that is not below the block's present scale and has max |y| <= M * scale
+ * over the rows this call puts there; the new rows become round(y / scale) (ties to even), and, where the scale grew, the codes
+ * of the slots before them round(code * old / new).  A page whose first slot this call writes starts without a scale.  So
+ * a block's scale is a power of two unless a caller put another one there, results do not depend on what else is in the
+ * batch, and a number is off by at most 2^-4 of itself or 2^-10 scale (e4m3) or scale / 2 (int8; at most one scale in all if
+ * the scale grew later).  A row with a value that is not finite makes its block's scale NaN.  Slots behind the rows written
+ * keep their codes (they hold nothing).  The requests of one call must not share a page that the call writes to.
+ * k_scale, v_scale may be NULL when the cache pointers are; pos_base is not read when positions are given.  One launch.
+ */
+int qf_rope_append_scaled(const void *q, const void *k, const void *v, void *q_out, void *k_out,
+                          void *k_cache, void *v_cache, float *k_scale, float *v_scale,
+                          const int32_t *block_table, const int32_t *cu_tokens, const int32_t *seq_lens,
+                          const int32_t *pos_base, const int32_t *positions, const int32_t *pair_axis, int num_axes,
+                          const void *q_gain, const void *k_gain, const float *inv_freq, int kv_type,
+                          const qf_params *p, const qf_rope_params *r, void *cuda_stream);
+
+/*
+ * qf_decode_partial and qf_decode_step over a scaled cache: same arguments, states and merges, workspace
+ * (qf_workspace_bytes), status (qf_read_status), limits and launches; the current token's fold (qf_combine_self) and the
+ * shard merge work on their states as on any.  The products take the codes exactly (as 16-bit floats), queries as bf16
+ * numbers brought into range by a power of two per head, and weights as two 16-bit terms (22 bits); scores, maxima, sums,
+ * scales and accumulators are fp32.
+ */
+int qf_decode_partial_scaled(const void *q, const void *k_cache, const void *v_cache,
+                             const float *k_scale, const float *v_scale,
+                             const int32_t *block_table, const int32_t *seq_lens, const int32_t *shard_ranges,
+                             float *o_part, float *m_part, float *lse_part, int kv_type,
+                             const qf_params *p, void *workspace, size_t workspace_bytes, void *cuda_stream);
+int qf_decode_step_scaled(const void *q, const void *k_cache, const void *v_cache,
+                          const float *k_scale, const float *v_scale,
+                          const int32_t *block_table, const int32_t *seq_lens, const int32_t *shard_ranges,
+                          const int32_t *shard_counts, float *o_part, float *m_part, float *lse_part,
+                          float *out, float *lse, int kv_type,
+                          const qf_params *p, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Attention over whole prompts: the rows cu_tokens[b] .. cu_tokens[b+1]-1 of q (packed as for qf_rope_append, same
  * seq_lens: positions cached BEFORE them) attend the paged cache, which already holds their own keys and values:
  * row i of request b sees positions 0 .. seq_lens[b] + i.  An empty cache (seq_lens 0) is a whole prompt, a filled
@@ -390,6 +463,17 @@ int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, co
  * the stream.
  */
 int qf_prompt_status(const void *workspace, int32_t *host_status, void *cuda_stream);
+
+/*
+ * qf_prompt_attend over a scaled cache (which already holds the rows' own keys and values): same arguments, workspace,
+ * status and limits.  Codes are expanded to bf16 on the way to the products: exactly where the scale is a power of two, as
+ * qf_rope_append_scaled leaves it, else with one rounding of code * scale.
+ */
+int qf_prompt_attend_scaled(const void *q, const void *k_cache, const void *v_cache,
+                            const float *k_scale, const float *v_scale, const int32_t *block_table,
+                            const int32_t *cu_tokens, const int32_t *seq_lens, void *out, float *lse, int kv_type,
+                            const qf_params *p, int total_tokens, int64_t q_stride,
+                            void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
  * A prefix that several requests share, swept ONCE for all of them (Section 5: states of disjoint token sets merge,

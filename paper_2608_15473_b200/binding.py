@@ -33,6 +33,9 @@ QF_FLAG_DRAW_ALWAYS = 8
 QF_FLAG_KV_NHD = 16
 QF_FLAG_NO_SMALL_MERGE = 32
 
+QF_KV_E4M3 = 1      # how a scaled cache holds its numbers
+QF_KV_INT8 = 2
+
 QF_STATUS_BAD_PAGE = 1
 QF_STATUS_TIMEOUT = 2
 
@@ -49,6 +52,8 @@ EXPORTS = (
     "qf_rope_frequencies", "qf_rope_append", "qf_prompt_workspace_bytes", "qf_prompt_attend", "qf_prompt_status",
     "qf_prefix_workspace_bytes", "qf_prefix_partial", "qf_prefix_step", "qf_prefix_status",
     "qf_rows_schedule",
+    "qf_rope_append_axes", "qf_rope_pair_axes", "qf_rope_append_scaled", "qf_decode_partial_scaled", "qf_decode_step_scaled",
+    "qf_prompt_attend_scaled",
 )
 
 
@@ -188,6 +193,19 @@ def lib() -> ctypes.CDLL:
         L.qf_prefix_status.argtypes = [vp, pp, ctypes.POINTER(ctypes.c_int32), vp]
         L.qf_rows_schedule.restype = ctypes.c_int
         L.qf_rows_schedule.argtypes = [ctypes.c_int, i32p, i32p] + [ctypes.c_int] * 6 + [i32p, ctypes.c_int]
+        L.qf_rope_append_axes.restype = ctypes.c_int
+        L.qf_rope_append_axes.argtypes = [vp] * 7 + [i32p] * 5 + [ctypes.c_int] + [vp] * 3 + [pp, rp, vp]
+        L.qf_rope_pair_axes.restype = ctypes.c_int
+        L.qf_rope_pair_axes.argtypes = [i32p, ctypes.c_int, i32p, ctypes.c_int, ctypes.c_int]
+        L.qf_rope_append_scaled.restype = ctypes.c_int
+        L.qf_rope_append_scaled.argtypes = [vp] * 9 + [i32p] * 6 + [ctypes.c_int] + [vp] * 3 + [ctypes.c_int, pp, rp, vp]
+        L.qf_decode_partial_scaled.restype = ctypes.c_int
+        L.qf_decode_partial_scaled.argtypes = [vp] * 5 + [i32p] * 3 + [vp] * 3 + [ctypes.c_int, pp, vp, ctypes.c_size_t, vp]
+        L.qf_decode_step_scaled.restype = ctypes.c_int
+        L.qf_decode_step_scaled.argtypes = [vp] * 5 + [i32p] * 4 + [vp] * 5 + [ctypes.c_int, pp, vp, ctypes.c_size_t, vp]
+        L.qf_prompt_attend_scaled.restype = ctypes.c_int
+        L.qf_prompt_attend_scaled.argtypes = [vp] * 5 + [i32p] * 3 + [vp, vp, ctypes.c_int, pp, ctypes.c_int, ctypes.c_int64, vp,
+                                              ctypes.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -439,12 +457,13 @@ _kinds = {}      # a call's letters -> the element types of its arrays
 
 
 def _kinds_of(letters):
-    """The element types of every array: b bf16 (or 16-bit integers that hold its bits), i int32, f fp32, * any."""
+    """The element types of every array: b bf16 (or 16-bit integers that hold its bits), i int32, f fp32, c one-byte codes, * any."""
     global _many_gpus
     import torch
     _many_gpus = torch.cuda.device_count() > 1
     anything = (torch.uint8, *{x for x in vars(torch).values() if isinstance(x, torch.dtype)})
-    types = {"b": (torch.bfloat16, torch.int16, torch.uint16), "i": (torch.int32,), "f": (torch.float32,), "*": anything}
+    types = {"b": (torch.bfloat16, torch.int16, torch.uint16), "i": (torch.int32,), "f": (torch.float32,), "*": anything,
+             "c": (torch.uint8, torch.int8, torch.float8_e4m3fn)}
     _kinds[letters] = tuple(types[x] for x in letters)
     return _kinds[letters]
 
@@ -512,6 +531,112 @@ def rope_append(q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens,
     rc = lib().qf_rope_append(*at, ctypes.byref(p), ctypes.byref(r), _stream(stream))
     if check and rc != QF_OK:
         raise QFError(rc, "qf_rope_append")
+    return rc
+
+
+def rope_pair_axes(rotary_dim: int, sections, interleaved: bool = False):
+    """Which axis turns each pair, as an int32 array [rotary_dim / 2]: sections[a] pairs belong to axis a, in stretches or
+    in turn (see qf_rope_pair_axes).  Host arithmetic: no GPU is touched."""
+    import numpy as np
+    sec = np.ascontiguousarray([int(x) for x in sections], np.int32)
+    out = np.zeros(max(int(rotary_dim), 2) // 2, np.int32)
+    rc = lib().qf_rope_pair_axes(out.ctypes.data, int(rotary_dim), sec.ctypes.data, len(sec), 1 if interleaved else 0)
+    if rc != QF_OK:
+        raise QFError(rc, "qf_rope_pair_axes")
+    return out
+
+
+def _num_axes(positions, num_axes: Optional[int]) -> int:
+    """Axes of a [num_axes, tokens] array, unless the caller (who may pass an address) says."""
+    if num_axes is not None:
+        return int(num_axes)
+    if positions is None or isinstance(positions, int):
+        return 0 if positions is None else 1
+    if positions.dim() != 2 or not positions.is_contiguous():
+        raise ValueError(f"positions: expected a contiguous [num_axes, tokens] tensor, got {tuple(positions.shape)}")
+    return int(positions.shape[0])
+
+
+def rope_append_axes(q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, positions, pair_axis, q_gain,
+                     k_gain, inv_freq, p: QFParams, r: QFRopeParams, num_axes: Optional[int] = None, stream=None,
+                     check: bool = True) -> int:
+    """rope_append with rotary positions of several axes: positions int32 [num_axes, tokens], pair_axis int32
+    [rotary_dim / 2] (rope_pair_axes makes it)."""
+    at = _arrays("bbbbbbbiiiiibbf", q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, positions,
+                 pair_axis, q_gain, k_gain, inv_freq)
+    if hasattr(positions, "shape") and positions.shape[-1] < r.total_tokens:
+        raise ValueError(f"positions: {positions.shape[-1]} tokens, but total_tokens is {r.total_tokens}")
+    rc = lib().qf_rope_append_axes(*at[:12], _num_axes(positions, num_axes), *at[12:], ctypes.byref(p), ctypes.byref(r), _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_rope_append_axes")
+    return rc
+
+
+def _kv_type(kv_type: Optional[int], *pools) -> int:
+    """The code type of a scaled cache: what the caller says, or what the pools' elements say; they must not differ."""
+    said = kv_type
+    for x in pools:
+        name = str(getattr(x, "dtype", ""))
+        of = QF_KV_E4M3 if name == "torch.float8_e4m3fn" else QF_KV_INT8 if name == "torch.int8" else None
+        if of is None:
+            continue
+        if said is not None and said != of:
+            raise ValueError(f"a pool of {name} does not hold codes of kv_type {said}")
+        said = of
+    if said is None:
+        raise ValueError("kv_type is needed: the pools' element type does not tell e4m3 from int8")
+    return int(said)
+
+
+def rope_append_scaled(q, k, v, q_out, k_out, k_cache, v_cache, k_scale, v_scale, block_table, cu_tokens, seq_lens, pos_base,
+                       positions, pair_axis, q_gain, k_gain, inv_freq, p: QFParams, r: QFRopeParams,
+                       kv_type: Optional[int] = None, num_axes: Optional[int] = None, stream=None, check: bool = True) -> int:
+    """rope_append (rope_append_axes with positions) into a scaled cache: one byte per number, a scale per page and KV head,
+    which the call keeps up to date."""
+    at = _arrays("bbbbbccffiiiiiibbf", q, k, v, q_out, k_out, k_cache, v_cache, k_scale, v_scale, block_table, cu_tokens, seq_lens,
+                 pos_base, positions, pair_axis, q_gain, k_gain, inv_freq)
+    if hasattr(positions, "shape") and positions.shape[-1] < r.total_tokens:
+        raise ValueError(f"positions: {positions.shape[-1]} tokens, but total_tokens is {r.total_tokens}")
+    rc = lib().qf_rope_append_scaled(*at[:15], _num_axes(positions, num_axes), *at[15:], _kv_type(kv_type, k_cache, v_cache),
+                                     ctypes.byref(p), ctypes.byref(r), _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_rope_append_scaled")
+    return rc
+
+
+def decode_partial_scaled(q, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part,
+                          p: QFParams, workspace, workspace_bytes: int, kv_type: Optional[int] = None, stream=None,
+                          check: bool = True) -> int:
+    """decode_partial over a scaled cache."""
+    *at, ws = _arrays("bccffiiifff*", q, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, shard_ranges, o_part, m_part,
+                      lse_part, workspace)
+    rc = lib().qf_decode_partial_scaled(*at, _kv_type(kv_type, k_cache, v_cache), ctypes.byref(p), ws, int(workspace_bytes), _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_decode_partial_scaled")
+    return rc
+
+
+def decode_step_scaled(q, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, shard_ranges, shard_counts, o_part, m_part,
+                       lse_part, out, lse, p: QFParams, workspace, workspace_bytes: int, kv_type: Optional[int] = None,
+                       stream=None, check: bool = True) -> int:
+    """decode_step over a scaled cache."""
+    *at, ws = _arrays("bccffiiiifffff*", q, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, shard_ranges, shard_counts,
+                      o_part, m_part, lse_part, out, lse, workspace)
+    rc = lib().qf_decode_step_scaled(*at, _kv_type(kv_type, k_cache, v_cache), ctypes.byref(p), ws, int(workspace_bytes), _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_decode_step_scaled")
+    return rc
+
+
+def prompt_attend_scaled(q, k_cache, v_cache, k_scale, v_scale, block_table, cu_tokens, seq_lens, out, lse, p: QFParams,
+                         total_tokens: int, workspace, workspace_bytes: int, q_stride: int = 0, kv_type: Optional[int] = None,
+                         stream=None, check: bool = True) -> int:
+    """prompt_attend over a scaled cache."""
+    *at, ws = _arrays("bccffiiibf*", q, k_cache, v_cache, k_scale, v_scale, block_table, cu_tokens, seq_lens, out, lse, workspace)
+    rc = lib().qf_prompt_attend_scaled(*at, _kv_type(kv_type, k_cache, v_cache), ctypes.byref(p), int(total_tokens), int(q_stride), ws,
+                                       int(workspace_bytes), _stream(stream))
+    if check and rc != QF_OK:
+        raise QFError(rc, "qf_prompt_attend_scaled")
     return rc
 
 

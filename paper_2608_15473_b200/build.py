@@ -9,7 +9,7 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libqf.so"
-SOURCES = [CSRC / "qf_api.cu", CSRC / "qf_static_scratch.cu", CSRC / "qf_prompt.cu"]
+SOURCES = [CSRC / "qf_api.cu", CSRC / "qf_static_scratch.cu", CSRC / "qf_prompt.cu", CSRC / "qf_scaled.cu"]
 HEADERS = sorted(CSRC.glob("*.cuh")) + sorted(CSRC.glob("*.h")) + sorted((PKG.parent / "include").glob("*.h"))
 
 NVCC_FLAGS = [

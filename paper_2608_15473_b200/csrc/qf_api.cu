@@ -18,6 +18,29 @@
 #include "qf_sweep.cuh"
 #include "qf_merge_small.cuh"
 
+namespace qf {
+
+// ------------------------------------------------------------------ bounded-wait self-test
+// Waits, with a short limit, on a barrier that nothing will ever complete, through the same wait
+// routine the sweep kernels use: the wait must give up, report QF_STATUS_TIMEOUT and let the kernel
+// return, leaving the context usable.
+__global__ void selftest_wait_kernel(unsigned long long *header, unsigned long long epoch, unsigned limit)
+{
+    __shared__ alignas(8) unsigned long long bar;
+    __shared__ int abort_flag;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&bar), 1);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        header[kHdrLastEpoch] = epoch;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && !mbar_wait(smem_u32(&bar), 0, &abort_flag, limit))
+        epoch_or(header + kHdrStatus, epoch, kStatusTimeout);
+}
+
+}  // namespace qf
+
 namespace {
 
 thread_local char g_cuda_msg[256] = "";
@@ -106,8 +129,8 @@ int launch_simple(const void *q, const void *k, const void *v, const int32_t *bt
                   unsigned long long *header, unsigned long long epoch, cudaStream_t st)
 {
     dim3 grid(P.max_shards, P.num_kv_heads, P.batch);
-    qf::sweep_simple_kernel<G><<<grid, qf::kSimpleWarps * 32, 0, st>>>(
-        (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v, bt, sl, sr, o, m, l, P, header, epoch);
+    qf::sweep_simple_kernel<G, qf::kKvBf16><<<grid, qf::kSimpleWarps * 32, 0, st>>>(
+        (const uint16_t *)q, k, v, nullptr, nullptr, bt, sl, sr, o, m, l, P, header, epoch);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, "sweep_simple_kernel launch");
     g_last_launches += 1;
@@ -162,14 +185,17 @@ int qf_set_profile_events(void *start_event, void *stop_event)
     return QF_OK;
 }
 
-namespace {
-// The sweep, shared by qf_decode_partial (shard states only) and qf_decode_step (states and the merge).
+}  // extern "C"
+
+namespace qf_host {
+// The sweep, shared by qf_decode_partial (shard states only) and qf_decode_step (states and the merge), and by their forms
+// for a scaled cache.
 // `step_out` / `step_lse` non-null: the caller wants the merged result too; *merged says whether the sweep
 // kernel produced it itself (small sweeps), else the caller still has to launch the merge.
-int sweep_impl(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
-               const int32_t *seq_lens, const int32_t *shard_ranges, const int32_t *shard_counts, float *o_part,
-               float *m_part, float *lse_part, float *step_out, float *step_lse, bool *merged, const qf_params *p,
-               void *workspace, size_t workspace_bytes, void *cuda_stream)
+int sweep(const void *q, const void *k_cache, const void *v_cache, const ScaledKv *scaled, const int32_t *block_table,
+          const int32_t *seq_lens, const int32_t *shard_ranges, const int32_t *shard_counts, float *o_part,
+          float *m_part, float *lse_part, float *step_out, float *step_lse, bool *merged, const qf_params *p,
+          void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
     g_last_launches = 0;
     if (merged) *merged = false;
@@ -177,9 +203,11 @@ int sweep_impl(const void *q, const void *k_cache, const void *v_cache, const in
     if (rc != QF_OK) return rc;
     if (!q || !k_cache || !v_cache || !seq_lens || !shard_ranges || !o_part || !m_part || !lse_part)
         return QF_ERR_NULL;
+    if (scaled && (!scaled->k_scale || !scaled->v_scale)) return QF_ERR_NULL;
     const size_t need = qf_workspace_bytes(p);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return QF_ERR_WORKSPACE;
     if (((uintptr_t)k_cache & 127) || ((uintptr_t)v_cache & 127) || ((uintptr_t)q & 15)) return QF_ERR_BAD_SHAPE;
+    if (scaled && (((uintptr_t)scaled->k_scale & 3) || ((uintptr_t)scaled->v_scale & 3))) return QF_ERR_BAD_SHAPE;
     int sms = 0;
     rc = check_device(&sms);
     if (rc != QF_OK) return rc;
@@ -191,6 +219,11 @@ int sweep_impl(const void *q, const void *k_cache, const void *v_cache, const in
     const unsigned long long epoch = qf::next_epoch();
 
     if (p->flags & QF_FLAG_SIMPLE_KERNEL) {
+        if (scaled) {
+            rc = launch_simple_scaled(q, k_cache, v_cache, *scaled, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part, P, header, epoch, st);
+            if (rc == QF_OK) g_last_launches = 1;
+            return rc;
+        }
         switch (P.group) {
         case 1: return launch_simple<1>(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part, P, header, epoch, st);
         case 2: return launch_simple<2>(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part, P, header, epoch, st);
@@ -206,12 +239,15 @@ int sweep_impl(const void *q, const void *k_cache, const void *v_cache, const in
     // A whole step over a small sweep: the sweep, then ONE kernel that merges both the pieces of cut units and
     // the request's shards (qf_merge_small.cuh) instead of the finish kernel and the merge kernel.
     const int n_ctas = sms < qf::kMaxSweepCtas ? sms : qf::kMaxSweepCtas;
-    const bool small = step_out && step_lse && !(p->flags & QF_FLAG_NO_SMALL_MERGE) && p->out_shards == 0 &&
+    const bool small = !scaled && step_out && step_lse && !(p->flags & QF_FLAG_NO_SMALL_MERGE) && p->out_shards == 0 &&
                        qf::sweep_is_small(P, n_ctas);
     int launches = 0;
-    rc = qf::launch_sweep(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part, P,
-                          (char *)workspace, wsl, sms, epoch, st, g_prof_start, g_prof_stop, g_cuda_msg,
-                          sizeof g_cuda_msg, &launches, small);
+    rc = scaled ? launch_sweep_scaled(q, k_cache, v_cache, *scaled, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part,
+                                      P, (char *)workspace, wsl, sms, epoch, st, g_prof_start, g_prof_stop, g_cuda_msg,
+                                      sizeof g_cuda_msg, &launches, small)
+                : qf::launch_sweep(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part, P,
+                                   (char *)workspace, wsl, sms, epoch, st, g_prof_start, g_prof_stop, g_cuda_msg,
+                                   sizeof g_cuda_msg, &launches, small);
     if (rc == QF_OK && small) {
         cudaError_t e = qf::launch_merge_small(seq_lens, shard_ranges, shard_counts, (char *)workspace, wsl, o_part,
                                                m_part, lse_part, step_out, step_lse, n_ctas, P, st);
@@ -222,15 +258,17 @@ int sweep_impl(const void *q, const void *k_cache, const void *v_cache, const in
     g_last_launches = launches;
     return rc;
 }
-}  // namespace
+}  // namespace qf_host
+
+extern "C" {
 
 int qf_decode_partial(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
                       const int32_t *seq_lens, const int32_t *shard_ranges, float *o_part, float *m_part,
                       float *lse_part, const qf_params *p, void *workspace, size_t workspace_bytes,
                       void *cuda_stream)
 {
-    return sweep_impl(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, nullptr, o_part, m_part, lse_part,
-                      nullptr, nullptr, nullptr, p, workspace, workspace_bytes, cuda_stream);
+    return qf_host::sweep(q, k_cache, v_cache, nullptr, block_table, seq_lens, shard_ranges, nullptr, o_part, m_part, lse_part,
+                          nullptr, nullptr, nullptr, p, workspace, workspace_bytes, cuda_stream);
 }
 
 int qf_enable_peer_access(int peer_device)
@@ -285,10 +323,12 @@ int qf_combine(const float *o_part, const float *lse_part, const int32_t *shard_
     return launch_combine(o_part, lse_part, shard_counts, nullptr, nullptr, nullptr, out, lse, p, cuda_stream);
 }
 
-int qf_decode_step(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
-                   const int32_t *seq_lens, const int32_t *shard_ranges, const int32_t *shard_counts,
-                   float *o_part, float *m_part, float *lse_part, float *out, float *lse, const qf_params *p,
-                   void *workspace, size_t workspace_bytes, void *cuda_stream)
+}  // extern "C"
+
+namespace qf_host {
+int step(const void *q, const void *k_cache, const void *v_cache, const ScaledKv *scaled, const int32_t *block_table,
+         const int32_t *seq_lens, const int32_t *shard_ranges, const int32_t *shard_counts, float *o_part, float *m_part,
+         float *lse_part, float *out, float *lse, const qf_params *p, void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
     if (!out || !lse) {
         g_last_launches = 0;
@@ -301,13 +341,25 @@ int qf_decode_step(const void *q, const void *k_cache, const void *v_cache, cons
         return rc0 != QF_OK ? rc0 : QF_ERR_BAD_SHAPE;
     }
     bool merged = false;
-    int rc = sweep_impl(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, shard_counts, o_part, m_part,
-                        lse_part, out, lse, &merged, p, workspace, workspace_bytes, cuda_stream);
+    int rc = sweep(q, k_cache, v_cache, scaled, block_table, seq_lens, shard_ranges, shard_counts, o_part, m_part,
+                   lse_part, out, lse, &merged, p, workspace, workspace_bytes, cuda_stream);
     if (rc != QF_OK || merged) return rc;
     const int sweep_launches = g_last_launches;
     rc = qf_combine(o_part, lse_part, shard_counts, out, lse, p, cuda_stream);
     if (rc == QF_OK) g_last_launches += sweep_launches;
     return rc;
+}
+}  // namespace qf_host
+
+extern "C" {
+
+int qf_decode_step(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
+                   const int32_t *seq_lens, const int32_t *shard_ranges, const int32_t *shard_counts,
+                   float *o_part, float *m_part, float *lse_part, float *out, float *lse, const qf_params *p,
+                   void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    return qf_host::step(q, k_cache, v_cache, nullptr, block_table, seq_lens, shard_ranges, shard_counts, o_part, m_part, lse_part,
+                         out, lse, p, workspace, workspace_bytes, cuda_stream);
 }
 
 int qf_combine_self(const float *o_part, const float *lse_part, const int32_t *shard_counts, const void *q,

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda_bf16.h>
+#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -11,6 +12,10 @@ constexpr int kHeadDim  = 128;  // D
 constexpr int kPageSize = 16;   // tokens per KV page
 constexpr int kPageElems = kPageSize * kHeadDim;  // elements of one (page, KV head) block
 constexpr int kPageBytes = kPageElems * 2;        // 4096
+
+// How a cache holds its numbers: bf16, or one byte each (a scaled cache: number = code * scale of its page and KV head).
+enum { kKvBf16 = 0, kKvE4m3 = 1, kKvInt8 = 2 };
+constexpr int kScaledPageBytes = kPageElems;      // 2048: one (page, KV head) block of codes
 
 constexpr int kStatusBadPage = 1;
 constexpr int kStatusTimeout = 2;
@@ -38,6 +43,24 @@ __host__ __device__ __forceinline__ size_t kv_row_offset(const DevParams &P, lon
 {
     return P.kv_nhd ? (((size_t)phys * kPageSize + t) * P.num_kv_heads + c) * kHeadDim
                     : (((size_t)phys * P.num_kv_heads + c) * kPageSize + t) * kHeadDim;
+}
+
+// Four neighbouring channels of a pool, as fp32 (codes of a scaled cache: not yet scaled).
+__device__ __forceinline__ float bf16lo_to_f32(uint32_t w);
+__device__ __forceinline__ float bf16hi_to_f32(uint32_t w);
+template <int KV>
+__device__ __forceinline__ float4 load_channels(const void *pool, size_t at)
+{
+    if constexpr (KV == kKvBf16) {
+        const uint2 w = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(pool) + at);
+        return make_float4(bf16lo_to_f32(w.x), bf16hi_to_f32(w.x), bf16lo_to_f32(w.y), bf16hi_to_f32(w.y));
+    } else if constexpr (KV == kKvE4m3) {
+        const __nv_fp8x4_e4m3 w = *reinterpret_cast<const __nv_fp8x4_e4m3 *>(reinterpret_cast<const uint8_t *>(pool) + at);
+        return static_cast<float4>(w);
+    } else {
+        const char4 w = *reinterpret_cast<const char4 *>(reinterpret_cast<const uint8_t *>(pool) + at);
+        return make_float4((float)w.x, (float)w.y, (float)w.z, (float)w.w);
+    }
 }
 
 // Programmatic dependent launch: every kernel of the path is launched with the programmatic-stream-

@@ -32,7 +32,7 @@ int launch_rows(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *
         const long long units = (long long)A.total_rows * P.num_q_heads;
         const long long blocks = (units + qf::kRowsSimpleWarps - 1) / qf::kRowsSimpleWarps;
         if (blocks > 0x7fffffffll) return QF_ERR_UNSUPPORTED;
-        qf::rows_simple_kernel<PREFIX><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
+        qf::rows_simple_kernel<PREFIX, qf::kKvBf16><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return qf_host::cuda_fail(e, "rows_simple_kernel launch");
         qf_host::set_launches(1);
@@ -48,7 +48,74 @@ int launch_rows(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *
     return QF_OK;
 }
 
+constexpr int kMostAxes = 8;
+
+// The bf16 cache's placing kernel, for checked arguments.
+int place(qf::RopeArgs &A, const qf_params *p, int sms, void *cuda_stream)
+{
+    // one token per CTA until there are several for every SM, then steps of more: fewer, longer row lists per group
+    A.tokens_per_cta = 1;
+    while (A.tokens_per_cta < qf::kRopeMaxTokens && A.total_tokens >= 8 * A.tokens_per_cta * sms) A.tokens_per_cta *= 2;
+    const long long steps = ((long long)A.total_tokens + A.tokens_per_cta - 1) / A.tokens_per_cta;
+    const long long blocks = std::min<long long>(steps, (long long)qf::kRopeCtasPerSm * sms);
+    cudaError_t e = qf::launch_rope(A, qf_host::dev_params(p), (unsigned)blocks, (cudaStream_t)cuda_stream);
+    if (e != cudaSuccess) return qf_host::cuda_fail(e, "rope_append_kernel launch");
+    qf_host::set_launches(1);
+    return QF_OK;
+}
+
 }  // namespace
+
+namespace qf_host {
+
+int rope_args(qf::RopeArgs *out, const void *q, const void *k, const void *v, void *q_out, void *k_out, void *k_cache,
+              void *v_cache, const int32_t *block_table, const int32_t *cu_tokens, const int32_t *seq_lens,
+              const int32_t *pos_base, const int32_t *positions, const int32_t *pair_axis, int num_axes, const void *q_gain,
+              const void *k_gain, const float *inv_freq, const qf_params *p, const qf_rope_params *r, int *sms)
+{
+    set_launches(0);
+    int rc = validate(p);
+    if (rc != QF_OK) return rc;
+    if (!r) return QF_ERR_NULL;
+    if (r->total_tokens > kMostPositions) return QF_ERR_UNSUPPORTED;
+    if (r->total_tokens <= 0 || r->rotary_dim < 0 || !(r->eps >= 0.f) || !std::isfinite(r->rot_scale)) return QF_ERR_BAD_SHAPE;
+    if (r->rotary_dim > qf::kHeadDim || (r->rotary_dim & 15)) return QF_ERR_UNSUPPORTED;
+    const long long D = qf::kHeadDim, Hq = p->num_q_heads, Hkv = p->num_kv_heads;
+    if (bad_stride(r->q_stride, Hq * D) || bad_stride(r->k_stride, Hkv * D) || bad_stride(r->v_stride, Hkv * D))
+        return QF_ERR_BAD_SHAPE;
+    const bool cache = k_cache || v_cache;
+    if (!cu_tokens || !seq_lens || (!q && !k) || (q && !q_out)) return QF_ERR_NULL;
+    if (cache && (!k || !v || !k_cache || !v_cache)) return QF_ERR_NULL;      // the cache takes both or neither
+    if (k && !cache && !k_out) return QF_ERR_NULL;                            // nowhere for the keys to go
+    if (k_out && !k) return QF_ERR_NULL;
+    if (r->rotary_dim > 0 && !inv_freq) return QF_ERR_NULL;
+    if (positions) {
+        if (r->rotary_dim > 0 && !pair_axis) return QF_ERR_NULL;
+        if (num_axes <= 0) return QF_ERR_BAD_SHAPE;
+        if (num_axes > kMostAxes) return QF_ERR_UNSUPPORTED;
+    }
+    for (const void *x : {q, k, v, (const void *)q_out, (const void *)k_out, (const void *)k_cache, (const void *)v_cache, q_gain, k_gain})
+        if (misaligned(x, 16)) return QF_ERR_BAD_SHAPE;
+    rc = check_device(sms);
+    if (rc != QF_OK) return rc;
+    qf::RopeArgs &A = *out;
+    A.q = (const uint16_t *)q; A.k = (const uint16_t *)k; A.v = cache ? (const uint16_t *)v : nullptr;
+    A.q_out = (uint16_t *)q_out; A.k_out = (uint16_t *)k_out;
+    A.k_cache = (uint16_t *)k_cache; A.v_cache = (uint16_t *)v_cache;
+    A.block_table = block_table; A.cu = cu_tokens; A.seq_lens = seq_lens; A.pos_base = pos_base;
+    A.positions = positions; A.pair_axis = pair_axis; A.num_axes = num_axes;
+    A.q_gain = (const uint16_t *)q_gain; A.k_gain = (const uint16_t *)k_gain; A.inv_freq = inv_freq;
+    A.q_stride = r->q_stride ? r->q_stride : Hq * D;
+    A.k_stride = r->k_stride ? r->k_stride : Hkv * D;
+    A.v_stride = r->v_stride ? r->v_stride : Hkv * D;
+    A.total_tokens = r->total_tokens; A.rotary_dim = r->rotary_dim; A.interleaved = r->interleaved != 0;
+    A.n_q = q ? (int)Hq : 0; A.n_k = k ? (int)Hkv : 0;
+    A.rows = A.n_q + A.n_k + (cache ? (int)Hkv : 0);
+    A.eps = r->eps; A.rot_scale = r->rot_scale;
+    return QF_OK;
+}
+
+}  // namespace qf_host
 
 extern "C" {
 
@@ -89,48 +156,55 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
                    const int32_t *pos_base, const void *q_gain, const void *k_gain, const float *inv_freq,
                    const qf_params *p, const qf_rope_params *r, void *cuda_stream)
 {
-    qf_host::set_launches(0);
-    int rc = qf_host::validate(p);
-    if (rc != QF_OK) return rc;
-    if (!r) return QF_ERR_NULL;
-    if (r->total_tokens > kMostPositions) return QF_ERR_UNSUPPORTED;
-    if (r->total_tokens <= 0 || r->rotary_dim < 0 || !(r->eps >= 0.f) || !std::isfinite(r->rot_scale)) return QF_ERR_BAD_SHAPE;
-    if (r->rotary_dim > qf::kHeadDim || (r->rotary_dim & 15)) return QF_ERR_UNSUPPORTED;
-    const long long D = qf::kHeadDim, Hq = p->num_q_heads, Hkv = p->num_kv_heads;
-    if (bad_stride(r->q_stride, Hq * D) || bad_stride(r->k_stride, Hkv * D) || bad_stride(r->v_stride, Hkv * D))
-        return QF_ERR_BAD_SHAPE;
-    const bool cache = k_cache || v_cache;
-    if (!cu_tokens || !seq_lens || (!q && !k) || (q && !q_out)) return QF_ERR_NULL;
-    if (cache && (!k || !v || !k_cache || !v_cache)) return QF_ERR_NULL;      // the cache takes both or neither
-    if (k && !cache && !k_out) return QF_ERR_NULL;                            // nowhere for the keys to go
-    if (k_out && !k) return QF_ERR_NULL;
-    if (r->rotary_dim > 0 && !inv_freq) return QF_ERR_NULL;
-    for (const void *x : {q, k, v, (const void *)q_out, (const void *)k_out, (const void *)k_cache, (const void *)v_cache, q_gain, k_gain})
-        if (misaligned(x, 16)) return QF_ERR_BAD_SHAPE;
-    int sms = 0;
-    rc = qf_host::check_device(&sms);
-    if (rc != QF_OK) return rc;
     qf::RopeArgs A = {};
-    A.q = (const uint16_t *)q; A.k = (const uint16_t *)k; A.v = cache ? (const uint16_t *)v : nullptr;
-    A.q_out = (uint16_t *)q_out; A.k_out = (uint16_t *)k_out;
-    A.k_cache = (uint16_t *)k_cache; A.v_cache = (uint16_t *)v_cache;
-    A.block_table = block_table; A.cu = cu_tokens; A.seq_lens = seq_lens; A.pos_base = pos_base;
-    A.q_gain = (const uint16_t *)q_gain; A.k_gain = (const uint16_t *)k_gain; A.inv_freq = inv_freq;
-    A.q_stride = r->q_stride ? r->q_stride : Hq * D;
-    A.k_stride = r->k_stride ? r->k_stride : Hkv * D;
-    A.v_stride = r->v_stride ? r->v_stride : Hkv * D;
-    A.total_tokens = r->total_tokens; A.rotary_dim = r->rotary_dim; A.interleaved = r->interleaved != 0;
-    A.n_q = q ? (int)Hq : 0; A.n_k = k ? (int)Hkv : 0;
-    A.rows = A.n_q + A.n_k + (cache ? (int)Hkv : 0);
-    A.eps = r->eps; A.rot_scale = r->rot_scale;
-    // one token per CTA until there are several for every SM, then steps of more: fewer, longer row lists per group
-    A.tokens_per_cta = 1;
-    while (A.tokens_per_cta < qf::kRopeMaxTokens && A.total_tokens >= 8 * A.tokens_per_cta * sms) A.tokens_per_cta *= 2;
-    const long long steps = ((long long)A.total_tokens + A.tokens_per_cta - 1) / A.tokens_per_cta;
-    const long long blocks = std::min<long long>(steps, (long long)qf::kRopeCtasPerSm * sms);
-    cudaError_t e = qf::launch_rope(A, qf_host::dev_params(p), (unsigned)blocks, (cudaStream_t)cuda_stream);
-    if (e != cudaSuccess) return qf_host::cuda_fail(e, "rope_append_kernel launch");
-    qf_host::set_launches(1);
+    int sms = 0;
+    const int rc = qf_host::rope_args(&A, q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base,
+                                      nullptr, nullptr, 0, q_gain, k_gain, inv_freq, p, r, &sms);
+    return rc != QF_OK ? rc : place(A, p, sms, cuda_stream);
+}
+
+int qf_rope_append_axes(const void *q, const void *k, const void *v, void *q_out, void *k_out, void *k_cache, void *v_cache,
+                        const int32_t *block_table, const int32_t *cu_tokens, const int32_t *seq_lens,
+                        const int32_t *positions, const int32_t *pair_axis, int num_axes, const void *q_gain,
+                        const void *k_gain, const float *inv_freq, const qf_params *p, const qf_rope_params *r,
+                        void *cuda_stream)
+{
+    if (!positions) {
+        qf_host::set_launches(0);
+        const int rc0 = qf_host::validate(p);
+        return rc0 != QF_OK ? rc0 : QF_ERR_NULL;
+    }
+    qf::RopeArgs A = {};
+    int sms = 0;
+    const int rc = qf_host::rope_args(&A, q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, nullptr, positions,
+                                      pair_axis, num_axes, q_gain, k_gain, inv_freq, p, r, &sms);
+    return rc != QF_OK ? rc : place(A, p, sms, cuda_stream);
+}
+
+int qf_rope_pair_axes(int32_t *pair_axis, int rotary_dim, const int32_t *sections, int num_axes, int interleaved)
+{
+    if (!pair_axis || !sections) return QF_ERR_NULL;
+    if (rotary_dim <= 0 || num_axes <= 0) return QF_ERR_BAD_SHAPE;
+    if (rotary_dim > qf::kHeadDim || (rotary_dim & 15) || num_axes > kMostAxes) return QF_ERR_UNSUPPORTED;
+    long long pairs = 0;
+    for (int a = 0; a < num_axes; ++a) {
+        if (sections[a] < 0) return QF_ERR_BAD_SHAPE;
+        pairs += sections[a];
+    }
+    if (pairs != rotary_dim / 2) return QF_ERR_BAD_SHAPE;
+    if (!interleaved) {
+        int j = 0;
+        for (int a = 0; a < num_axes; ++a)
+            for (int i = 0; i < sections[a]; ++i) pair_axis[j++] = a;
+        return QF_OK;
+    }
+    // axis a > 0 owns the pairs a, a + num_axes, ... as far as its section reaches; axis 0 owns the others
+    for (int j = 0; j < pairs; ++j) {
+        const int a = j % num_axes;
+        pair_axis[j] = a > 0 && j / num_axes < sections[a] ? a : 0;
+    }
+    for (int a = 1; a < num_axes; ++a)
+        if (sections[a] > 0 && (long long)(sections[a] - 1) * num_axes + a >= pairs) return QF_ERR_BAD_SHAPE;   // no room in turn
     return QF_OK;
 }
 
@@ -140,31 +214,49 @@ size_t qf_prompt_workspace_bytes(const qf_params *p, int total_tokens)
     return align256(qf::rows_layout().total);
 }
 
-int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
-                     const int32_t *cu_tokens, const int32_t *seq_lens, void *out, float *lse, const qf_params *p,
-                     int total_tokens, int64_t q_stride, void *workspace, size_t workspace_bytes, void *cuda_stream)
+}  // extern "C"
+
+namespace qf_host {
+int prompt(const void *q, const void *k_cache, const void *v_cache, const ScaledKv *scaled, const int32_t *block_table,
+           const int32_t *cu_tokens, const int32_t *seq_lens, void *out, float *lse, const qf_params *p, int total_tokens,
+           int64_t q_stride, void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
-    qf_host::set_launches(0);
-    int rc = qf_host::validate(p);
+    set_launches(0);
+    int rc = validate(p);
     if (rc != QF_OK) return rc;
     const long long width = (long long)p->num_q_heads * qf::kHeadDim;
     if (total_tokens <= 0 || bad_stride(q_stride, width)) return QF_ERR_BAD_SHAPE;
     if (total_tokens > kMostPositions) return QF_ERR_UNSUPPORTED;
     if (!q || !k_cache || !v_cache || !cu_tokens || !seq_lens || !out || !lse) return QF_ERR_NULL;
+    if (scaled && (!scaled->k_scale || !scaled->v_scale)) return QF_ERR_NULL;
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < qf_prompt_workspace_bytes(p, total_tokens))
         return QF_ERR_WORKSPACE;
     if (misaligned(k_cache, 128) || misaligned(v_cache, 128) || misaligned(q, 16) || misaligned(out, 32)) return QF_ERR_BAD_SHAPE;
+    if (scaled && (misaligned(scaled->k_scale, 4) || misaligned(scaled->v_scale, 4))) return QF_ERR_BAD_SHAPE;
     int sms = 0;
-    rc = qf_host::check_device(&sms);
+    rc = check_device(&sms);
     if (rc != QF_OK) return rc;
-    const qf::DevParams P = qf_host::dev_params(p);
+    const qf::DevParams P = dev_params(p);
     qf::RowsArgs A = {};
-    A.q = (const uint16_t *)q; A.k_cache = (const uint16_t *)k_cache; A.v_cache = (const uint16_t *)v_cache;
+    A.q = (const uint16_t *)q; A.k_cache = k_cache; A.v_cache = v_cache;
+    if (scaled) { A.k_scale = scaled->k_scale; A.v_scale = scaled->v_scale; }
     A.cu = cu_tokens; A.lens = seq_lens; A.table = block_table;
     A.out = (uint16_t *)out; A.lse = lse; A.status = (unsigned long long *)workspace;
     A.q_stride = q_stride ? q_stride : width;
     A.n_seq = p->batch; A.table_width = p->max_pages_per_req; A.max_tokens = std::min(P.max_tokens, kMostPositions); A.total_rows = total_tokens;
+    if (scaled) return launch_rows_scaled(A, P, p, scaled->kind, (char *)workspace, sms, (cudaStream_t)cuda_stream);
     return launch_rows<false>(A, P, p, (char *)workspace, sms, (cudaStream_t)cuda_stream);
+}
+}  // namespace qf_host
+
+extern "C" {
+
+int qf_prompt_attend(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_table,
+                     const int32_t *cu_tokens, const int32_t *seq_lens, void *out, float *lse, const qf_params *p,
+                     int total_tokens, int64_t q_stride, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    return qf_host::prompt(q, k_cache, v_cache, nullptr, block_table, cu_tokens, seq_lens, out, lse, p, total_tokens, q_stride, workspace,
+                           workspace_bytes, cuda_stream);
 }
 
 size_t qf_prefix_workspace_bytes(const qf_params *p)
@@ -191,7 +283,7 @@ int qf_prefix_partial(const void *q, const void *k_cache, const void *v_cache, c
     if (rc != QF_OK) return rc;
     const qf::DevParams P = qf_host::dev_params(p);
     qf::RowsArgs A = {};
-    A.q = (const uint16_t *)q; A.k_cache = (const uint16_t *)k_cache; A.v_cache = (const uint16_t *)v_cache;
+    A.q = (const uint16_t *)q; A.k_cache = k_cache; A.v_cache = v_cache;
     A.cu = group_offsets; A.lens = prefix_lens; A.table = prefix_table;
     A.o_part = o_part; A.m_part = m_part; A.lse_part = lse_part; A.status = (unsigned long long *)workspace;
     A.q_stride = (long long)p->num_q_heads * qf::kHeadDim;

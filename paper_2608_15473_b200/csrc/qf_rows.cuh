@@ -493,7 +493,7 @@ __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const 
         const long long at = (long long)b.seq * A.table_width + (pos >> 4);
         const long long phys = A.table ? (long long)A.table[at] : at;
         if (phys < 0 || phys >= P.num_pages) continue;
-        const uint16_t *v = A.v_cache + kv_row_offset(P, phys, b.head, pos & 15);
+        const uint16_t *v = reinterpret_cast<const uint16_t *>(A.v_cache) + kv_row_offset(P, phys, b.head, pos & 15);
 #pragma unroll 1
         for (int d = c0 * 32; d < c1 * 32; ++d) {
             if ((v[d] & 0x7f80u) != 0x7f80u) continue;
@@ -525,7 +525,7 @@ __device__ QF_COLD void mend_infinite(const RowsArgs &A, const DevParams &P, con
             const long long at = (long long)b.seq * A.table_width + (i >> 4);
             const long long phys = A.table ? (long long)A.table[at] : at;
             if (phys < 0 || phys >= P.num_pages) continue;
-            const uint4 *v = reinterpret_cast<const uint4 *>(A.v_cache + kv_row_offset(P, phys, b.head, i & 15) + c * 32);
+            const uint4 *v = reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(A.v_cache) + kv_row_offset(P, phys, b.head, i & 15) + c * 32);
 #pragma unroll 1
             for (int k = 0; k < 4; ++k) {
                 const uint4 x = v[k];

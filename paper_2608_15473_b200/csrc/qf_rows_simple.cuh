@@ -14,7 +14,8 @@ namespace qf {
 
 struct RowsArgs {
     const uint16_t *q;               // row r, query head h: q + r * q_stride + h * 128
-    const uint16_t *k_cache, *v_cache;
+    const void *k_cache, *v_cache;
+    const float *k_scale, *v_scale;  // of a scaled cache: [num_pages, Hkv]
     const int *cu, *lens, *table;    // [n_seq + 1], [n_seq], [n_seq, table_width] (nullptr: identity)
     uint16_t *out;                   // prompt: [rows, Hq, 128] bf16
     float *lse;                      // prompt: [rows, Hq]
@@ -68,7 +69,7 @@ __device__ __forceinline__ bool seq_overruns(const RowsArgs &A, int s)
 constexpr int kRowsSimpleWarps = 8;
 
 // One warp per (row, query head), lane owns four channels, fp32 online softmax over the positions in order.
-template <bool PREFIX>
+template <bool PREFIX, int KV>
 __global__ void __launch_bounds__(kRowsSimpleWarps * 32)
 rows_simple_kernel(RowsArgs A, DevParams P)
 {
@@ -103,23 +104,24 @@ rows_simple_kernel(RowsArgs A, DevParams P)
             continue;
         }
         const size_t off = kv_row_offset(P, phys, c, i & 15) + lane * 4;
-        const uint2 kw = *reinterpret_cast<const uint2 *>(A.k_cache + off);
-        const uint2 vw = *reinterpret_cast<const uint2 *>(A.v_cache + off);
-        float d = bf16lo_to_f32(qw.x) * bf16lo_to_f32(kw.x);
-        d = fmaf(bf16hi_to_f32(qw.x), bf16hi_to_f32(kw.x), d);
-        d = fmaf(bf16lo_to_f32(qw.y), bf16lo_to_f32(kw.y), d);
-        d = fmaf(bf16hi_to_f32(qw.y), bf16hi_to_f32(kw.y), d);
+        const float4 k4 = load_channels<KV>(A.k_cache, off), v4 = load_channels<KV>(A.v_cache, off);
+        const float ks = KV == kKvBf16 ? 1.f : A.k_scale[phys * P.num_kv_heads + c], vs = KV == kKvBf16 ? 1.f : A.v_scale[phys * P.num_kv_heads + c];
+        float d = bf16lo_to_f32(qw.x) * k4.x;
+        d = fmaf(bf16hi_to_f32(qw.x), k4.y, d);
+        d = fmaf(bf16lo_to_f32(qw.y), k4.z, d);
+        d = fmaf(bf16hi_to_f32(qw.y), k4.w, d);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-        const float sc = d * P.sm_scale;
+        const float sc = d * P.sm_scale * ks;
         if (sc == neg_inf()) continue;            // weight 0 against any other score
         const float mn = max_nan(m, sc);          // NaN from the first NaN score on
         const float alpha = __expf(m - mn), p = __expf(sc - mn);
         l = l * alpha + p;
-        acc[0] = fmaf(p, bf16lo_to_f32(vw.x), acc[0] * alpha);
-        acc[1] = fmaf(p, bf16hi_to_f32(vw.x), acc[1] * alpha);
-        acc[2] = fmaf(p, bf16lo_to_f32(vw.y), acc[2] * alpha);
-        acc[3] = fmaf(p, bf16hi_to_f32(vw.y), acc[3] * alpha);
+        const float pv = p * vs;
+        acc[0] = fmaf(pv, v4.x, acc[0] * alpha);
+        acc[1] = fmaf(pv, v4.y, acc[1] * alpha);
+        acc[2] = fmaf(pv, v4.z, acc[2] * alpha);
+        acc[3] = fmaf(pv, v4.w, acc[3] * alpha);
         m = mn;
     }
     const bool empty = l == 0.f;                  // nothing visible; a NaN score makes maximum and sum NaN

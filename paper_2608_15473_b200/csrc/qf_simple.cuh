@@ -1,7 +1,7 @@
 // Plain-load sweep kernel: one CTA per (request, KV head, shard), no staging,
 // no tensor cores.  It exists as a validation aid for the staged kernel (it is
 // selected by QF_FLAG_SIMPLE_KERNEL); it follows the same online-softmax
-// recurrence (Section 5: (W, Z) add over disjoint sets) warp by warp.
+// recurrence (Section 5: (W, Z) add over disjoint sets) warp by warp.  KV says how the pools hold their numbers.
 #pragma once
 
 #include "qf_common.cuh"
@@ -10,10 +10,10 @@ namespace qf {
 
 constexpr int kSimpleWarps = 8;
 
-template <int G>
+template <int G, int KV>
 __global__ void __launch_bounds__(kSimpleWarps * 32)
-sweep_simple_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache,
-                    const uint16_t *__restrict__ v_cache, const int *__restrict__ block_table,
+sweep_simple_kernel(const uint16_t *__restrict__ q, const void *__restrict__ k_cache, const void *__restrict__ v_cache,
+                    const float *__restrict__ k_scale, const float *__restrict__ v_scale, const int *__restrict__ block_table,
                     const int *__restrict__ seq_lens, const int *__restrict__ shard_ranges,
                     float *__restrict__ o_part, float *__restrict__ m_part, float *__restrict__ lse_part,
                     DevParams P, unsigned long long *header, unsigned long long epoch)
@@ -50,34 +50,31 @@ sweep_simple_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__
         const int lp = i >> 4, slot = i & 15;
         long long phys = block_table ? (long long)block_table[(size_t)b * P.max_pages_per_req + lp]
                                      : (long long)b * P.max_pages_per_req + lp;
-        if (P.check_bounds && (phys < 0 || phys >= P.num_pages)) {
-            if (lane == 0) epoch_or(header + kHdrStatus, epoch, kStatusBadPage);
+        if ((KV != kKvBf16 || P.check_bounds) && (phys < 0 || phys >= P.num_pages)) {
+            if (P.check_bounds && lane == 0) epoch_or(header + kHdrStatus, epoch, kStatusBadPage);
             continue;
         }
         const size_t row = kv_row_offset(P, phys, c, slot) + lane * 4;
-        const uint2 kw = *reinterpret_cast<const uint2 *>(k_cache + row);
-        const uint2 vw = *reinterpret_cast<const uint2 *>(v_cache + row);
-        const float k0 = bf16lo_to_f32(kw.x), k1 = bf16hi_to_f32(kw.x);
-        const float k2 = bf16lo_to_f32(kw.y), k3 = bf16hi_to_f32(kw.y);
-        const float v0 = bf16lo_to_f32(vw.x), v1 = bf16hi_to_f32(vw.x);
-        const float v2 = bf16lo_to_f32(vw.y), v3 = bf16hi_to_f32(vw.y);
+        const float4 k4 = load_channels<KV>(k_cache, row), v4 = load_channels<KV>(v_cache, row);
+        const float ks = KV == kKvBf16 ? 1.f : k_scale[phys * Hkv + c], vs = KV == kKvBf16 ? 1.f : v_scale[phys * Hkv + c];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            float d = qr[g][0] * k0;
-            d = fmaf(qr[g][1], k1, d);
-            d = fmaf(qr[g][2], k2, d);
-            d = fmaf(qr[g][3], k3, d);
+            float d = qr[g][0] * k4.x;
+            d = fmaf(qr[g][1], k4.y, d);
+            d = fmaf(qr[g][2], k4.z, d);
+            d = fmaf(qr[g][3], k4.w, d);
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
-            const float sc = d * P.sm_scale;
+            const float sc = d * P.sm_scale * ks;
             const float mn = max_nan(m[g], sc);      // NaN from the first NaN score on
             const float alpha = __expf(m[g] - mn);   // m = -inf on the first token: e^{-inf} = 0
             const float p = __expf(sc - mn);
             l[g] = l[g] * alpha + p;
-            acc[g][0] = fmaf(p, v0, acc[g][0] * alpha);
-            acc[g][1] = fmaf(p, v1, acc[g][1] * alpha);
-            acc[g][2] = fmaf(p, v2, acc[g][2] * alpha);
-            acc[g][3] = fmaf(p, v3, acc[g][3] * alpha);
+            const float pv = p * vs;
+            acc[g][0] = fmaf(pv, v4.x, acc[g][0] * alpha);
+            acc[g][1] = fmaf(pv, v4.y, acc[g][1] * alpha);
+            acc[g][2] = fmaf(pv, v4.z, acc[g][2] * alpha);
+            acc[g][3] = fmaf(pv, v4.w, acc[g][3] * alpha);
             m[g] = mn;
         }
     }

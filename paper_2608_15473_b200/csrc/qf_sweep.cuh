@@ -183,7 +183,7 @@ __host__ __device__ __forceinline__ void piece_range(const PieceGrid &g, int n_c
 
 // ------------------------------------------------------------------ plan kernel (large batches only)
 // prefix[e] = number of stage units before entry e = b*S + s, left in scratch.
-__global__ void __launch_bounds__(1024)
+static __global__ void __launch_bounds__(1024)
 plan_kernel(const int *__restrict__ seq_lens, const int *__restrict__ shard_ranges, int *__restrict__ prefix,
             int n_entries, int max_shards, int num_kv_heads, int max_tokens)
 {
@@ -645,25 +645,6 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         }
         if (++stage == kStages) { stage = 0; phase ^= 1; }
     }
-}
-
-// ------------------------------------------------------------------ bounded-wait self-test
-// Waits, with a short limit, on a barrier that nothing will ever complete, through the same wait
-// routine the sweep kernels use: the wait must give up, report QF_STATUS_TIMEOUT and let the kernel
-// return, leaving the context usable.
-__global__ void selftest_wait_kernel(unsigned long long *header, unsigned long long epoch, unsigned limit)
-{
-    __shared__ alignas(8) unsigned long long bar;
-    __shared__ int abort_flag;
-    if (threadIdx.x == 0) {
-        mbar_init(smem_u32(&bar), 1);
-        abort_flag = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        header[kHdrLastEpoch] = epoch;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0 && !mbar_wait(smem_u32(&bar), 0, &abort_flag, limit))
-        epoch_or(header + kHdrStatus, epoch, kStatusTimeout);
 }
 
 // ------------------------------------------------------------------ host side
