@@ -140,10 +140,12 @@ merge_small_kernel(const int *__restrict__ seq_lens, const int *__restrict__ sha
         // loads below: this kernel runs once per CTA from cold instruction caches, straight-line length is latency)
         if (d < kB) {
             const float *row = nullptr, *sc = nullptr;
+            int cut = 0;
             if (base + d < n_items) {
                 int s2 = cs, k2 = ck;
                 for (int i = 0; i < d; ++i) advance(s2, k2);
-                if (s_nseg[s2] > 1) {
+                if (s_nseg[s2] > 1) {      // not by where the scalars lie: the caller's arrays may follow one another like a slot's
+                    cut = 1;
                     row = seg + (size_t)(s_first[s2] + k2) * seg_stride;
                     sc = row + G * kHeadDim;
                 } else {
@@ -154,7 +156,7 @@ merge_small_kernel(const int *__restrict__ seq_lens, const int *__restrict__ sha
             }
             s_rows[d] = row;
             s_sc[d] = sc;
-            s_cut[d] = (row != nullptr && sc == row + G * kHeadDim) ? 1 : 0;
+            s_cut[d] = cut;
         }
         for (int i = 0; i < kB && base + i < n_items; ++i) advance(cs, ck);   // the cursor moves past the batch
         __syncthreads();
