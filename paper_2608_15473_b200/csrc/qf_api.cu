@@ -137,6 +137,18 @@ int launch_simple(const void *q, const void *k, const void *v, const int32_t *bt
     return QF_OK;
 }
 
+int launch_sweep_bf16(const void *q, const void *k_cache, const void *v_cache, const int32_t *bt, const int32_t *sl,
+                      const int32_t *sr, float *o, float *m, float *l, const qf::DevParams &P, char *ws,
+                      const qf::WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st,
+                      cudaEvent_t ev0, cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish)
+{
+    CUtensorMap kmap, vmap;
+    if (qf::make_pool_map(&kmap, k_cache, P.num_pages, P.num_kv_heads, qf::kPageSize, P.kv_nhd != 0, msg, msg_len)) return QF_ERR_CUDA;
+    if (qf::make_pool_map(&vmap, v_cache, P.num_pages, P.num_kv_heads, qf::kPageSize, P.kv_nhd != 0, msg, msg_len)) return QF_ERR_CUDA;
+    return qf::launch_sweep_kv<qf::kKvBf16>(kmap, vmap, nullptr, nullptr, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1,
+                                            msg, msg_len, launches, skip_finish);
+}
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
@@ -239,15 +251,15 @@ int sweep(const void *q, const void *k_cache, const void *v_cache, const ScaledK
     // A whole step over a small sweep: the sweep, then ONE kernel that merges both the pieces of cut units and
     // the request's shards (qf_merge_small.cuh) instead of the finish kernel and the merge kernel.
     const int n_ctas = sms < qf::kMaxSweepCtas ? sms : qf::kMaxSweepCtas;
-    const bool small = !scaled && step_out && step_lse && !(p->flags & QF_FLAG_NO_SMALL_MERGE) && p->out_shards == 0 &&
+    const bool small = step_out && step_lse && !(p->flags & QF_FLAG_NO_SMALL_MERGE) && p->out_shards == 0 &&
                        qf::sweep_is_small(P, n_ctas);
     int launches = 0;
     rc = scaled ? launch_sweep_scaled(q, k_cache, v_cache, *scaled, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part,
-                                      P, (char *)workspace, wsl, sms, epoch, st, g_prof_start, g_prof_stop, g_cuda_msg,
+                                      P, (char *)workspace, wsl, n_ctas, epoch, st, g_prof_start, g_prof_stop, g_cuda_msg,
                                       sizeof g_cuda_msg, &launches, small)
-                : qf::launch_sweep(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part, P,
-                                   (char *)workspace, wsl, sms, epoch, st, g_prof_start, g_prof_stop, g_cuda_msg,
-                                   sizeof g_cuda_msg, &launches, small);
+                : launch_sweep_bf16(q, k_cache, v_cache, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part, P,
+                                    (char *)workspace, wsl, n_ctas, epoch, st, g_prof_start, g_prof_stop, g_cuda_msg,
+                                    sizeof g_cuda_msg, &launches, small);
     if (rc == QF_OK && small) {
         cudaError_t e = qf::launch_merge_small(seq_lens, shard_ranges, shard_counts, (char *)workspace, wsl, o_part,
                                                m_part, lse_part, step_out, step_lse, n_ctas, P, st);

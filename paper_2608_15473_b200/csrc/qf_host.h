@@ -43,7 +43,7 @@ int launch_simple_scaled(const void *q, const void *k, const void *v, const Scal
                          unsigned long long epoch, cudaStream_t st);
 int launch_sweep_scaled(const void *q, const void *k, const void *v, const ScaledKv &s, const int32_t *bt, const int32_t *sl,
                         const int32_t *sr, float *o, float *m, float *l, const qf::DevParams &P, char *ws,
-                        const qf::WorkspaceLayout &wsl, int sm_count, unsigned long long epoch, cudaStream_t st, cudaEvent_t ev0,
+                        const qf::WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st, cudaEvent_t ev0,
                         cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish);
 
 }  // namespace qf_host

@@ -1,0 +1,224 @@
+// The page step of the decode sweep over a scaled cache (one byte per number): what qf_page_math.cuh's process_page does
+// for a bf16 page.
+//
+//   s_i = ks * (q . k_i) / sqrt(d),   W += vs * sum_i e^{s_i} v_i        (k_i, v_i codes; ks, vs the page's scales)
+//
+// Codes become f16 numbers in registers, exactly (e4m3 by the conversion instruction, integers by placing the byte in
+// the mantissa of 1024 and subtracting), and go through m16n8k16 products with fp32 accumulators.  Queries become f16
+// too: each head is brought to magnitudes below 2^15 by a power of two first, so its eight significant bits survive
+// down to 2^-39 of its largest channel.  Both scales stay out of the products: ks multiplies the finished score, and a
+// page's weights are taken relative to the page's own maximum, times 2^14, so that hi + lo (two f16 terms) hold 22 bits
+// of every weight that is not 2^-39 of the page's largest, whatever the page weighs against the others and however its
+// scale compares with theirs; the page's product then enters the accumulators with one factor, vs e^{m_page - m}.
+//
+// Fragments.  K: a lane reads 32 channels of rows g and g + 8 (16-byte words 2t and 2t+1 of the swizzled row: eight
+// lanes hit eight different bank groups); the words' channels, taken four at a time, are a k-step (which channel is
+// which k is free as long as Q agrees).  V: transposing loads move byte pairs (two channels of a token); one byte
+// permutation per register separates them, so row g of a 16-channel tile is channel 2g and row g + 8 channel 2g + 1.
+// With at most four heads, Q's columns 4..7 repeat columns 0..3, and P's carry lo beside hi: one product instead of two.
+//
+// Per page and warp about 32 conversions and 4 loads each for K and V, 8 + 8 products (16 for G > 4) and 32
+// multiply-adds, against 4 KB from memory: an SM's share of 6.5 TB/s is 4 KB in 170 cycles, 680 issue slots.
+#pragma once
+
+#include "qf_common.cuh"
+#include "qf_page_math.cuh"
+
+namespace qf {
+
+// D = A(16x16, row) * B(16x8, col) + D, f16 inputs, fp32 accumulate.
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    uint32_t w;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+    return w;
+}
+__device__ __forceinline__ void unpack_f16(uint32_t w, float &lo, float &hi)
+{
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(w));
+}
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b)
+{
+    uint32_t w;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(w) : "r"(a), "r"(b));
+    return w;
+}
+__device__ __forceinline__ uint4 ld_shared_16(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+    return v;
+}
+// Four codes of a word -> f16 pairs: bytes (0, 1) and (2, 3), or, PAIRED, bytes (0, 2) and (1, 3).
+template <int KV, bool PAIRED>
+__device__ __forceinline__ void halves_of(uint32_t w, uint32_t &first, uint32_t &second)
+{
+    if constexpr (KV == kKvE4m3) {
+        if (PAIRED) w = __byte_perm(w, 0u, 0x3120);
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+            : "=r"(first), "=r"(second) : "r"(w));
+    } else {
+        const uint32_t u = w ^ 0x80808080u;      // code + 128 as the low mantissa byte of 1024: minus 1152 is exact
+        first = sub_f16x2(__byte_perm(u, 0x64646464u, PAIRED ? 0x4240 : 0x4140), 0x64806480u);
+        second = sub_f16x2(__byte_perm(u, 0x64646464u, PAIRED ? 0x4341 : 0x4342), 0x64806480u);
+    }
+}
+
+constexpr float kWeightScale = 16384.f;      // 2^14: f16 weights of up to 1, with room below
+
+// Q's fragments and the factor that its normalisation left out.  qs: the G heads' rows in shared memory.  Returns the factor
+// of this lane's head (lane >> 2).
+template <int G>
+__device__ __forceinline__ float load_q_scaled(const uint16_t *qs, uint32_t (&qf)[8][2], int lane)
+{
+    const int t = lane & 3, g = G <= 4 ? (lane >> 2) & 3 : lane >> 2;
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (g < G) x = *reinterpret_cast<const uint4 *>(qs + g * kHeadDim + 32 * t + 8 * i);
+        w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+    }
+    uint32_t top = 0;      // the largest finite magnitude: infinities and NaN stay what they are
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t a = w[i] & 0x7fffu, b = (w[i] >> 16) & 0x7fffu;
+        top = max(top, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const uint32_t e = max(top >> 7, 20u);                                 // biased exponent; smaller heads than 2^-107 stay small
+    const float down = __uint_as_float((268u - e) << 23);                  // 2^(14 - (e - 127))
+#pragma unroll
+    for (int i = 0; i < 16; ++i) qf[i >> 1][i & 1] = pack_f16(bf16lo_to_f32(w[i]) * down, bf16hi_to_f32(w[i]) * down);
+    return __uint_as_float((e - 14u) << 23);
+}
+
+// k_base, v_base: shared-memory addresses of the page's K and V codes ([16 rows][128 B], 128B-swizzled); [tlo, thi) the rows
+// inside the shard (at least one); qs: factors of the scores of heads 2t, 2t+1 in units of log 2; m2, l, acc as in
+// process_page, with acc[i][e], acc[i][2 + e] channels 16 i + 2 g and 16 i + 2 g + 1 of head 2t + e (FOLD: of the sum of
+// columns 2t + e and 2t + e + 4).
+template <int KV, bool FOLD>
+__device__ __forceinline__ void process_page_scaled(uint32_t k_base, uint32_t v_base, float ks, float vs, int tlo, int thi, bool ragged,
+                                                    const uint32_t (&qf)[8][2], const float (&qs)[2], float (&m2)[2], float (&l)[2],
+                                                    float (&acc)[8][4], int lane)
+{
+    const int g = lane >> 2, t = lane & 3;
+    if (ragged) {
+        // values outside the range must contribute nothing, whatever bits they hold: 0 times a NaN is not 0
+        for (int idx = lane; idx < kScaledPageBytes / 16; idx += 32) {
+            const int row = idx >> 3;
+            if (row < tlo || row >= thi) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_base + idx * 16), "r"(0) : "memory");
+        }
+        __syncwarp();
+    }
+    // ---- S[token, head] = K Q^T
+    float sc[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t vr[4][4];
+    {
+        float odd[4] = {0.f, 0.f, 0.f, 0.f};      // two accumulators: half the dependent chain
+        uint32_t kr[2][8];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint4 x = ld_shared_16(k_base + (g + 8 * r) * 128 + (((2 * t + j) ^ (g & 7)) << 4));
+                kr[r][4 * j] = x.x; kr[r][4 * j + 1] = x.y; kr[r][4 * j + 2] = x.z; kr[r][4 * j + 3] = x.w;
+            }
+        const int vrow = (lane & 7) + ((lane >> 3) & 1) * 8, vsel = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ldmatrix_x4_trans(vr[i], v_base + vrow * 128 + (((2 * i + vsel) ^ (vrow & 7)) << 4));
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            uint32_t a[4];
+            halves_of<KV, false>(kr[0][w], a[0], a[2]);
+            halves_of<KV, false>(kr[1][w], a[1], a[3]);
+            mma_f16(w & 1 ? odd : sc, a, qf[w][0], qf[w][1]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[i] += odd[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sc[i] = sc[i] * qs[i & 1] * ks;
+    if (ragged) {
+        if (g < tlo || g >= thi) { sc[0] = neg_inf(); sc[1] = neg_inf(); }
+        if (g + 8 < tlo || g + 8 >= thi) { sc[2] = neg_inf(); sc[3] = neg_inf(); }
+    }
+    // ---- the page's own softmax
+    float mx0 = fmaxf(sc[0], sc[2]), mx1 = fmaxf(sc[1], sc[3]);
+#pragma unroll
+    for (int off = 4; off < 32; off <<= 1) {
+        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
+        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
+    }
+    const float mp0 = mx0 == neg_inf() ? 0.f : mx0, mp1 = mx1 == neg_inf() ? 0.f : mx1;      // nothing above -inf: avoid inf - inf
+    const float p0 = fast_exp2(sc[0] - mp0), p1 = fast_exp2(sc[1] - mp1);
+    const float p2 = fast_exp2(sc[2] - mp0), p3 = fast_exp2(sc[3] - mp1);
+    const float mn0 = fmaxf(m2[0], mx0), mn1 = fmaxf(m2[1], mx1);
+    const float ms0 = mn0 == neg_inf() ? 0.f : mn0, ms1 = mn1 == neg_inf() ? 0.f : mn1;
+    const float al0 = fast_exp2(m2[0] - ms0), al1 = fast_exp2(m2[1] - ms1);      // of what came before
+    const float be0 = fast_exp2(mx0 - ms0), be1 = fast_exp2(mx1 - ms1);          // of this page
+    m2[0] = mn0; m2[1] = mn1;
+    l[0] = fmaf(l[0], al0, (p0 + p2) * be0);      // Z from the unrounded weights
+    l[1] = fmaf(l[1], al1, (p1 + p3) * be1);
+    // ---- P^T as the B operand, hi and lo
+    const float w0 = p0 * kWeightScale, w1 = p1 * kWeightScale, w2 = p2 * kWeightScale, w3 = p3 * kWeightScale;
+    uint32_t h0 = pack_f16(w0, w1), h1 = pack_f16(w2, w3);
+    float f0, f1, f2, f3;
+    unpack_f16(h0, f0, f1);
+    unpack_f16(h1, f2, f3);
+    const uint32_t e0 = pack_f16(w0 - f0, w1 - f1), e1 = pack_f16(w2 - f2, w3 - f3);
+    uint32_t bl0 = 0u, bl1 = 0u;
+    if (FOLD) {
+        if (t >= 2) { h0 = e0; h1 = e1; }      // columns 4..7 repeat the heads of 0..3
+    } else {
+        bl0 = movmatrix_trans(e0);
+        bl1 = movmatrix_trans(e1);
+    }
+    const uint32_t bh0 = movmatrix_trans(h0), bh1 = movmatrix_trans(h1);
+    if (__any_sync(0xffffffffu, (al0 != 1.f) || (al1 != 1.f))) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            acc[i][0] *= al0; acc[i][1] *= al1; acc[i][2] *= al0; acc[i][3] *= al1;
+        }
+    }
+    // ---- O^T[d, head] += factor * (V^T P^T)
+    const float vb0 = be0 * (1.f / kWeightScale) * vs, vb1 = be1 * (1.f / kWeightScale) * vs;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        uint32_t a[4];
+        halves_of<KV, true>(vr[i >> 1][2 * (i & 1)], a[0], a[1]);
+        halves_of<KV, true>(vr[i >> 1][2 * (i & 1) + 1], a[2], a[3]);
+        float d[4] = {0.f, 0.f, 0.f, 0.f};
+        mma_f16(d, a, bh0, bh1);
+        if (!FOLD) mma_f16(d, a, bl0, bl1);
+        acc[i][0] = fmaf(d[0], vb0, acc[i][0]); acc[i][1] = fmaf(d[1], vb1, acc[i][1]);
+        acc[i][2] = fmaf(d[2], vb0, acc[i][2]); acc[i][3] = fmaf(d[3], vb1, acc[i][3]);
+    }
+}
+
+// One TMA box of a scaled pool: a page of one KV head, 16 rows of 128 B.
+__device__ __forceinline__ void tma_load_page_scaled(uint32_t dst, const CUtensorMap *map, int y, int z, uint32_t bar, unsigned long long policy)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
+        ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(z), "r"(bar), "l"(policy) : "memory");
+}
+// Four bytes into shared memory, and the arrival on `bar` once all such copies of this thread have landed.
+__device__ __forceinline__ void copy_async_4(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(real ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void arrive_after_copies(uint32_t bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+}  // namespace qf

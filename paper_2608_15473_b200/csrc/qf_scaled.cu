@@ -56,15 +56,17 @@ int launch_simple_scaled(const void *q, const void *k, const void *v, const Scal
 
 int launch_sweep_scaled(const void *q, const void *k, const void *v, const ScaledKv &s, const int32_t *bt, const int32_t *sl,
                         const int32_t *sr, float *o, float *m, float *l, const qf::DevParams &P, char *ws,
-                        const qf::WorkspaceLayout &wsl, int sm_count, unsigned long long epoch, cudaStream_t st, cudaEvent_t ev0,
+                        const qf::WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st, cudaEvent_t ev0,
                         cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish)
 {
-    (void)wsl; (void)sm_count; (void)msg; (void)msg_len; (void)skip_finish;
-    if (ev0) cudaEventRecord(ev0, st);
-    const int rc = launch_simple_scaled(q, k, v, s, bt, sl, sr, o, m, l, P, reinterpret_cast<unsigned long long *>(ws), epoch, st);
-    if (ev1) cudaEventRecord(ev1, st);
-    *launches = 1;
-    return rc;
+    CUtensorMap kmap, vmap;
+    if (qf::make_scaled_map(&kmap, k, P.num_pages, P.num_kv_heads, P.kv_nhd != 0, true, msg, msg_len)) return QF_ERR_CUDA;
+    if (qf::make_scaled_map(&vmap, v, P.num_pages, P.num_kv_heads, P.kv_nhd != 0, true, msg, msg_len)) return QF_ERR_CUDA;
+    return s.kind == qf::kKvE4m3
+               ? qf::launch_sweep_kv<qf::kKvE4m3>(kmap, vmap, s.k_scale, s.v_scale, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0,
+                                                  ev1, msg, msg_len, launches, skip_finish)
+               : qf::launch_sweep_kv<qf::kKvInt8>(kmap, vmap, s.k_scale, s.v_scale, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0,
+                                                  ev1, msg, msg_len, launches, skip_finish);
 }
 
 int launch_rows_scaled(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *, int kind, char *, int, cudaStream_t st)

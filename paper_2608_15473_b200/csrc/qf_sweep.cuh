@@ -38,6 +38,7 @@
 
 #include "qf_common.cuh"
 #include "qf_page_math.cuh"
+#include "qf_page_scaled.cuh"
 #include "qf_finish.cuh"
 
 namespace qf {
@@ -46,7 +47,9 @@ constexpr int kConsumerWarps = 8;
 constexpr int kPagesPerStage = kConsumerWarps;    // pages (of one KV head) per ring stage, one per consumer warp
 constexpr int kConsumerThreads = kConsumerWarps * 32;
 constexpr int kSweepThreads  = (kConsumerWarps + 1) * 32;
-constexpr int kStages        = 3;                 // 3 x 64 KB of K and V in flight per SM
+// How much of K and V is in flight per SM: 3 stages of 64 KB, or, for a scaled cache, 5 of 32 KB.
+template <int KV> constexpr int kStages = KV == kKvBf16 ? 3 : 5;
+template <int KV> constexpr int kPageBlockBytes = KV == kKvBf16 ? kPageBytes : kScaledPageBytes;
 constexpr int kMaxSweepCtas  = 160;               // persistent CTAs (one per SM) are capped at this
 constexpr int kHalfTileBytes = 2048;              // 16 rows x 64 channels of bf16
 constexpr int kRedStride     = kHeadDim + 4;      // padded row of the warp-merge buffer
@@ -229,17 +232,20 @@ struct __align__(16) StageMeta {
 };
 enum { kSegFirst = 1, kSegLast = 2 };
 
-template <int G>
+template <int G, int KV>
 struct SweepSmem {
     // every K/V half tile is a 1024-byte-aligned 128B-swizzled TMA destination
-    alignas(1024) uint8_t kv[kStages][2][kPagesPerStage][kPageBytes];  // [stage][K|V][page][half][row][128B]
-    alignas(16) uint16_t q[kStages][G * kHeadDim];
+    // [stage][K|V][page][half][row][128B]; codes of a scaled cache: [stage][K|V][page][row][128B]
+    static constexpr int kRing = kStages<KV>;
+    alignas(1024) uint8_t kv[kRing][2][kPagesPerStage][kPageBlockBytes<KV>];
+    alignas(16) uint16_t q[kRing][G * kHeadDim];
     static constexpr int kRoundHeads = G < 4 ? G : 4;  // heads merged per epilogue round
     alignas(16) float red_acc[kConsumerWarps][kRoundHeads][kRedStride];
     alignas(16) float red_ml[kConsumerWarps][G][2];
-    alignas(16) StageMeta meta[kStages];
-    alignas(8) unsigned long long full_bar[kStages];
-    alignas(8) unsigned long long empty_bar[kStages];
+    alignas(16) StageMeta meta[kRing];
+    alignas(8) unsigned long long full_bar[kRing];
+    alignas(8) unsigned long long empty_bar[kRing];
+    float scales[kRing][2][kPagesPerStage];      // of a scaled cache's pages
     alignas(8) unsigned long long red_bar[2];
     int abort_flag;
     unsigned long long epoch;   // this launch's epoch, read once per CTA
@@ -247,7 +253,7 @@ struct SweepSmem {
     int prefix[kMaxSmemEntries + 1];
 };
 
-template <int G>
+template <int G, int KV>
 __global__ void __launch_bounds__(kSweepThreads, 1)
 sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
              const uint16_t *__restrict__ q, const int *__restrict__ block_table,
@@ -255,10 +261,11 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
              float *__restrict__ o_part, float *__restrict__ m_part, float *__restrict__ lse_part,
              unsigned long long *__restrict__ header, const int *__restrict__ global_prefix,
              int4 *__restrict__ piece_info, float *__restrict__ seg, int seg_stride,
-             unsigned long long host_epoch, DevParams P)
+             unsigned long long host_epoch, const float *__restrict__ k_scale, const float *__restrict__ v_scale, DevParams P)
 {
+    constexpr int kRing = kStages<KV>;
     extern __shared__ uint8_t smem_raw[];
-    SweepSmem<G> &sm = *reinterpret_cast<SweepSmem<G> *>(
+    SweepSmem<G, KV> &sm = *reinterpret_cast<SweepSmem<G, KV> *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -268,8 +275,9 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
     volatile int *abort_flag = &sm.abort_flag;
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_u32(&sm.full_bar[s]), 1);
+        for (int s = 0; s < kRing; ++s) {
+            // one arrival with the bytes to expect and, for a scaled cache, one per lane once its scale has landed
+            mbar_init(smem_u32(&sm.full_bar[s]), KV == kKvBf16 ? 1 : 33);
             mbar_init(smem_u32(&sm.empty_bar[s]), kConsumerWarps);
         }
         mbar_init(smem_u32(&sm.red_bar[0]), kConsumerWarps);
@@ -435,7 +443,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                     const int part = lane / kPagesPerStage; // 0: K page, 1: V page (>= 2: idle lane)
                     int phys = __shfl_sync(0xffffffffu, tbl, (page0 - tbl_page0) + i);
                     bool bad = false;
-                    if (P.check_bounds && (phys < 0 || (long long)phys >= P.num_pages)) { bad = true; phys = 0; }
+                    if ((KV != kKvBf16 || P.check_bounds) && (phys < 0 || (long long)phys >= P.num_pages)) { bad = true; phys = 0; }
                     const unsigned bad_mask = __ballot_sync(0xffffffffu, bad && i < np && part == 0) & 0xffu;
                     const bool issuer = (i < np) && (part < 2);
 
@@ -451,11 +459,33 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                         mt.aux = (int)bad_mask;
                         mt.slot = e * Hkv + c + piece;
                         sm.meta[stage] = mt;
-                        mbar_arrive_expect_tx(full, (uint32_t)np * 2u * kPageBytes + (first ? (uint32_t)G * 256u : 0u));
-                        if (bad_mask) epoch_or(header + kHdrStatus, epoch, kStatusBadPage);
+                        mbar_arrive_expect_tx(full, (uint32_t)np * 2u * kPageBlockBytes<KV> + (first ? (uint32_t)G * 256u : 0u));
+                        if (bad_mask && P.check_bounds) epoch_or(header + kHdrStatus, epoch, kStatusBadPage);
                     }
                     __syncwarp();
-                    if (issuer) {
+                    if constexpr (KV != kKvBf16) {
+                        // scales: lanes 0..7 of the K pages, 8..15 of the V pages
+                        if (part < 2)
+                            copy_async_4(smem_u32(&sm.scales[stage][part][i]), (part ? v_scale : k_scale) + (size_t)phys * Hkv + c, i < np);
+                        arrive_after_copies(full);
+                        // codes: one thread issues every copy, with operands that are the same for the warp (a lane per page makes
+                        // each copy a turn of a loop over lanes, and here there are twice as many copies per byte)
+                        const int at0 = P.kv_nhd ? phys * kPageSize : (phys * Hkv + c) * kPageSize;
+                        int at[kPagesPerStage];
+#pragma unroll
+                        for (int k = 0; k < kPagesPerStage; ++k) at[k] = __shfl_sync(0xffffffffu, at0, k);
+                        if (elect_one()) {
+                            const uint32_t dst = smem_u32(&sm.kv[stage][0][0][0]);
+#pragma unroll
+                            for (int k = 0; k < kPagesPerStage; ++k) {
+                                if (k >= np) break;
+                                const int y = P.kv_nhd ? c : at[k], z = P.kv_nhd ? at[k] : 0;
+                                tma_load_page_scaled(dst + k * kScaledPageBytes, &k_map, y, z, full, kv_policy);
+                                tma_load_page_scaled(dst + (kPagesPerStage + k) * kScaledPageBytes, &v_map, y, z, full, kv_policy);
+                            }
+                        }
+                        __syncwarp();
+                    } else if (issuer) {
                         const uint32_t dst = smem_u32(&sm.kv[stage][part][i][0]);
                         if (P.kv_nhd)
                             tma_load_page_nhd(dst, part ? &v_map : &k_map, c, phys * kPageSize, full, kv_policy);
@@ -466,7 +496,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                         bulk_load_1d(smem_u32(&sm.q[stage][0]), q + ((size_t)b * Hq + (size_t)c * G) * kHeadDim,
                                      (uint32_t)G * 256u, full);
                     ++issued;
-                    if (++stage == kStages) { stage = 0; phase ^= 1; }
+                    if (++stage == kRing) { stage = 0; phase ^= 1; }
                 }
                 pos += seg_len;
             }
@@ -490,6 +520,10 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                     sm.meta[stage] = mt;
                     mbar_arrive(smem_u32(&sm.full_bar[stage]));
                 }
+                if (KV != kKvBf16) {
+                    __syncwarp();
+                    mbar_arrive(smem_u32(&sm.full_bar[stage]));      // as every lane does for its scale
+                }
             } else ok = false;
         }
         if (!ok) {
@@ -498,8 +532,8 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             __syncwarp();
             int s2 = stage;
             uint32_t ph2 = phase;
-            for (int k = 0; k < min(issued, kStages); ++k) {
-                if (--s2 < 0) { s2 = kStages - 1; ph2 ^= 1; }
+            for (int k = 0; k < min(issued, kRing); ++k) {
+                if (--s2 < 0) { s2 = kRing - 1; ph2 ^= 1; }
                 for (unsigned it = 0; it < (1u << 20); ++it)
                     if (mbar_try_wait(smem_u32(&sm.full_bar[s2]), ph2)) break;
             }
@@ -524,6 +558,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
     const float scale2 = P.sm_scale * 1.4426950408889634f;  // scores are kept in units of log 2
     const float kLn2 = 0.6931471805599453f;
     uint32_t qf[8][2];
+    float qs[2] = {0.f, 0.f};      // scaled cache: factors of the scores of heads 2t, 2t+1
     float m2[2] = {neg_inf(), neg_inf()};
     float l[2] = {0.f, 0.f};
     float acc[8][4];
@@ -552,11 +587,17 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         if (mt.entry < 0) return;   // end of this CTA's work (the producer warp has counted the CTA as done)
 
         if (mt.flags & kSegFirst) {
-            const uint16_t *qs = sm.q[stage];
+            const uint16_t *q_rows = sm.q[stage];
+            if constexpr (KV != kKvBf16) {
+                const float f = load_q_scaled<G>(q_rows, qf, lane) * scale2;
+                qs[0] = __shfl_sync(0xffffffffu, f, 8 * t);          // heads 2t and 2t+1: lanes 4 * head
+                qs[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+            } else {
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-                qf[ks][0] = (g < G) ? *reinterpret_cast<const uint32_t *>(qs + g * kHeadDim + ks * 16 + 2 * t) : 0u;
-                qf[ks][1] = (g < G) ? *reinterpret_cast<const uint32_t *>(qs + g * kHeadDim + ks * 16 + 2 * t + 8) : 0u;
+                for (int ks = 0; ks < 8; ++ks) {
+                    qf[ks][0] = (g < G) ? *reinterpret_cast<const uint32_t *>(q_rows + g * kHeadDim + ks * 16 + 2 * t) : 0u;
+                    qf[ks][1] = (g < G) ? *reinterpret_cast<const uint32_t *>(q_rows + g * kHeadDim + ks * 16 + 2 * t + 8) : 0u;
+                }
             }
             m2[0] = m2[1] = neg_inf();
             l[0] = l[1] = 0.f;
@@ -572,7 +613,12 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             const uint32_t k_base = smem_u32(&sm.kv[stage][0][wp][0]);
             const uint32_t v_base = smem_u32(&sm.kv[stage][1][wp][0]);
 
-            process_page(k_base, v_base, kHalfTileBytes, tlo, thi, ragged, qf, m2, l, acc, scale2, lane);
+            if constexpr (KV != kKvBf16) {
+                if (tlo < thi)      // a page that is skipped has no scale either
+                    process_page_scaled<KV, (G <= 4)>(k_base, v_base, sm.scales[stage][0][wp], sm.scales[stage][1][wp], tlo, thi, ragged, qf, qs, m2, l, acc, lane);
+            } else {
+                process_page(k_base, v_base, kHalfTileBytes, tlo, thi, ragged, qf, m2, l, acc, scale2, lane);
+            }
             if (ragged) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         __syncwarp();
@@ -585,7 +631,13 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                 l[0] += __shfl_xor_sync(0xffffffffu, l[0], off);
                 l[1] += __shfl_xor_sync(0xffffffffu, l[1], off);
             }
-            constexpr int RG = SweepSmem<G>::kRoundHeads;
+            if constexpr (KV != kKvBf16 && G <= 4) {      // the columns that carried the weights' second terms
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][e] += __shfl_xor_sync(0xffffffffu, acc[i][e], 2);
+            }
+            constexpr int RG = SweepSmem<G, KV>::kRoundHeads;
             const int nseg = mt.flags >> 8;
             const size_t out_row = out_entry(P, mt.entry) * Hq + (size_t)mt.kv_head * G;  // + head
             float *seg_slot = seg + (size_t)mt.slot * seg_stride;
@@ -597,8 +649,8 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                     if (head < G && head / RG == hr) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            sm.red_acc[warp][head - hr * RG][16 * i + g] = acc[i][hh];
-                            sm.red_acc[warp][head - hr * RG][16 * i + g + 8] = acc[i][2 + hh];
+                            sm.red_acc[warp][head - hr * RG][16 * i + (KV != kKvBf16 ? 2 * g : g)] = acc[i][hh];
+                            sm.red_acc[warp][head - hr * RG][16 * i + (KV != kKvBf16 ? 2 * g + 1 : g + 8)] = acc[i][2 + hh];
                         }
                         if (g == 0) { sm.red_ml[warp][head][0] = m2[hh]; sm.red_ml[warp][head][1] = l[hh]; }
                     }
@@ -643,7 +695,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                 if (!red_sync(1, red_phase1)) return;
             }
         }
-        if (++stage == kStages) { stage = 0; phase ^= 1; }
+        if (++stage == kRing) { stage = 0; phase ^= 1; }
     }
 }
 
@@ -653,6 +705,45 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
 
+inline EncodeTiledFn encode_tiled(char *msg, size_t msg_len)
+{
+    static std::mutex mu;
+    static EncodeTiledFn encode = nullptr;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!encode) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+        if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) {
+            snprintf(msg, msg_len, "cuTensorMapEncodeTiled entry point not available");
+            return nullptr;
+        }
+        encode = (EncodeTiledFn)fn;
+    }
+    return encode;
+}
+
+// A pool of codes as [., rows, 128 B] in boxes of one (page, KV head) block: 16 neighbouring rows (head-major) or 16 token rows of
+// one head, Hkv rows apart (token-major).  swizzled: 128B swizzle, else rows as they are.  Encoded for every call (under a
+// microsecond), so nothing is remembered about a pointer.
+inline int make_scaled_map(CUtensorMap *out, const void *pool, long long num_pages, int num_kv_heads, bool nhd, bool swizzled,
+                           char *msg, size_t msg_len)
+{
+    EncodeTiledFn encode = encode_tiled(msg, msg_len);
+    if (!encode) return -1;
+    const cuuint64_t hkv = (cuuint64_t)num_kv_heads, rows = (cuuint64_t)num_pages * kPageSize;
+    const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, nhd ? hkv : rows * hkv, nhd ? rows : 1};
+    const cuuint64_t strides[2] = {(cuuint64_t)kHeadDim, (nhd ? hkv : rows * hkv) * kHeadDim};
+    const cuuint32_t box[3] = {(cuuint32_t)kHeadDim, nhd ? 1u : (cuuint32_t)kPageSize, nhd ? (cuuint32_t)kPageSize : 1u}, ones[3] = {1, 1, 1};
+    const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(pool), dims, strides, box, ones,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                              nhd ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return 0;
+    snprintf(msg, msg_len, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+    return -1;
+}
+
 // A [2 halves, rows, 64] bf16 view of a KV pool, one 4 KB box per (page, KV head), 128B swizzle.
 // box_rows = 16 boxes one (page, KV head) block (4 KB).  For a token-major pool (nhd) the view has a fourth
 // dimension, the KV head between the channel half and the token row, and a box takes 16 token rows of one head,
@@ -660,7 +751,6 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
 inline int make_pool_map(CUtensorMap *out, const void *pool, long long num_pages, int num_kv_heads, int box_rows,
                          bool nhd, char *msg, size_t msg_len)
 {
-    static EncodeTiledFn encode = nullptr;
     static std::mutex mu;
     struct Entry { const void *pool; long long pages; int heads; int rows; CUtensorMap map; };   // rows < 0: token-major
     // One descriptor per (pointer, shape), hashed by the pointer: a decode loop walks every layer's pools each
@@ -679,16 +769,8 @@ inline int make_pool_map(CUtensorMap *out, const void *pool, long long num_pages
         }
         if (c.pool == nullptr) { victim = (home + i) % kCacheEntries; break; }
     }
-    if (!encode) {
-        void *fn = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
-        if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) {
-            snprintf(msg, msg_len, "cuTensorMapEncodeTiled entry point not available");
-            return -1;
-        }
-        encode = (EncodeTiledFn)fn;
-    }
+    EncodeTiledFn encode = encode_tiled(msg, msg_len);
+    if (!encode) return -1;
     // dims: 64 channels (128 B, the swizzle span), rows (256 B apart), the two halves of a row (128 B apart);
     // a box is one whole 4 KB (page, KV head) block, landing in shared memory as [half][row][128 B]
     const cuuint64_t dims[3] = {64, (cuuint64_t)num_pages * num_kv_heads * kPageSize, 2};
@@ -722,8 +804,8 @@ inline unsigned long long next_epoch()
     return (counter.fetch_add(1) + 1) & ((1ull << 54) - 1);
 }
 
-template <int G>
-int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const void *q, const int32_t *bt,
+template <int G, int KV>
+int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const float *k_scale, const float *v_scale, const void *q, const int32_t *bt,
                    const int32_t *sl, const int32_t *sr, float *o, float *m, float *l, const DevParams &P,
                    char *ws, const WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st,
                    cudaEvent_t ev0, cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish)
@@ -734,7 +816,8 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const void 
     unsigned long long *counters = reinterpret_cast<unsigned long long *>(ws + wsl.counter_off);
     float *seg = reinterpret_cast<float *>(ws + wsl.seg_off);
     const int n_entries = P.batch * P.max_shards;
-    const size_t smem = sizeof(SweepSmem<G>) + 1024;
+    const size_t smem = sizeof(SweepSmem<G, KV>) + 1024;
+    static_assert(sizeof(SweepSmem<G, KV>) + 1024 <= 227 * 1024, "one CTA per SM");
     {   // per-device kernel attribute, set once under a lock (any host thread may come first)
         static std::mutex attr_mu;
         static bool attr_set[64];
@@ -742,7 +825,7 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const void 
         cudaGetDevice(&dev);
         std::lock_guard<std::mutex> lock(attr_mu);
         if (!attr_set[dev & 63]) {
-            cudaError_t e = cudaFuncSetAttribute(sweep_kernel<G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            cudaError_t e = cudaFuncSetAttribute(sweep_kernel<G, KV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e != cudaSuccess) { snprintf(msg, msg_len, "cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return -5; }
             attr_set[dev & 63] = true;
         }
@@ -757,9 +840,9 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const void 
         *launches += 1;
     }
     if (ev0) cudaEventRecord(ev0, st);
-    cudaError_t e = launch_pdl(sweep_kernel<G>, dim3(n_ctas), dim3(kSweepThreads), smem, st, kmap, vmap,
+    cudaError_t e = launch_pdl(sweep_kernel<G, KV>, dim3(n_ctas), dim3(kSweepThreads), smem, st, kmap, vmap,
                                (const uint16_t *)q, bt, sl, sr, o, m, l, header, global_prefix, piece_info, seg,
-                               wsl.seg_stride, epoch, P);
+                               wsl.seg_stride, epoch, k_scale, v_scale, P);
     if (ev1) cudaEventRecord(ev1, st);
     if (e != cudaSuccess) { snprintf(msg, msg_len, "sweep_kernel launch: %s", cudaGetErrorString(e)); return -5; }
     *launches += 1;
@@ -774,26 +857,20 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const void 
     return 0;
 }
 
-inline int launch_sweep(const void *q, const void *k_cache, const void *v_cache, const int32_t *bt,
-                        const int32_t *sl, const int32_t *sr, float *o, float *m, float *l, const DevParams &P,
-                        char *ws, const WorkspaceLayout &wsl, int sm_count, unsigned long long epoch,
-                        cudaStream_t st, cudaEvent_t ev0, cudaEvent_t ev1, char *msg, size_t msg_len, int *launches,
-                        bool skip_finish = false)
+// The kernel of the batch's group size, over either kind of cache (scales: null for bf16).
+template <int KV, int G = 8>
+int launch_sweep_kv(const CUtensorMap &kmap, const CUtensorMap &vmap, const float *k_scale, const float *v_scale, const void *q,
+                    const int32_t *bt, const int32_t *sl, const int32_t *sr, float *o, float *m, float *l, const DevParams &P,
+                    char *ws, const WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st,
+                    cudaEvent_t ev0, cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish)
 {
-    CUtensorMap kmap, vmap;
-    if (make_pool_map(&kmap, k_cache, P.num_pages, P.num_kv_heads, kPageSize, P.kv_nhd != 0, msg, msg_len)) return -5;
-    if (make_pool_map(&vmap, v_cache, P.num_pages, P.num_kv_heads, kPageSize, P.kv_nhd != 0, msg, msg_len)) return -5;
-    const int n_ctas = sm_count < kMaxSweepCtas ? sm_count : kMaxSweepCtas;
-    switch (P.group) {
-    case 1: return launch_sweep_g<1>(kmap, vmap, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len, launches, skip_finish);
-    case 2: return launch_sweep_g<2>(kmap, vmap, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len, launches, skip_finish);
-    case 3: return launch_sweep_g<3>(kmap, vmap, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len, launches, skip_finish);
-    case 4: return launch_sweep_g<4>(kmap, vmap, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len, launches, skip_finish);
-    case 5: return launch_sweep_g<5>(kmap, vmap, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len, launches, skip_finish);
-    case 6: return launch_sweep_g<6>(kmap, vmap, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len, launches, skip_finish);
-    case 7: return launch_sweep_g<7>(kmap, vmap, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len, launches, skip_finish);
-    default: return launch_sweep_g<8>(kmap, vmap, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len, launches, skip_finish);
+    if constexpr (G > 1) {
+        if (P.group < G)
+            return launch_sweep_kv<KV, G - 1>(kmap, vmap, k_scale, v_scale, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1,
+                                              msg, msg_len, launches, skip_finish);
     }
+    return launch_sweep_g<G, KV>(kmap, vmap, k_scale, v_scale, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len,
+                                 launches, skip_finish);
 }
 
 }  // namespace qf

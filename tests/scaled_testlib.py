@@ -77,7 +77,8 @@ class Scaled(Paged):
 
 def states64(pg, q, ranges, scale=None):
     """Shard states of single queries q [B, Hq, D] over [beg, end) ranges [B, S, 2] of each request's cached positions: a
-    dict of [B, S, Hq(, D)] arrays out, lse, m and slack, what a relative error of 2^-20 of every |q_i k_i| could do."""
+    dict of [B, S, Hq(, D)] arrays out, lse, m and slack, what a relative error of 2^-20 of every |q_i k_i| and the weights'
+    rounding could do."""
     B, Hq, _ = q.shape
     S, grp = ranges.shape[1], Hq // pg.Hkv
     r = dict(out=torch.zeros((B, S, Hq, D), dtype=torch.float64), lse=torch.full((B, S, Hq), -np.inf, dtype=torch.float64),
@@ -101,7 +102,10 @@ def states64(pg, q, ranges, scale=None):
             err = 2.0 ** -20 * mass[..., lo:hi].amax(-1)      # of any score
             r["out"][b, s] = torch.einsum("cgn,cnd->cgd", w, v[:, lo:hi]).reshape(Hq, D).cpu()
             spread = torch.einsum("cgn,cnd->cgd", w, v[:, lo:hi].abs())
-            r["slack"][b, s] = ((2 * err[..., None] + 2.0 ** -19) * spread).reshape(Hq, D).cpu()
+            # a weight's second 16-bit term ends at 2^-25 where its page's largest weight is 2^14, so at 2^-39 of that: sixteen
+            # such errors per page, and the pages' largest weights add up to 1 at most, are 2^-35 of the largest value
+            floor = 2.0 ** -35 * v[:, lo:hi].abs().amax(1)
+            r["slack"][b, s] = ((2 * err[..., None] + 2.0 ** -19) * spread + floor[:, None]).reshape(Hq, D).cpu()
             r["lse_slack"][b, s] = err.reshape(Hq).cpu()
             r["m"][b, s], r["lse"][b, s] = m.reshape(Hq).cpu(), z.reshape(Hq).cpu()
     return r
