@@ -35,12 +35,12 @@ constexpr int kSmallMaxShards  = 32;   // shard slots per request this kernel pl
 
 // Can this sweep be treated as small?  Decided on the host from an upper bound on the stage units: every shard of
 // every request at the longest length the parameters allow.
-inline bool sweep_is_small(const DevParams &P, int n_ctas)
+inline bool sweep_is_small(const DevParams &P, int n_ctas, int unit_pages)
 {
     const long long entries = (long long)P.batch * P.max_shards;
     if (entries > kMaxSmemEntries || P.max_shards > kSmallMaxShards) return false;
     const long long pages = ((long long)P.max_tokens + kPageSize - 1) / kPageSize;
-    const long long units = entries * P.num_kv_heads * ((pages + kPagesPerStage - 1) / kPagesPerStage);
+    const long long units = entries * P.num_kv_heads * ((pages + unit_pages - 1) / unit_pages);
     return units <= (long long)kSmallUnitsPerCta * n_ctas;
 }
 
@@ -53,7 +53,7 @@ inline bool sweep_is_small(const DevParams &P, int n_ctas)
 //            state in the caller's shard arrays; otherwise nothing to do.
 // Both roles are the same code: a list of states walked kB at a time, all loads of a batch in flight together,
 // merged against the batch's common maximum in list order (the order of every sum is fixed), one destination.
-template <int G>
+template <int G, int KV>
 __global__ void __launch_bounds__(kFinThreads)
 merge_small_kernel(const int *__restrict__ seq_lens, const int *__restrict__ shard_ranges,
                    const int *__restrict__ shard_counts, const float *__restrict__ seg, int seg_stride, int seg_slots,
@@ -82,7 +82,7 @@ merge_small_kernel(const int *__restrict__ seq_lens, const int *__restrict__ sha
     // ---- the plan, from the step's inputs alone (nothing here was written by the sweep)
     int before = 0, all = 0;
     for (int e = d; e < n_entries; e += kFinThreads) {
-        const int u = entry_units(seq_lens, shard_ranges, e, S, Hkv, P.max_tokens);
+        const int u = entry_units<KV>(seq_lens, shard_ranges, e, S, Hkv, P.max_tokens);
         all += u;
         if (e < b * S) before += u;
         if (e >= b * S && e < (b + 1) * S) s_units[e - b * S] = u;
@@ -218,32 +218,19 @@ merge_small_kernel(const int *__restrict__ seq_lens, const int *__restrict__ sha
     }
 }
 
-// Enqueue the merge of a small sweep: one CTA per (request, KV head).
-template <int G>
-inline cudaError_t launch_merge_small_g(const int32_t *sl, const int32_t *sr, const int32_t *sc, char *ws,
-                                        const WorkspaceLayout &wsl, float *o, float *m, float *l, float *out, float *lse,
-                                        int n_sweep_ctas, const DevParams &P, cudaStream_t st)
-{
-    const float *seg = reinterpret_cast<const float *>(ws + wsl.seg_off);
-    // one CTA per (request, KV head, role): S unit roles and the request role
-    return launch_pdl(merge_small_kernel<G>, dim3((unsigned)(P.batch * P.num_kv_heads * (P.max_shards + 1))),
-                      dim3(kFinThreads), 0, st, sl, sr,
-                      sc, seg, wsl.seg_stride, (int)wsl.seg_slots, o, m, l, out, lse, n_sweep_ctas, P);
-}
+// Enqueue the merge of a small sweep: one CTA per (request, KV head, role): S unit roles and the request role.
+template <int KV, int G = 8>
 inline cudaError_t launch_merge_small(const int32_t *sl, const int32_t *sr, const int32_t *sc, char *ws,
                                       const WorkspaceLayout &wsl, float *o, float *m, float *l, float *out, float *lse,
                                       int n_sweep_ctas, const DevParams &P, cudaStream_t st)
 {
-    switch (P.group) {
-    case 1: return launch_merge_small_g<1>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
-    case 2: return launch_merge_small_g<2>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
-    case 3: return launch_merge_small_g<3>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
-    case 4: return launch_merge_small_g<4>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
-    case 5: return launch_merge_small_g<5>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
-    case 6: return launch_merge_small_g<6>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
-    case 7: return launch_merge_small_g<7>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
-    default: return launch_merge_small_g<8>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
+    if constexpr (G > 1) {
+        if (P.group < G) return launch_merge_small<KV, G - 1>(sl, sr, sc, ws, wsl, o, m, l, out, lse, n_sweep_ctas, P, st);
     }
+    const float *seg = reinterpret_cast<const float *>(ws + wsl.seg_off);
+    return launch_pdl(merge_small_kernel<G, KV>, dim3((unsigned)(P.batch * P.num_kv_heads * (P.max_shards + 1))),
+                      dim3(kFinThreads), 0, st, sl, sr,
+                      sc, seg, wsl.seg_stride, (int)wsl.seg_slots, o, m, l, out, lse, n_sweep_ctas, P);
 }
 
 }  // namespace qf

@@ -34,6 +34,25 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// The same with nothing to add to (zeros as an operand, not as registers to be cleared).
+__device__ __forceinline__ void mma_f16_fresh(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+// (a0, a1) += (x0, x1) * (f0, f1), one instruction
+__device__ __forceinline__ void fma_two(float &a0, float &a1, float x0, float x1, float f0, float f1)
+{
+    asm("{\n\t.reg .b64 a, x, f;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 x, {%2, %3};\n\tmov.b64 f, {%4, %5};\n\t"
+        "fma.rn.f32x2 a, x, f, a;\n\tmov.b64 {%0, %1}, a;\n\t}" : "+f"(a0), "+f"(a1) : "f"(x0), "f"(x1), "f"(f0), "f"(f1));
+}
+__device__ __forceinline__ void mul_two(float &a0, float &a1, float f0, float f1)
+{
+    asm("{\n\t.reg .b64 a, f;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 f, {%2, %3};\n\tmul.rn.f32x2 a, a, f;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(a0), "+f"(a1) : "f"(f0), "f"(f1));
+}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
     uint32_t w;
@@ -71,7 +90,7 @@ __device__ __forceinline__ void halves_of(uint32_t w, uint32_t &first, uint32_t 
     }
 }
 
-constexpr float kWeightScale = 16384.f;      // 2^14: f16 weights of up to 1, with room below
+constexpr float kWeightLog2 = 14.f;      // f16 weights of up to 2^14, with room below
 
 // Q's fragments and the factor that its normalisation left out.  qs: the G heads' rows in shared memory.  Returns the factor
 // of this lane's head (lane >> 2).
@@ -101,106 +120,120 @@ __device__ __forceinline__ float load_q_scaled(const uint16_t *qs, uint32_t (&qf
     return __uint_as_float((e - 14u) << 23);
 }
 
-// k_base, v_base: shared-memory addresses of the page's K and V codes ([16 rows][128 B], 128B-swizzled); [tlo, thi) the rows
-// inside the shard (at least one); qs: factors of the scores of heads 2t, 2t+1 in units of log 2; m2, l, acc as in
-// process_page, with acc[i][e], acc[i][2 + e] channels 16 i + 2 g and 16 i + 2 g + 1 of head 2t + e (FOLD: of the sum of
-// columns 2t + e and 2t + e + 4).
+// Two neighbouring pages (32 tokens): one pass for both halves what the softmax costs beside the exponentials, and one page's
+// products fill the other's latencies.
+// k_base, v_base: shared-memory addresses of the first page's K and V codes ([16 rows][128 B], 128B-swizzled; the second page
+// follows); [tlo, thi) rows of each page inside the shard (none of a page that is skipped, whose scales are 0); qs: factors of the
+// scores of heads 2t, 2t+1 in units of log 2; m2, l, acc as in process_page, with acc[i][e], acc[i][2 + e] channels 16 i + 2 g
+// and 16 i + 2 g + 1 of head 2t + e (FOLD: of the sum of columns 2t + e and 2t + e + 4).
 template <int KV, bool FOLD>
-__device__ __forceinline__ void process_page_scaled(uint32_t k_base, uint32_t v_base, float ks, float vs, int tlo, int thi, bool ragged,
-                                                    const uint32_t (&qf)[8][2], const float (&qs)[2], float (&m2)[2], float (&l)[2],
-                                                    float (&acc)[8][4], int lane)
+__device__ __forceinline__ void process_pages_scaled(uint32_t k_base, uint32_t v_base, const float (&ks)[2], const float (&vs)[2],
+                                                     const int (&tlo)[2], const int (&thi)[2], bool ragged, const uint32_t (&qf)[8][2],
+                                                     const float (&qs)[2], float (&m2)[2], float (&l)[2], float (&acc)[8][4], int lane)
 {
     const int g = lane >> 2, t = lane & 3;
     if (ragged) {
         // values outside the range must contribute nothing, whatever bits they hold: 0 times a NaN is not 0
-        for (int idx = lane; idx < kScaledPageBytes / 16; idx += 32) {
-            const int row = idx >> 3;
-            if (row < tlo || row >= thi) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_base + idx * 16), "r"(0) : "memory");
+#pragma unroll 1
+        for (int idx = lane; idx < 2 * kScaledPageBytes / 16; idx += 32) {
+            const int row = (idx >> 3) & 15;
+            const bool second = idx >> 7;
+            if (row < (second ? tlo[1] : tlo[0]) || row >= (second ? thi[1] : thi[0])) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_base + idx * 16), "r"(0) : "memory");
         }
         __syncwarp();
     }
-    // ---- S[token, head] = K Q^T
-    float sc[4] = {0.f, 0.f, 0.f, 0.f};
-    uint32_t vr[4][4];
-    {
-        float odd[4] = {0.f, 0.f, 0.f, 0.f};      // two accumulators: half the dependent chain
+    // ---- S[token, head] = K Q^T: sc[p][0], sc[p][1] token g of page p, heads 2t, 2t+1; sc[p][2], sc[p][3] token g + 8
+    float sc[2][4];
+    uint32_t vr[2][4][4];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
         uint32_t kr[2][8];
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const uint4 x = ld_shared_16(k_base + (g + 8 * r) * 128 + (((2 * t + j) ^ (g & 7)) << 4));
+                const uint4 x = ld_shared_16(k_base + p * kScaledPageBytes + (g + 8 * r) * 128 + (((2 * t + j) ^ (g & 7)) << 4));
                 kr[r][4 * j] = x.x; kr[r][4 * j + 1] = x.y; kr[r][4 * j + 2] = x.z; kr[r][4 * j + 3] = x.w;
             }
-        const int vrow = (lane & 7) + ((lane >> 3) & 1) * 8, vsel = lane >> 4;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ldmatrix_x4_trans(vr[i], v_base + vrow * 128 + (((2 * i + vsel) ^ (vrow & 7)) << 4));
+        float odd[4];      // two accumulators: half the dependent chain
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
             uint32_t a[4];
             halves_of<KV, false>(kr[0][w], a[0], a[2]);
             halves_of<KV, false>(kr[1][w], a[1], a[3]);
-            mma_f16(w & 1 ? odd : sc, a, qf[w][0], qf[w][1]);
+            if (w < 2) mma_f16_fresh(w ? odd : sc[p], a, qf[w][0], qf[w][1]);
+            else mma_f16(w & 1 ? odd : sc[p], a, qf[w][0], qf[w][1]);
         }
+        const float f0 = qs[0] * ks[p], f1 = qs[1] * ks[p];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[i] += odd[i];
+        for (int i = 0; i < 4; ++i) sc[p][i] = (sc[p][i] + odd[i]) * ((i & 1) ? f1 : f0);
+        if (ragged) {
+            if (g < tlo[p] || g >= thi[p]) { sc[p][0] = neg_inf(); sc[p][1] = neg_inf(); }
+            if (g + 8 < tlo[p] || g + 8 >= thi[p]) { sc[p][2] = neg_inf(); sc[p][3] = neg_inf(); }
+        }
     }
+    const int vrow = (lane & 7) + ((lane >> 3) & 1) * 8, vsel = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sc[i] = sc[i] * qs[i & 1] * ks;
-    if (ragged) {
-        if (g < tlo || g >= thi) { sc[0] = neg_inf(); sc[1] = neg_inf(); }
-        if (g + 8 < tlo || g + 8 >= thi) { sc[2] = neg_inf(); sc[3] = neg_inf(); }
-    }
-    // ---- the page's own softmax
-    float mx0 = fmaxf(sc[0], sc[2]), mx1 = fmaxf(sc[1], sc[3]);
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            ldmatrix_x4_trans(vr[p][i], v_base + p * kScaledPageBytes + vrow * 128 + (((2 * i + vsel) ^ (vrow & 7)) << 4));
+    // ---- the pages' own softmax
+    float mx0 = fmaxf(fmaxf(sc[0][0], sc[0][2]), fmaxf(sc[1][0], sc[1][2])), mx1 = fmaxf(fmaxf(sc[0][1], sc[0][3]), fmaxf(sc[1][1], sc[1][3]));
 #pragma unroll
     for (int off = 4; off < 32; off <<= 1) {
         mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
         mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
     }
-    const float mp0 = mx0 == neg_inf() ? 0.f : mx0, mp1 = mx1 == neg_inf() ? 0.f : mx1;      // nothing above -inf: avoid inf - inf
-    const float p0 = fast_exp2(sc[0] - mp0), p1 = fast_exp2(sc[1] - mp1);
-    const float p2 = fast_exp2(sc[2] - mp0), p3 = fast_exp2(sc[3] - mp1);
+    // Weights are taken against the pages' maximum less 14 (in log 2), the same number in w and be, so its rounding cancels.
+    const float mp0 = mx0 == neg_inf() ? 0.f : mx0 - kWeightLog2, mp1 = mx1 == neg_inf() ? 0.f : mx1 - kWeightLog2;
+    float w[2][4];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[p][i] = fast_exp2(sc[p][i] - ((i & 1) ? mp1 : mp0));
     const float mn0 = fmaxf(m2[0], mx0), mn1 = fmaxf(m2[1], mx1);
-    const float ms0 = mn0 == neg_inf() ? 0.f : mn0, ms1 = mn1 == neg_inf() ? 0.f : mn1;
+    const float ms0 = mn0 == neg_inf() ? 0.f : mn0, ms1 = mn1 == neg_inf() ? 0.f : mn1;      // nothing above -inf: avoid inf - inf
     const float al0 = fast_exp2(m2[0] - ms0), al1 = fast_exp2(m2[1] - ms1);      // of what came before
-    const float be0 = fast_exp2(mx0 - ms0), be1 = fast_exp2(mx1 - ms1);          // of this page
+    const float be0 = fast_exp2(mp0 - ms0), be1 = fast_exp2(mp1 - ms1);          // of these pages
     m2[0] = mn0; m2[1] = mn1;
-    l[0] = fmaf(l[0], al0, (p0 + p2) * be0);      // Z from the unrounded weights
-    l[1] = fmaf(l[1], al1, (p1 + p3) * be1);
-    // ---- P^T as the B operand, hi and lo
-    const float w0 = p0 * kWeightScale, w1 = p1 * kWeightScale, w2 = p2 * kWeightScale, w3 = p3 * kWeightScale;
-    uint32_t h0 = pack_f16(w0, w1), h1 = pack_f16(w2, w3);
-    float f0, f1, f2, f3;
-    unpack_f16(h0, f0, f1);
-    unpack_f16(h1, f2, f3);
-    const uint32_t e0 = pack_f16(w0 - f0, w1 - f1), e1 = pack_f16(w2 - f2, w3 - f3);
-    uint32_t bl0 = 0u, bl1 = 0u;
-    if (FOLD) {
-        if (t >= 2) { h0 = e0; h1 = e1; }      // columns 4..7 repeat the heads of 0..3
-    } else {
-        bl0 = movmatrix_trans(e0);
-        bl1 = movmatrix_trans(e1);
-    }
-    const uint32_t bh0 = movmatrix_trans(h0), bh1 = movmatrix_trans(h1);
+    l[0] = fmaf(l[0], al0, ((w[0][0] + w[0][2]) + (w[1][0] + w[1][2])) * be0);      // Z from the unrounded weights
+    l[1] = fmaf(l[1], al1, ((w[0][1] + w[0][3]) + (w[1][1] + w[1][3])) * be1);
     if (__any_sync(0xffffffffu, (al0 != 1.f) || (al1 != 1.f))) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            acc[i][0] *= al0; acc[i][1] *= al1; acc[i][2] *= al0; acc[i][3] *= al1;
+            mul_two(acc[i][0], acc[i][1], al0, al1);
+            mul_two(acc[i][2], acc[i][3], al0, al1);
         }
     }
-    // ---- O^T[d, head] += factor * (V^T P^T)
-    const float vb0 = be0 * (1.f / kWeightScale) * vs, vb1 = be1 * (1.f / kWeightScale) * vs;
+    // ---- O^T[d, head] += factor * (V^T P^T), P^T as the B operand, hi and lo
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        uint32_t a[4];
-        halves_of<KV, true>(vr[i >> 1][2 * (i & 1)], a[0], a[1]);
-        halves_of<KV, true>(vr[i >> 1][2 * (i & 1) + 1], a[2], a[3]);
-        float d[4] = {0.f, 0.f, 0.f, 0.f};
-        mma_f16(d, a, bh0, bh1);
-        if (!FOLD) mma_f16(d, a, bl0, bl1);
-        acc[i][0] = fmaf(d[0], vb0, acc[i][0]); acc[i][1] = fmaf(d[1], vb1, acc[i][1]);
-        acc[i][2] = fmaf(d[2], vb0, acc[i][2]); acc[i][3] = fmaf(d[3], vb1, acc[i][3]);
+    for (int p = 0; p < 2; ++p) {
+        uint32_t h0 = pack_f16(w[p][0], w[p][1]), h1 = pack_f16(w[p][2], w[p][3]);
+        float r0, r1, r2, r3;
+        unpack_f16(h0, r0, r1);
+        unpack_f16(h1, r2, r3);
+        const uint32_t e0 = pack_f16(w[p][0] - r0, w[p][1] - r1), e1 = pack_f16(w[p][2] - r2, w[p][3] - r3);
+        uint32_t bl0 = 0u, bl1 = 0u;
+        if (FOLD) {
+            if (t >= 2) { h0 = e0; h1 = e1; }      // columns 4..7 repeat the heads of 0..3
+        } else {
+            bl0 = movmatrix_trans(e0);
+            bl1 = movmatrix_trans(e1);
+        }
+        const uint32_t bh0 = movmatrix_trans(h0), bh1 = movmatrix_trans(h1);
+        const float vb0 = be0 * vs[p], vb1 = be1 * vs[p];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t a[4];
+            halves_of<KV, true>(vr[p][i >> 1][2 * (i & 1)], a[0], a[1]);
+            halves_of<KV, true>(vr[p][i >> 1][2 * (i & 1) + 1], a[2], a[3]);
+            float d[4];
+            mma_f16_fresh(d, a, bh0, bh1);
+            if (!FOLD) mma_f16(d, a, bl0, bl1);
+            fma_two(acc[i][0], acc[i][1], d[0], d[1], vb0, vb1);
+            fma_two(acc[i][2], acc[i][3], d[2], d[3], vb0, vb1);
+        }
     }
 }
 

@@ -44,11 +44,14 @@
 namespace qf {
 
 constexpr int kConsumerWarps = 8;
-constexpr int kPagesPerStage = kConsumerWarps;    // pages (of one KV head) per ring stage, one per consumer warp
 constexpr int kConsumerThreads = kConsumerWarps * 32;
-constexpr int kSweepThreads  = (kConsumerWarps + 1) * 32;
-// How much of K and V is in flight per SM: 3 stages of 64 KB, or, for a scaled cache, 5 of 32 KB.
-template <int KV> constexpr int kStages = KV == kKvBf16 ? 3 : 5;
+// Pages (of one KV head) per ring stage, a stage unit: one per consumer warp, or, for a scaled cache, two, of half the bytes.
+template <int KV> constexpr int kPagesPerStage = KV == kKvBf16 ? kConsumerWarps : 2 * kConsumerWarps;
+// A scaled cache's pages are half as long, so there are twice as many copies per byte, and one thread cannot issue them fast
+// enough: one more warp issues the copies of K, one those of V, from the places that the producer leaves in shared memory.
+template <int KV> constexpr int kIssuers = KV == kKvBf16 ? 0 : 2;
+template <int KV> constexpr int kSweepThreads = (kConsumerWarps + 1 + kIssuers<KV>) * 32;
+constexpr int kStages        = 3;                 // 3 x 64 KB of K and V in flight per SM
 template <int KV> constexpr int kPageBlockBytes = KV == kKvBf16 ? kPageBytes : kScaledPageBytes;
 constexpr int kMaxSweepCtas  = 160;               // persistent CTAs (one per SM) are capped at this
 constexpr int kHalfTileBytes = 2048;              // 16 rows x 64 channels of bf16
@@ -98,8 +101,9 @@ inline WorkspaceLayout workspace_layout(int batch, int max_shards, int num_kv_he
     return L;
 }
 
-// Work units of entry e = (request, shard), all KV heads together: stage units of kPagesPerStage pages
+// Work units of entry e = (request, shard), all KV heads together: stage units of kPagesPerStage<KV> pages
 // per KV head.
+template <int KV>
 __device__ __forceinline__ int entry_units(const int *__restrict__ seq_lens, const int *__restrict__ shard_ranges,
                                            int e, int max_shards, int num_kv_heads, int max_tokens)
 {
@@ -107,7 +111,7 @@ __device__ __forceinline__ int entry_units(const int *__restrict__ seq_lens, con
     clamp_range(shard_ranges[2 * e], shard_ranges[2 * e + 1], seq_lens[e / max_shards], max_tokens, beg, end);
     if (end <= beg) return 0;
     const int npages = ((end - 1) >> 4) - (beg >> 4) + 1;
-    return ((npages + kPagesPerStage - 1) / kPagesPerStage) * num_kv_heads;
+    return ((npages + kPagesPerStage<KV> - 1) / kPagesPerStage<KV>) * num_kv_heads;
 }
 
 // The stage-unit space [0, total) is cut into pieces, each swept by one CTA front to back.  Pieces
@@ -186,7 +190,8 @@ __host__ __device__ __forceinline__ void piece_range(const PieceGrid &g, int n_c
 
 // ------------------------------------------------------------------ plan kernel (large batches only)
 // prefix[e] = number of stage units before entry e = b*S + s, left in scratch.
-static __global__ void __launch_bounds__(1024)
+template <int KV>
+__global__ void __launch_bounds__(1024)
 plan_kernel(const int *__restrict__ seq_lens, const int *__restrict__ shard_ranges, int *__restrict__ prefix,
             int n_entries, int max_shards, int num_kv_heads, int max_tokens)
 {
@@ -195,7 +200,7 @@ plan_kernel(const int *__restrict__ seq_lens, const int *__restrict__ shard_rang
     int carry = 0;
     for (int base = 0; base < n_entries; base += 1024) {
         const int e = base + tid;
-        const int cnt = (e < n_entries) ? entry_units(seq_lens, shard_ranges, e, max_shards, num_kv_heads, max_tokens) : 0;
+        const int cnt = (e < n_entries) ? entry_units<KV>(seq_lens, shard_ranges, e, max_shards, num_kv_heads, max_tokens) : 0;
         int x = cnt;  // inclusive scan within the warp
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
@@ -222,11 +227,11 @@ struct __align__(16) StageMeta {
     int entry;     // b*S + s; -1 = no more work
     int kv_head;
     int page0;     // first logical page of this stage
-    int npages;    // 1..8
+    int npages;    // 1..8 (16: scaled)
     int tok_beg;   // clamped shard range
     int tok_end;
     int flags;     // bit0 first stage of a segment, bit1 last stage; bits 8..: segments the unit is cut into
-    int aux;       // bits 0..7: pages whose table entry was out of range
+    int aux;       // bits 0..7 (15: scaled): pages whose table entry was out of range
     int slot;      // this segment's slot: the unit's first slot + the segment's ordinal (used when the unit is cut)
     int pad[3];
 };
@@ -236,25 +241,27 @@ template <int G, int KV>
 struct SweepSmem {
     // every K/V half tile is a 1024-byte-aligned 128B-swizzled TMA destination
     // [stage][K|V][page][half][row][128B]; codes of a scaled cache: [stage][K|V][page][row][128B]
-    static constexpr int kRing = kStages<KV>;
-    alignas(1024) uint8_t kv[kRing][2][kPagesPerStage][kPageBlockBytes<KV>];
-    alignas(16) uint16_t q[kRing][G * kHeadDim];
+    alignas(1024) uint8_t kv[kStages][2][kPagesPerStage<KV>][kPageBlockBytes<KV>];
+    alignas(16) uint16_t q[kStages][G * kHeadDim];
     static constexpr int kRoundHeads = G < 4 ? G : 4;  // heads merged per epilogue round
     alignas(16) float red_acc[kConsumerWarps][kRoundHeads][kRedStride];
     alignas(16) float red_ml[kConsumerWarps][G][2];
-    alignas(16) StageMeta meta[kRing];
-    alignas(8) unsigned long long full_bar[kRing];
-    alignas(8) unsigned long long empty_bar[kRing];
-    float scales[kRing][2][kPagesPerStage];      // of a scaled cache's pages
+    alignas(16) StageMeta meta[kStages];
+    alignas(8) unsigned long long full_bar[kStages];
+    alignas(8) unsigned long long empty_bar[kStages];
+    // of a scaled cache's pages: scales, and where the issuing warps find them
+    alignas(16) float scales[kStages][2][kPagesPerStage<KV>];
+    alignas(16) int at[kStages][kPagesPerStage<KV>];
+    alignas(8) unsigned long long issue_bar[kStages];
     alignas(8) unsigned long long red_bar[2];
     int abort_flag;
     unsigned long long epoch;   // this launch's epoch, read once per CTA
-    int scan_ws[kConsumerWarps + 1];
+    int scan_ws[kSweepThreads<KV> / 32];
     int prefix[kMaxSmemEntries + 1];
 };
 
 template <int G, int KV>
-__global__ void __launch_bounds__(kSweepThreads, 1)
+__global__ void __launch_bounds__(kSweepThreads<KV>, 1)
 sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
              const uint16_t *__restrict__ q, const int *__restrict__ block_table,
              const int *__restrict__ seq_lens, const int *__restrict__ shard_ranges,
@@ -263,7 +270,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
              int4 *__restrict__ piece_info, float *__restrict__ seg, int seg_stride,
              unsigned long long host_epoch, const float *__restrict__ k_scale, const float *__restrict__ v_scale, DevParams P)
 {
-    constexpr int kRing = kStages<KV>;
+    constexpr int kPages = kPagesPerStage<KV>;
     extern __shared__ uint8_t smem_raw[];
     SweepSmem<G, KV> &sm = *reinterpret_cast<SweepSmem<G, KV> *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -275,10 +282,11 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
     volatile int *abort_flag = &sm.abort_flag;
 
     if (tid == 0) {
-        for (int s = 0; s < kRing; ++s) {
+        for (int s = 0; s < kStages; ++s) {
             // one arrival with the bytes to expect and, for a scaled cache, one per lane once its scale has landed
             mbar_init(smem_u32(&sm.full_bar[s]), KV == kKvBf16 ? 1 : 33);
             mbar_init(smem_u32(&sm.empty_bar[s]), kConsumerWarps);
+            if (KV != kKvBf16) mbar_init(smem_u32(&sm.issue_bar[s]), 1);
         }
         mbar_init(smem_u32(&sm.red_bar[0]), kConsumerWarps);
         mbar_init(smem_u32(&sm.red_bar[1]), kConsumerWarps);
@@ -304,7 +312,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         for (int base = 0; base < n_entries; base += kConsumerThreads) {
             const int e = base + tid;
             const int cnt = (tid < kConsumerThreads && e < n_entries)
-                                ? entry_units(seq_lens, shard_ranges, e, S, Hkv, max_tokens) : 0;
+                                ? entry_units<KV>(seq_lens, shard_ranges, e, S, Hkv, max_tokens) : 0;
             int x = cnt;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
@@ -331,7 +339,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
     const unsigned long long epoch = sm.epoch;   // written before the plan's barriers
     if (P.check_bounds && blockIdx.x == 0) {
         // a cached length that the request's block-table row cannot address was clamped by the plan: report it
-        for (int b = tid; b < P.batch; b += kSweepThreads)
+        for (int b = tid; b < P.batch; b += kSweepThreads<KV>)
             if (seq_lens[b] > max_tokens) epoch_or(header + kHdrStatus, epoch, kStatusBadPage);
     }
     const int total = prefix[n_entries];
@@ -421,9 +429,9 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                 // table entries are fetched 32 pages at a time
                 int tbl_page0 = 0, tbl = 0;
                 for (int u = 0; ok && u < seg_len; ++u) {
-                    const int page0 = first_page + (j + u) * kPagesPerStage;
-                    const int np = min(kPagesPerStage, last_page + 1 - page0);
-                    if ((u & (32 / kPagesPerStage - 1)) == 0) {
+                    const int page0 = first_page + (j + u) * kPages;
+                    const int np = min(kPages, last_page + 1 - page0);
+                    if ((u & (32 / kPages - 1)) == 0) {
                         tbl_page0 = page0;
                         if (j + u == 0 && head_tbl_e == e) {
                             tbl = head_tbl;           // the shard's first pages: same for every KV head
@@ -439,12 +447,12 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                         nxt_tbl = load_tbl(nxt_e / S, nb >> 4, (ne - 1) >> 4);
                         nxt_tbl_e = nxt_e;
                     }
-                    const int i = lane % kPagesPerStage;    // page within the stage
-                    const int part = lane / kPagesPerStage; // 0: K page, 1: V page (>= 2: idle lane)
+                    const int i = lane % kPages;    // page within the stage
+                    const int part = lane / kPages; // 0: K page, 1: V page (>= 2: idle lane)
                     int phys = __shfl_sync(0xffffffffu, tbl, (page0 - tbl_page0) + i);
                     bool bad = false;
                     if ((KV != kKvBf16 || P.check_bounds) && (phys < 0 || (long long)phys >= P.num_pages)) { bad = true; phys = 0; }
-                    const unsigned bad_mask = __ballot_sync(0xffffffffu, bad && i < np && part == 0) & 0xffu;
+                    const unsigned bad_mask = __ballot_sync(0xffffffffu, bad && i < np && part == 0) & ((1u << kPages) - 1);
                     const bool issuer = (i < np) && (part < 2);
 
                     if (pg.n_chunks > 0 && pos + u == draw_at && lane == 0) drawn = atomicAdd(header + kHdrChunk, 1ull);
@@ -464,26 +472,12 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                     }
                     __syncwarp();
                     if constexpr (KV != kKvBf16) {
-                        // scales: lanes 0..7 of the K pages, 8..15 of the V pages
-                        if (part < 2)
-                            copy_async_4(smem_u32(&sm.scales[stage][part][i]), (part ? v_scale : k_scale) + (size_t)phys * Hkv + c, i < np);
+                        // scales: lanes 0..15 of the K pages, 16..31 of the V pages; 0 for a page that is not there
+                        copy_async_4(smem_u32(&sm.scales[stage][part][i]), (part ? v_scale : k_scale) + (size_t)phys * Hkv + c, i < np && !bad);
                         arrive_after_copies(full);
-                        // codes: one thread issues every copy, with operands that are the same for the warp (a lane per page makes
-                        // each copy a turn of a loop over lanes, and here there are twice as many copies per byte)
-                        const int at0 = P.kv_nhd ? phys * kPageSize : (phys * Hkv + c) * kPageSize;
-                        int at[kPagesPerStage];
-#pragma unroll
-                        for (int k = 0; k < kPagesPerStage; ++k) at[k] = __shfl_sync(0xffffffffu, at0, k);
-                        if (elect_one()) {
-                            const uint32_t dst = smem_u32(&sm.kv[stage][0][0][0]);
-#pragma unroll
-                            for (int k = 0; k < kPagesPerStage; ++k) {
-                                if (k >= np) break;
-                                const int y = P.kv_nhd ? c : at[k], z = P.kv_nhd ? at[k] : 0;
-                                tma_load_page_scaled(dst + k * kScaledPageBytes, &k_map, y, z, full, kv_policy);
-                                tma_load_page_scaled(dst + (kPagesPerStage + k) * kScaledPageBytes, &v_map, y, z, full, kv_policy);
-                            }
-                        }
+                        if (lane < kPages) sm.at[stage][lane] = P.kv_nhd ? phys * kPageSize : phys * Hkv + c;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&sm.issue_bar[stage]));
                         __syncwarp();
                     } else if (issuer) {
                         const uint32_t dst = smem_u32(&sm.kv[stage][part][i][0]);
@@ -496,7 +490,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                         bulk_load_1d(smem_u32(&sm.q[stage][0]), q + ((size_t)b * Hq + (size_t)c * G) * kHeadDim,
                                      (uint32_t)G * 256u, full);
                     ++issued;
-                    if (++stage == kRing) { stage = 0; phase ^= 1; }
+                    if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
                 pos += seg_len;
             }
@@ -523,6 +517,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                 if (KV != kKvBf16) {
                     __syncwarp();
                     mbar_arrive(smem_u32(&sm.full_bar[stage]));      // as every lane does for its scale
+                    if (lane == 0) mbar_arrive(smem_u32(&sm.issue_bar[stage]));
                 }
             } else ok = false;
         }
@@ -532,13 +527,40 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             __syncwarp();
             int s2 = stage;
             uint32_t ph2 = phase;
-            for (int k = 0; k < min(issued, kRing); ++k) {
-                if (--s2 < 0) { s2 = kRing - 1; ph2 ^= 1; }
+            for (int k = 0; k < min(issued, kStages); ++k) {
+                if (--s2 < 0) { s2 = kStages - 1; ph2 ^= 1; }
                 for (unsigned it = 0; it < (1u << 20); ++it)
                     if (mbar_try_wait(smem_u32(&sm.full_bar[s2]), ph2)) break;
             }
         }
         return;
+    }
+
+    if constexpr (kIssuers<KV> > 0) {
+        if (warp > kConsumerWarps) {
+            // ============================ issuing warps (scaled cache) ============================
+            const int part = warp - kConsumerWarps - 1;      // 0: K, 1: V
+            const CUtensorMap *map = part ? &v_map : &k_map;
+            const unsigned long long kv_policy = l2_evict_first_policy();
+            for (int stage = 0, phase = 0;;) {
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.issue_bar[stage]), (uint32_t)phase, abort_flag))) break;
+                if (sm.meta[stage].entry < 0) break;
+                if (elect_one()) {      // one thread, with operands that are the same for the warp
+                    const int np = sm.meta[stage].npages, y = P.kv_nhd ? sm.meta[stage].kv_head : 0;
+                    const uint32_t full = smem_u32(&sm.full_bar[stage]), dst = smem_u32(&sm.kv[stage][part][0][0]);
+                    int4 a[kPages / 4];
+#pragma unroll
+                    for (int k = 0; k < kPages / 4; ++k) a[k] = *reinterpret_cast<const int4 *>(&sm.at[stage][4 * k]);
+#pragma unroll
+                    for (int k = 0; k < kPages; ++k)
+                        if (k < np)
+                            tma_load_page_scaled(dst + k * kScaledPageBytes, map, y, (k & 3) == 0 ? a[k / 4].x : (k & 3) == 1 ? a[k / 4].y : (k & 3) == 2 ? a[k / 4].z : a[k / 4].w, full, kv_policy);
+                }
+                __syncwarp();
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+            return;
+        }
     }
 
     // ================================ consumer warps ================================
@@ -564,7 +586,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
     float acc[8][4];
     int stage = 0;
     uint32_t phase = 0, red_phase0 = 0, red_phase1 = 0;
-    const int wp = warp;  // this warp's page within a stage
+    const int wp = KV == kKvBf16 ? warp : 2 * warp;  // this warp's (first) page within a stage
 
     // every consumer warp waits on the warp-merge barriers through this; false = abort
     auto red_sync = [&](int which, uint32_t &ph) -> bool {
@@ -606,17 +628,25 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         }
 
         if (wp < mt.npages) {
-            const int tok0 = (mt.page0 + wp) << 4;
-            int tlo = max(mt.tok_beg - tok0, 0), thi = min(mt.tok_end - tok0, kPageSize);
-            if ((mt.aux >> wp) & 1) { tlo = 0; thi = 0; }
-            const bool ragged = (tlo > 0) || (thi < kPageSize);
             const uint32_t k_base = smem_u32(&sm.kv[stage][0][wp][0]);
             const uint32_t v_base = smem_u32(&sm.kv[stage][1][wp][0]);
-
+            const int tok0 = (mt.page0 + wp) << 4;
+            bool ragged;
             if constexpr (KV != kKvBf16) {
-                if (tlo < thi)      // a page that is skipped has no scale either
-                    process_page_scaled<KV, (G <= 4)>(k_base, v_base, sm.scales[stage][0][wp], sm.scales[stage][1][wp], tlo, thi, ragged, qf, qs, m2, l, acc, lane);
+                int tlo[2], thi[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    tlo[k] = max(mt.tok_beg - tok0 - 16 * k, 0);
+                    thi[k] = ((mt.aux >> (wp + k)) & 1) ? 0 : min(mt.tok_end - tok0 - 16 * k, kPageSize);
+                }
+                ragged = tlo[0] > 0 || thi[0] < kPageSize || thi[1] < kPageSize;
+                const float2 ks2 = *reinterpret_cast<const float2 *>(&sm.scales[stage][0][wp]), vs2 = *reinterpret_cast<const float2 *>(&sm.scales[stage][1][wp]);
+                const float ks[2] = {ks2.x, ks2.y}, vs[2] = {vs2.x, vs2.y};
+                process_pages_scaled<KV, (G <= 4)>(k_base, v_base, ks, vs, tlo, thi, ragged, qf, qs, m2, l, acc, lane);
             } else {
+                int tlo = max(mt.tok_beg - tok0, 0), thi = min(mt.tok_end - tok0, kPageSize);
+                if ((mt.aux >> wp) & 1) { tlo = 0; thi = 0; }
+                ragged = (tlo > 0) || (thi < kPageSize);
                 process_page(k_base, v_base, kHalfTileBytes, tlo, thi, ragged, qf, m2, l, acc, scale2, lane);
             }
             if (ragged) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -695,7 +725,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                 if (!red_sync(1, red_phase1)) return;
             }
         }
-        if (++stage == kRing) { stage = 0; phase ^= 1; }
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
     }
 }
 
@@ -723,8 +753,8 @@ inline EncodeTiledFn encode_tiled(char *msg, size_t msg_len)
     return encode;
 }
 
-// A pool of codes as [., rows, 128 B] in boxes of one (page, KV head) block: 16 neighbouring rows (head-major) or 16 token rows of
-// one head, Hkv rows apart (token-major).  swizzled: 128B swizzle, else rows as they are.  Encoded for every call (under a
+// A pool of codes in boxes of one (page, KV head) block of 16 rows: [block, row, 128 B] (head-major), or [token row, head, 128 B],
+// 16 rows of one head (token-major).  Either way the outermost coordinate says which page.  swizzled: 128B swizzle, else rows as they are.  Encoded for every call (under a
 // microsecond), so nothing is remembered about a pointer.
 inline int make_scaled_map(CUtensorMap *out, const void *pool, long long num_pages, int num_kv_heads, bool nhd, bool swizzled,
                            char *msg, size_t msg_len)
@@ -732,8 +762,8 @@ inline int make_scaled_map(CUtensorMap *out, const void *pool, long long num_pag
     EncodeTiledFn encode = encode_tiled(msg, msg_len);
     if (!encode) return -1;
     const cuuint64_t hkv = (cuuint64_t)num_kv_heads, rows = (cuuint64_t)num_pages * kPageSize;
-    const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, nhd ? hkv : rows * hkv, nhd ? rows : 1};
-    const cuuint64_t strides[2] = {(cuuint64_t)kHeadDim, (nhd ? hkv : rows * hkv) * kHeadDim};
+    const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, nhd ? hkv : (cuuint64_t)kPageSize, nhd ? rows : (cuuint64_t)num_pages * hkv};
+    const cuuint64_t strides[2] = {(cuuint64_t)kHeadDim, (nhd ? hkv : (cuuint64_t)kPageSize) * kHeadDim};
     const cuuint32_t box[3] = {(cuuint32_t)kHeadDim, nhd ? 1u : (cuuint32_t)kPageSize, nhd ? (cuuint32_t)kPageSize : 1u}, ones[3] = {1, 1, 1};
     const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(pool), dims, strides, box, ones,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
@@ -833,14 +863,14 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const float
     *launches = 0;
     const int *global_prefix = nullptr;
     if (n_entries > kMaxSmemEntries) {
-        plan_kernel<<<1, 1024, 0, st>>>(sl, sr, prefix, n_entries, P.max_shards, P.num_kv_heads, P.max_tokens);
+        plan_kernel<KV><<<1, 1024, 0, st>>>(sl, sr, prefix, n_entries, P.max_shards, P.num_kv_heads, P.max_tokens);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) { snprintf(msg, msg_len, "plan_kernel launch: %s", cudaGetErrorString(e)); return -5; }
         global_prefix = prefix;
         *launches += 1;
     }
     if (ev0) cudaEventRecord(ev0, st);
-    cudaError_t e = launch_pdl(sweep_kernel<G, KV>, dim3(n_ctas), dim3(kSweepThreads), smem, st, kmap, vmap,
+    cudaError_t e = launch_pdl(sweep_kernel<G, KV>, dim3(n_ctas), dim3(kSweepThreads<KV>), smem, st, kmap, vmap,
                                (const uint16_t *)q, bt, sl, sr, o, m, l, header, global_prefix, piece_info, seg,
                                wsl.seg_stride, epoch, k_scale, v_scale, P);
     if (ev1) cudaEventRecord(ev1, st);

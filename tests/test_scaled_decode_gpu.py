@@ -108,9 +108,11 @@ def test_long_and_many(kind, hq, hkv, batch, n, S):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-def test_more_pairs_than_the_sweep_plans_by_itself(kind):
-    pg = Scaled([0] * 300, np.arange(300) % 67, 1, kind, seed=8)
-    check(pg, 4, 8)
+@pytest.mark.parametrize("batch,S", [(32, 9), (255, 1), (257, 1), (300, 5), (64, 32), (300, 8)])
+def test_many_pairs_of_requests_and_shards(kind, batch, S):
+    """Fewer than the sweep's threads scan at once, several rounds of them, and (2,400) more than it plans by itself."""
+    pg = Scaled([0] * batch, 1 + np.arange(batch) * 7 % 167, 1, kind, seed=8)
+    check(pg, 4, S)
 
 
 @pytest.mark.parametrize("kind", KINDS)
