@@ -105,7 +105,7 @@ merge_small_kernel(const int *__restrict__ seq_lens, const int *__restrict__ sha
         int nseg = 0, first = 0;
         if (nunits > 0) {
             const int p0 = pos + c * nunits;
-            const int fp = piece_of(pg, n_sweep_ctas, p0), lp = piece_of(pg, n_sweep_ctas, p0 + nunits - 1);
+            const int fp = piece_of(pg, n_sweep_ctas, p0 + kSegmentCost<KV>), lp = piece_of(pg, n_sweep_ctas, p0 + nunits - 1);
             nseg = lp - fp + 1;
             first = (b * S + d) * Hkv + c + fp;
             if (nseg > 1 && (first < 0 || (long long)first + nseg > (long long)seg_slots)) nseg = 0;   // cannot happen; never leave the scratch

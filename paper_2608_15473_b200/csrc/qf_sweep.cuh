@@ -75,6 +75,11 @@ constexpr int kMaxDynChunks     = kDynRounds * kMaxSweepCtas;   // bounds the se
 constexpr int kDynMinUnitsPerCta = 112;               // shorter sweeps (under ~150 us) stay fully static: measured break-even
 static_assert(kMaxSweepCtas + kMaxDynChunks < (1 << kEpochShift), "segments of one unit must fit the arrival count");
 
+// What the end of a shard's head costs (warps meet, states merge), in stage units: such a range takes this many places of the
+// unit axis before its stages.  For a scaled cache it is about a stage's 2,300 cycles, so that slices full of short shards would
+// last half as long again as the others (32 ragged requests in 9 shards: 286 us without it).  The bf16 schedule has none.
+template <int KV> constexpr int kSegmentCost = KV == kKvBf16 ? 0 : 1;
+
 struct WorkspaceLayout {
     size_t header_off, prefix_off, counter_off, piece_off, seg_off, total;
     size_t seg_slots;
@@ -111,7 +116,7 @@ __device__ __forceinline__ int entry_units(const int *__restrict__ seq_lens, con
     clamp_range(shard_ranges[2 * e], shard_ranges[2 * e + 1], seq_lens[e / max_shards], max_tokens, beg, end);
     if (end <= beg) return 0;
     const int npages = ((end - 1) >> 4) - (beg >> 4) + 1;
-    return ((npages + kPagesPerStage<KV> - 1) / kPagesPerStage<KV>) * num_kv_heads;
+    return ((npages + kPagesPerStage<KV> - 1) / kPagesPerStage<KV> + kSegmentCost<KV>) * num_kv_heads;
 }
 
 // The stage-unit space [0, total) is cut into pieces, each swept by one CTA front to back.  Pieces
@@ -397,8 +402,15 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                 const int base = prefix[e];
                 const int nunits = (prefix[e + 1] - base) / Hkv;
                 const int r = pos - base;
-                const int c = r / nunits, j = r - c * nunits;
-                const int seg_len = min(nunits - j, pos1 - pos);
+                const int c = r / nunits, at_unit = r - c * nunits;
+                if (kSegmentCost<KV> > 0 && at_unit < kSegmentCost<KV>) {      // the range's cost: nothing is there
+                    if (pos == piece_pos0 && lane == 0) piece_info[piece] = make_int4(-1, 0, 0, (int)(unsigned)epoch);
+                    if (pg.n_chunks > 0 && pos == draw_at && lane == 0) drawn = atomicAdd(header + kHdrChunk, 1ull);
+                    ++pos;
+                    continue;
+                }
+                const int j = at_unit - kSegmentCost<KV>;      // stage
+                const int seg_len = min(nunits - at_unit, pos1 - pos);
                 const int b = e / S;
                 if (e != cur_e) {
                     if (e == nxt_e) clamp_range(nxt_r0, nxt_r1, nxt_len, max_tokens, beg, end);
@@ -420,7 +432,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                 // the pieces that touch this unit: one segment each, slot = unit + piece (both increase along
                 // the unit space, so no two segments share a slot)
                 const int p0 = base + c * nunits;
-                const int first_piece = piece_of(pg, n_ctas, p0), last_piece = piece_of(pg, n_ctas, p0 + nunits - 1);
+                const int first_piece = piece_of(pg, n_ctas, p0 + kSegmentCost<KV>), last_piece = piece_of(pg, n_ctas, p0 + nunits - 1);
                 const int nseg = last_piece - first_piece + 1;
                 const int first_slot = e * Hkv + c + first_piece;
                 if (pos == piece_pos0 && lane == 0)   // does this piece start inside a unit?  (the finish kernel's input)
