@@ -41,8 +41,8 @@ int launch_rows(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *
     qf::RowsMaps maps;
     size_t len;
     char *msg = qf_host::cuda_msg(&len);
-    if (qf::make_rows_maps(&maps, A, P, msg, len)) return QF_ERR_CUDA;
-    cudaError_t e = qf::launch_rows_kernels<PREFIX>(maps, A, P, ws, sms, st);
+    if (qf::make_rows_maps(&maps, A, P, false, msg, len)) return QF_ERR_CUDA;
+    cudaError_t e = qf::launch_rows_kernels<PREFIX, qf::kKvBf16>(maps, A, P, ws, sms, st);
     if (e != cudaSuccess) return qf_host::cuda_fail(e, "rows_kernel launch");
     qf_host::set_launches(2);
     return QF_OK;

@@ -54,16 +54,21 @@
 
 #include "qf_common.cuh"
 #include "qf_page_math.cuh"
+#include "qf_page_scaled.cuh"
 #include "qf_proj.cuh"
 #include "qf_rows_simple.cuh"
+#include "qf_tensor_map.h"
 
 namespace qf {
 
 constexpr int kRowTile = 128;                    // query rows of a tile, and cached positions of a tile
 constexpr int kTilePages = kRowTile / kPageSize;
 constexpr int kUnit = 64;                        // positions of one product S = Q K^T and of one softmax pass
-constexpr int kRowsThreads = 12 * 32;
-constexpr int kRowsRing = 5;                     // K and V tiles in flight or in use
+// A scaled cache has four more warps, which expand tiles of codes to bf16 on their way into the ring, and two tiles of codes in
+// flight in the place of one in the ring.
+template <int KV> constexpr int kRowsThreads = (KV == kKvBf16 ? 12 : 16) * 32;
+template <int KV> constexpr int kRowsRing = KV == kKvBf16 ? 5 : 4;      // K and V tiles in flight or in use
+constexpr int kRawTiles = 2;
 constexpr int kTileBytes = kRowTile * kHeadDim * 2;
 constexpr int kHalfPageBytes = kPageBytes / 2;    // 16 rows x 64 channels
 constexpr int kInfoRing = 4;
@@ -330,12 +335,12 @@ __device__ __forceinline__ void pin32(float *v)
         asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7]));
 }
 // A bounded wait of a whole warp: every lane leaves with the same answer.  The loop is a function of its own.
-__device__ QF_COLD bool warp_wait_loop(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+static __device__ QF_COLD bool warp_wait_loop(uint32_t bar, uint32_t parity, volatile int *abort_flag)
 {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
 // The same for one thread.
-__device__ QF_COLD bool wait_loop(uint32_t bar, uint32_t parity, volatile int *abort_flag) { return mbar_wait(bar, parity, abort_flag); }
+static __device__ QF_COLD bool wait_loop(uint32_t bar, uint32_t parity, volatile int *abort_flag) { return mbar_wait(bar, parity, abort_flag); }
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
 {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
@@ -422,27 +427,37 @@ __device__ __forceinline__ int unit_end(const RowsBlock &b, int w, int tile_rows
     const int lim = PREFIX ? b.len : min(b.off + b.i0 + last, b.len);
     return min(2 * b.t_hi, (lim + kUnit - 1) / kUnit);
 }
+// Tiles of codes: [page][16 rows][128 B], their pages' scales, and what they are (0: K, 1: V, -1: there is no more).
+template <int KV> struct RowsRaw {
+    alignas(128) uint8_t codes[kRawTiles][kTileBytes / 2];
+    alignas(16) float scales[kRawTiles][kTilePages];
+    alignas(8) unsigned long long full[kRawTiles], empty[kRawTiles];
+    int kind[kRawTiles];
+};
+template <> struct RowsRaw<kKvBf16> {};
+template <int KV>
 struct RowsSmem {
     alignas(1024) uint8_t q[2][kTileBytes];            // [row tile][channel half][128 rows][128 B]
-    alignas(1024) uint8_t kv[kRowsRing][kTileBytes];   // K: [half][128 positions][128 B]; V: [page][half][16][128 B]
+    alignas(1024) uint8_t kv[kRowsRing<KV>][kTileBytes];   // K: [half][128 positions][128 B]; V: [page][half][16][128 B]
     alignas(16) RowsBlock info[kInfoRing];
-    alignas(8) unsigned long long kv_full[kRowsRing], kv_empty[kRowsRing], q_full, q_empty, s_full[2][2], p_full[2][2], o_full[2], o_last[2],
+    alignas(8) unsigned long long kv_full[kRowsRing<KV>], kv_empty[kRowsRing<KV>], q_full, q_empty, s_full[2][2], p_full[2][2], o_full[2], o_last[2],
         info_full[kInfoRing], info_empty[kInfoRing], pair[2], drain[2];
     float2 ml[2][kRowTile];          // narrow blocks: each group's (maximum, sum) per row
     unsigned bad_pages[8];           // per position tile (by its running number): pages without a valid table entry
     int dirty[kInfoRing];            // a value the mask hides from some row of the block is not finite
     SlicePos cut[2];
-    long long scan[kRowsThreads / 32];
+    long long scan[kRowsThreads<KV> / 32];
     long long cut_rest[2];
     int cut_seq[2];
     uint32_t tmem_base;
     int abort_flag;
+    RowsRaw<KV> raw;
 };
-static_assert(sizeof(RowsSmem) <= 227 * 1024, "one CTA per SM");
+static_assert(sizeof(RowsSmem<kKvBf16>) <= 227 * 1024 && sizeof(RowsSmem<kKvE4m3>) <= 227 * 1024, "one CTA per SM");
 
 // A thread's row of an accumulator plus f times the part set aside (if any), into memory or back into tensor memory.
 // All 32 lanes call it together.
-__device__ QF_COLD void exchange_aside(uint32_t t_o, float *aside, bool has_aside, bool to_memory, float f)
+static __device__ QF_COLD void exchange_aside(uint32_t t_o, float *aside, bool has_aside, bool to_memory, float f)
 {
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
@@ -478,7 +493,8 @@ __device__ QF_COLD void exchange_aside(uint32_t t_o, float *aside, bool has_asid
 
 // The rare end of a block whose last tiles hold non-finite values (see clean_values): this thread's row, already
 // written, gets those it sees.  A weight is positive, so an infinity stays one and two of opposite signs make a NaN.
-__device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const RowsBlock &b, int lim, int c0, int c1,
+template <int KV>
+static __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const RowsBlock &b, int lim, int c0, int c1,
                                    float *slot_base, int slot_row, size_t out_row)
 {
     const int common = min(b.off + b.i0 + 1, b.len);
@@ -487,11 +503,19 @@ __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const 
         const long long at = (long long)b.seq * A.table_width + (pos >> 4);
         const long long phys = A.table ? (long long)A.table[at] : at;
         if (phys < 0 || phys >= P.num_pages) continue;
-        const uint16_t *v = reinterpret_cast<const uint16_t *>(A.v_cache) + kv_row_offset(P, phys, b.head, pos & 15);
+        const size_t at_row = kv_row_offset(P, phys, b.head, pos & 15);
 #pragma unroll 1
         for (int d = c0 * 32; d < c1 * 32; ++d) {
-            if ((v[d] & 0x7f80u) != 0x7f80u) continue;
-            const float x = __uint_as_float((uint32_t)v[d] << 16);
+            uint32_t bits;
+            if constexpr (KV == kKvBf16) {
+                bits = reinterpret_cast<const uint16_t *>(A.v_cache)[at_row + d];
+            } else {
+                const float4 four = load_channels<KV>(A.v_cache, at_row + (d & ~3));
+                const float code = (d & 3) == 0 ? four.x : (d & 3) == 1 ? four.y : (d & 3) == 2 ? four.z : four.w;
+                bits = pack_bf16(code * A.v_scale[phys * P.num_kv_heads + b.head], 0.f) & 0xffffu;
+            }
+            if ((bits & 0x7f80u) != 0x7f80u) continue;
+            const float x = __uint_as_float(bits << 16);
             if (b.slot >= 0) {
                 float *o = slot_base + ((size_t)(d >> 2) * (2 * kRowTile) + slot_row) * 4 + (d & 3);
                 __stcg(o, __ldcg(o) + x);
@@ -507,7 +531,7 @@ __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const 
 // be 0 or negative, and an infinity times that, or an accumulator's infinity times a factor that underflows, is NaN.  So the
 // warp searches the values of the stretch, and every row that is not NaN or empty itself gets what it sees, over what it
 // has written: NaN, or both infinities, make NaN, infinities of one sign make that infinity.
-__device__ QF_COLD void mend_infinite(const RowsArgs &A, const DevParams &P, const RowsBlock &b, bool mine, int c0, int c1,
+static __device__ QF_COLD void mend_infinite(const RowsArgs &A, const DevParams &P, const RowsBlock &b, bool mine, int c0, int c1,
                                       float *slot_base, int slot_row, size_t out_row)
 {
     const int lane = threadIdx.x & 31;
@@ -550,7 +574,7 @@ __device__ QF_COLD void mend_infinite(const RowsArgs &A, const DevParams &P, con
 
 // A tile of values in shared memory, by one warp: rows from `exist` on, as far as their page goes, become 0, and so do
 // non-finite values among rows seen_by_all .. used - 1 (from the page's start), which `dirty` then reports.
-__device__ QF_COLD void clean_tile(uint8_t *v, int exist, int seen_by_all, int used, volatile int *dirty)
+static __device__ QF_COLD void clean_tile(uint8_t *v, int exist, int seen_by_all, int used, volatile int *dirty)
 {
     const int lane = threadIdx.x & 31;
     if (exist & 15) {
@@ -594,20 +618,80 @@ __device__ QF_COLD void clean_tile(uint8_t *v, int exist, int seen_by_all, int u
 
 struct RowsMaps { CUtensorMap q, k, v; };
 
-template <bool PREFIX>
-__global__ void __launch_bounds__(kRowsThreads, 1)
+// Sixteen codes of one row -> sixteen bf16 numbers, code * scale (exact for a power of two, else rounded once), in two words of
+// eight channels; the words come in the order (swap, 1 - swap).
+template <int KV>
+__device__ __forceinline__ void expand_codes(uint4 codes, float scale, bool swap, uint4 &first, uint4 &second)
+{
+    const uint32_t in[4] = {swap ? codes.z : codes.x, swap ? codes.w : codes.y, swap ? codes.x : codes.z, swap ? codes.y : codes.w};
+    uint32_t out[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x[4];
+        if constexpr (KV == kKvE4m3) {
+            uint32_t lo, hi;
+            halves_of<KV, false>(in[i], lo, hi);
+            unpack_f16(lo, x[0], x[1]);
+            unpack_f16(hi, x[2], x[3]);
+        } else {
+            const uint32_t u = in[i] ^ 0x80808080u;      // code + 128 as the low mantissa byte of 2^23: the difference is exact
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650 + e)) - 8388736.f;
+        }
+        mul_two(x[0], x[1], scale, scale);
+        mul_two(x[2], x[3], scale, scale);
+        out[2 * i] = pack_bf16(x[0], x[1]);
+        out[2 * i + 1] = pack_bf16(x[2], x[3]);
+    }
+    first = make_uint4(out[0], out[1], out[2], out[3]);
+    second = make_uint4(out[4], out[5], out[6], out[7]);
+}
+__device__ __forceinline__ void st_shared_16(uint32_t addr, const uint4 &v)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// A quarter of a tile (two pages) by one warp.  raw: the quarter's codes; tile: the ring's slot.  Eight lanes share a row, sixteen
+// channels each; lanes of the upper half of the channels write their words in the other order, so that the eight words of a
+// row that are written together lie in eight different bank groups.
+template <int KV>
+__device__ __forceinline__ void expand_quarter(uint32_t raw, uint32_t tile, int quarter, bool is_v, float s0, float s1)
+{
+    const int lane = threadIdx.x & 31, c16 = lane & 7, half = c16 >> 2;
+    const int half_step = is_v ? kHalfPageBytes : kTileBytes / 2, page_step = is_v ? kPageBytes : kPageSize * 128;
+#pragma unroll 4
+    for (int it = 0; it < 8; ++it) {
+        const int row = 4 * (it & 3) + (lane >> 3);
+        const uint4 codes = ld_shared_16(raw + it * 512 + lane * 16);
+        uint4 a, b;
+        expand_codes<KV>(codes, it < 4 ? s0 : s1, half != 0, a, b);
+        const uint32_t at = tile + (2 * quarter + (it >> 2)) * page_step + half * half_step + row * 128;
+        const int ch = 2 * (c16 & 3);
+        st_shared_16(at + (((ch + half) ^ (row & 7)) << 4), a);
+        st_shared_16(at + (((ch + 1 - half) ^ (row & 7)) << 4), b);
+    }
+}
+
+template <bool PREFIX, int KV>
+__global__ void __launch_bounds__(kRowsThreads<KV>, 1)
 rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsArgs A, const __grid_constant__ DevParams P,
             RowsRecord *__restrict__ records, float *__restrict__ asides, float *__restrict__ slots)
 {
     extern __shared__ __align__(1024) uint8_t rows_smem[];
-    RowsSmem &sm = *reinterpret_cast<RowsSmem *>(rows_smem);
+    RowsSmem<KV> &sm = *reinterpret_cast<RowsSmem<KV> *>(rows_smem);
+    constexpr int kRing = kRowsRing<KV>, kThreads = kRowsThreads<KV>;
+    static_assert(!PREFIX || KV == kKvBf16, "prefixes are swept in bf16");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int Hq = P.num_q_heads, Hkv = P.num_kv_heads, G = P.group;
     const int tile_rows = kRowTile / G;               // tokens per row tile
     volatile int *abort_flag = &sm.abort_flag;
 
     if (tid == 0) {
-        for (int i = 0; i < kRowsRing; ++i) { mbar_init(smem_u32(&sm.kv_full[i]), 1); mbar_init(smem_u32(&sm.kv_empty[i]), 2); }
+        for (int i = 0; i < kRing; ++i) { mbar_init(smem_u32(&sm.kv_full[i]), KV == kKvBf16 ? 1 : 4); mbar_init(smem_u32(&sm.kv_empty[i]), 2); }
+        if constexpr (KV != kKvBf16)
+            for (int i = 0; i < kRawTiles; ++i) {
+                mbar_init(smem_u32(&sm.raw.full[i]), 33);      // the bytes, and every lane of the loading warp once its scale has landed
+                mbar_init(smem_u32(&sm.raw.empty[i]), 4);      // one per expanding warp
+            }
         mbar_init(smem_u32(&sm.q_full), 1);
         mbar_init(smem_u32(&sm.q_empty), 2);         // one per product warp
         for (int w = 0; w < 2; ++w) {
@@ -650,7 +734,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         auto empties = [&](int lo, int hi) {
             const long long n4 = (long long)max(hi - lo, 0) * Hq * (kHeadDim / 4);
 #pragma unroll 1
-            for (long long i = tid; i < n4; i += kRowsThreads) {
+            for (long long i = tid; i < n4; i += kThreads) {
                 const long long row = lo + i / (Hq * (kHeadDim / 4));
                 const int rest = (int)(i % (Hq * (kHeadDim / 4)));
                 const size_t o = ((size_t)row * A.out_shards + A.slot) * Hq;
@@ -669,13 +753,13 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
     }
 
     if (P.check_bounds)
-        for (int s = (int)blockIdx.x * kRowsThreads + tid; s < A.n_seq; s += (int)gridDim.x * kRowsThreads)
+        for (int s = (int)blockIdx.x * kThreads + tid; s < A.n_seq; s += (int)gridDim.x * kThreads)
             if (seq_overruns<PREFIX>(A, s)) rows_status_or(A.status, kStatusBadPage);
 
     // ---- this CTA's slice.  A thread adds up a sequence's blocks, or a warp does while there are no more sequences
     // than warps.
     const int n_ctas = (int)gridDim.x;
-    constexpr int kWarps = kRowsThreads / 32;
+    constexpr int kWarps = kThreads / 32;
     if (A.n_seq <= kWarps) {
         if (warp < A.n_seq) {
             const SeqPlan q = seq_plan(warp);
@@ -730,7 +814,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             }
         } else {
 #pragma unroll 1
-            for (int base = 0; base < A.n_seq; base += kRowsThreads) {
+            for (int base = 0; base < A.n_seq; base += kThreads) {
                 scan_round(base, before, cost);
                 if (pass) offer(base + tid);
             }
@@ -743,7 +827,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         ha = head_of(cut_at(total, n_eff, me), running, ra);
         hb = Hkv;
         if (me + 1 < n_eff) hb = head_of(cut_at(total, n_eff, me + 1), running, rb);
-        if (A.n_seq <= kRowsThreads) {
+        if (A.n_seq <= kThreads) {
             offer(tid);
             break;
         }
@@ -763,8 +847,38 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&sm.tmem_base);
     const uint32_t t_s0 = tmem, t_o0 = tmem + 256;      // S (and P over it) of the two groups, then their O
 
+    // 512 threads start with 128 registers each; a softmax thread needs 160, the others fewer: 256 * 168 + 256 * 88 = 65,536
+    if constexpr (KV != kKvBf16) {
+        if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    }
     if (!working) {
         if (tid == 0) { records[me].has_tail = 0; records[me].head_state = 0; }
+    } else if (KV != kKvBf16 && warp >= 12) {
+        // ============================ codes to bf16 (scaled cache) ============================
+        if constexpr (KV != kKvBf16) {
+            const int quarter = warp - 12;
+            int stage = 0, raw = 0;
+            uint32_t phase = 0, raw_phase = 0;
+            bool ok = true;
+            for (;;) {
+                if (!warp_wait(smem_u32(&sm.raw.full[raw]), raw_phase, abort_flag)) { ok = false; break; }
+                const int kind = sm.raw.kind[raw];
+                if (kind < 0) break;
+                const float s0 = sm.raw.scales[raw][2 * quarter], s1 = sm.raw.scales[raw][2 * quarter + 1];
+                if (!warp_wait(smem_u32(&sm.kv_empty[stage]), phase ^ 1, abort_flag)) { ok = false; break; }
+                expand_quarter<KV>(smem_u32(sm.raw.codes[raw]) + quarter * (kTileBytes / 8), smem_u32(sm.kv[stage]), quarter, kind == 1, s0, s1);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the products read what is there now
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&sm.kv_full[stage]));
+                    mbar_arrive(smem_u32(&sm.raw.empty[raw]));
+                }
+                if (++stage == kRing) { stage = 0; phase ^= 1; }
+                if (++raw == kRawTiles) { raw = 0; raw_phase ^= 1; }
+            }
+            if (!ok && lane == 0) give_up();
+        }
     } else if (warp == 11) {
         // ============================ schedule ============================
         if (lane == 0) {
@@ -805,6 +919,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
         int q_fill = -1;
         bool ok = true;
         const int none_c2 = (int)(P.kv_nhd ? P.num_pages * kPageSize : P.num_pages * Hkv);   // out of range: zeros
+        constexpr int kSlots = KV == kKvBf16 ? kRing : kRawTiles;      // what this warp fills: the ring, or the tiles of codes
         const uint32_t q_box = (uint32_t)(64 * 2) * G * tile_rows;
         if (A.table) {      // the first block's table entries, while the schedule names it
             const int at = sm.cut[0].tile * kTilePages + lane;
@@ -842,6 +957,28 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 const bool in = page0 + (lane & 7) <= last_page;
                 const bool bad = in && (phys < 0 || (long long)phys >= P.num_pages);
                 const unsigned bad_mask = __ballot_sync(0xffffffffu, bad) & 0xffu;
+                if constexpr (KV != kKvBf16) {
+                    if (!warp_wait(smem_u32(&sm.raw.empty[stage]), phase ^ 1, abort_flag)) { ok = false; return; }
+                    const uint32_t full = smem_u32(&sm.raw.full[stage]);
+                    const bool there = in && !bad;
+                    const size_t scale_at = there ? (size_t)phys * Hkv + b.head : 0;      // a page that is not there has scale 0
+                    if (lane < kTilePages) copy_async_4(smem_u32(&sm.raw.scales[stage][lane]), (is_v ? A.v_scale : A.k_scale) + scale_at, there);
+                    const int at0 = !there ? none_c2 : P.kv_nhd ? phys * kPageSize : phys * Hkv + b.head;
+                    int at[kTilePages];
+#pragma unroll
+                    for (int i = 0; i < kTilePages; ++i) at[i] = __shfl_sync(0xffffffffu, at0, i);
+                    if (elect_one()) {
+                        const uint32_t dst = smem_u32(sm.raw.codes[stage]);
+                        sm.raw.kind[stage] = is_v ? 1 : 0;
+                        if (!is_v) sm.bad_pages[tile_no & 7] = bad_mask;
+                        if (!is_v && bad_mask && P.check_bounds) rows_status_or(A.status, kStatusBadPage);
+                        mbar_arrive_expect_tx(full, kTileBytes / 2);
+#pragma unroll
+                        for (int i = 0; i < kTilePages; ++i) tma_load_3d(dst + i * kScaledPageBytes, is_v ? &maps.v : &maps.k, 0, c1, at[i], full);
+                    }
+                    __syncwarp();
+                    arrive_after_copies(full);
+                } else {
                 if (!warp_wait(smem_u32(&sm.kv_empty[stage]), phase ^ 1, abort_flag)) { ok = false; return; }
                 // One thread issues every copy, with operands that are the same for the warp: a lane per page made each copy
                 // a turn of a loop over lanes, 1,500 cycles per tile and the bound of the whole kernel.
@@ -865,9 +1002,10 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     }
                 }
                 __syncwarp();
+                }
                 if (!is_v) ++tile_no;
                 ++issued;
-                if (++stage == kRowsRing) { stage = 0; phase ^= 1; }
+                if (++stage == kSlots) { stage = 0; phase ^= 1; }
             };
             // The order the products consume them in: K is one tile (wide) or two (narrow) ahead of V.  Q after the first.
             const int ahead = b.narrow ? 2 : 1;
@@ -893,16 +1031,32 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 q_fill = idx;
             }
         }
+        if constexpr (KV != kKvBf16) {
+            if (ok) {      // no more tiles
+                if (warp_wait(smem_u32(&sm.raw.empty[stage]), phase ^ 1, abort_flag)) {
+                    if (lane == 0) {
+                        sm.raw.kind[stage] = -1;
+                        mbar_arrive(smem_u32(&sm.raw.full[stage]));
+                    }
+                    __syncwarp();
+                    mbar_arrive(smem_u32(&sm.raw.full[stage]));
+                } else {
+                    ok = false;
+                }
+            }
+        }
         if (!ok) {
             // flag it, then wait (bounded) for the copies still in flight
             if (lane == 0) give_up();
             __syncwarp();
             int s2 = stage;
             uint32_t ph2 = phase;
-            for (int k = 0; k < min(issued, kRowsRing); ++k) {
-                if (--s2 < 0) { s2 = kRowsRing - 1; ph2 ^= 1; }
+            unsigned long long *bars;
+            if constexpr (KV == kKvBf16) bars = sm.kv_full; else bars = sm.raw.full;
+            for (int k = 0; k < min(issued, kSlots); ++k) {
+                if (--s2 < 0) { s2 = kSlots - 1; ph2 ^= 1; }
                 for (unsigned it = 0; it < (1u << 20); ++it)
-                    if (mbar_try_wait(smem_u32(&sm.kv_full[s2]), ph2)) break;
+                    if (mbar_try_wait(smem_u32(&bars[s2]), ph2)) break;
             }
             if (q_fill >= 0)
                 for (unsigned it = 0; it < (1u << 20); ++it)
@@ -941,7 +1095,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
             // This warp is done with the ring's next tile when its products so far are.
             auto release = [&]() {
                 if (elect_one()) umma_commit(bar_empty + stage * 8);
-                if (++stage == kRowsRing) { stage = 0; phase ^= 1; }
+                if (++stage == kRing) { stage = 0; phase ^= 1; }
             };
             // A unit's slot: its half of the tile, or, narrow, where a group has one half of every tile, the tile's parity.
             // S[slot] = Q (K half h)^T
@@ -1019,7 +1173,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     for (int t = b.t_lo; t < t_plain; ++t) {
                         const int v_at = at;
                         const uint32_t v_ph = ph;
-                        if (++at == kRowsRing) { at = 0; ph ^= 1; }
+                        if (++at == kRing) { at = 0; ph ^= 1; }
                         wait(bar_full + v_at * 8, v_ph);
                         wait(bar_full + at * 8, ph);
                         if (!fine) break;
@@ -1056,7 +1210,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                         if (!fine) break;
                         umma_commit(bar_empty + v_at * 8);
                         umma_commit(bar_empty + at * 8);
-                        if (++at == kRowsRing) { at = 0; ph ^= 1; }
+                        if (++at == kRing) { at = 0; ph ^= 1; }
                     }
                 }
                 if (!__all_sync(0xffffffffu, fine)) { ok = false; break; }
@@ -1069,13 +1223,13 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     if ((n >> 1) & 1) p_phase ^= 2u >> (b.t_lo & 1);
                 }
                 const int moved = stage + 2 * n;
-                phase ^= (uint32_t)((moved / kRowsRing) & 1);
-                stage = moved % kRowsRing;
+                phase ^= (uint32_t)((moved / kRing) & 1);
+                stage = moved % kRing;
             }
             if (ok && t_plain > b.t_lo && t_plain + ahead == b.t_hi) q_done();
             for (int t = t_plain; ok && t < b.t_hi; ++t) {
                 const bool more = t + ahead < b.t_hi;
-                const int v_at = stage, k_at = stage + 1 == kRowsRing ? 0 : stage + 1;
+                const int v_at = stage, k_at = stage + 1 == kRing ? 0 : stage + 1;
                 const uint32_t v_phase = phase, k_phase = k_at ? phase : phase ^ 1;
                 if (!take(v_at, v_phase)) break;
                 if (needs_clean(t)) clean_values(t, v_at);
@@ -1330,7 +1484,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 }
                 finish(c, o);
             }
-            if (dirty && live && !empty) add_hidden(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
+            if (dirty && live && !empty) add_hidden<KV>(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
             if (PREFIX) {
                 const bool mine = live && !empty && l == l;
                 if (__any_sync(0xffffffffu, mine && odd != odd)) mend_infinite(A, P, sm.info[slot], mine, c0, c1, slot_base, slot_row, out_row);
@@ -1496,31 +1650,13 @@ rows_merge_kernel(const __grid_constant__ RowsArgs A, const __grid_constant__ De
 }
 
 // ------------------------------------------------------------------ host side
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-inline EncodeTiledFn encode_tiled_fn()
-{
-    static std::mutex mu;
-    static EncodeTiledFn fn = nullptr;
-    std::lock_guard<std::mutex> lock(mu);
-    if (!fn) {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-            qres == cudaDriverEntryPointSuccess)
-            fn = (EncodeTiledFn)p;
-    }
-    return fn;
-}
 // Descriptors of one call (encoded every call: under a microsecond each).  q: [rows, Hq, 128] in boxes of 64 channels
 // x G heads x 128 / G rows; K pages in boxes of one channel half (so that a tile is two K-major operands of 128
 // positions), V pages whole (a page is one step of the second product).
-inline int make_rows_maps(RowsMaps *m, const RowsArgs &A, const DevParams &P, char *msg, size_t msg_len)
+inline int make_rows_maps(RowsMaps *m, const RowsArgs &A, const DevParams &P, bool scaled, char *msg, size_t msg_len)
 {
-    EncodeTiledFn encode = encode_tiled_fn();
-    if (!encode) { snprintf(msg, msg_len, "cuTensorMapEncodeTiled entry point not available"); return -1; }
+    EncodeTiledFn encode = encode_tiled(msg, msg_len);
+    if (!encode) return -1;
     const cuuint32_t ones[4] = {1, 1, 1, 1};
     auto make = [&](CUtensorMap *out, const void *base, int dims, const cuuint64_t *size, const cuuint64_t *stride, const cuuint32_t *box) {
         return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dims, const_cast<void *>(base), size, stride, box, ones,
@@ -1531,6 +1667,10 @@ inline int make_rows_maps(RowsMaps *m, const RowsArgs &A, const DevParams &P, ch
     const cuuint64_t q_stride[2] = {(cuuint64_t)kHeadDim * 2, (cuuint64_t)A.q_stride * 2};
     const cuuint32_t q_box[3] = {64, (cuuint32_t)P.group, (cuuint32_t)(kRowTile / P.group)};
     CUresult r = make(&m->q, A.q, 3, q_size, q_stride, q_box);
+    if (scaled && r == CUDA_SUCCESS) {      // pages of codes as they are: the expanding warps lay them out
+        return make_scaled_map(&m->k, A.k_cache, P.num_pages, P.num_kv_heads, P.kv_nhd != 0, false, msg, msg_len) ||
+               make_scaled_map(&m->v, A.v_cache, P.num_pages, P.num_kv_heads, P.kv_nhd != 0, false, msg, msg_len) ? -1 : 0;
+    }
     const cuuint64_t hkv = (cuuint64_t)P.num_kv_heads, rows = (cuuint64_t)P.num_pages * kPageSize;
     // both layouts as [half][.][.][64 channels]: a page of a head is 16 rows of one plane, or one head of 16 planes
     const cuuint64_t hnd[4] = {64, kPageSize, (cuuint64_t)P.num_pages * hkv, 2}, hnd_stride[3] = {(cuuint64_t)kHeadDim * 2, kPageBytes, 128};
@@ -1546,7 +1686,7 @@ inline int make_rows_maps(RowsMaps *m, const RowsArgs &A, const DevParams &P, ch
     return 0;
 }
 
-template <bool PREFIX>
+template <bool PREFIX, int KV>
 cudaError_t launch_rows_kernels(const RowsMaps &maps, const RowsArgs &A, const DevParams &P, char *ws, int sms, cudaStream_t st)
 {
     {   // per-device kernel attribute, set once under a lock
@@ -1556,7 +1696,7 @@ cudaError_t launch_rows_kernels(const RowsMaps &maps, const RowsArgs &A, const D
         cudaGetDevice(&dev);
         std::lock_guard<std::mutex> lock(mu);
         if (!done[dev & 63]) {
-            const cudaError_t e = cudaFuncSetAttribute(rows_kernel<PREFIX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowsSmem));
+            const cudaError_t e = cudaFuncSetAttribute(rows_kernel<PREFIX, KV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowsSmem<KV>));
             if (e != cudaSuccess) return e;
             done[dev & 63] = true;
         }
@@ -1565,7 +1705,7 @@ cudaError_t launch_rows_kernels(const RowsMaps &maps, const RowsArgs &A, const D
     RowsRecord *records = reinterpret_cast<RowsRecord *>(ws + L.record_off);
     float *asides = reinterpret_cast<float *>(ws + L.aside_off), *slots = reinterpret_cast<float *>(ws + L.slot_off);
     const int n = sms < kRowsMaxCtas ? sms : kRowsMaxCtas;
-    cudaError_t e = launch_pdl(rows_kernel<PREFIX>, dim3(n), dim3(kRowsThreads), sizeof(RowsSmem), st, maps, A, P, records, asides, slots);
+    cudaError_t e = launch_pdl(rows_kernel<PREFIX, KV>, dim3(n), dim3(kRowsThreads<KV>), sizeof(RowsSmem<KV>), st, maps, A, P, records, asides, slots);
     if (e != cudaSuccess) return e;
     return launch_pdl(rows_merge_kernel<PREFIX>, dim3(n, kRowsMergeParts), dim3(2 * kRowTile), 0, st, A, P,
                       (const RowsRecord *)records, (const float *)slots, n);

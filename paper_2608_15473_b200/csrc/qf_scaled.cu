@@ -9,7 +9,7 @@
 #include "qf_common.cuh"
 #include "qf_host.h"
 #include "qf_place_scaled.cuh"
-#include "qf_rows_simple.cuh"
+#include "qf_rows.cuh"
 #include "qf_simple.cuh"
 #include "qf_sweep.cuh"
 
@@ -24,7 +24,7 @@ int refuse(const qf_params *p, int code)
     const int rc = qf_host::validate(p);
     return rc != QF_OK ? rc : code;
 }
-static_assert(QF_KV_E4M3 == qf::kKvE4m3 && QF_KV_INT8 == qf::kKvInt8, "the header's types are the kernels'");
+static_assert((int)QF_KV_E4M3 == (int)qf::kKvE4m3 && (int)QF_KV_INT8 == (int)qf::kKvInt8, "the header's types are the kernels'");
 
 template <int KV, int G>
 void launch_simple_g(const void *q, const void *k, const void *v, const qf_host::ScaledKv &s, const int32_t *bt, const int32_t *sl,
@@ -69,16 +69,28 @@ int launch_sweep_scaled(const void *q, const void *k, const void *v, const Scale
                                                   ev1, msg, msg_len, launches, skip_finish);
 }
 
-int launch_rows_scaled(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *, int kind, char *, int, cudaStream_t st)
+int launch_rows_scaled(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *p, int kind, char *ws, int sms, cudaStream_t st)
 {
-    const long long units = (long long)A.total_rows * P.num_q_heads;
-    const long long blocks = (units + qf::kRowsSimpleWarps - 1) / qf::kRowsSimpleWarps;
-    if (blocks > 0x7fffffffll) return QF_ERR_UNSUPPORTED;
-    if (kind == qf::kKvE4m3) qf::rows_simple_kernel<false, qf::kKvE4m3><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
-    else qf::rows_simple_kernel<false, qf::kKvInt8><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail(e, "rows_simple_kernel launch");
-    set_launches(1);
+    const bool e4m3 = kind == qf::kKvE4m3;
+    if (p->flags & QF_FLAG_SIMPLE_KERNEL) {
+        const long long units = (long long)A.total_rows * P.num_q_heads;
+        const long long blocks = (units + qf::kRowsSimpleWarps - 1) / qf::kRowsSimpleWarps;
+        if (blocks > 0x7fffffffll) return QF_ERR_UNSUPPORTED;
+        if (e4m3) qf::rows_simple_kernel<false, qf::kKvE4m3><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
+        else qf::rows_simple_kernel<false, qf::kKvInt8><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return cuda_fail(e, "rows_simple_kernel launch");
+        set_launches(1);
+        return QF_OK;
+    }
+    qf::RowsMaps maps;
+    size_t len;
+    char *msg = cuda_msg(&len);
+    if (qf::make_rows_maps(&maps, A, P, true, msg, len)) return QF_ERR_CUDA;
+    const cudaError_t e = e4m3 ? qf::launch_rows_kernels<false, qf::kKvE4m3>(maps, A, P, ws, sms, st)
+                               : qf::launch_rows_kernels<false, qf::kKvInt8>(maps, A, P, ws, sms, st);
+    if (e != cudaSuccess) return cuda_fail(e, "rows_kernel launch");
+    set_launches(2);
     return QF_OK;
 }
 
