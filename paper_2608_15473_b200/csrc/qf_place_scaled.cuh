@@ -12,12 +12,13 @@
 // exactness, exact expansion to bf16, and scales that can be applied anywhere in a product without another rounding.
 // Codes are rounded once, from the fp32 result of norm and rotation (half a step; to bf16 first would add 2^-9).
 //
-// Who does what: a block must be owned by one place, because its scale follows from all of its new rows.  A CTA takes
-// the page runs (rows of one request that fall into one page) that BEGIN within its `tile` packed tokens: at most 31
-// rows in all.  It forms sines and cosines for these once, then its warps take units: a query head over all rows,
-// or the keys or values of one run and KV head.  A warp holds a unit's 16 rows in registers (sixteen lanes per row, 16
-// bytes each), finds the largest magnitude, and turns the rows into codes; keys are turned twice rather than kept in
-// fp32, which would halve the warps that fit.  gridDim.y splits the KV heads when there are too few runs to fill the GPU.
+// Who does what: a block's scale follows from all of its new rows, so they meet in one CTA.  A CTA takes the page runs (rows of
+// one request that fall into one page) that BEGIN within its `tile` packed tokens, in passes of at most 16 rows.  Sixteen
+// lanes own a head row (16 bytes each); a warp has two rows, and turns them for one head after the other with the angles and
+// gains in registers: all query heads, or an eighth of them when there is but one token.  For keys and values each warp does
+// four heads at a time, the runs' largest magnitudes meet in shared memory (as integers, so that their order is no matter),
+// and the rows become codes from the registers they were turned in.  gridDim.y splits the KV heads when there are too few
+// runs to fill the GPU.
 //
 // Bound: HBM for prompts (256 bytes in per head row, 256 out per query and 128 per key or value), latency for a decode batch.
 #pragma once
@@ -51,15 +52,16 @@ __device__ __forceinline__ float held_scale(float s)
     if (s != s || s == __int_as_float(0x7f800000)) return __uint_as_float(0x7fc00000u);
     return s > 0.f ? s : 0.f;
 }
-// x / s: a product where s is a power of two (every scale that this kernel forms; a caller's own may be anything)
+// x / s: a product where s is a power of two (every scale that this kernel forms; a caller's own may be anything, also NaN)
 struct Divider {
     float s, inv;
     bool power;
     __device__ __forceinline__ explicit Divider(float by)
     {
+        const unsigned bits = __float_as_uint(by);
         s = by;
-        inv = 1.f / by;
-        power = (__float_as_uint(by) & 0x7fffffu) == 0;
+        power = (bits & 0x807fffffu) == 0 && bits - 0x00800000u < 0x7e800000u - 0x00800000u + 1u;      // 2^-126 .. 2^126
+        inv = __uint_as_float(0x7f000000u - bits);                                                     // 2^-k
     }
     __device__ __forceinline__ float operator()(float x) const { return power ? x * inv : x / s; }
 };
@@ -93,76 +95,107 @@ __device__ __forceinline__ void numbers_of(uint32_t w, float (&y)[4])
     }
 }
 
-// A lane's eight channels of a head row, and how they turn.
+// A lane's eight channels of a head row, and how they turn.  Sixteen lanes own a row, so a warp works on two rows.
 struct TurnLane {
     int ch, pch, partner;      // first channel, the partners' first channel, the lane of the sixteen that holds them
     bool turns, upper;
 };
-
-// Norm and rotation of one row: `w` this lane's eight channels, `turn` the row's (cos, sin) of every pair.
+// Where a row's table keeps (cos, sin) of pair j, so that the sixteen lanes' 16-byte reads are neighbours: four words of a lane's
+// eight channels in four planes, or, interleaved, its four pairs in two.
 template <bool INTERLEAVED>
-__device__ __forceinline__ void turn_row(const uint4 &w, bool works, const uint16_t *gain, const uint4 &own_gain, const uint4 &partner_gain,
-                                         const TurnLane &L, const float2 *turn, float eps, float (&y)[8])
+__device__ __forceinline__ int turn_place(int j)
 {
-    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { y[2 * i] = bf16lo_to_f32(ww[i]); y[2 * i + 1] = bf16hi_to_f32(ww[i]); }
-    if (!works) return;
-    float rs = 1.f;
+    return INTERLEAVED ? ((j >> 1) & 1) * 32 + (j >> 2) * 2 + (j & 1) : ((j >> 1) & 3) * 16 + (j >> 3) * 2 + (j & 1);
+}
+// Gain and angle of a row in one pair of coefficients per channel: y_c = (x_c * own_c + x_partner * other_c) / rms.
+struct TurnCoefs { unsigned long long own[4], other[4]; };
+template <bool INTERLEAVED>
+__device__ __forceinline__ TurnCoefs turn_coefs(const uint16_t *gain, const TurnLane &L, const float2 *turn)
+{
+    TurnCoefs k;
+    uint4 ga = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), gb = ga;      // ones
     if (gain) {
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(y[i], y[i], ss);
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-        rs = rsqrtf(fmaf(ss, 1.0f / kHeadDim, eps));
+        ga = *reinterpret_cast<const uint4 *>(gain + L.ch);
+        gb = *reinterpret_cast<const uint4 *>(gain + L.pch);
     }
-    const uint32_t gw[4] = {own_gain.x, own_gain.y, own_gain.z, own_gain.w};
-    const uint32_t pw[4] = {partner_gain.x, partner_gain.y, partner_gain.z, partner_gain.w};
-    float p[8];
-    if (!INTERLEAVED) {
+    const uint32_t gw[4] = {ga.x, ga.y, ga.z, ga.w}, pw[4] = {gb.x, gb.y, gb.z, gb.w};
+    const float4 *t4 = reinterpret_cast<const float4 *>(turn);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t o = __shfl_sync(0xffffffffu, ww[i], L.partner, 16);
-            p[2 * i] = bf16lo_to_f32(o);
-            p[2 * i + 1] = bf16hi_to_f32(o);
-        }
-    }
-    if (gain) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            y[2 * i] *= bf16lo_to_f32(gw[i]); y[2 * i + 1] *= bf16hi_to_f32(gw[i]);
-            if (!INTERLEAVED) { p[2 * i] *= bf16lo_to_f32(pw[i]); p[2 * i + 1] *= bf16hi_to_f32(pw[i]); }
-        }
-    }
-    if (L.turns) {      // channels that do not turn have no partner: an infinity elsewhere must not reach them
-        if (INTERLEAVED) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {      // word i is pair 4 lane + i
-                const float2 t = turn[L.ch / 2 + i];
-                const float a = y[2 * i], b = y[2 * i + 1];
-                y[2 * i] = fmaf(-b, t.y, a * t.x);
-                y[2 * i + 1] = fmaf(a, t.y, b * t.x);
-            }
+    for (int i = 0; i < 4; ++i) {
+        k.own[i] = pair_of_bf16(gw[i]);
+        k.other[i] = 0ull;
+        if (!L.turns) continue;
+        if (INTERLEAVED) {      // word i is pair 4 lane + i
+            const float4 two = t4[(i >> 1) * 16 + L.ch / 8];
+            const float c = (i & 1) ? two.z : two.x, sn = (i & 1) ? two.w : two.y;
+            k.other[i] = mul_pair(swap_pair(k.own[i]), pair_of(-sn, sn));
+            k.own[i] = mul_pair(k.own[i], pair_of(c, c));
         } else {
-            const float4 *t4 = reinterpret_cast<const float4 *>(turn + (L.upper ? L.pch : L.ch));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4 t = t4[i];
-                y[2 * i] = fmaf(L.upper ? p[2 * i] : -p[2 * i], t.y, y[2 * i] * t.x);
-                y[2 * i + 1] = fmaf(L.upper ? p[2 * i + 1] : -p[2 * i + 1], t.w, y[2 * i + 1] * t.z);
-            }
+            const float4 two = t4[i * 8 + (L.upper ? L.pch : L.ch) / 8];
+            k.other[i] = mul_pair(pair_of_bf16(pw[i]), L.upper ? pair_of(two.y, two.w) : pair_of(-two.y, -two.w));
+            k.own[i] = mul_pair(k.own[i], pair_of(two.x, two.z));
         }
     }
-    if (gain) {
+    return k;
+}
+// Norm and rotation of N rows (of one token, by sixteen lanes each), step by step over all of them so that their shuffles overlap.
+template <bool INTERLEAVED, int N>
+__device__ __forceinline__ void turn_rows(const uint4 (&w)[N], bool works, bool norm, const TurnCoefs &k, const TurnLane &L, float eps,
+                                          unsigned long long (&y)[N][4])
+{
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] *= rs;
+    for (int b = 0; b < N; ++b) {
+        y[b][0] = pair_of_bf16(w[b].x); y[b][1] = pair_of_bf16(w[b].y); y[b][2] = pair_of_bf16(w[b].z); y[b][3] = pair_of_bf16(w[b].w);
+    }
+    if (!works) return;
+    float rs[N];
+    if (norm) {
+#pragma unroll
+        for (int b = 0; b < N; ++b) {
+            float u0, u1, u2, u3;
+            split_pair(fma_pair(y[b][2], y[b][2], mul_pair(y[b][0], y[b][0])), u0, u1);
+            split_pair(fma_pair(y[b][3], y[b][3], mul_pair(y[b][1], y[b][1])), u2, u3);
+            rs[b] = (u0 + u1) + (u2 + u3);
+        }
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1)
+#pragma unroll
+            for (int b = 0; b < N; ++b) rs[b] += __shfl_xor_sync(0xffffffffu, rs[b], off);
+#pragma unroll
+        for (int b = 0; b < N; ++b) rs[b] = rsqrtf(fmaf(rs[b], 1.0f / kHeadDim, eps));
+    }
+#pragma unroll
+    for (int b = 0; b < N; ++b) {
+        const uint32_t ww[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned long long px = INTERLEAVED ? swap_pair(y[b][i]) : pair_of_bf16(__shfl_sync(0xffffffffu, ww[i], L.partner, 16));
+            const unsigned long long own = mul_pair(y[b][i], k.own[i]);
+            // channels that do not turn have no partner: an infinity elsewhere must not reach them
+            y[b][i] = L.turns ? fma_pair(px, k.other[i], own) : own;
+            if (norm) y[b][i] = mul_pair(y[b][i], pair_of(rs[b], rs[b]));
+        }
     }
 }
-
-__device__ __forceinline__ uint4 bf16_row(const float (&y)[8])
+__device__ __forceinline__ uint4 bf16_row(const unsigned long long (&y)[4])
 {
-    return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        split_pair(y[i], lo, hi);
+        w[i] = pack_bf16(lo, hi);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The codes of a row's eight channels at `to`.
+template <int KV>
+__device__ __forceinline__ void store_codes(uint8_t *to, const unsigned long long (&y)[4], const Divider &by)
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split_pair(y[i], v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<uint2 *>(to) = make_uint2(codes_of<KV>(by(v[0]), by(v[1]), by(v[2]), by(v[3])), codes_of<KV>(by(v[4]), by(v[5]), by(v[6]), by(v[7])));
 }
 
 template <int KV, bool INTERLEAVED>
@@ -170,21 +203,21 @@ __global__ void __launch_bounds__(kPlaceWarps * 32, 2)
 place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_scale, float *__restrict__ v_scale, int tile,
                     const __grid_constant__ DevParams P)
 {
-    __shared__ __align__(16) float2 turns[kPlaceWindow][64];      // (cos, sin) of every pair
+    constexpr int kQ = 8, kKv = 4;                      // rows that a warp's half works on at a time: query heads, KV heads
+    __shared__ __align__(16) float2 turns[kPlaceWarps][2][64];      // (cos, sin) of every pair, of a warp's two tokens
+    __shared__ unsigned tops[2][kPlaceTile][kKv * kPlaceWarps];     // the largest magnitude of keys and values: [side][run][head]
     grid_dependency_wait();
     grid_launch_dependents();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l16 = lane & 15, half = lane >> 4;
     const int t0 = (int)blockIdx.x * tile;
     // ---- lane k looks up token t0 + k: its request, place and whether a run begins there
-    int b = -1, slot = 0, rows_left = 0;
+    int b = -1, slot = 0;
     long long pos = 0, phys = -1;
     if (t0 + lane < A.total_tokens && lane < tile + kPageSize - 1) {
         b = request_of(A.cu, P.batch, t0 + lane);
         if (b >= 0) {
-            const long long i = (long long)(t0 + lane) - A.cu[b];
-            pos = (long long)max(A.seq_lens[b], 0) + i;
+            pos = (long long)max(A.seq_lens[b], 0) + ((long long)(t0 + lane) - A.cu[b]);
             slot = (int)(pos & (kPageSize - 1));
-            rows_left = min(A.cu[b + 1], A.total_tokens) - (t0 + lane);
             if (A.k_cache && (pos >> 4) < P.max_pages_per_req) {      // nothing is stored where the position has no page
                 const long long at = (long long)b * P.max_pages_per_req + (pos >> 4);
                 phys = A.block_table ? (long long)A.block_table[at] : at;
@@ -197,150 +230,191 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
     const unsigned mine = starts & ((1u << tile) - 1);      // runs of this CTA (tile <= 16)
     if (mine == 0) return;                                  // the same for every warp
     const unsigned upto = starts & ((2u << lane) - 1);      // runs that begin at or before this token
-    const bool covered = b >= 0 && upto != 0 && ((mine >> (31 - __clz((int)upto))) & 1);
-    const unsigned cover = __ballot_sync(0xffffffffu, covered);
-    const int lo = __ffs((int)cover) - 1, hi = 32 - __clz((int)cover);      // rows [lo, hi) of the window, with gaps
-    // ---- angles: formed and reduced to a fraction of a turn in fp64 (see qf_rope.cuh)
-    const int pairs = A.rotary_dim / 2;
-    if (pairs > 0) {
-        const long long r0 = pos + (b >= 0 && A.pos_base ? A.pos_base[b] : 0);
-        for (int k = lo + warp; k < hi; k += kPlaceWarps) {
-            if (!((cover >> k) & 1)) continue;
-            const long long row_pos = __shfl_sync(0xffffffffu, r0, k);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int j = lane + 32 * h;
-                if (j >= pairs) continue;
-                double r = (double)row_pos;
-                if (A.positions) {
-                    const int axis = min(max(A.pair_axis[j], 0), A.num_axes - 1);
-                    r = (double)A.positions[(long long)axis * A.total_tokens + t0 + k];
-                }
-                const double turn = r * ((double)A.inv_freq[j] * 0.15915494309189533577);      // / (2 pi)
-                float sn, cs;
-                sincospif(2.f * (float)(turn - rint(turn)), &sn, &cs);
-                turns[k][j] = make_float2(cs * A.rot_scale, sn * A.rot_scale);
-            }
-        }
-    }
-    __syncthreads();
+    const unsigned cover = __ballot_sync(0xffffffffu, b >= 0 && upto != 0 && ((mine >> (31 - __clz((int)upto))) & 1));
+    const long long rotary = pos + (b >= 0 && A.pos_base ? A.pos_base[b] : 0);
 
-    // ---- units
     const int Hkv = P.num_kv_heads, G = P.group, parts = (int)gridDim.y, part = (int)blockIdx.y;
     const int heads = (Hkv - part + parts - 1) / parts;                  // KV heads part, part + parts, ...
-    const int n_q = A.n_q ? heads * G : 0, n_kv = A.n_k ? heads : 0, n_runs = __popc(mine);
-    const int sides = A.v ? 2 : 1;                                       // keys, and values if they are placed
-    const int units = n_q + n_runs * n_kv * sides;
+    const int pairs = A.rotary_dim / 2, half_chunks = A.rotary_dim >> 4;
     TurnLane L;
-    const int l16 = lane & 15, half = lane >> 4, half_chunks = A.rotary_dim >> 4;
     L.ch = l16 * 8;
     L.turns = l16 < 2 * half_chunks;
     L.upper = l16 >= half_chunks;
     L.partner = INTERLEAVED || !L.turns ? l16 : L.upper ? l16 - half_chunks : l16 + half_chunks;
     L.pch = L.partner * 8;
-    for (int u = warp; u < units; u += kPlaceWarps) {
-        if (u < n_q) {
-            // ---- a query head over the window
-            const int h = (part + (u / G) * parts) * G + u % G;
+
+    // ---- passes of whole runs, at most 16 rows of the window each (nearly always one pass)
+    unsigned left = mine;
+    while (left) {
+        const int lo = __ffs((int)left) - 1;
+        int hi = lo;
+        unsigned runs = 0;
+        while (left) {      // the run's rows are covered and contiguous, up to the next run's first
+            const int k = __ffs((int)left) - 1;
+            const unsigned past = (~cover | (starts & ~(1u << k))) & ~((1u << k) - 1);
+            const int end = past ? __ffs((int)past) - 1 : 32;
+            if (end - lo > kPageSize) break;
+            hi = end;
+            runs |= 1u << k;
+            left &= left - 1;
+        }
+        const int n_pairs = (hi - lo + 1) >> 1;
+        const int slices = n_pairs > 4 ? 8 : n_pairs > 2 ? 4 : n_pairs;      // a warp has one pair of rows, and its share of the heads
+        const int pair = warp & (slices - 1), hg = warp / slices, hgs = kPlaceWarps / slices;
+        const int k = lo + 2 * pair + half;
+        const bool live = k < hi && ((cover >> k) & 1);
+        const int my_k = min(k, 31), t = t0 + k;
+        const int my_slot = __shfl_sync(0xffffffffu, slot, my_k);
+        const long long page = __shfl_sync(0xffffffffu, phys, my_k);
+        const int run = __popc(runs & ((2u << my_k) - 1)) - 1;
+        const bool leads = live && ((runs >> my_k) & 1);                    // this row is its run's first
+        // ---- angles: formed and reduced to a fraction of a turn in fp64 (see qf_rope.cuh)
+        __syncwarp();
+#pragma unroll 1
+        for (int r = 0; r < 2; ++r) {
+            const int kk = lo + 2 * pair + r;
+            if (kk >= hi || !((cover >> kk) & 1)) continue;
+            const long long row_pos = __shfl_sync(0xffffffffu, rotary, kk);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = lane + 32 * h;
+                if (j >= pairs) continue;
+                double x = (double)row_pos;
+                if (A.positions)
+                    x = (double)A.positions[(long long)min(max(A.pair_axis[j], 0), A.num_axes - 1) * A.total_tokens + t0 + kk];
+                const double turn = x * ((double)A.inv_freq[j] * 0.15915494309189533577);      // / (2 pi)
+                float sn, cs;
+                sincospif(2.f * (float)(turn - rint(turn)), &sn, &cs);
+                turns[warp][r][turn_place<INTERLEAVED>(j)] = make_float2(cs * A.rot_scale, sn * A.rot_scale);
+            }
+        }
+        __syncwarp();
+        const float2 *turn = turns[warp][half];
+        // ---- queries
+        if (A.n_q) {
             const bool works = A.q_gain || A.rotary_dim > 0;
-            uint4 ga = make_uint4(0u, 0u, 0u, 0u), gb = ga;
-            if (A.q_gain) {
-                ga = *reinterpret_cast<const uint4 *>(A.q_gain + L.ch);
-                gb = *reinterpret_cast<const uint4 *>(A.q_gain + L.pch);
-            }
-            for (int k0 = lo; k0 < hi; k0 += 2 * kPlaceBatch) {
-                uint4 w[kPlaceBatch];
+            const TurnCoefs co = turn_coefs<INTERLEAVED>(A.q_gain, L, turn);
+            const uint16_t *src = A.q + (long long)t * A.q_stride + L.ch;
+            uint16_t *dst = A.q_out + (long long)t * A.n_q * kHeadDim + L.ch;
+            auto head_of = [&](int i) { const int c = i / G; return (part + c * parts) * G + i - c * G; };
+            for (int i0 = hg; i0 < heads * G; i0 += kQ * hgs) {
+                uint4 w[kQ];
 #pragma unroll
-                for (int i = 0; i < kPlaceBatch; ++i) {
-                    const int k = k0 + 2 * i + half;
-                    w[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (k < hi && ((cover >> k) & 1))
-                        w[i] = __ldcs(reinterpret_cast<const uint4 *>(A.q + (long long)(t0 + k) * A.q_stride + h * kHeadDim + L.ch));
+                for (int n = 0; n < kQ; ++n) {
+                    const int i = i0 + n * hgs;
+                    w[n] = make_uint4(0u, 0u, 0u, 0u);
+                    if (live && i < heads * G) w[n] = __ldcs(reinterpret_cast<const uint4 *>(src + head_of(i) * kHeadDim));
                 }
 #pragma unroll
-                for (int i = 0; i < kPlaceBatch; ++i) {
-                    if (k0 + 2 * i >= hi) break;
-                    const int k = k0 + 2 * i + half;
-                    float y[8];
-                    turn_row<INTERLEAVED>(w[i], works, A.q_gain, ga, gb, L, turns[min(k, kPlaceWindow - 1)], A.eps, y);
-                    if (k < hi && ((cover >> k) & 1))
-                        *reinterpret_cast<uint4 *>(A.q_out + ((long long)(t0 + k) * A.n_q + h) * kHeadDim + L.ch) = bf16_row(y);
+                for (int n4 = 0; n4 < kQ; n4 += 4) {
+                    if (i0 + n4 * hgs >= heads * G) break;
+                    const uint4 wb[4] = {w[n4], w[n4 + 1], w[n4 + 2], w[n4 + 3]};
+                    unsigned long long y[4][4];
+                    turn_rows<INTERLEAVED, 4>(wb, works, A.q_gain != nullptr, co, L, A.eps, y);
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        const int i = i0 + (n4 + n) * hgs;
+                        if (live && i < heads * G) *reinterpret_cast<uint4 *>(dst + head_of(i) * kHeadDim) = bf16_row(y[n]);
+                    }
                 }
             }
-            continue;
         }
-        // ---- the keys or values of a run and KV head
-        const int v = u - n_q, run = v / (n_kv * sides), rest = v - run * n_kv * sides;
-        const bool is_v = rest >= n_kv;
-        const int c = part + (is_v ? rest - n_kv : rest) * parts;
-        unsigned from = mine;
-        for (int i = 0; i < run; ++i) from &= from - 1;
-        const int k0 = __ffs((int)from) - 1;
-        const int s0 = __shfl_sync(0xffffffffu, slot, k0);
-        const int n = min(__shfl_sync(0xffffffffu, rows_left, k0), kPageSize - s0);
-        const long long page = __shfl_sync(0xffffffffu, phys, k0);
-        const uint16_t *src = (is_v ? A.v + (long long)(t0 + k0) * A.v_stride : A.k + (long long)(t0 + k0) * A.k_stride) + c * kHeadDim + L.ch;
-        const long long stride = is_v ? A.v_stride : A.k_stride;
-        uint8_t *pool = reinterpret_cast<uint8_t *>(is_v ? A.v_cache : A.k_cache);
-        float *scale_at = page < 0 ? nullptr : (is_v ? v_scale : k_scale) + page * Hkv + c;
-        float old = 0.f;
-        if (s0 > 0 && page >= 0) old = held_scale(*scale_at);
-        uint4 w[kPlaceBatch];
+        if (!A.n_k) continue;
+        // ---- keys and values, a few heads at a time: largest magnitudes of the runs meet in shared memory
+        const bool works = A.k_gain || A.rotary_dim > 0;
+        const TurnCoefs co = turn_coefs<INTERLEAVED>(A.k_gain, L, turn);
+        for (int c0 = 0; c0 < heads; c0 += kKv * hgs) {
+            uint4 kw[kKv], vw[kKv];
+            float k_old[kKv], v_old[kKv];
 #pragma unroll
-        for (int i = 0; i < kPlaceBatch; ++i) {
-            const int r = 2 * i + half;
-            w[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < n) w[i] = __ldcs(reinterpret_cast<const uint4 *>(src + r * stride));
-        }
-        const uint16_t *gain = is_v ? nullptr : A.k_gain;
-        const bool works = !is_v && (gain || A.rotary_dim > 0);
-        uint4 ga = make_uint4(0u, 0u, 0u, 0u), gb = ga;
-        if (gain) {
-            ga = *reinterpret_cast<const uint4 *>(gain + L.ch);
-            gb = *reinterpret_cast<const uint4 *>(gain + L.pch);
-        }
-        float top = 0.f;
+            for (int n = 0; n < kKv; ++n) {
+                const int i = c0 + hg + n * hgs, c = part + i * parts;
+                kw[n] = vw[n] = make_uint4(0u, 0u, 0u, 0u);
+                k_old[n] = v_old[n] = 0.f;
+                if (!live || i >= heads) continue;
+                kw[n] = __ldcs(reinterpret_cast<const uint4 *>(A.k + (long long)t * A.k_stride + c * kHeadDim + L.ch));
+                if (A.v) vw[n] = __ldcs(reinterpret_cast<const uint4 *>(A.v + (long long)t * A.v_stride + c * kHeadDim + L.ch));
+                if (page >= 0) { k_old[n] = __ldcg(k_scale + page * Hkv + c); v_old[n] = __ldcg(v_scale + page * Hkv + c); }
+            }
+            __syncthreads();                                 // the last heads' magnitudes have been read
+            for (int i = tid; i < 2 * kPlaceTile * kKv * kPlaceWarps; i += kPlaceWarps * 32) (&tops[0][0][0])[i] = 0u;
+            unsigned long long y[kKv][4];
+            turn_rows<INTERLEAVED, kKv>(kw, works, A.k_gain != nullptr, co, L, A.eps, y);
+            float top_k[kKv];
+            unsigned top_v[kKv];
 #pragma unroll
-        for (int i = 0; i < kPlaceBatch; ++i) {
-            if (2 * i >= n) break;
-            const int r = 2 * i + half;
-            float y[8];
-            turn_row<INTERLEAVED>(w[i], works, gain, ga, gb, L, turns[min(k0 + r, kPlaceWindow - 1)], A.eps, y);
-            if (r < n) {
+            for (int n = 0; n < kKv; ++n) {
+                top_k[n] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = max_nan(top, fabsf(y[e]));
-                if (!is_v && A.k_out)
-                    *reinterpret_cast<uint4 *>(A.k_out + ((long long)(t0 + k0 + r) * A.n_k + c) * kHeadDim + L.ch) = bf16_row(y);
+                for (int e = 0; e < 4; ++e) {
+                    float v0, v1;
+                    split_pair(y[n][e], v0, v1);
+                    top_k[n] = max_nan(top_k[n], max_nan(fabsf(v0), fabsf(v1)));
+                }
+                const uint32_t a = __vmaxu2(__vmaxu2(vw[n].x & 0x7fff7fffu, vw[n].y & 0x7fff7fffu), __vmaxu2(vw[n].z & 0x7fff7fffu, vw[n].w & 0x7fff7fffu));
+                top_v[n] = max(a & 0xffffu, a >> 16) << 16;
+            }
+#pragma unroll
+            for (int off = 1; off < 16; off <<= 1)
+#pragma unroll
+                for (int n = 0; n < kKv; ++n) {
+                    top_k[n] = max_nan(top_k[n], __shfl_xor_sync(0xffffffffu, top_k[n], off));
+                    top_v[n] = max(top_v[n], __shfl_xor_sync(0xffffffffu, top_v[n], off));
+                }
+            __syncthreads();
+            if (live && l16 == 0) {      // bits of magnitudes order like the magnitudes, NaN above infinity
+#pragma unroll
+                for (int n = 0; n < kKv; ++n) {
+                    atomicMax(&tops[0][run][hg * kKv + n], __float_as_uint(top_k[n]));
+                    atomicMax(&tops[1][run][hg * kKv + n], top_v[n]);
+                }
+            }
+            if (A.k_out && live) {
+#pragma unroll
+                for (int n = 0; n < kKv; ++n) {
+                    const int i = c0 + hg + n * hgs;
+                    if (i < heads) *reinterpret_cast<uint4 *>(A.k_out + ((long long)t * A.n_k + part + i * parts) * kHeadDim + L.ch) = bf16_row(y[n]);
+                }
+            }
+            __syncthreads();
+            if (!live || page < 0) continue;
+            // rows of earlier calls in the block: those before the run's first slot (this row's slot, where it leads)
+            const int held = my_slot - (k - (31 - __clz((int)(runs & ((2u << my_k) - 1)))));
+#pragma unroll
+            for (int n = 0; n < kKv; ++n) {
+                const int i = c0 + hg + n * hgs, c = part + i * parts;
+                if (i >= heads) break;
+#pragma unroll
+                for (int side = 0; side < 2; ++side) {
+                    uint8_t *pool = reinterpret_cast<uint8_t *>(side ? A.v_cache : A.k_cache);
+                    const float old = held > 0 ? held_scale(side ? v_old[n] : k_old[n]) : 0.f;
+                    const float scale = max_nan(old, scale_for<KV>(__uint_as_float(tops[side][run][hg * kKv + n])));
+                    const Divider by(scale);
+                    if (leads) {
+                        if (held > 0 && scale != old) {      // (a NaN scale is unequal to itself: harmless)
+                            const float ratio = by(old);
+                            for (int r = 0; r < held; ++r) {
+                                uint2 *at = reinterpret_cast<uint2 *>(pool + kv_row_offset(P, page, c, r) + L.ch);
+                                const uint2 codes = *at;
+                                float y0[4], y1[4];
+                                numbers_of<KV>(codes.x, y0);
+                                numbers_of<KV>(codes.y, y1);
+                                *at = make_uint2(codes_of<KV>(y0[0] * ratio, y0[1] * ratio, y0[2] * ratio, y0[3] * ratio),
+                                                 codes_of<KV>(y1[0] * ratio, y1[1] * ratio, y1[2] * ratio, y1[3] * ratio));
+                            }
+                        }
+                        if (l16 == 0) (side ? v_scale : k_scale)[page * Hkv + c] = scale;
+                    }
+                    uint8_t *to = pool + kv_row_offset(P, page, c, my_slot) + L.ch;
+                    if (side == 0) {
+                        store_codes<KV>(to, y[n], by);
+                    } else {
+                        const unsigned long long v[4] = {pair_of_bf16(vw[n].x), pair_of_bf16(vw[n].y), pair_of_bf16(vw[n].z), pair_of_bf16(vw[n].w)};
+                        store_codes<KV>(to, v, by);
+                    }
+                }
             }
         }
-        if (page < 0) continue;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, off));
-        const float scale = max_nan(old, scale_for<KV>(top));
-        const Divider by(scale);
-        if (s0 > 0 && scale != old) {      // the rows that earlier calls left in the block (a NaN scale is unequal to itself: harmless)
-            const float ratio = by(old);
-            for (int r = half; r < s0; r += 2) {
-                uint2 *at = reinterpret_cast<uint2 *>(pool + kv_row_offset(P, page, c, r) + L.ch);
-                const uint2 codes = *at;
-                float y0[4], y1[4];
-                numbers_of<KV>(codes.x, y0);
-                numbers_of<KV>(codes.y, y1);
-                *at = make_uint2(codes_of<KV>(y0[0] * ratio, y0[1] * ratio, y0[2] * ratio, y0[3] * ratio),
-                                 codes_of<KV>(y1[0] * ratio, y1[1] * ratio, y1[2] * ratio, y1[3] * ratio));
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kPlaceBatch; ++i) {
-            if (2 * i >= n) break;
-            const int r = 2 * i + half;
-            float y[8];
-            turn_row<INTERLEAVED>(w[i], works, gain, ga, gb, L, turns[min(k0 + r, kPlaceWindow - 1)], A.eps, y);
-            if (r < n)
-                *reinterpret_cast<uint2 *>(pool + kv_row_offset(P, page, c, s0 + r) + L.ch) =
-                    make_uint2(codes_of<KV>(by(y[0]), by(y[1]), by(y[2]), by(y[3])), codes_of<KV>(by(y[4]), by(y[5]), by(y[6]), by(y[7])));
-        }
-        if (lane == 0) *scale_at = scale;
     }
 }
 
