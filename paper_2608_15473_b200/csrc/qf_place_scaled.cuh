@@ -16,8 +16,8 @@
 // one request that fall into one page) that BEGIN within its `tile` packed tokens, in passes of at most 16 rows.  Sixteen
 // lanes own a head row (16 bytes each); a warp has two rows, and turns them for one head after the other with the angles and
 // gains in registers: all query heads, or an eighth of them when there is but one token.  For keys and values each warp does
-// four heads at a time, the runs' largest magnitudes meet in shared memory (as integers, so that their order is no matter),
-// and the rows become codes from the registers they were turned in.  gridDim.y splits the KV heads when there are too few
+// two heads at a time, the rows' largest magnitudes meet in shared memory, and the rows become codes from the registers they
+// were turned in.  gridDim.y splits the KV heads when there are too few
 // runs to fill the GPU.
 //
 // Bound: HBM for prompts (256 bytes in per head row, 256 out per query and 128 per key or value), latency for a decode batch.
@@ -99,6 +99,7 @@ __device__ __forceinline__ void numbers_of(uint32_t w, float (&y)[4])
 struct TurnLane {
     int ch, pch, partner;      // first channel, the partners' first channel, the lane of the sixteen that holds them
     bool turns, upper;
+    uint32_t mask;             // all ones where the lane turns: what has no partner must not be reached by another channel's infinity
 };
 // Where a row's table keeps (cos, sin) of pair j, so that the sixteen lanes' 16-byte reads are neighbours: four words of a lane's
 // eight channels in four planes, or, interleaved, its four pairs in two.
@@ -169,10 +170,9 @@ __device__ __forceinline__ void turn_rows(const uint4 (&w)[N], bool works, bool 
         const uint32_t ww[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const unsigned long long px = INTERLEAVED ? swap_pair(y[b][i]) : pair_of_bf16(__shfl_sync(0xffffffffu, ww[i], L.partner, 16));
-            const unsigned long long own = mul_pair(y[b][i], k.own[i]);
-            // channels that do not turn have no partner: an infinity elsewhere must not reach them
-            y[b][i] = L.turns ? fma_pair(px, k.other[i], own) : own;
+            const uint32_t pw = (INTERLEAVED ? ww[i] : __shfl_sync(0xffffffffu, ww[i], L.partner, 16)) & L.mask;
+            const unsigned long long px = INTERLEAVED ? swap_pair(pair_of_bf16(pw)) : pair_of_bf16(pw);
+            y[b][i] = fma_pair(px, k.other[i], mul_pair(y[b][i], k.own[i]));
             if (norm) y[b][i] = mul_pair(y[b][i], pair_of(rs[b], rs[b]));
         }
     }
@@ -195,7 +195,14 @@ __device__ __forceinline__ void store_codes(uint8_t *to, const unsigned long lon
     float v[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) split_pair(y[i], v[2 * i], v[2 * i + 1]);
-    *reinterpret_cast<uint2 *>(to) = make_uint2(codes_of<KV>(by(v[0]), by(v[1]), by(v[2]), by(v[3])), codes_of<KV>(by(v[4]), by(v[5]), by(v[6]), by(v[7])));
+    if (by.power) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= by.inv;
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) v[i] /= by.s;
+    }
+    *reinterpret_cast<uint2 *>(to) = make_uint2(codes_of<KV>(v[0], v[1], v[2], v[3]), codes_of<KV>(v[4], v[5], v[6], v[7]));
 }
 
 template <int KV, bool INTERLEAVED>
@@ -203,9 +210,9 @@ __global__ void __launch_bounds__(kPlaceWarps * 32, 2)
 place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_scale, float *__restrict__ v_scale, int tile,
                     const __grid_constant__ DevParams P)
 {
-    constexpr int kQ = 8, kKv = 4;                      // rows that a warp's half works on at a time: query heads, KV heads
+    constexpr int kQ = 4, kKv = 2;                      // heads that a warp works on at a time, the next ones on their way: of queries, KV heads
     __shared__ __align__(16) float2 turns[kPlaceWarps][2][64];      // (cos, sin) of every pair, of a warp's two tokens
-    __shared__ unsigned tops[2][kPlaceTile][kKv * kPlaceWarps];     // the largest magnitude of keys and values: [side][run][head]
+    __shared__ unsigned tops[2][2][kKv * kPlaceWarps][kPageSize];   // every row's largest magnitude: [turn][keys, values][head][row]
     grid_dependency_wait();
     grid_launch_dependents();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l16 = lane & 15, half = lane >> 4;
@@ -234,17 +241,19 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
     const long long rotary = pos + (b >= 0 && A.pos_base ? A.pos_base[b] : 0);
 
     const int Hkv = P.num_kv_heads, G = P.group, parts = (int)gridDim.y, part = (int)blockIdx.y;
-    const int heads = (Hkv - part + parts - 1) / parts;                  // KV heads part, part + parts, ...
+    const int head0 = (int)((long long)part * Hkv / parts), heads = (int)((long long)(part + 1) * Hkv / parts) - head0;      // this part's KV heads
     const int pairs = A.rotary_dim / 2, half_chunks = A.rotary_dim >> 4;
     TurnLane L;
     L.ch = l16 * 8;
     L.turns = l16 < 2 * half_chunks;
     L.upper = l16 >= half_chunks;
+    L.mask = L.turns ? 0xffffffffu : 0u;
     L.partner = INTERLEAVED || !L.turns ? l16 : L.upper ? l16 - half_chunks : l16 + half_chunks;
     L.pch = L.partner * 8;
 
     // ---- passes of whole runs, at most 16 rows of the window each (nearly always one pass)
     unsigned left = mine;
+    int turn_no = 0;
     while (left) {
         const int lo = __ffs((int)left) - 1;
         int hi = lo;
@@ -266,7 +275,6 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
         const int my_k = min(k, 31), t = t0 + k;
         const int my_slot = __shfl_sync(0xffffffffu, slot, my_k);
         const long long page = __shfl_sync(0xffffffffu, phys, my_k);
-        const int run = __popc(runs & ((2u << my_k) - 1)) - 1;
         const bool leads = live && ((runs >> my_k) & 1);                    // this row is its run's first
         // ---- angles: formed and reduced to a fraction of a turn in fp64 (see qf_rope.cuh)
         __syncwarp();
@@ -294,50 +302,66 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
         if (A.n_q) {
             const bool works = A.q_gain || A.rotary_dim > 0;
             const TurnCoefs co = turn_coefs<INTERLEAVED>(A.q_gain, L, turn);
-            const uint16_t *src = A.q + (long long)t * A.q_stride + L.ch;
-            uint16_t *dst = A.q_out + (long long)t * A.n_q * kHeadDim + L.ch;
-            auto head_of = [&](int i) { const int c = i / G; return (part + c * parts) * G + i - c * G; };
-            for (int i0 = hg; i0 < heads * G; i0 += kQ * hgs) {
-                uint4 w[kQ];
+            const uint16_t *src = A.q + (long long)t * A.q_stride + head0 * G * kHeadDim + L.ch;
+            uint16_t *dst = A.q_out + ((long long)t * A.n_q + head0 * G) * kHeadDim + L.ch;
+            uint4 w[kQ], next[kQ];
+            auto fetch = [&](int i0, uint4 (&to)[kQ]) {
 #pragma unroll
                 for (int n = 0; n < kQ; ++n) {
                     const int i = i0 + n * hgs;
-                    w[n] = make_uint4(0u, 0u, 0u, 0u);
-                    if (live && i < heads * G) w[n] = __ldcs(reinterpret_cast<const uint4 *>(src + head_of(i) * kHeadDim));
+                    to[n] = make_uint4(0u, 0u, 0u, 0u);
+                    if (live && i < heads * G) to[n] = __ldcs(reinterpret_cast<const uint4 *>(src + i * kHeadDim));
                 }
+            };
+            fetch(hg, w);
+#pragma unroll 1
+            for (int i0 = hg; i0 < heads * G; i0 += kQ * hgs) {
+                fetch(i0 + kQ * hgs, next);
 #pragma unroll
-                for (int n4 = 0; n4 < kQ; n4 += 4) {
-                    if (i0 + n4 * hgs >= heads * G) break;
-                    const uint4 wb[4] = {w[n4], w[n4 + 1], w[n4 + 2], w[n4 + 3]};
-                    unsigned long long y[4][4];
-                    turn_rows<INTERLEAVED, 4>(wb, works, A.q_gain != nullptr, co, L, A.eps, y);
+                for (int n2 = 0; n2 < kQ; n2 += 2) {
+                    const uint4 wb[2] = {w[n2], w[n2 + 1]};
+                    unsigned long long y[2][4];
+                    turn_rows<INTERLEAVED, 2>(wb, works, A.q_gain != nullptr, co, L, A.eps, y);
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const int i = i0 + (n4 + n) * hgs;
-                        if (live && i < heads * G) *reinterpret_cast<uint4 *>(dst + head_of(i) * kHeadDim) = bf16_row(y[n]);
+                    for (int n = 0; n < 2; ++n) {
+                        const int i = i0 + (n2 + n) * hgs;
+                        if (live && i < heads * G) *reinterpret_cast<uint4 *>(dst + i * kHeadDim) = bf16_row(y[n]);
                     }
                 }
+#pragma unroll
+                for (int n = 0; n < kQ; ++n) w[n] = next[n];
             }
         }
         if (!A.n_k) continue;
-        // ---- keys and values, a few heads at a time: largest magnitudes of the runs meet in shared memory
+        // ---- keys and values, a few heads at a time: the rows' largest magnitudes meet in shared memory
         const bool works = A.k_gain || A.rotary_dim > 0;
         const TurnCoefs co = turn_coefs<INTERLEAVED>(A.k_gain, L, turn);
-        for (int c0 = 0; c0 < heads; c0 += kKv * hgs) {
-            uint4 kw[kKv], vw[kKv];
-            float k_old[kKv], v_old[kKv];
+        const int first = 31 - __clz((int)(runs & ((2u << my_k) - 1)));      // where this row's run begins
+        const int held = my_slot - (k - first);      // rows of earlier calls in the block: those before the run's first slot
+        // row l16 of the pass belongs to this row's run
+        const bool same = live && lo + l16 >= first && lo + l16 < hi && (31 - __clz((int)(runs & ((2u << (lo + l16)) - 1)))) == first;
+        uint4 kw[kKv], vw[kKv], k_next[kKv], v_next[kKv];
+        float k_old[kKv], v_old[kKv];
+        auto fetch = [&](int c0, uint4 (&to_k)[kKv], uint4 (&to_v)[kKv]) {
 #pragma unroll
             for (int n = 0; n < kKv; ++n) {
-                const int i = c0 + hg + n * hgs, c = part + i * parts;
-                kw[n] = vw[n] = make_uint4(0u, 0u, 0u, 0u);
-                k_old[n] = v_old[n] = 0.f;
+                const int i = c0 + hg + n * hgs, c = head0 + i;
+                to_k[n] = to_v[n] = make_uint4(0u, 0u, 0u, 0u);
                 if (!live || i >= heads) continue;
-                kw[n] = __ldcs(reinterpret_cast<const uint4 *>(A.k + (long long)t * A.k_stride + c * kHeadDim + L.ch));
-                if (A.v) vw[n] = __ldcs(reinterpret_cast<const uint4 *>(A.v + (long long)t * A.v_stride + c * kHeadDim + L.ch));
-                if (page >= 0) { k_old[n] = __ldcg(k_scale + page * Hkv + c); v_old[n] = __ldcg(v_scale + page * Hkv + c); }
+                to_k[n] = __ldcs(reinterpret_cast<const uint4 *>(A.k + (long long)t * A.k_stride + c * kHeadDim + L.ch));
+                if (A.v) to_v[n] = __ldcs(reinterpret_cast<const uint4 *>(A.v + (long long)t * A.v_stride + c * kHeadDim + L.ch));
             }
-            __syncthreads();                                 // the last heads' magnitudes have been read
-            for (int i = tid; i < 2 * kPlaceTile * kKv * kPlaceWarps; i += kPlaceWarps * 32) (&tops[0][0][0])[i] = 0u;
+        };
+        fetch(0, kw, vw);
+#pragma unroll 1
+        for (int c0 = 0; c0 < heads; c0 += kKv * hgs, turn_no ^= 1) {
+            fetch(c0 + kKv * hgs, k_next, v_next);
+#pragma unroll
+            for (int n = 0; n < kKv; ++n) {
+                const int i = c0 + hg + n * hgs, c = head0 + i;
+                k_old[n] = v_old[n] = 0.f;
+                if (live && i < heads && held > 0 && page >= 0) { k_old[n] = __ldcg(k_scale + page * Hkv + c); v_old[n] = __ldcg(v_scale + page * Hkv + c); }
+            }
             unsigned long long y[kKv][4];
             turn_rows<INTERLEAVED, kKv>(kw, works, A.k_gain != nullptr, co, L, A.eps, y);
             float top_k[kKv];
@@ -352,7 +376,7 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
                     top_k[n] = max_nan(top_k[n], max_nan(fabsf(v0), fabsf(v1)));
                 }
                 const uint32_t a = __vmaxu2(__vmaxu2(vw[n].x & 0x7fff7fffu, vw[n].y & 0x7fff7fffu), __vmaxu2(vw[n].z & 0x7fff7fffu, vw[n].w & 0x7fff7fffu));
-                top_v[n] = max(a & 0xffffu, a >> 16) << 16;
+                top_v[n] = max(a & 0xffffu, a >> 16) << 16;      // bits of magnitudes order like the magnitudes, NaN above infinity
             }
 #pragma unroll
             for (int off = 1; off < 16; off <<= 1)
@@ -361,34 +385,45 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
                     top_k[n] = max_nan(top_k[n], __shfl_xor_sync(0xffffffffu, top_k[n], off));
                     top_v[n] = max(top_v[n], __shfl_xor_sync(0xffffffffu, top_v[n], off));
                 }
-            __syncthreads();
-            if (live && l16 == 0) {      // bits of magnitudes order like the magnitudes, NaN above infinity
+            if (live && l16 == 0) {
 #pragma unroll
                 for (int n = 0; n < kKv; ++n) {
-                    atomicMax(&tops[0][run][hg * kKv + n], __float_as_uint(top_k[n]));
-                    atomicMax(&tops[1][run][hg * kKv + n], top_v[n]);
+                    tops[turn_no][0][hg * kKv + n][k - lo] = __float_as_uint(top_k[n]);
+                    tops[turn_no][1][hg * kKv + n][k - lo] = top_v[n];
                 }
             }
             if (A.k_out && live) {
 #pragma unroll
                 for (int n = 0; n < kKv; ++n) {
                     const int i = c0 + hg + n * hgs;
-                    if (i < heads) *reinterpret_cast<uint4 *>(A.k_out + ((long long)t * A.n_k + part + i * parts) * kHeadDim + L.ch) = bf16_row(y[n]);
+                    if (i < heads) *reinterpret_cast<uint4 *>(A.k_out + ((long long)t * A.n_k + head0 + i) * kHeadDim + L.ch) = bf16_row(y[n]);
                 }
             }
-            __syncthreads();
+            __syncthreads();      // (the other half of `tops` is free by now: its readers came before this barrier)
+            unsigned top[2][kKv];
+#pragma unroll
+            for (int n = 0; n < kKv; ++n)
+#pragma unroll
+                for (int side = 0; side < 2; ++side) top[side][n] = same ? tops[turn_no][side][hg * kKv + n][l16] : 0u;
+#pragma unroll
+            for (int off = 1; off < 16; off <<= 1)
+#pragma unroll
+                for (int n = 0; n < kKv; ++n)
+#pragma unroll
+                    for (int side = 0; side < 2; ++side) top[side][n] = max(top[side][n], __shfl_xor_sync(0xffffffffu, top[side][n], off));
+            const uint4 v_now[kKv] = {vw[0], vw[1]};
+#pragma unroll
+            for (int n = 0; n < kKv; ++n) { kw[n] = k_next[n]; vw[n] = v_next[n]; }
             if (!live || page < 0) continue;
-            // rows of earlier calls in the block: those before the run's first slot (this row's slot, where it leads)
-            const int held = my_slot - (k - (31 - __clz((int)(runs & ((2u << my_k) - 1)))));
 #pragma unroll
             for (int n = 0; n < kKv; ++n) {
-                const int i = c0 + hg + n * hgs, c = part + i * parts;
+                const int i = c0 + hg + n * hgs, c = head0 + i;
                 if (i >= heads) break;
 #pragma unroll
                 for (int side = 0; side < 2; ++side) {
                     uint8_t *pool = reinterpret_cast<uint8_t *>(side ? A.v_cache : A.k_cache);
                     const float old = held > 0 ? held_scale(side ? v_old[n] : k_old[n]) : 0.f;
-                    const float scale = max_nan(old, scale_for<KV>(__uint_as_float(tops[side][run][hg * kKv + n])));
+                    const float scale = max_nan(old, scale_for<KV>(__uint_as_float(top[side][n])));
                     const Divider by(scale);
                     if (leads) {
                         if (held > 0 && scale != old) {      // (a NaN scale is unequal to itself: harmless)
@@ -409,7 +444,7 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
                     if (side == 0) {
                         store_codes<KV>(to, y[n], by);
                     } else {
-                        const unsigned long long v[4] = {pair_of_bf16(vw[n].x), pair_of_bf16(vw[n].y), pair_of_bf16(vw[n].z), pair_of_bf16(vw[n].w)};
+                        const unsigned long long v[4] = {pair_of_bf16(v_now[n].x), pair_of_bf16(v_now[n].y), pair_of_bf16(v_now[n].z), pair_of_bf16(v_now[n].w)};
                         store_codes<KV>(to, v, by);
                     }
                 }
