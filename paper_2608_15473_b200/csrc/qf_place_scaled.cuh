@@ -65,9 +65,9 @@ struct Divider {
     }
     __device__ __forceinline__ float operator()(float x) const { return power ? x * inv : x / s; }
 };
-// Four numbers within range -> four codes, ties to even.
+// Four numbers within range -> four codes, ties to even.  (Integers come with 1.5 * 2^23 added, which has rounded them.)
 template <int KV>
-__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
+__device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float d)
 {
     if constexpr (KV == kKvE4m3) {
         uint32_t w;
@@ -75,11 +75,16 @@ __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
             "mov.b32 %0, {lo, hi};\n\t}" : "=r"(w) : "f"(a), "f"(b), "f"(c), "f"(d));
         return w;
     } else {
-        constexpr float kRound = 12582912.f;      // 1.5 * 2^23: the sum's low byte is the rounded integer
-        const uint32_t ab = __byte_perm(__float_as_uint(a + kRound), __float_as_uint(b + kRound), 0x0040);
-        const uint32_t cd = __byte_perm(__float_as_uint(c + kRound), __float_as_uint(d + kRound), 0x0040);
+        const uint32_t ab = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
+        const uint32_t cd = __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040);
         return __byte_perm(ab, cd, 0x5410);
     }
+}
+template <int KV>
+__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
+{
+    constexpr float kRound = KV == kKvInt8 ? 12582912.f : 0.f;
+    return KV == kKvInt8 ? pack_codes<KV>(a + kRound, b + kRound, c + kRound, d + kRound) : pack_codes<KV>(a, b, c, d);
 }
 template <int KV>
 __device__ __forceinline__ void numbers_of(uint32_t w, float (&y)[4])
@@ -95,6 +100,21 @@ __device__ __forceinline__ void numbers_of(uint32_t w, float (&y)[4])
     }
 }
 
+// Magnitudes travel as 16 bits, two to a word (keys low, values high): the upper half of the fp32 number, with the last bit set
+// where the lower half is not 0.  They order like the magnitudes, NaN above infinity, and a scale asks for no more: whether a
+// mantissa is above 1.75 or 127/64, whose lower halves are 0.
+__device__ __forceinline__ unsigned half_of(float x)
+{
+    const unsigned bits = __float_as_uint(x) & 0x7fffffffu;
+    return (bits >> 16) | ((bits & 0xffffu) ? 1u : 0u);
+}
+// The largest of sixteen lanes' pairs.  (By shuffles: a reduction instruction for each half of the warp took longer.)
+__device__ __forceinline__ unsigned max_of_row(unsigned x)
+{
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) x = __vmaxu2(x, __shfl_xor_sync(0xffffffffu, x, off));
+    return x;
+}
 // A lane's eight channels of a head row, and how they turn.  Sixteen lanes own a row, so a warp works on two rows.
 struct TurnLane {
     int ch, pch, partner;      // first channel, the partners' first channel, the lane of the sixteen that holds them
@@ -192,17 +212,22 @@ __device__ __forceinline__ uint4 bf16_row(const unsigned long long (&y)[4])
 template <int KV>
 __device__ __forceinline__ void store_codes(uint8_t *to, const unsigned long long (&y)[4], const Divider &by)
 {
+    constexpr float kRound = 12582912.f;      // 1.5 * 2^23: the sum's low byte is the rounded integer
     float v[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) split_pair(y[i], v[2 * i], v[2 * i + 1]);
     if (by.power) {
+        const unsigned long long inv = pair_of(by.inv, by.inv);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= by.inv;
+        for (int i = 0; i < 4; ++i)      // (a product with a power of two is exact, so the sum rounds once)
+            split_pair(KV == kKvInt8 ? fma_pair(y[i], inv, pair_of(kRound, kRound)) : mul_pair(y[i], inv), v[2 * i], v[2 * i + 1]);
     } else {
-#pragma unroll 1
-        for (int i = 0; i < 8; ++i) v[i] /= by.s;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            split_pair(y[i], v[2 * i], v[2 * i + 1]);
+            v[2 * i] /= by.s; v[2 * i + 1] /= by.s;
+            if (KV == kKvInt8) { v[2 * i] += kRound; v[2 * i + 1] += kRound; }
+        }
     }
-    *reinterpret_cast<uint2 *>(to) = make_uint2(codes_of<KV>(v[0], v[1], v[2], v[3]), codes_of<KV>(v[4], v[5], v[6], v[7]));
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_codes<KV>(v[0], v[1], v[2], v[3]), pack_codes<KV>(v[4], v[5], v[6], v[7]));
 }
 
 template <int KV, bool INTERLEAVED>
@@ -212,7 +237,7 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
 {
     constexpr int kQ = 4, kKv = 2;                      // heads that a warp works on at a time, the next ones on their way: of queries, KV heads
     __shared__ __align__(16) float2 turns[kPlaceWarps][2][64];      // (cos, sin) of every pair, of a warp's two tokens
-    __shared__ unsigned tops[2][2][kKv * kPlaceWarps][kPageSize];   // every row's largest magnitude: [turn][keys, values][head][row]
+    __shared__ unsigned tops[2][kKv * kPlaceWarps][kPageSize];      // every row's largest magnitudes: [turn][head][row]
     grid_dependency_wait();
     grid_launch_dependents();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l16 = lane & 15, half = lane >> 4;
@@ -313,13 +338,10 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
                     if (live && i < heads * G) to[n] = __ldcs(reinterpret_cast<const uint4 *>(src + i * kHeadDim));
                 }
             };
-            fetch(hg, w);
-#pragma unroll 1
-            for (int i0 = hg; i0 < heads * G; i0 += kQ * hgs) {
-                fetch(i0 + kQ * hgs, next);
+            auto finish = [&](int i0, const uint4 (&from)[kQ]) {
 #pragma unroll
                 for (int n2 = 0; n2 < kQ; n2 += 2) {
-                    const uint4 wb[2] = {w[n2], w[n2 + 1]};
+                    const uint4 wb[2] = {from[n2], from[n2 + 1]};
                     unsigned long long y[2][4];
                     turn_rows<INTERLEAVED, 2>(wb, works, A.q_gain != nullptr, co, L, A.eps, y);
 #pragma unroll
@@ -328,8 +350,15 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
                         if (live && i < heads * G) *reinterpret_cast<uint4 *>(dst + i * kHeadDim) = bf16_row(y[n]);
                     }
                 }
-#pragma unroll
-                for (int n = 0; n < kQ; ++n) w[n] = next[n];
+            };
+            fetch(hg, w);
+#pragma unroll 1
+            for (int i0 = hg; i0 < heads * G; i0 += 2 * kQ * hgs) {
+                fetch(i0 + kQ * hgs, next);
+                finish(i0, w);
+                if (i0 + kQ * hgs >= heads * G) break;
+                fetch(i0 + 2 * kQ * hgs, w);
+                finish(i0 + kQ * hgs, next);
             }
         }
         if (!A.n_k) continue;
@@ -341,56 +370,47 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
         // row l16 of the pass belongs to this row's run
         const bool same = live && lo + l16 >= first && lo + l16 < hi && (31 - __clz((int)(runs & ((2u << (lo + l16)) - 1)))) == first;
         uint4 kw[kKv], vw[kKv], k_next[kKv], v_next[kKv];
-        float k_old[kKv], v_old[kKv];
+        const uint16_t *k_src = A.k + (long long)t * A.k_stride + head0 * kHeadDim + L.ch, *v_src = A.v + (long long)t * A.v_stride + head0 * kHeadDim + L.ch;
+        const size_t row_at = kv_row_offset(P, page < 0 ? 0 : page, head0, my_slot) + L.ch, scale_at = (size_t)(page < 0 ? 0 : page) * Hkv + head0;
+        uint8_t *k_row = reinterpret_cast<uint8_t *>(A.k_cache) + row_at, *v_row = reinterpret_cast<uint8_t *>(A.v_cache) + row_at;
+        float *ks_at = k_scale + scale_at, *vs_at = v_scale + scale_at;
+        const int head_step = P.kv_nhd ? kHeadDim : kPageElems, row_step = P.kv_nhd ? Hkv * kHeadDim : kHeadDim;
+        const bool placed = live && page >= 0;
         auto fetch = [&](int c0, uint4 (&to_k)[kKv], uint4 (&to_v)[kKv]) {
 #pragma unroll
             for (int n = 0; n < kKv; ++n) {
-                const int i = c0 + hg + n * hgs, c = head0 + i;
+                const int i = c0 + hg + n * hgs;
                 to_k[n] = to_v[n] = make_uint4(0u, 0u, 0u, 0u);
                 if (!live || i >= heads) continue;
-                to_k[n] = __ldcs(reinterpret_cast<const uint4 *>(A.k + (long long)t * A.k_stride + c * kHeadDim + L.ch));
-                if (A.v) to_v[n] = __ldcs(reinterpret_cast<const uint4 *>(A.v + (long long)t * A.v_stride + c * kHeadDim + L.ch));
+                to_k[n] = __ldcs(reinterpret_cast<const uint4 *>(k_src + i * kHeadDim));
+                if (A.v) to_v[n] = __ldcs(reinterpret_cast<const uint4 *>(v_src + i * kHeadDim));
             }
         };
         fetch(0, kw, vw);
 #pragma unroll 1
         for (int c0 = 0; c0 < heads; c0 += kKv * hgs, turn_no ^= 1) {
             fetch(c0 + kKv * hgs, k_next, v_next);
+            float old_k[kKv], old_v[kKv];      // the scales that earlier calls left with the block, if they left rows
 #pragma unroll
             for (int n = 0; n < kKv; ++n) {
-                const int i = c0 + hg + n * hgs, c = head0 + i;
-                k_old[n] = v_old[n] = 0.f;
-                if (live && i < heads && held > 0 && page >= 0) { k_old[n] = __ldcg(k_scale + page * Hkv + c); v_old[n] = __ldcg(v_scale + page * Hkv + c); }
+                const int i = c0 + hg + n * hgs;
+                old_k[n] = old_v[n] = 0.f;
+                if (placed && held > 0 && i < heads) { old_k[n] = __ldcg(ks_at + i); old_v[n] = __ldcg(vs_at + i); }
             }
             unsigned long long y[kKv][4];
             turn_rows<INTERLEAVED, kKv>(kw, works, A.k_gain != nullptr, co, L, A.eps, y);
-            float top_k[kKv];
-            unsigned top_v[kKv];
 #pragma unroll
             for (int n = 0; n < kKv; ++n) {
-                top_k[n] = 0.f;
+                float top = 0.f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float v0, v1;
                     split_pair(y[n][e], v0, v1);
-                    top_k[n] = max_nan(top_k[n], max_nan(fabsf(v0), fabsf(v1)));
+                    top = max3_nan(top, fabsf(v0), fabsf(v1));
                 }
                 const uint32_t a = __vmaxu2(__vmaxu2(vw[n].x & 0x7fff7fffu, vw[n].y & 0x7fff7fffu), __vmaxu2(vw[n].z & 0x7fff7fffu, vw[n].w & 0x7fff7fffu));
-                top_v[n] = max(a & 0xffffu, a >> 16) << 16;      // bits of magnitudes order like the magnitudes, NaN above infinity
-            }
-#pragma unroll
-            for (int off = 1; off < 16; off <<= 1)
-#pragma unroll
-                for (int n = 0; n < kKv; ++n) {
-                    top_k[n] = max_nan(top_k[n], __shfl_xor_sync(0xffffffffu, top_k[n], off));
-                    top_v[n] = max(top_v[n], __shfl_xor_sync(0xffffffffu, top_v[n], off));
-                }
-            if (live && l16 == 0) {
-#pragma unroll
-                for (int n = 0; n < kKv; ++n) {
-                    tops[turn_no][0][hg * kKv + n][k - lo] = __float_as_uint(top_k[n]);
-                    tops[turn_no][1][hg * kKv + n][k - lo] = top_v[n];
-                }
+                const unsigned both = max_of_row(half_of(top) | (__vmaxu2(a, a << 16) & 0xffff0000u));
+                if (live && l16 == 0) tops[turn_no][hg * kKv + n][k - lo] = both;
             }
             if (A.k_out && live) {
 #pragma unroll
@@ -400,36 +420,28 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
                 }
             }
             __syncthreads();      // (the other half of `tops` is free by now: its readers came before this barrier)
-            unsigned top[2][kKv];
+            unsigned top[kKv];
 #pragma unroll
-            for (int n = 0; n < kKv; ++n)
-#pragma unroll
-                for (int side = 0; side < 2; ++side) top[side][n] = same ? tops[turn_no][side][hg * kKv + n][l16] : 0u;
-#pragma unroll
-            for (int off = 1; off < 16; off <<= 1)
-#pragma unroll
-                for (int n = 0; n < kKv; ++n)
-#pragma unroll
-                    for (int side = 0; side < 2; ++side) top[side][n] = max(top[side][n], __shfl_xor_sync(0xffffffffu, top[side][n], off));
+            for (int n = 0; n < kKv; ++n) top[n] = max_of_row(same ? tops[turn_no][hg * kKv + n][l16] : 0u);
             const uint4 v_now[kKv] = {vw[0], vw[1]};
 #pragma unroll
             for (int n = 0; n < kKv; ++n) { kw[n] = k_next[n]; vw[n] = v_next[n]; }
-            if (!live || page < 0) continue;
+            if (!placed) continue;
 #pragma unroll
             for (int n = 0; n < kKv; ++n) {
-                const int i = c0 + hg + n * hgs, c = head0 + i;
+                const int i = c0 + hg + n * hgs;
                 if (i >= heads) break;
 #pragma unroll
                 for (int side = 0; side < 2; ++side) {
-                    uint8_t *pool = reinterpret_cast<uint8_t *>(side ? A.v_cache : A.k_cache);
-                    const float old = held > 0 ? held_scale(side ? v_old[n] : k_old[n]) : 0.f;
-                    const float scale = max_nan(old, scale_for<KV>(__uint_as_float(top[side][n])));
+                    const float old = held > 0 ? held_scale(side ? old_v[n] : old_k[n]) : 0.f;
+                    const float scale = max_nan(old, scale_for<KV>(__uint_as_float(side ? top[n] & 0xffff0000u : top[n] << 16)));
                     const Divider by(scale);
+                    uint8_t *to = (side ? v_row : k_row) + (size_t)i * head_step;
                     if (leads) {
                         if (held > 0 && scale != old) {      // (a NaN scale is unequal to itself: harmless)
                             const float ratio = by(old);
-                            for (int r = 0; r < held; ++r) {
-                                uint2 *at = reinterpret_cast<uint2 *>(pool + kv_row_offset(P, page, c, r) + L.ch);
+                            for (int r = 1; r <= held; ++r) {
+                                uint2 *at = reinterpret_cast<uint2 *>(to - (size_t)r * row_step);
                                 const uint2 codes = *at;
                                 float y0[4], y1[4];
                                 numbers_of<KV>(codes.x, y0);
@@ -438,9 +450,8 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
                                                  codes_of<KV>(y1[0] * ratio, y1[1] * ratio, y1[2] * ratio, y1[3] * ratio));
                             }
                         }
-                        if (l16 == 0) (side ? v_scale : k_scale)[page * Hkv + c] = scale;
+                        if (l16 == 0) (side ? vs_at : ks_at)[i] = scale;
                     }
-                    uint8_t *to = pool + kv_row_offset(P, page, c, my_slot) + L.ch;
                     if (side == 0) {
                         store_codes<KV>(to, y[n], by);
                     } else {
@@ -462,7 +473,7 @@ inline cudaError_t launch_place_scaled(const RopeArgs &A, float *k_scale, float 
     while (tile < kPlaceTile && (long long)A.total_tokens >= 2ll * tile * P.batch) tile *= 2;
     const long long tiles = ((long long)A.total_tokens + tile - 1) / tile;
     int parts = 1;
-    while (parts < P.num_kv_heads && tiles * parts < 8ll * sms) parts *= 2;
+    while (parts < P.num_kv_heads && tiles * parts < 2ll * sms) parts *= 2;
     if (parts > P.num_kv_heads) parts = P.num_kv_heads;
     auto kernel = A.interleaved ? place_scaled_kernel<KV, true> : place_scaled_kernel<KV, false>;
     return launch_pdl(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(kPlaceWarps * 32), 0, st, A, k_scale, v_scale, tile, P);

@@ -376,12 +376,6 @@ __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigne
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ float max3_nan(float a, float b, float c)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
 // 2^x for a pair, on the multiply-add units (the special-function unit makes 16 exponentials per SM and cycle, which
 // is what bounds a softmax): x = n + f with n the nearest integer (added into the low mantissa bits of 1.5 * 2^23),
 // 2^f on [-1/2, 1/2] by a polynomial whose largest relative error is least among those with p(0) = 1 (linear program
