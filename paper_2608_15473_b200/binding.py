@@ -546,14 +546,17 @@ def rope_pair_axes(rotary_dim: int, sections, interleaved: bool = False):
     return out
 
 
-def _num_axes(positions, num_axes: Optional[int]) -> int:
-    """Axes of a [num_axes, tokens] array, unless the caller (who may pass an address) says."""
-    if num_axes is not None:
+def _num_axes(positions, num_axes: Optional[int], total_tokens: int) -> int:
+    """Axes of a [num_axes, total_tokens] tensor, or what the caller, who may pass an address, says."""
+    if positions is None:
+        return 0 if num_axes is None else int(num_axes)
+    if isinstance(positions, int):
+        if num_axes is None:
+            raise ValueError("num_axes is needed: an address does not tell")
         return int(num_axes)
-    if positions is None or isinstance(positions, int):
-        return 0 if positions is None else 1
-    if positions.dim() != 2 or not positions.is_contiguous():
-        raise ValueError(f"positions: expected a contiguous [num_axes, tokens] tensor, got {tuple(positions.shape)}")
+    if positions.dim() != 2 or not positions.is_contiguous() or positions.shape[1] != total_tokens or \
+            num_axes not in (None, positions.shape[0]):
+        raise ValueError(f"positions: expected a contiguous [{num_axes or 'num_axes'}, {total_tokens}] tensor, got {tuple(positions.shape)}")
     return int(positions.shape[0])
 
 
@@ -564,9 +567,7 @@ def rope_append_axes(q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_to
     [rotary_dim / 2] (rope_pair_axes makes it)."""
     at = _arrays("bbbbbbbiiiiibbf", q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, positions,
                  pair_axis, q_gain, k_gain, inv_freq)
-    if hasattr(positions, "shape") and positions.shape[-1] < r.total_tokens:
-        raise ValueError(f"positions: {positions.shape[-1]} tokens, but total_tokens is {r.total_tokens}")
-    rc = lib().qf_rope_append_axes(*at[:12], _num_axes(positions, num_axes), *at[12:], ctypes.byref(p), ctypes.byref(r), _stream(stream))
+    rc = lib().qf_rope_append_axes(*at[:12], _num_axes(positions, num_axes, r.total_tokens), *at[12:], ctypes.byref(p), ctypes.byref(r), _stream(stream))
     if check and rc != QF_OK:
         raise QFError(rc, "qf_rope_append_axes")
     return rc
@@ -583,6 +584,8 @@ def _kv_type(kv_type: Optional[int], *pools) -> int:
         if said is not None and said != of:
             raise ValueError(f"a pool of {name} does not hold codes of kv_type {said}")
         said = of
+    if said is None and all(x is None for x in pools):
+        said = QF_KV_E4M3      # no cache, no codes
     if said is None:
         raise ValueError("kv_type is needed: the pools' element type does not tell e4m3 from int8")
     return int(said)
@@ -595,9 +598,7 @@ def rope_append_scaled(q, k, v, q_out, k_out, k_cache, v_cache, k_scale, v_scale
     which the call keeps up to date."""
     at = _arrays("bbbbbccffiiiiiibbf", q, k, v, q_out, k_out, k_cache, v_cache, k_scale, v_scale, block_table, cu_tokens, seq_lens,
                  pos_base, positions, pair_axis, q_gain, k_gain, inv_freq)
-    if hasattr(positions, "shape") and positions.shape[-1] < r.total_tokens:
-        raise ValueError(f"positions: {positions.shape[-1]} tokens, but total_tokens is {r.total_tokens}")
-    rc = lib().qf_rope_append_scaled(*at[:15], _num_axes(positions, num_axes), *at[15:], _kv_type(kv_type, k_cache, v_cache),
+    rc = lib().qf_rope_append_scaled(*at[:15], _num_axes(positions, num_axes, r.total_tokens), *at[15:], _kv_type(kv_type, k_cache, v_cache),
                                      ctypes.byref(p), ctypes.byref(r), _stream(stream))
     if check and rc != QF_OK:
         raise QFError(rc, "qf_rope_append_scaled")
