@@ -53,6 +53,11 @@ __device__ __forceinline__ void mul_two(float &a0, float &a1, float f0, float f1
     asm("{\n\t.reg .b64 a, f;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 f, {%2, %3};\n\tmul.rn.f32x2 a, a, f;\n\tmov.b64 {%0, %1}, a;\n\t}"
         : "+f"(a0), "+f"(a1) : "f"(f0), "f"(f1));
 }
+__device__ __forceinline__ void add_two(float &a0, float &a1, float f)
+{
+    asm("{\n\t.reg .b64 a, f;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 f, {%2, %2};\n\tadd.rn.f32x2 a, a, f;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(a0), "+f"(a1) : "f"(f));
+}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
     uint32_t w;

@@ -66,6 +66,8 @@ constexpr int kTilePages = kRowTile / kPageSize;
 constexpr int kUnit = 64;                        // positions of one product S = Q K^T and of one softmax pass
 // A scaled cache has four more warps, which expand tiles of codes to bf16 on their way into the ring, and two tiles of codes in
 // flight in the place of one in the ring.
+// (512 threads leave 128 registers each, enough for the softmax loop; moving registers to its warps with setmaxnreg made the same
+// kernel 11 % slower.)
 template <int KV> constexpr int kRowsThreads = (KV == kKvBf16 ? 12 : 16) * 32;
 template <int KV> constexpr int kRowsRing = KV == kKvBf16 ? 5 : 4;      // K and V tiles in flight or in use
 constexpr int kRawTiles = 2;
@@ -612,15 +614,14 @@ static __device__ QF_COLD void clean_tile(uint8_t *v, int exist, int seen_by_all
 
 struct RowsMaps { CUtensorMap q, k, v; };
 
-// Sixteen codes of one row -> sixteen bf16 numbers, code * scale (exact for a power of two, else rounded once), in two words of
-// eight channels; the words come in the order (swap, 1 - swap).
+// Eight codes -> eight bf16 numbers, code * scale (exact for a power of two, else rounded once).
 template <int KV>
-__device__ __forceinline__ void expand_codes(uint4 codes, float scale, bool swap, uint4 &first, uint4 &second)
+__device__ __forceinline__ uint4 expand_codes(uint32_t w0, uint32_t w1, float scale)
 {
-    const uint32_t in[4] = {swap ? codes.z : codes.x, swap ? codes.w : codes.y, swap ? codes.x : codes.z, swap ? codes.y : codes.w};
-    uint32_t out[8];
+    const uint32_t in[2] = {w0, w1};
+    uint32_t out[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
         float x[4];
         if constexpr (KV == kKvE4m3) {
             uint32_t lo, hi;
@@ -630,38 +631,44 @@ __device__ __forceinline__ void expand_codes(uint4 codes, float scale, bool swap
         } else {
             const uint32_t u = in[i] ^ 0x80808080u;      // code + 128 as the low mantissa byte of 2^23: the difference is exact
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650 + e)) - 8388736.f;
+            for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650 + e));
+            add_two(x[0], x[1], -8388736.f);
+            add_two(x[2], x[3], -8388736.f);
         }
         mul_two(x[0], x[1], scale, scale);
         mul_two(x[2], x[3], scale, scale);
         out[2 * i] = pack_bf16(x[0], x[1]);
         out[2 * i + 1] = pack_bf16(x[2], x[3]);
     }
-    first = make_uint4(out[0], out[1], out[2], out[3]);
-    second = make_uint4(out[4], out[5], out[6], out[7]);
+    return make_uint4(out[0], out[1], out[2], out[3]);
 }
 __device__ __forceinline__ void st_shared_16(uint32_t addr, const uint4 &v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-// A quarter of a tile (two pages) by one warp.  raw: the quarter's codes; tile: the ring's slot.  Eight lanes share a row, sixteen
-// channels each; lanes of the upper half of the channels write their words in the other order, so that the eight words of a
-// row that are written together lie in eight different bank groups.
+// A quarter of a tile (two pages) by one warp.  raw: the quarter's codes; tile: the ring's slot.  Eight lanes share two rows, sixteen
+// channels each: four lanes the first half of one, four the second half of the other, whose swizzle differs in the last bit,
+// so that the eight words that are written together lie in eight different bank groups.  A tile's 128 x 128 numbers are 360
+// instructions of each of the four warps, and what bounds this form: without the arithmetic a prompt takes as long as in bf16.
+// (Sign, exponent and mantissa put in place by integer operations and a product with 2^120 * scale took longer.)
 template <int KV>
 __device__ __forceinline__ void expand_quarter(uint32_t raw, uint32_t tile, int quarter, bool is_v, float s0, float s1)
 {
-    const int lane = threadIdx.x & 31, c16 = lane & 7, half = c16 >> 2;
+    const int lane = threadIdx.x & 31, c16 = lane & 7, half = c16 >> 2, r = (lane >> 3) ^ half;
     const int half_step = is_v ? kHalfPageBytes : kTileBytes / 2, page_step = is_v ? kPageBytes : kPageSize * 128;
-#pragma unroll 4
-    for (int it = 0; it < 8; ++it) {
-        const int row = 4 * (it & 3) + (lane >> 3);
-        const uint4 codes = ld_shared_16(raw + it * 512 + lane * 16);
-        uint4 a, b;
-        expand_codes<KV>(codes, it < 4 ? s0 : s1, half != 0, a, b);
-        const uint32_t at = tile + (2 * quarter + (it >> 2)) * page_step + half * half_step + row * 128;
-        const int ch = 2 * (c16 & 3);
-        st_shared_16(at + (((ch + half) ^ (row & 7)) << 4), a);
-        st_shared_16(at + (((ch + 1 - half) ^ (row & 7)) << 4), b);
+    // rows r, r + 4, ...: the swizzle of every other one differs in bit 2 of the word's place
+    const uint32_t to = tile + 2 * quarter * page_step + half * half_step + r * 128, at = ((2 * (c16 & 3)) ^ r) << 4;
+    const uint32_t from = raw + r * 128 + c16 * 16;
+#pragma unroll 1
+    for (int page = 0; page < 2; ++page) {
+        const float scale = page ? s1 : s0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 codes = ld_shared_16(from + page * kScaledPageBytes + i * 512);
+            const uint32_t row = to + page * page_step + i * 512, word = at ^ ((i & 1) << 6);
+            st_shared_16(row + word, expand_codes<KV>(codes.x, codes.y, scale));
+            st_shared_16(row + (word ^ 16), expand_codes<KV>(codes.z, codes.w, scale));
+        }
     }
 }
 
@@ -841,11 +848,6 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&sm.tmem_base);
     const uint32_t t_s0 = tmem, t_o0 = tmem + 256;      // S (and P over it) of the two groups, then their O
 
-    // 512 threads start with 128 registers each; a softmax thread needs 160, the others fewer: 256 * 168 + 256 * 88 = 65,536
-    if constexpr (KV != kKvBf16) {
-        if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-    }
     if (!working) {
         if (tid == 0) { records[me].has_tail = 0; records[me].head_state = 0; }
     } else if (KV != kKvBf16 && warp >= 12) {
