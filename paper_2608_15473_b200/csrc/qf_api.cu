@@ -219,7 +219,7 @@ int sweep(const void *q, const void *k_cache, const void *v_cache, const ScaledK
     const size_t need = qf_workspace_bytes(p);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return QF_ERR_WORKSPACE;
     if (((uintptr_t)k_cache & 127) || ((uintptr_t)v_cache & 127) || ((uintptr_t)q & 15)) return QF_ERR_BAD_SHAPE;
-    if (scaled && (((uintptr_t)scaled->k_scale & 3) || ((uintptr_t)scaled->v_scale & 3))) return QF_ERR_BAD_SHAPE;
+    if (scaled && (((uintptr_t)scaled->k_scale & 3) || ((uintptr_t)scaled->v_scale & 3) || ((uintptr_t)o_part & 15))) return QF_ERR_BAD_SHAPE;
     int sms = 0;
     rc = check_device(&sms);
     if (rc != QF_OK) return rc;

@@ -614,8 +614,14 @@ static __device__ QF_COLD void clean_tile(uint8_t *v, int exist, int seen_by_all
 
 struct RowsMaps { CUtensorMap q, k, v; };
 
-// Eight codes -> eight bf16 numbers, code * scale (exact for a power of two, else rounded once).
-template <int KV>
+// Eight codes -> eight bf16 numbers, code * scale (exact for a power of two, else rounded once).  HANDY (e4m3): the scale is a
+// power of two within f16's range, and is applied by the instruction that widens a code.
+__device__ __forceinline__ bool handy_scale(float s)
+{
+    const unsigned bits = __float_as_uint(s);
+    return (bits & 0x807fffffu) == 0 && bits >= (113u << 23) && bits <= (142u << 23);      // 2^-14 .. 2^15
+}
+template <int KV, bool HANDY>
 __device__ __forceinline__ uint4 expand_codes(uint32_t w0, uint32_t w1, float scale)
 {
     const uint32_t in[2] = {w0, w1};
@@ -626,17 +632,27 @@ __device__ __forceinline__ uint4 expand_codes(uint32_t w0, uint32_t w1, float sc
         if constexpr (KV == kKvE4m3) {
             uint32_t lo, hi;
             halves_of<KV, false>(in[i], lo, hi);
-            unpack_f16(lo, x[0], x[1]);
-            unpack_f16(hi, x[2], x[3]);
+            if (HANDY) {
+                const uint32_t f = pack_f16(scale, scale);
+                asm("{\n\t.reg .b16 a, b, s, z;\n\tmov.b32 {a, b}, %2;\n\tmov.b32 {s, z}, %3;\n\tfma.rn.f32.f16 %0, a, s, %4;\n\tfma.rn.f32.f16 %1, b, s, %4;\n\t}"
+                    : "=f"(x[0]), "=f"(x[1]) : "r"(lo), "r"(f), "f"(0.f));
+                asm("{\n\t.reg .b16 a, b, s, z;\n\tmov.b32 {a, b}, %2;\n\tmov.b32 {s, z}, %3;\n\tfma.rn.f32.f16 %0, a, s, %4;\n\tfma.rn.f32.f16 %1, b, s, %4;\n\t}"
+                    : "=f"(x[2]), "=f"(x[3]) : "r"(hi), "r"(f), "f"(0.f));
+            } else {
+                unpack_f16(lo, x[0], x[1]);
+                unpack_f16(hi, x[2], x[3]);
+                mul_two(x[0], x[1], scale, scale);
+                mul_two(x[2], x[3], scale, scale);
+            }
         } else {
             const uint32_t u = in[i] ^ 0x80808080u;      // code + 128 as the low mantissa byte of 2^23: the difference is exact
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650 + e));
             add_two(x[0], x[1], -8388736.f);
             add_two(x[2], x[3], -8388736.f);
+            mul_two(x[0], x[1], scale, scale);
+            mul_two(x[2], x[3], scale, scale);
         }
-        mul_two(x[0], x[1], scale, scale);
-        mul_two(x[2], x[3], scale, scale);
         out[2 * i] = pack_bf16(x[0], x[1]);
         out[2 * i + 1] = pack_bf16(x[2], x[3]);
     }
@@ -662,12 +678,23 @@ __device__ __forceinline__ void expand_quarter(uint32_t raw, uint32_t tile, int 
 #pragma unroll 1
     for (int page = 0; page < 2; ++page) {
         const float scale = page ? s1 : s0;
+        const uint32_t src = from + page * kScaledPageBytes, dst = to + page * page_step;
+        if (KV == kKvE4m3 && handy_scale(scale)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 codes = ld_shared_16(from + page * kScaledPageBytes + i * 512);
-            const uint32_t row = to + page * page_step + i * 512, word = at ^ ((i & 1) << 6);
-            st_shared_16(row + word, expand_codes<KV>(codes.x, codes.y, scale));
-            st_shared_16(row + (word ^ 16), expand_codes<KV>(codes.z, codes.w, scale));
+            for (int i = 0; i < 4; ++i) {
+                const uint4 codes = ld_shared_16(src + i * 512);
+                const uint32_t word = at ^ ((i & 1) << 6);
+                st_shared_16(dst + i * 512 + word, expand_codes<KV, true>(codes.x, codes.y, scale));
+                st_shared_16(dst + i * 512 + (word ^ 16), expand_codes<KV, true>(codes.z, codes.w, scale));
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                const uint4 codes = ld_shared_16(src + i * 512);
+                const uint32_t word = at ^ ((i & 1) << 6);
+                st_shared_16(dst + i * 512 + word, expand_codes<KV, false>(codes.x, codes.y, scale));
+                st_shared_16(dst + i * 512 + (word ^ 16), expand_codes<KV, false>(codes.z, codes.w, scale));
+            }
         }
     }
 }

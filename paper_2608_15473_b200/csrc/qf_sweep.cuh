@@ -51,7 +51,10 @@ template <int KV> constexpr int kPagesPerStage = KV == kKvBf16 ? kConsumerWarps 
 // A scaled cache's pages are half as long, so there are twice as many copies per byte, and one thread cannot issue them fast
 // enough: one more warp issues the copies of K, one those of V, from the places that the producer leaves in shared memory.
 template <int KV> constexpr int kIssuers = KV == kKvBf16 ? 0 : 2;
-template <int KV> constexpr int kSweepThreads = (kConsumerWarps + 1 + kIssuers<KV>) * 32;
+// With up to four heads per group (one round of red_acc) one more warp merges the consumer warps' states at the end of a range, while
+// they go on with the next (256 requests of 500 tokens 76 -> 73 us; with two rounds the second waits for the first, 63 -> 65 us).
+template <int G, int KV> constexpr int kMergers = KV != kKvBf16 && G <= 4 ? 1 : 0;
+template <int G, int KV> constexpr int kSweepThreads = (kConsumerWarps + 1 + kIssuers<KV> + kMergers<G, KV>) * 32;
 constexpr int kStages        = 3;                 // 3 x 64 KB of K and V in flight per SM
 template <int KV> constexpr int kPageBlockBytes = KV == kKvBf16 ? kPageBytes : kScaledPageBytes;
 constexpr int kMaxSweepCtas  = 160;               // persistent CTAs (one per SM) are capped at this
@@ -251,7 +254,7 @@ struct SweepSmem {
     alignas(16) uint16_t q[kStages][G * kHeadDim];
     static constexpr int kRoundHeads = G < 4 ? G : 4;  // heads merged per epilogue round
     alignas(16) float red_acc[kConsumerWarps][kRoundHeads][kRedStride];
-    alignas(16) float red_ml[kConsumerWarps][G][2];
+    alignas(16) float red_ml[kConsumerWarps][G][2];   // [maximum, sum]
     alignas(16) StageMeta meta[kStages];
     alignas(8) unsigned long long full_bar[kStages];
     alignas(8) unsigned long long empty_bar[kStages];
@@ -259,15 +262,17 @@ struct SweepSmem {
     alignas(16) float scales[kStages][2][kPagesPerStage<KV>];
     alignas(16) int at[kStages][kPagesPerStage<KV>];
     alignas(8) unsigned long long issue_bar[kStages];
+    alignas(8) unsigned long long merge_full, merge_empty;
+    int merge_entry, merge_head, merge_slot, merge_info;      // the range in red_acc: info = segments of its unit << 8 | round of heads
     alignas(8) unsigned long long red_bar[2];
     int abort_flag;
     unsigned long long epoch;   // this launch's epoch, read once per CTA
-    int scan_ws[kSweepThreads<KV> / 32];
+    int scan_ws[kSweepThreads<G, KV> / 32];
     int prefix[kMaxSmemEntries + 1];
 };
 
 template <int G, int KV>
-__global__ void __launch_bounds__(kSweepThreads<KV>, 1)
+__global__ void __launch_bounds__(kSweepThreads<G, KV>, 1)
 sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
              const uint16_t *__restrict__ q, const int *__restrict__ block_table,
              const int *__restrict__ seq_lens, const int *__restrict__ shard_ranges,
@@ -293,6 +298,10 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             mbar_init(smem_u32(&sm.full_bar[s]), KV == kKvBf16 ? 1 : 33);
             mbar_init(smem_u32(&sm.empty_bar[s]), kConsumerWarps);
             if (KV != kKvBf16) mbar_init(smem_u32(&sm.issue_bar[s]), 1);
+        }
+        if (KV != kKvBf16) {
+            mbar_init(smem_u32(&sm.merge_full), kConsumerWarps);
+            mbar_init(smem_u32(&sm.merge_empty), 1);
         }
         mbar_init(smem_u32(&sm.red_bar[0]), kConsumerWarps);
         mbar_init(smem_u32(&sm.red_bar[1]), kConsumerWarps);
@@ -345,7 +354,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
     const unsigned long long epoch = sm.epoch;   // written before the plan's barriers
     if (P.check_bounds && blockIdx.x == 0) {
         // a cached length that the request's block-table row cannot address was clamped by the plan: report it
-        for (int b = tid; b < P.batch; b += kSweepThreads<KV>)
+        for (int b = tid; b < P.batch; b += kSweepThreads<G, KV>)
             if (seq_lens[b] > max_tokens) epoch_or(header + kHdrStatus, epoch, kStatusBadPage);
     }
     const int total = prefix[n_entries];
@@ -549,6 +558,59 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         return;
     }
 
+    const float kLn2 = 0.6931471805599453f;
+    if constexpr (kMergers<G, KV> > 0) {
+        if (warp == kConsumerWarps + 1 + kIssuers<KV>) {
+            // ============================ merging warp (scaled cache) ============================
+            constexpr int RG = SweepSmem<G, KV>::kRoundHeads;
+            for (uint32_t ph = 0;; ph ^= 1) {
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.merge_full), ph, abort_flag))) break;
+                if (sm.merge_entry < 0) break;
+                const int hr = sm.merge_info & 0xff, nseg = sm.merge_info >> 8;
+                const size_t out_row = out_entry(P, sm.merge_entry) * Hq + (size_t)sm.merge_head * G;
+                float *seg_slot = seg + (size_t)sm.merge_slot * seg_stride;
+#pragma unroll 1
+                for (int hl = 0; hl < RG && hr * RG + hl < G; ++hl) {
+                    const int head = hr * RG + hl;
+                    float M = neg_inf(), z = 0.f, ew[kConsumerWarps];
+                    float2 ml[kConsumerWarps];
+#pragma unroll
+                    for (int w = 0; w < kConsumerWarps; ++w) {
+                        ml[w] = *reinterpret_cast<const float2 *>(sm.red_ml[w][head]);
+                        M = fmaxf(M, ml[w].x);
+                    }
+                    const float Ms = (M == neg_inf()) ? 0.f : M;
+                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < kConsumerWarps; ++w) {
+                        ew[w] = fast_exp2(ml[w].x - Ms);
+                        z = fmaf(ml[w].y, ew[w], z);
+                        const float4 x = *reinterpret_cast<const float4 *>(&sm.red_acc[w][hl][4 * lane]);
+                        sum.x = fmaf(x.x, ew[w], sum.x); sum.y = fmaf(x.y, ew[w], sum.y);
+                        sum.z = fmaf(x.z, ew[w], sum.z); sum.w = fmaf(x.w, ew[w], sum.w);
+                    }
+                    const bool empty = M == neg_inf() && z == 0.f;   // scores that are all NaN leave M, not z
+                    if (nseg == 1) {
+                        const float inv = empty ? 0.f : 1.f / z;
+                        reinterpret_cast<float4 *>(o_part + (out_row + head) * kHeadDim)[lane] = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+                        if (lane == 0) {
+                            m_part[out_row + head] = empty ? neg_inf() : M * kLn2;
+                            lse_part[out_row + head] = empty ? neg_inf() : (M + log2f(z)) * kLn2;
+                        }
+                    } else {
+                        __stcg(reinterpret_cast<float4 *>(seg_slot + head * kHeadDim) + lane, sum);
+                        if (lane == 0) {
+                            __stcg(seg_slot + G * kHeadDim + 2 * head, M);
+                            __stcg(seg_slot + G * kHeadDim + 2 * head + 1, z);
+                        }
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm.merge_empty));
+            }
+            return;
+        }
+    }
     if constexpr (kIssuers<KV> > 0) {
         if (warp > kConsumerWarps) {
             // ============================ issuing warps (scaled cache) ============================
@@ -591,7 +653,6 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
 
     const int g = lane >> 2, t = lane & 3;
     const float scale2 = P.sm_scale * 1.4426950408889634f;  // scores are kept in units of log 2
-    const float kLn2 = 0.6931471805599453f;
     uint32_t qf[8][2];
     float qs[2] = {0.f, 0.f};      // scaled cache: factors of the scores of heads 2t, 2t+1
     float m2[2] = {neg_inf(), neg_inf()};
@@ -613,13 +674,34 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         return true;
     };
 
+    // scaled cache: red_acc may be written (the merging warp is done with what it held); false = abort
+    auto merge_free = [&]() -> bool {
+        if (!mbar_wait(smem_u32(&sm.merge_empty), red_phase0 ^ 1, abort_flag)) {
+            if (lane == 0) { sm.abort_flag = 1; epoch_or(header + kHdrStatus, epoch, kStatusTimeout); }
+            return false;
+        }
+        red_phase0 ^= 1;
+        return true;
+    };
+    auto merge_go = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.merge_full));
+    };
+
     for (;;) {
         if (!mbar_wait(smem_u32(&sm.full_bar[stage]), phase, abort_flag)) {
             if (lane == 0) { sm.abort_flag = 1; epoch_or(header + kHdrStatus, epoch, kStatusTimeout); }
             return;
         }
         const StageMeta mt = sm.meta[stage];
-        if (mt.entry < 0) return;   // end of this CTA's work (the producer warp has counted the CTA as done)
+        if (mt.entry < 0) {         // end of this CTA's work (the producer warp has counted the CTA as done)
+            if constexpr (kMergers<G, KV> > 0) {
+                if (!merge_free()) return;
+                if (tid == 0) sm.merge_entry = -1;
+                merge_go();
+            }
+            return;
+        }
 
         if (mt.flags & kSegFirst) {
             const uint16_t *q_rows = sm.q[stage];
@@ -686,17 +768,29 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             float *seg_slot = seg + (size_t)mt.slot * seg_stride;
 #pragma unroll
             for (int hr = 0; hr < (G + RG - 1) / RG; ++hr) {
+                if constexpr (kMergers<G, KV> > 0) {
+                    if (!merge_free()) return;
+                    if (tid == 0) { sm.merge_entry = mt.entry; sm.merge_head = mt.kv_head; sm.merge_slot = mt.slot; sm.merge_info = (nseg << 8) | hr; }
+                }
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                     const int head = 2 * t + hh;
                     if (head < G && head / RG == hr) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            sm.red_acc[warp][head - hr * RG][16 * i + (KV != kKvBf16 ? 2 * g : g)] = acc[i][hh];
-                            sm.red_acc[warp][head - hr * RG][16 * i + (KV != kKvBf16 ? 2 * g + 1 : g + 8)] = acc[i][2 + hh];
+                            if constexpr (KV != kKvBf16) {
+                                *reinterpret_cast<float2 *>(&sm.red_acc[warp][head - hr * RG][16 * i + 2 * g]) = make_float2(acc[i][hh], acc[i][2 + hh]);
+                            } else {
+                                sm.red_acc[warp][head - hr * RG][16 * i + g] = acc[i][hh];
+                                sm.red_acc[warp][head - hr * RG][16 * i + g + 8] = acc[i][2 + hh];
+                            }
                         }
                         if (g == 0) { sm.red_ml[warp][head][0] = m2[hh]; sm.red_ml[warp][head][1] = l[hh]; }
                     }
+                }
+                if constexpr (kMergers<G, KV> > 0) {
+                    merge_go();
+                    continue;
                 }
                 if (!red_sync(0, red_phase0)) return;
                 // kThreadsPerHead threads share a head: the eight warps' weights are computed once per thread
@@ -839,7 +933,7 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const float
         *launches += 1;
     }
     if (ev0) cudaEventRecord(ev0, st);
-    cudaError_t e = launch_pdl(sweep_kernel<G, KV>, dim3(n_ctas), dim3(kSweepThreads<KV>), smem, st, kmap, vmap,
+    cudaError_t e = launch_pdl(sweep_kernel<G, KV>, dim3(n_ctas), dim3(kSweepThreads<G, KV>), smem, st, kmap, vmap,
                                (const uint16_t *)q, bt, sl, sr, o, m, l, header, global_prefix, piece_info, seg,
                                wsl.seg_stride, epoch, k_scale, v_scale, P);
     if (ev1) cudaEventRecord(ev1, st);
