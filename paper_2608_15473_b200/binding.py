@@ -573,16 +573,21 @@ def rope_append_axes(q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_to
     return rc
 
 
+_code_types = {}      # element types that tell what their codes are
+
+
 def _kv_type(kv_type: Optional[int], *pools) -> int:
     """The code type of a scaled cache: what the caller says, or what the pools' elements say; they must not differ."""
+    if not _code_types:
+        import torch
+        _code_types.update({torch.float8_e4m3fn: QF_KV_E4M3, torch.int8: QF_KV_INT8})
     said = kv_type
     for x in pools:
-        name = str(getattr(x, "dtype", ""))
-        of = QF_KV_E4M3 if name == "torch.float8_e4m3fn" else QF_KV_INT8 if name == "torch.int8" else None
+        of = _code_types.get(getattr(x, "dtype", None))
         if of is None:
             continue
         if said is not None and said != of:
-            raise ValueError(f"a pool of {name} does not hold codes of kv_type {said}")
+            raise ValueError(f"a pool of {x.dtype} does not hold codes of kv_type {said}")
         said = of
     if said is None and all(x is None for x in pools):
         said = QF_KV_E4M3      # no cache, no codes
