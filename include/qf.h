@@ -363,8 +363,7 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
 /*
  * Rotary positions with several axes (time, height and width of images and video): the same pass, but pair j turns by
  *     t = positions[pair_axis[j], row] * inv_freq[j]
- * instead of by the row's place in its sequence.  positions: int32 [num_axes, total_tokens], any values (tokens of no
- * request are not read as far as their results go); pair_axis: int32 [rotary_dim / 2] (device; see qf_rope_pair_axes),
+ * instead of by the row's place in its sequence.  positions: int32 [num_axes, total_tokens], any values; pair_axis: int32 [rotary_dim / 2] (device; see qf_rope_pair_axes),
  * entries outside [0, num_axes) count as the nearest axis; num_axes 1 to 8.  The row's place in the CACHE still follows
  * from seq_lens.  With every axis equal to that place the results are qf_rope_append's.  Everything else as there.
  */
@@ -419,7 +418,7 @@ int qf_rope_append_scaled(const void *q, const void *k, const void *v, void *q_o
  * (qf_workspace_bytes), status (qf_read_status), limits and launches; the current token's fold (qf_combine_self) and the
  * shard merge work on their states as on any.  The products take the codes exactly (as 16-bit floats), queries as bf16
  * numbers brought into range by a power of two per head, and weights as two 16-bit terms (22 bits); scores, maxima, sums,
- * scales and accumulators are fp32.
+ * scales and accumulators are fp32.  o_part must be 16-byte aligned.
  */
 int qf_decode_partial_scaled(const void *q, const void *k_cache, const void *v_cache,
                              const float *k_scale, const float *v_scale,
