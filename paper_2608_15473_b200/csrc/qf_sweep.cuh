@@ -23,6 +23,9 @@
 //             merges after the sweep.  Empty shards get (0, -inf, -inf) from the consumer
 //             warps' prologue.
 //
+// A scaled cache (one byte per number; KV != kKvBf16) goes the same way with stages of 16 pages, two per consumer warp, whose
+// scales arrive on the stage's barrier too, and with warps of their own for the copies and the merging: kIssuers, kMergers.
+//
 // All waits are bounded: a wait that runs out sets QF_STATUS_TIMEOUT, raises a
 // CTA-wide abort flag and every warp leaves.  No CTA ever waits for another CTA
 // (drawing a chunk is one atomic add; it never blocks on another CTA's progress).
@@ -50,6 +53,7 @@ constexpr int kConsumerThreads = kConsumerWarps * 32;
 template <int KV> constexpr int kPagesPerStage = KV == kKvBf16 ? kConsumerWarps : 2 * kConsumerWarps;
 // A scaled cache's pages are half as long, so there are twice as many copies per byte, and one thread cannot issue them fast
 // enough: one more warp issues the copies of K, one those of V, from the places that the producer leaves in shared memory.
+// (The copies issued by a lane each: 248 us for 32 requests of 16,384 tokens, where this form takes 167.)
 template <int KV> constexpr int kIssuers = KV == kKvBf16 ? 0 : 2;
 // With up to four heads per group (one round of red_acc) one more warp merges the consumer warps' states at the end of a range, while
 // they go on with the next (256 requests of 500 tokens 76 -> 73 us; with two rounds the second waits for the first, 63 -> 65 us).
