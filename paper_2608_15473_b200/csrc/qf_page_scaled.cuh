@@ -192,15 +192,17 @@ __device__ __forceinline__ void process_pages_scaled(uint32_t k_base, uint32_t v
         mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
         mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
     }
-    // Weights are taken against the pages' maximum less 14 (in log 2), the same number in w and be, so its rounding cancels.
-    const float mp0 = mx0 == neg_inf() ? 0.f : mx0 - kWeightLog2, mp1 = mx1 == neg_inf() ? 0.f : mx1 - kWeightLog2;
+    const float mn0 = fmaxf(m2[0], mx0), mn1 = fmaxf(m2[1], mx1);
+    const float ms0 = mn0 == neg_inf() ? 0.f : mn0, ms1 = mn1 == neg_inf() ? 0.f : mn1;      // nothing above -inf: avoid inf - inf
+    // Weights are taken against the pages' maximum less 14 (in log 2), the same number in w and be, so its rounding cancels.  Pages with
+    // no score above -inf (both skipped, say) have weights 0 against any number: the running one, so that be, which they
+    // are multiplied by, is 1 and not an infinity that a running maximum far below 0 would make of it.
+    const float mp0 = mx0 == neg_inf() ? ms0 : mx0 - kWeightLog2, mp1 = mx1 == neg_inf() ? ms1 : mx1 - kWeightLog2;
     float w[2][4];
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[p][i] = fast_exp2(sc[p][i] - ((i & 1) ? mp1 : mp0));
-    const float mn0 = fmaxf(m2[0], mx0), mn1 = fmaxf(m2[1], mx1);
-    const float ms0 = mn0 == neg_inf() ? 0.f : mn0, ms1 = mn1 == neg_inf() ? 0.f : mn1;      // nothing above -inf: avoid inf - inf
     const float al0 = fast_exp2(m2[0] - ms0), al1 = fast_exp2(m2[1] - ms1);      // of what came before
     const float be0 = fast_exp2(mp0 - ms0), be1 = fast_exp2(mp1 - ms1);          // of these pages
     m2[0] = mn0; m2[1] = mn1;
