@@ -397,9 +397,11 @@ enum { QF_KV_E4M3 = 1, QF_KV_INT8 = 2 };
 /*
  * qf_rope_append (or, with positions, qf_rope_append_axes) into a scaled cache.  Norms, rotation, q_out and k_out are
  * theirs; keys and values go from the fp32 result straight to codes.  With M = 448 or 127, the scale of a block (page, head)
- * becomes the smallest power of two, 2^-100 at least, that is not below the block's present scale and has max |y| <= M * scale
- * over the rows this call puts there; the new rows become round(y / scale) (ties to even), and, where the scale grew, the codes
- * of the slots before them round(code * old / new).  A page whose first slot this call writes starts without a scale.  So
+ * stays what it is while |scale| is 2^-100 at least and max |y| <= M * |scale| over the rows this call puts there, and else becomes the
+ * smallest power of two, 2^-100 at least, with max |y| <= M * scale; the new rows become round(y / scale) (ties to even), and, where
+ * the scale changed,
+ * the codes of the slots before them round(code * old / new) (127 where that is 128).  A page whose first slot this call
+ * writes starts without a scale; a scale that is not finite makes what the block holds, and gets, NaN.  So
  * a block's scale is a power of two unless a caller put another one there, results do not depend on what else is in the
  * batch, and a number is off by at most 2^-4 of itself or 2^-10 scale (e4m3) or scale / 2 (int8; at most one scale in all if
  * the scale grew later).  A row with a value that is not finite makes its block's scale NaN.  Slots behind the rows written

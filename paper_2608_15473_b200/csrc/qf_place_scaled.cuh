@@ -47,11 +47,11 @@ __device__ __forceinline__ float scale_for(float top)
     const int k = (int)(bits >> 23) - 127 - kTopExponent + ((bits & 0x7fffffu) > kTopMantissa ? 1 : 0);
     return __uint_as_float((unsigned)(max(k, kMinScaleExponent) + 127) << 23);
 }
-// What a block's stored scale says about the rows it holds: nothing readable counts as no scale at all.
+// What a block's stored scale says about the rows it holds: itself, and NaN for an infinity.  (Scales below zero come from other
+// software only; the rows under them are read like any, so they are kept like any.)
 __device__ __forceinline__ float held_scale(float s)
 {
-    if (s != s || s == __int_as_float(0x7f800000)) return __uint_as_float(0x7fc00000u);
-    return s > 0.f ? s : 0.f;
+    return (__float_as_uint(s) & 0x7fffffffu) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : s;
 }
 // x / s: a product where s is a power of two (every scale that this kernel forms; a caller's own may be anything, also NaN)
 struct Divider {
@@ -84,8 +84,9 @@ __device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float 
 template <int KV>
 __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
 {
-    constexpr float kRound = KV == kKvInt8 ? 12582912.f : 0.f;
-    return KV == kKvInt8 ? pack_codes<KV>(a + kRound, b + kRound, c + kRound, d + kRound) : pack_codes<KV>(a, b, c, d);
+    constexpr float kRound = 12582912.f, kTop = 127.f;      // (-128 under a scale below zero would round to 128)
+    if constexpr (KV == kKvInt8) return pack_codes<KV>(fminf(a, kTop) + kRound, fminf(b, kTop) + kRound, fminf(c, kTop) + kRound, fminf(d, kTop) + kRound);
+    else return pack_codes<KV>(a, b, c, d);
 }
 template <int KV>
 __device__ __forceinline__ void numbers_of(uint32_t w, float (&y)[4])
@@ -435,7 +436,8 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
 #pragma unroll
                 for (int side = 0; side < 2; ++side) {
                     const float old = held > 0 ? held_scale(side ? old_v[n] : old_k[n]) : 0.f;
-                    const float scale = max_nan(old, scale_for<KV>(__uint_as_float(side ? top[n] & 0xffff0000u : top[n] << 16)));
+                    const float least = max_nan(fabsf(old), scale_for<KV>(__uint_as_float(side ? top[n] & 0xffff0000u : top[n] << 16)));
+                    const float scale = fabsf(old) == least ? old : least;      // the present one where it suffices, with its sign
                     const Divider by(scale);
                     uint8_t *to = (side ? v_row : k_row) + (size_t)i * head_step;
                     if (leads) {
