@@ -402,9 +402,10 @@ enum { QF_KV_E4M3 = 1, QF_KV_INT8 = 2 };
  * the scale changed,
  * the codes of the slots before them round(code * old / new) (127 where that is 128).  A page whose first slot this call
  * writes starts without a scale; a scale that is not finite makes what the block holds, and gets, NaN.  So
- * a block's scale is a power of two unless a caller put another one there, results do not depend on what else is in the
- * batch, and a number is off by at most 2^-4 of itself or 2^-10 scale (e4m3) or scale / 2 (int8; at most one scale in all if
- * the scale grew later).  A row with a value that is not finite makes its block's scale NaN.  Slots behind the rows written
+ * a block's scale is a power of two unless a caller put another one there, and results do not depend on what else is in the
+ * batch.  A number is off by at most 2^-4 of itself or 2^-10 scale (e4m3) or scale / 2 (int8); where the scale grew later, by at
+ * most 2^-4 of itself or 2^-9 scale (e4m3), or one scale (int8), in all.  (Under a caller's scale that was no power of two, e4m3
+ * numbers are rounded by 2^-4 of themselves once more when it grows.)  A row with a value that is not finite makes its block's scale NaN.  Slots behind the rows written
  * keep their codes (they hold nothing).  The requests of one call must not share a page that the call writes to.
  * k_scale, v_scale may be NULL when the cache pointers are; pos_base is not read when positions are given.  One launch.
  */

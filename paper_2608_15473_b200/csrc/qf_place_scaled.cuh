@@ -6,7 +6,8 @@
 //
 // A block (the 16 rows of one KV head in one page) fills over many calls.  When a row does not fit, the scale grows
 // and the codes that earlier calls left in the block are rounded again, to code * old / new.  The ratio is a power
-// of two, so for e4m3 nothing but numbers that fall below its smallest normal one changes at all; integers lose the
+// of two (of the kernel's own scales), so for e4m3 nothing but numbers that fall below its smallest normal one changes at all: they
+// lose 2^-10 of each new scale, 2^-9 of the last one in all with the first rounding.  Integers lose the
 // bits that leave at the bottom, half a step of the new scale at most.  A block that is written from its first slot on
 // starts afresh.  Powers of two cost e4m3 no precision and integers up to one bit of seven against max / M, and buy that
 // exactness, exact expansion to bf16, and scales that can be applied anywhere in a product without another rounding.
