@@ -419,8 +419,11 @@ int qf_rope_append_scaled(const void *q, const void *k, const void *v, void *q_o
 /*
  * qf_decode_partial and qf_decode_step over a scaled cache: same arguments, states and merges, workspace
  * (qf_workspace_bytes), status (qf_read_status), limits and launches; the current token's fold (qf_combine_self) and the
- * shard merge work on their states as on any.  The products take the codes exactly (as 16-bit floats), queries as bf16
- * numbers brought into range by a power of two per head, and weights as two 16-bit terms (22 bits); scores, maxima, sums,
+ * shard merge work on their states as on any.  The products take the codes exactly (as 16-bit floats).  Queries become
+ * 16-bit floats, each head times a power of two: channels of at least 2^-31 of the head's largest are exact, smaller ones are off by
+ * 2^-39 of the largest at most.  Weights are two 16-bit terms, off by 2^-22 of themselves or by 2^-39 of the largest weight
+ * among two neighbouring pages, whichever is more, so a page whose weights are less than 2^-17 of its neighbour's keeps fewer
+ * than 22 bits of them (which shows where its values are the larger ones by as much).  Scores, maxima, sums,
  * scales and accumulators are fp32.  o_part must be 16-byte aligned.
  */
 int qf_decode_partial_scaled(const void *q, const void *k_cache, const void *v_cache,

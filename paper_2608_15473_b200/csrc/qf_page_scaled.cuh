@@ -5,11 +5,14 @@
 //
 // Codes become f16 numbers in registers, exactly (e4m3 by the conversion instruction, integers by placing the byte in
 // the mantissa of 1024 and subtracting), and go through m16n8k16 products with fp32 accumulators.  Queries become f16
-// too: each head is brought to magnitudes below 2^15 by a power of two first, so its eight significant bits survive
-// down to 2^-39 of its largest channel.  Both scales stay out of the products: ks multiplies the finished score, and the
-// weights are taken relative to the two pages' own maximum, times 2^14, so that hi + lo (two f16 terms) hold 22 bits
-// of every weight down to 2^-39 of the two pages' largest, whatever they weigh against the others and however their
-// scales compare; each page's product then enters the accumulators with one factor, vs e^{m_pages - m}.
+// too: each head is brought to magnitudes below 2^15 by a power of two first.  f16 steps end at 2^-24, so a channel keeps its eight
+// significant bits down to 2^-31 of the head's largest, and is off by 2^-39 of the largest at most below that.
+// Both scales stay out of the products: ks multiplies the finished score, and the
+// weights are taken relative to the two pages' own maximum, times 2^14, so that hi + lo (two f16 terms) are off by 2^-22
+// of a weight or by 2^-39 of the two pages' largest: 22 bits down to 2^-17 of the largest, whatever the pages weigh against the
+// others.  Each page's product then enters the accumulators with one factor, vs e^{m_pages - m}, so scales take no bits from the
+// weights; but 2^-39 of one page's weight may count where the other's values are very much larger (weights 2^-30 of the
+// neighbour's under a scale 2^60 times its: 2^-9 of the result).
 //
 // Fragments.  K: a lane reads 32 channels of rows g and g + 8 (16-byte words 2t and 2t+1 of the swizzled row: eight
 // lanes hit eight different bank groups); the words' channels, taken four at a time, are a k-step (which channel is
