@@ -145,7 +145,7 @@ int launch_sweep_bf16(const void *q, const void *k_cache, const void *v_cache, c
     CUtensorMap kmap, vmap;
     if (qf::make_pool_map(&kmap, k_cache, P.num_pages, P.num_kv_heads, qf::kPageSize, P.kv_nhd != 0, msg, msg_len)) return QF_ERR_CUDA;
     if (qf::make_pool_map(&vmap, v_cache, P.num_pages, P.num_kv_heads, qf::kPageSize, P.kv_nhd != 0, msg, msg_len)) return QF_ERR_CUDA;
-    return qf::launch_sweep_kv<qf::kKvBf16>(kmap, vmap, nullptr, nullptr, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1,
+    return qf::launch_sweep_kv<qf::kKvBf16>(kmap, vmap, {}, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1,
                                             msg, msg_len, launches, skip_finish);
 }
 

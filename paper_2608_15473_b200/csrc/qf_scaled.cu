@@ -63,9 +63,9 @@ int launch_sweep_scaled(const void *q, const void *k, const void *v, const Scale
     if (qf::make_scaled_map(&kmap, k, P.num_pages, P.num_kv_heads, P.kv_nhd != 0, true, msg, msg_len)) return QF_ERR_CUDA;
     if (qf::make_scaled_map(&vmap, v, P.num_pages, P.num_kv_heads, P.kv_nhd != 0, true, msg, msg_len)) return QF_ERR_CUDA;
     return s.kind == qf::kKvE4m3
-               ? qf::launch_sweep_kv<qf::kKvE4m3>(kmap, vmap, s.k_scale, s.v_scale, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0,
+               ? qf::launch_sweep_kv<qf::kKvE4m3>(kmap, vmap, {s.k_scale, s.v_scale}, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0,
                                                   ev1, msg, msg_len, launches, skip_finish)
-               : qf::launch_sweep_kv<qf::kKvInt8>(kmap, vmap, s.k_scale, s.v_scale, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0,
+               : qf::launch_sweep_kv<qf::kKvInt8>(kmap, vmap, {s.k_scale, s.v_scale}, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0,
                                                   ev1, msg, msg_len, launches, skip_finish);
 }
 

@@ -250,6 +250,22 @@ struct __align__(16) StageMeta {
 };
 enum { kSegFirst = 1, kSegLast = 2 };
 
+// What only a scaled cache needs beside the rest.  Nothing for bf16, whose kernel is to be what it would be without these: with
+// the members in its shared memory, the scales among its parameters and the page's addresses formed before its rows, sweeps took
+// 0.15 to 0.3 % longer (one million tokens 606.5 us against 604.8); as it stands there is no difference to be seen (604.65 and 604.6).
+template <int KV> struct SweepScaled {
+    // of the stages' pages: scales, and where the issuing warps find them
+    alignas(16) float scales[kStages][2][kPagesPerStage<KV>];
+    alignas(16) int at[kStages][kPagesPerStage<KV>];
+    alignas(8) unsigned long long issue_bar[kStages];
+    alignas(8) unsigned long long merge_full, merge_empty;
+    int merge_entry, merge_head, merge_slot, merge_info;      // the range in red_acc: info = segments of its unit << 8 | round of heads
+};
+template <> struct SweepScaled<kKvBf16> {};
+template <int KV> struct SweepScales { const float *k, *v; };      // [num_pages, Hkv]
+template <> struct SweepScales<kKvBf16> {};
+static_assert(sizeof(SweepScaled<kKvBf16>) == 1 && sizeof(SweepScales<kKvBf16>) == 1, "empty for bf16");
+
 template <int G, int KV>
 struct SweepSmem {
     // every K/V half tile is a 1024-byte-aligned 128B-swizzled TMA destination
@@ -262,17 +278,12 @@ struct SweepSmem {
     alignas(16) StageMeta meta[kStages];
     alignas(8) unsigned long long full_bar[kStages];
     alignas(8) unsigned long long empty_bar[kStages];
-    // of a scaled cache's pages: scales, and where the issuing warps find them
-    alignas(16) float scales[kStages][2][kPagesPerStage<KV>];
-    alignas(16) int at[kStages][kPagesPerStage<KV>];
-    alignas(8) unsigned long long issue_bar[kStages];
-    alignas(8) unsigned long long merge_full, merge_empty;
-    int merge_entry, merge_head, merge_slot, merge_info;      // the range in red_acc: info = segments of its unit << 8 | round of heads
     alignas(8) unsigned long long red_bar[2];
     int abort_flag;
     unsigned long long epoch;   // this launch's epoch, read once per CTA
     int scan_ws[kSweepThreads<G, KV> / 32];
     int prefix[kMaxSmemEntries + 1];
+    SweepScaled<KV> scaled;
 };
 
 template <int G, int KV>
@@ -283,7 +294,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
              float *__restrict__ o_part, float *__restrict__ m_part, float *__restrict__ lse_part,
              unsigned long long *__restrict__ header, const int *__restrict__ global_prefix,
              int4 *__restrict__ piece_info, float *__restrict__ seg, int seg_stride,
-             unsigned long long host_epoch, const float *__restrict__ k_scale, const float *__restrict__ v_scale, DevParams P)
+             unsigned long long host_epoch, DevParams P, SweepScales<KV> scales)
 {
     constexpr int kPages = kPagesPerStage<KV>;
     extern __shared__ uint8_t smem_raw[];
@@ -301,11 +312,11 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             // one arrival with the bytes to expect and, for a scaled cache, one per lane once its scale has landed
             mbar_init(smem_u32(&sm.full_bar[s]), KV == kKvBf16 ? 1 : 33);
             mbar_init(smem_u32(&sm.empty_bar[s]), kConsumerWarps);
-            if (KV != kKvBf16) mbar_init(smem_u32(&sm.issue_bar[s]), 1);
+            if constexpr (KV != kKvBf16) mbar_init(smem_u32(&sm.scaled.issue_bar[s]), 1);
         }
-        if (KV != kKvBf16) {
-            mbar_init(smem_u32(&sm.merge_full), kConsumerWarps);
-            mbar_init(smem_u32(&sm.merge_empty), 1);
+        if constexpr (KV != kKvBf16) {
+            mbar_init(smem_u32(&sm.scaled.merge_full), kConsumerWarps);
+            mbar_init(smem_u32(&sm.scaled.merge_empty), 1);
         }
         mbar_init(smem_u32(&sm.red_bar[0]), kConsumerWarps);
         mbar_init(smem_u32(&sm.red_bar[1]), kConsumerWarps);
@@ -494,16 +505,16 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                         mt.slot = e * Hkv + c + piece;
                         sm.meta[stage] = mt;
                         mbar_arrive_expect_tx(full, (uint32_t)np * 2u * kPageBlockBytes<KV> + (first ? (uint32_t)G * 256u : 0u));
-                        if (bad_mask && P.check_bounds) epoch_or(header + kHdrStatus, epoch, kStatusBadPage);
+                        if (bad_mask && (KV == kKvBf16 || P.check_bounds)) epoch_or(header + kHdrStatus, epoch, kStatusBadPage);
                     }
                     __syncwarp();
                     if constexpr (KV != kKvBf16) {
                         // scales: lanes 0..15 of the K pages, 16..31 of the V pages; 0 for a page that is not there
-                        copy_async_4(smem_u32(&sm.scales[stage][part][i]), (part ? v_scale : k_scale) + (size_t)phys * Hkv + c, i < np && !bad);
+                        copy_async_4(smem_u32(&sm.scaled.scales[stage][part][i]), (part ? scales.v : scales.k) + (size_t)phys * Hkv + c, i < np && !bad);
                         arrive_after_copies(full);
-                        if (lane < kPages) sm.at[stage][lane] = P.kv_nhd ? phys * kPageSize : phys * Hkv + c;
+                        if (lane < kPages) sm.scaled.at[stage][lane] = P.kv_nhd ? phys * kPageSize : phys * Hkv + c;
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&sm.issue_bar[stage]));
+                        if (lane == 0) mbar_arrive(smem_u32(&sm.scaled.issue_bar[stage]));
                         __syncwarp();
                     } else if (issuer) {
                         const uint32_t dst = smem_u32(&sm.kv[stage][part][i][0]);
@@ -540,10 +551,10 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                     sm.meta[stage] = mt;
                     mbar_arrive(smem_u32(&sm.full_bar[stage]));
                 }
-                if (KV != kKvBf16) {
+                if constexpr (KV != kKvBf16) {
                     __syncwarp();
                     mbar_arrive(smem_u32(&sm.full_bar[stage]));      // as every lane does for its scale
-                    if (lane == 0) mbar_arrive(smem_u32(&sm.issue_bar[stage]));
+                    if (lane == 0) mbar_arrive(smem_u32(&sm.scaled.issue_bar[stage]));
                 }
             } else ok = false;
         }
@@ -562,17 +573,17 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         return;
     }
 
-    const float kLn2 = 0.6931471805599453f;
     if constexpr (kMergers<G, KV> > 0) {
+        const float kLn2 = 0.6931471805599453f;
         if (warp == kConsumerWarps + 1 + kIssuers<KV>) {
             // ============================ merging warp (scaled cache) ============================
             constexpr int RG = SweepSmem<G, KV>::kRoundHeads;
             for (uint32_t ph = 0;; ph ^= 1) {
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.merge_full), ph, abort_flag))) break;
-                if (sm.merge_entry < 0) break;
-                const int hr = sm.merge_info & 0xff, nseg = sm.merge_info >> 8;
-                const size_t out_row = out_entry(P, sm.merge_entry) * Hq + (size_t)sm.merge_head * G;
-                float *seg_slot = seg + (size_t)sm.merge_slot * seg_stride;
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.scaled.merge_full), ph, abort_flag))) break;
+                if (sm.scaled.merge_entry < 0) break;
+                const int hr = sm.scaled.merge_info & 0xff, nseg = sm.scaled.merge_info >> 8;
+                const size_t out_row = out_entry(P, sm.scaled.merge_entry) * Hq + (size_t)sm.scaled.merge_head * G;
+                float *seg_slot = seg + (size_t)sm.scaled.merge_slot * seg_stride;
 #pragma unroll 1
                 for (int hl = 0; hl < RG && hr * RG + hl < G; ++hl) {
                     const int head = hr * RG + hl;
@@ -610,7 +621,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                     }
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sm.merge_empty));
+                if (lane == 0) mbar_arrive(smem_u32(&sm.scaled.merge_empty));
             }
             return;
         }
@@ -622,14 +633,14 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             const CUtensorMap *map = part ? &v_map : &k_map;
             const unsigned long long kv_policy = l2_evict_first_policy();
             for (int stage = 0, phase = 0;;) {
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.issue_bar[stage]), (uint32_t)phase, abort_flag))) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.scaled.issue_bar[stage]), (uint32_t)phase, abort_flag))) break;
                 if (sm.meta[stage].entry < 0) break;
                 if (elect_one()) {      // one thread, with operands that are the same for the warp
                     const int np = sm.meta[stage].npages, y = P.kv_nhd ? sm.meta[stage].kv_head : 0;
                     const uint32_t full = smem_u32(&sm.full_bar[stage]), dst = smem_u32(&sm.kv[stage][part][0][0]);
                     int4 a[kPages / 4];
 #pragma unroll
-                    for (int k = 0; k < kPages / 4; ++k) a[k] = *reinterpret_cast<const int4 *>(&sm.at[stage][4 * k]);
+                    for (int k = 0; k < kPages / 4; ++k) a[k] = *reinterpret_cast<const int4 *>(&sm.scaled.at[stage][4 * k]);
 #pragma unroll
                     for (int k = 0; k < kPages; ++k)
                         if (k < np)
@@ -657,6 +668,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
 
     const int g = lane >> 2, t = lane & 3;
     const float scale2 = P.sm_scale * 1.4426950408889634f;  // scores are kept in units of log 2
+    const float kLn2 = 0.6931471805599453f;
     uint32_t qf[8][2];
     float qs[2] = {0.f, 0.f};      // scaled cache: factors of the scores of heads 2t, 2t+1
     float m2[2] = {neg_inf(), neg_inf()};
@@ -680,16 +692,20 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
 
     // scaled cache: red_acc may be written (the merging warp is done with what it held); false = abort
     auto merge_free = [&]() -> bool {
-        if (!mbar_wait(smem_u32(&sm.merge_empty), red_phase0 ^ 1, abort_flag)) {
-            if (lane == 0) { sm.abort_flag = 1; epoch_or(header + kHdrStatus, epoch, kStatusTimeout); }
-            return false;
+        if constexpr (kMergers<G, KV> > 0) {
+            if (!mbar_wait(smem_u32(&sm.scaled.merge_empty), red_phase0 ^ 1, abort_flag)) {
+                if (lane == 0) { sm.abort_flag = 1; epoch_or(header + kHdrStatus, epoch, kStatusTimeout); }
+                return false;
+            }
+            red_phase0 ^= 1;
         }
-        red_phase0 ^= 1;
         return true;
     };
     auto merge_go = [&]() {
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sm.merge_full));
+        if constexpr (kMergers<G, KV> > 0) {
+            if (lane == 0) mbar_arrive(smem_u32(&sm.scaled.merge_full));
+        }
     };
 
     for (;;) {
@@ -701,7 +717,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         if (mt.entry < 0) {         // end of this CTA's work (the producer warp has counted the CTA as done)
             if constexpr (kMergers<G, KV> > 0) {
                 if (!merge_free()) return;
-                if (tid == 0) sm.merge_entry = -1;
+                if (tid == 0) sm.scaled.merge_entry = -1;
                 merge_go();
             }
             return;
@@ -727,10 +743,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         }
 
         if (wp < mt.npages) {
-            const uint32_t k_base = smem_u32(&sm.kv[stage][0][wp][0]);
-            const uint32_t v_base = smem_u32(&sm.kv[stage][1][wp][0]);
             const int tok0 = (mt.page0 + wp) << 4;
-            bool ragged;
             if constexpr (KV != kKvBf16) {
                 int tlo[2], thi[2];
 #pragma unroll
@@ -738,17 +751,23 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
                     tlo[k] = max(mt.tok_beg - tok0 - 16 * k, 0);
                     thi[k] = ((mt.aux >> (wp + k)) & 1) ? 0 : min(mt.tok_end - tok0 - 16 * k, kPageSize);
                 }
-                ragged = tlo[0] > 0 || thi[0] < kPageSize || thi[1] < kPageSize;
-                const float2 ks2 = *reinterpret_cast<const float2 *>(&sm.scales[stage][0][wp]), vs2 = *reinterpret_cast<const float2 *>(&sm.scales[stage][1][wp]);
+                const bool ragged = tlo[0] > 0 || thi[0] < kPageSize || thi[1] < kPageSize;
+                const uint32_t k_base = smem_u32(&sm.kv[stage][0][wp][0]);
+                const uint32_t v_base = smem_u32(&sm.kv[stage][1][wp][0]);
+                const float2 ks2 = *reinterpret_cast<const float2 *>(&sm.scaled.scales[stage][0][wp]), vs2 = *reinterpret_cast<const float2 *>(&sm.scaled.scales[stage][1][wp]);
                 const float ks[2] = {ks2.x, ks2.y}, vs[2] = {vs2.x, vs2.y};
                 process_pages_scaled<KV, (G <= 4)>(k_base, v_base, ks, vs, tlo, thi, ragged, qf, qs, m2, l, acc, lane);
+                if (ragged) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             } else {
                 int tlo = max(mt.tok_beg - tok0, 0), thi = min(mt.tok_end - tok0, kPageSize);
                 if ((mt.aux >> wp) & 1) { tlo = 0; thi = 0; }
-                ragged = (tlo > 0) || (thi < kPageSize);
+                const bool ragged = (tlo > 0) || (thi < kPageSize);
+                const uint32_t k_base = smem_u32(&sm.kv[stage][0][wp][0]);
+                const uint32_t v_base = smem_u32(&sm.kv[stage][1][wp][0]);
+
                 process_page(k_base, v_base, kHalfTileBytes, tlo, thi, ragged, qf, m2, l, acc, scale2, lane);
+                if (ragged) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
-            if (ragged) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.empty_bar[stage]));
@@ -774,7 +793,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             for (int hr = 0; hr < (G + RG - 1) / RG; ++hr) {
                 if constexpr (kMergers<G, KV> > 0) {
                     if (!merge_free()) return;
-                    if (tid == 0) { sm.merge_entry = mt.entry; sm.merge_head = mt.kv_head; sm.merge_slot = mt.slot; sm.merge_info = (nseg << 8) | hr; }
+                    if (tid == 0) { sm.scaled.merge_entry = mt.entry; sm.scaled.merge_head = mt.kv_head; sm.scaled.merge_slot = mt.slot; sm.scaled.merge_info = (nseg << 8) | hr; }
                 }
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
@@ -902,7 +921,7 @@ inline unsigned long long next_epoch()
 }
 
 template <int G, int KV>
-int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const float *k_scale, const float *v_scale, const void *q, const int32_t *bt,
+int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, SweepScales<KV> scales, const void *q, const int32_t *bt,
                    const int32_t *sl, const int32_t *sr, float *o, float *m, float *l, const DevParams &P,
                    char *ws, const WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st,
                    cudaEvent_t ev0, cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish)
@@ -939,7 +958,7 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const float
     if (ev0) cudaEventRecord(ev0, st);
     cudaError_t e = launch_pdl(sweep_kernel<G, KV>, dim3(n_ctas), dim3(kSweepThreads<G, KV>), smem, st, kmap, vmap,
                                (const uint16_t *)q, bt, sl, sr, o, m, l, header, global_prefix, piece_info, seg,
-                               wsl.seg_stride, epoch, k_scale, v_scale, P);
+                               wsl.seg_stride, epoch, P, scales);
     if (ev1) cudaEventRecord(ev1, st);
     if (e != cudaSuccess) { snprintf(msg, msg_len, "sweep_kernel launch: %s", cudaGetErrorString(e)); return -5; }
     *launches += 1;
@@ -954,19 +973,19 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, const float
     return 0;
 }
 
-// The kernel of the batch's group size, over either kind of cache (scales: null for bf16).
+// The kernel of the batch's group size, over either kind of cache.
 template <int KV, int G = 8>
-int launch_sweep_kv(const CUtensorMap &kmap, const CUtensorMap &vmap, const float *k_scale, const float *v_scale, const void *q,
+int launch_sweep_kv(const CUtensorMap &kmap, const CUtensorMap &vmap, SweepScales<KV> scales, const void *q,
                     const int32_t *bt, const int32_t *sl, const int32_t *sr, float *o, float *m, float *l, const DevParams &P,
                     char *ws, const WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st,
                     cudaEvent_t ev0, cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish)
 {
     if constexpr (G > 1) {
         if (P.group < G)
-            return launch_sweep_kv<KV, G - 1>(kmap, vmap, k_scale, v_scale, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1,
+            return launch_sweep_kv<KV, G - 1>(kmap, vmap, scales, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1,
                                               msg, msg_len, launches, skip_finish);
     }
-    return launch_sweep_g<G, KV>(kmap, vmap, k_scale, v_scale, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len,
+    return launch_sweep_g<G, KV>(kmap, vmap, scales, q, bt, sl, sr, o, m, l, P, ws, wsl, n_ctas, epoch, st, ev0, ev1, msg, msg_len,
                                  launches, skip_finish);
 }
 
