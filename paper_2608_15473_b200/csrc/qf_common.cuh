@@ -16,6 +16,9 @@ constexpr int kPageBytes = kPageElems * 2;        // 4096
 // How a cache holds its numbers: bf16, or one byte each (a scaled cache: number = code * scale of its page and KV head).
 enum { kKvBf16 = 0, kKvE4m3 = 1, kKvInt8 = 2 };
 constexpr int kScaledPageBytes = kPageElems;      // 2048: one (page, KV head) block of codes
+// A scaled cache's scales, [num_pages, Hkv]; empty for bf16, whose kernels are to be what they would be without.
+template <int KV> struct KvScales { const float *k, *v; };
+template <> struct KvScales<kKvBf16> {};
 
 constexpr int kStatusBadPage = 1;
 constexpr int kStatusTimeout = 2;

@@ -7,7 +7,7 @@
 #include "../../include/qf.h"
 #include "qf_common.cuh"
 
-namespace qf { struct RopeArgs; struct RowsArgs; struct WorkspaceLayout; }
+namespace qf { struct RopeArgs; struct RopeAxes; struct RowsArgs; struct WorkspaceLayout; }
 
 namespace qf_host {
 
@@ -18,7 +18,7 @@ int cuda_fail(cudaError_t e, const char *what);          // records the text, re
 char *cuda_msg(size_t *len);                             // the buffer qf_strerror(QF_ERR_CUDA) reads
 void set_launches(int n);                                // what qf_last_launch_count reports
 // The checks that the placing calls share, and their kernels' arguments.
-int rope_args(qf::RopeArgs *out, const void *q, const void *k, const void *v, void *q_out, void *k_out, void *k_cache,
+int rope_args(qf::RopeArgs *out, qf::RopeAxes *axes, const void *q, const void *k, const void *v, void *q_out, void *k_out, void *k_cache,
               void *v_cache, const int32_t *block_table, const int32_t *cu_tokens, const int32_t *seq_lens,
               const int32_t *pos_base, const int32_t *positions, const int32_t *pair_axis, int num_axes, const void *q_gain,
               const void *k_gain, const float *inv_freq, const qf_params *p, const qf_rope_params *r, int *sms);
@@ -37,7 +37,7 @@ int step(const void *q, const void *k_cache, const void *v_cache, const ScaledKv
 int prompt(const void *q, const void *k_cache, const void *v_cache, const ScaledKv *scaled, const int32_t *block_table,
            const int32_t *cu_tokens, const int32_t *seq_lens, void *out, float *lse, const qf_params *p, int total_tokens,
            int64_t q_stride, void *workspace, size_t workspace_bytes, void *cuda_stream);
-int launch_rows_scaled(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *p, int kind, char *ws, int sms, cudaStream_t st);
+int launch_rows_scaled(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *p, const ScaledKv &s, char *ws, int sms, cudaStream_t st);
 int launch_simple_scaled(const void *q, const void *k, const void *v, const ScaledKv &s, const int32_t *bt, const int32_t *sl,
                          const int32_t *sr, float *o, float *m, float *l, const qf::DevParams &P, unsigned long long *header,
                          unsigned long long epoch, cudaStream_t st);

@@ -235,7 +235,7 @@ __device__ __forceinline__ void store_codes(uint8_t *to, const unsigned long lon
 
 template <int KV, bool INTERLEAVED>
 __global__ void __launch_bounds__(kPlaceWarps * 32, 2)
-place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_scale, float *__restrict__ v_scale, int tile,
+place_scaled_kernel(const __grid_constant__ RopeArgs A, const __grid_constant__ RopeAxes X, float *__restrict__ k_scale, float *__restrict__ v_scale, int tile,
                     const __grid_constant__ DevParams P)
 {
     constexpr int kQ = 4, kKv = 2;                      // heads that a warp works on at a time, the next ones on their way: of queries, KV heads
@@ -316,8 +316,8 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
                 const int j = lane + 32 * h;
                 if (j >= pairs) continue;
                 double x = (double)row_pos;
-                if (A.positions)
-                    x = (double)A.positions[(long long)min(max(A.pair_axis[j], 0), A.num_axes - 1) * A.total_tokens + t0 + kk];
+                if (X.positions)
+                    x = (double)X.positions[(long long)min(max(X.pair_axis[j], 0), X.num_axes - 1) * A.total_tokens + t0 + kk];
                 const double turn = x * ((double)A.inv_freq[j] * 0.15915494309189533577);      // / (2 pi)
                 float sn, cs;
                 sincospif(2.f * (float)(turn - rint(turn)), &sn, &cs);
@@ -471,7 +471,7 @@ place_scaled_kernel(const __grid_constant__ RopeArgs A, float *__restrict__ k_sc
 // One CTA per decode token; prompts in tiles of up to 16.  KV heads are split until every SM has its two CTAs: 8 requests of one
 // token take a CTA per head, 16,000 packed tokens one part.
 template <int KV>
-inline cudaError_t launch_place_scaled(const RopeArgs &A, float *k_scale, float *v_scale, const DevParams &P, int sms, cudaStream_t st)
+inline cudaError_t launch_place_scaled(const RopeArgs &A, const RopeAxes &X, float *k_scale, float *v_scale, const DevParams &P, int sms, cudaStream_t st)
 {
     int tile = 1;      // about the rows of a request: a CTA's runs share its angles, a decode batch wants a CTA each
     while (tile < kPlaceTile && (long long)A.total_tokens >= 2ll * tile * P.batch) tile *= 2;
@@ -480,7 +480,7 @@ inline cudaError_t launch_place_scaled(const RopeArgs &A, float *k_scale, float 
     while (parts < P.num_kv_heads && tiles * parts < 2ll * sms) parts *= 2;
     if (parts > P.num_kv_heads) parts = P.num_kv_heads;
     auto kernel = A.interleaved ? place_scaled_kernel<KV, true> : place_scaled_kernel<KV, false>;
-    return launch_pdl(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(kPlaceWarps * 32), 0, st, A, k_scale, v_scale, tile, P);
+    return launch_pdl(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(kPlaceWarps * 32), 0, st, A, X, k_scale, v_scale, tile, P);
 }
 
 }  // namespace qf

@@ -32,7 +32,7 @@ int launch_rows(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *
         const long long units = (long long)A.total_rows * P.num_q_heads;
         const long long blocks = (units + qf::kRowsSimpleWarps - 1) / qf::kRowsSimpleWarps;
         if (blocks > 0x7fffffffll) return QF_ERR_UNSUPPORTED;
-        qf::rows_simple_kernel<PREFIX, qf::kKvBf16><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
+        qf::rows_simple_kernel<PREFIX, qf::kKvBf16><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P, {});
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return qf_host::cuda_fail(e, "rows_simple_kernel launch");
         qf_host::set_launches(1);
@@ -42,7 +42,7 @@ int launch_rows(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *
     size_t len;
     char *msg = qf_host::cuda_msg(&len);
     if (qf::make_rows_maps(&maps, A, P, false, msg, len)) return QF_ERR_CUDA;
-    cudaError_t e = qf::launch_rows_kernels<PREFIX, qf::kKvBf16>(maps, A, P, ws, sms, st);
+    cudaError_t e = qf::launch_rows_kernels<PREFIX, qf::kKvBf16>(maps, A, P, {}, ws, sms, st);
     if (e != cudaSuccess) return qf_host::cuda_fail(e, "rows_kernel launch");
     qf_host::set_launches(2);
     return QF_OK;
@@ -51,14 +51,16 @@ int launch_rows(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *
 constexpr int kMostAxes = 8;
 
 // The bf16 cache's placing kernel, for checked arguments.
-int place(qf::RopeArgs &A, const qf_params *p, int sms, void *cuda_stream)
+int place(qf::RopeArgs &A, const qf::RopeAxes &X, const qf_params *p, int sms, void *cuda_stream)
 {
     // one token per CTA until there are several for every SM, then steps of more: fewer, longer row lists per group
     A.tokens_per_cta = 1;
     while (A.tokens_per_cta < qf::kRopeMaxTokens && A.total_tokens >= 8 * A.tokens_per_cta * sms) A.tokens_per_cta *= 2;
     const long long steps = ((long long)A.total_tokens + A.tokens_per_cta - 1) / A.tokens_per_cta;
     const long long blocks = std::min<long long>(steps, (long long)qf::kRopeCtasPerSm * sms);
-    cudaError_t e = qf::launch_rope(A, qf_host::dev_params(p), (unsigned)blocks, (cudaStream_t)cuda_stream);
+    const qf::DevParams P = qf_host::dev_params(p);
+    cudaError_t e = X.positions ? qf::launch_rope<true>(A, X, P, (unsigned)blocks, (cudaStream_t)cuda_stream)
+                                : qf::launch_rope<false>(A, {}, P, (unsigned)blocks, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) return qf_host::cuda_fail(e, "rope_append_kernel launch");
     qf_host::set_launches(1);
     return QF_OK;
@@ -68,7 +70,7 @@ int place(qf::RopeArgs &A, const qf_params *p, int sms, void *cuda_stream)
 
 namespace qf_host {
 
-int rope_args(qf::RopeArgs *out, const void *q, const void *k, const void *v, void *q_out, void *k_out, void *k_cache,
+int rope_args(qf::RopeArgs *out, qf::RopeAxes *axes, const void *q, const void *k, const void *v, void *q_out, void *k_out, void *k_cache,
               void *v_cache, const int32_t *block_table, const int32_t *cu_tokens, const int32_t *seq_lens,
               const int32_t *pos_base, const int32_t *positions, const int32_t *pair_axis, int num_axes, const void *q_gain,
               const void *k_gain, const float *inv_freq, const qf_params *p, const qf_rope_params *r, int *sms)
@@ -103,7 +105,7 @@ int rope_args(qf::RopeArgs *out, const void *q, const void *k, const void *v, vo
     A.q_out = (uint16_t *)q_out; A.k_out = (uint16_t *)k_out;
     A.k_cache = (uint16_t *)k_cache; A.v_cache = (uint16_t *)v_cache;
     A.block_table = block_table; A.cu = cu_tokens; A.seq_lens = seq_lens; A.pos_base = pos_base;
-    A.positions = positions; A.pair_axis = pair_axis; A.num_axes = num_axes;
+    axes->positions = positions; axes->pair_axis = pair_axis; axes->num_axes = num_axes;
     A.q_gain = (const uint16_t *)q_gain; A.k_gain = (const uint16_t *)k_gain; A.inv_freq = inv_freq;
     A.q_stride = r->q_stride ? r->q_stride : Hq * D;
     A.k_stride = r->k_stride ? r->k_stride : Hkv * D;
@@ -157,10 +159,11 @@ int qf_rope_append(const void *q, const void *k, const void *v, void *q_out, voi
                    const qf_params *p, const qf_rope_params *r, void *cuda_stream)
 {
     qf::RopeArgs A = {};
+    qf::RopeAxes X = {};
     int sms = 0;
-    const int rc = qf_host::rope_args(&A, q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base,
+    const int rc = qf_host::rope_args(&A, &X, q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base,
                                       nullptr, nullptr, 0, q_gain, k_gain, inv_freq, p, r, &sms);
-    return rc != QF_OK ? rc : place(A, p, sms, cuda_stream);
+    return rc != QF_OK ? rc : place(A, X, p, sms, cuda_stream);
 }
 
 int qf_rope_append_axes(const void *q, const void *k, const void *v, void *q_out, void *k_out, void *k_cache, void *v_cache,
@@ -175,10 +178,11 @@ int qf_rope_append_axes(const void *q, const void *k, const void *v, void *q_out
         return rc0 != QF_OK ? rc0 : QF_ERR_NULL;
     }
     qf::RopeArgs A = {};
+    qf::RopeAxes X = {};
     int sms = 0;
-    const int rc = qf_host::rope_args(&A, q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, nullptr, positions,
+    const int rc = qf_host::rope_args(&A, &X, q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, nullptr, positions,
                                       pair_axis, num_axes, q_gain, k_gain, inv_freq, p, r, &sms);
-    return rc != QF_OK ? rc : place(A, p, sms, cuda_stream);
+    return rc != QF_OK ? rc : place(A, X, p, sms, cuda_stream);
 }
 
 int qf_rope_pair_axes(int32_t *pair_axis, int rotary_dim, const int32_t *sections, int num_axes, int interleaved)
@@ -239,12 +243,11 @@ int prompt(const void *q, const void *k_cache, const void *v_cache, const Scaled
     const qf::DevParams P = dev_params(p);
     qf::RowsArgs A = {};
     A.q = (const uint16_t *)q; A.k_cache = k_cache; A.v_cache = v_cache;
-    if (scaled) { A.k_scale = scaled->k_scale; A.v_scale = scaled->v_scale; }
     A.cu = cu_tokens; A.lens = seq_lens; A.table = block_table;
     A.out = (uint16_t *)out; A.lse = lse; A.status = (unsigned long long *)workspace;
     A.q_stride = q_stride ? q_stride : width;
     A.n_seq = p->batch; A.table_width = p->max_pages_per_req; A.max_tokens = std::min(P.max_tokens, kMostPositions); A.total_rows = total_tokens;
-    if (scaled) return launch_rows_scaled(A, P, p, scaled->kind, (char *)workspace, sms, (cudaStream_t)cuda_stream);
+    if (scaled) return launch_rows_scaled(A, P, p, *scaled, (char *)workspace, sms, (cudaStream_t)cuda_stream);
     return launch_rows<false>(A, P, p, (char *)workspace, sms, (cudaStream_t)cuda_stream);
 }
 }  // namespace qf_host

@@ -26,6 +26,7 @@
 
 #include <mutex>
 #include <stddef.h>
+#include <type_traits>
 
 #include "qf_common.cuh"
 #include "qf_page_math.cuh"
@@ -47,8 +48,6 @@ struct RopeArgs {
     const int *block_table, *cu, *seq_lens, *pos_base;
     const uint16_t *q_gain, *k_gain;
     const float *inv_freq;
-    const int *positions, *pair_axis; // several axes: [num_axes, T] and [rotary_dim / 2]; nullptr: positions follow from seq_lens
-    int num_axes;
     long long q_stride, k_stride, v_stride;
     int total_tokens, rotary_dim, interleaved;
     int rows;                         // head rows per token that this call touches
@@ -56,6 +55,13 @@ struct RopeArgs {
     int tokens_per_cta;               // 1, 2, 4 or 8
     float eps, rot_scale;
 };
+
+// Positions of several axes: [num_axes, T] and [rotary_dim / 2]; positions nullptr: they follow from seq_lens.
+struct RopeAxes {
+    const int *positions, *pair_axis;
+    int num_axes;
+};
+struct RopeNoAxes {};      // the kernel without them is to be what it would be if there were none
 
 // The request that owns packed token t: the last b with cu[b] <= t, if t < cu[b + 1]; -1 for a token of none.
 __device__ __forceinline__ int request_of(const int *__restrict__ cu, int batch, int t)
@@ -111,10 +117,11 @@ struct __align__(16) RopeStep {
     int slot[kRopeMaxTokens];            // slot within the page; -1: a token of no request
 };
 // With AXES, pair j turns by positions[pair_axis[j]][t] instead of t's place in its sequence: an image's tokens share one time
-// and have a row and a column each.  (A template argument, so that the calls without axes run the code they ran before.)
+// and have a row and a column each.
 static_assert(alignof(RopeStep) >= 16 && offsetof(RopeStep, turn) % 16 == 0, "two pairs of a turn are read as one float4");
 template <bool AXES>
-__device__ __forceinline__ void rope_prepare(RopeStep &st, const RopeArgs &A, const DevParams &P, int t0, int tokens)
+__device__ __forceinline__ void rope_prepare(RopeStep &st, const RopeArgs &A, const DevParams &P, const std::conditional_t<AXES, RopeAxes, RopeNoAxes> &X,
+                                             int t0, int tokens)
 {
     const int lane = threadIdx.x & 31;
     // lane k looks up token k, then all lanes turn its angle
@@ -140,21 +147,19 @@ __device__ __forceinline__ void rope_prepare(RopeStep &st, const RopeArgs &A, co
 #pragma unroll
     for (int i = 0; i < 2; ++i) f[i] = lane + 32 * i < pairs ? (double)A.inv_freq[lane + 32 * i] * 0.15915494309189533577 : 0.0;   // / (2 pi)
     const int *at[2] = {nullptr, nullptr};
-    if (AXES) {
+    if constexpr (AXES) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (lane + 32 * i < pairs) at[i] = A.positions + (long long)min(max(A.pair_axis[lane + 32 * i], 0), A.num_axes - 1) * A.total_tokens;
+            if (lane + 32 * i < pairs) at[i] = X.positions + (long long)min(max(X.pair_axis[lane + 32 * i], 0), X.num_axes - 1) * A.total_tokens;
     }
     for (int k = 0; k < tokens; ++k) {
-        double r = 0.0;
-        if (AXES) { if (t0 + k >= A.total_tokens) break; }
-        else r = (double)__shfl_sync(0xffffffffu, pos + base, k);
+        if (AXES && t0 + k >= A.total_tokens) break;
+        const double place = AXES ? 0.0 : (double)__shfl_sync(0xffffffffu, pos + base, k);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int j = lane + 32 * i;
             if (j >= pairs) continue;
-            if (AXES) r = (double)at[i][t0 + k];
-            const double turn = r * f[i];
+            const double turn = (AXES ? (double)at[i][t0 + k] : place) * f[i];
             float sn, cs;
             sincospif(2.f * (float)(turn - rint(turn)), &sn, &cs);
             st.turn[k][j] = make_float2(cs * A.rot_scale, sn * A.rot_scale);
@@ -169,7 +174,7 @@ __device__ __forceinline__ void copy_async_16(uint32_t dst, const void *src)
 
 template <bool INTERLEAVED, bool AXES>
 __global__ void __launch_bounds__(kRopeThreads + 32, kRopeCtasPerSm)
-rope_append_kernel(const __grid_constant__ RopeArgs A, const __grid_constant__ DevParams P)
+rope_append_kernel(const __grid_constant__ RopeArgs A, const __grid_constant__ DevParams P, const __grid_constant__ std::conditional_t<AXES, RopeAxes, RopeNoAxes> X)
 {
     __shared__ RopeStep steps[2];
     extern __shared__ __align__(16) uint4 ring[];        // [stage][row of the batch][thread]: a thread's own words
@@ -179,10 +184,10 @@ rope_append_kernel(const __grid_constant__ RopeArgs A, const __grid_constant__ D
     const int tokens = A.tokens_per_cta, stride = (int)gridDim.x * tokens;
     int t0 = (int)blockIdx.x * tokens;
     if (tid >= kRopeThreads) {      // the preparing warp: one step ahead
-        rope_prepare<AXES>(steps[0], A, P, t0, tokens);
+        rope_prepare<AXES>(steps[0], A, P, X, t0, tokens);
         __syncthreads();
         for (int n = 1; t0 < A.total_tokens; ++n, t0 += stride) {
-            if (t0 + stride < A.total_tokens) rope_prepare<AXES>(steps[n & 1], A, P, t0 + stride, tokens);
+            if (t0 + stride < A.total_tokens) rope_prepare<AXES>(steps[n & 1], A, P, X, t0 + stride, tokens);
             __syncthreads();
         }
         return;
@@ -326,26 +331,26 @@ rope_append_kernel(const __grid_constant__ RopeArgs A, const __grid_constant__ D
     }
 }
 
-inline cudaError_t launch_rope(const RopeArgs &A, const DevParams &P, unsigned blocks, cudaStream_t st)
+template <bool AXES>
+inline cudaError_t launch_rope(const RopeArgs &A, const std::conditional_t<AXES, RopeAxes, RopeNoAxes> &X, const DevParams &P, unsigned blocks,
+                               cudaStream_t st)
 {
     constexpr int kSmem = kRopeStages * kRopeBatch * kRopeThreads * (int)sizeof(uint4);
-    const bool axes = A.positions != nullptr;
-    auto kernel = axes ? (A.interleaved ? rope_append_kernel<true, true> : rope_append_kernel<false, true>)
-                       : (A.interleaved ? rope_append_kernel<true, false> : rope_append_kernel<false, false>);
+    auto kernel = A.interleaved ? rope_append_kernel<true, AXES> : rope_append_kernel<false, AXES>;
     {   // per-device kernel attribute, set once under a lock
         static std::mutex mu;
-        static bool done[4][64];
+        static bool done[2][64];
         int dev = 0;
         cudaGetDevice(&dev);
         std::lock_guard<std::mutex> lock(mu);
-        bool &d = done[(A.interleaved ? 1 : 0) + (axes ? 2 : 0)][dev & 63];
+        bool &d = done[A.interleaved ? 1 : 0][dev & 63];
         if (!d) {
             const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
             if (e != cudaSuccess) return e;
             d = true;
         }
     }
-    return launch_pdl(kernel, dim3(blocks), dim3(kRopeThreads + 32), kSmem, st, A, P);
+    return launch_pdl(kernel, dim3(blocks), dim3(kRopeThreads + 32), kSmem, st, A, P, X);
 }
 
 }  // namespace qf

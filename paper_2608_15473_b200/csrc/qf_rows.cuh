@@ -495,7 +495,7 @@ static __device__ QF_COLD void exchange_aside(uint32_t t_o, float *aside, bool h
 // written, gets those it sees.  A weight is positive, so an infinity stays one and two of opposite signs make a NaN.
 template <int KV>
 static __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P, const RowsBlock &b, int lim, int c0, int c1,
-                                   float *slot_base, int slot_row, size_t out_row)
+                                   float *slot_base, int slot_row, size_t out_row, KvScales<KV> scales)
 {
     const int common = min(b.off + b.i0 + 1, b.len);
 #pragma unroll 1
@@ -512,7 +512,7 @@ static __device__ QF_COLD void add_hidden(const RowsArgs &A, const DevParams &P,
             } else {
                 const float4 four = load_channels<KV>(A.v_cache, at_row + (d & ~3));
                 const float code = (d & 3) == 0 ? four.x : (d & 3) == 1 ? four.y : (d & 3) == 2 ? four.z : four.w;
-                bits = pack_bf16(code * A.v_scale[phys * P.num_kv_heads + b.head], 0.f) & 0xffffu;
+                bits = pack_bf16(code * scales.v[phys * P.num_kv_heads + b.head], 0.f) & 0xffffu;
             }
             if ((bits & 0x7f80u) != 0x7f80u) continue;
             const float x = __uint_as_float(bits << 16);
@@ -705,7 +705,7 @@ __device__ __forceinline__ void expand_quarter(uint32_t raw, uint32_t tile, int 
 template <bool PREFIX, int KV>
 __global__ void __launch_bounds__(kRowsThreads<KV>, 1)
 rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsArgs A, const __grid_constant__ DevParams P,
-            RowsRecord *__restrict__ records, float *__restrict__ asides, float *__restrict__ slots)
+            RowsRecord *__restrict__ records, float *__restrict__ asides, float *__restrict__ slots, KvScales<KV> scales)
 {
     extern __shared__ __align__(1024) uint8_t rows_smem[];
     RowsSmem<KV> &sm = *reinterpret_cast<RowsSmem<KV> *>(rows_smem);
@@ -988,7 +988,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                     const uint32_t full = smem_u32(&sm.raw.full[stage]);
                     const bool there = in && !bad;
                     const size_t scale_at = there ? (size_t)phys * Hkv + b.head : 0;      // a page that is not there has scale 0
-                    if (lane < kTilePages) copy_async_4(smem_u32(&sm.raw.scales[stage][lane]), (is_v ? A.v_scale : A.k_scale) + scale_at, there);
+                    if (lane < kTilePages) copy_async_4(smem_u32(&sm.raw.scales[stage][lane]), (is_v ? scales.v : scales.k) + scale_at, there);
                     const int at0 = !there ? none_c2 : P.kv_nhd ? phys * kPageSize : phys * Hkv + b.head;
                     int at[kTilePages];
 #pragma unroll
@@ -1510,7 +1510,7 @@ rows_kernel(const __grid_constant__ RowsMaps maps, const __grid_constant__ RowsA
                 }
                 finish(c, o);
             }
-            if (dirty && live && !empty) add_hidden<KV>(A, P, b, lim, c0, c1, slot_base, slot_row, out_row);
+            if (dirty && live && !empty) add_hidden<KV>(A, P, b, lim, c0, c1, slot_base, slot_row, out_row, scales);
             if (PREFIX) {
                 const bool mine = live && !empty && l == l;
                 if (__any_sync(0xffffffffu, mine && odd != odd)) mend_infinite(A, P, sm.info[slot], mine, c0, c1, slot_base, slot_row, out_row);
@@ -1713,7 +1713,7 @@ inline int make_rows_maps(RowsMaps *m, const RowsArgs &A, const DevParams &P, bo
 }
 
 template <bool PREFIX, int KV>
-cudaError_t launch_rows_kernels(const RowsMaps &maps, const RowsArgs &A, const DevParams &P, char *ws, int sms, cudaStream_t st)
+cudaError_t launch_rows_kernels(const RowsMaps &maps, const RowsArgs &A, const DevParams &P, KvScales<KV> scales, char *ws, int sms, cudaStream_t st)
 {
     {   // per-device kernel attribute, set once under a lock
         static std::mutex mu;
@@ -1731,7 +1731,7 @@ cudaError_t launch_rows_kernels(const RowsMaps &maps, const RowsArgs &A, const D
     RowsRecord *records = reinterpret_cast<RowsRecord *>(ws + L.record_off);
     float *asides = reinterpret_cast<float *>(ws + L.aside_off), *slots = reinterpret_cast<float *>(ws + L.slot_off);
     const int n = sms < kRowsMaxCtas ? sms : kRowsMaxCtas;
-    cudaError_t e = launch_pdl(rows_kernel<PREFIX, KV>, dim3(n), dim3(kRowsThreads<KV>), sizeof(RowsSmem<KV>), st, maps, A, P, records, asides, slots);
+    cudaError_t e = launch_pdl(rows_kernel<PREFIX, KV>, dim3(n), dim3(kRowsThreads<KV>), sizeof(RowsSmem<KV>), st, maps, A, P, records, asides, slots, scales);
     if (e != cudaSuccess) return e;
     return launch_pdl(rows_merge_kernel<PREFIX>, dim3(n, kRowsMergeParts), dim3(2 * kRowTile), 0, st, A, P,
                       (const RowsRecord *)records, (const float *)slots, n);

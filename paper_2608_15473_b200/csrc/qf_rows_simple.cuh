@@ -15,7 +15,6 @@ namespace qf {
 struct RowsArgs {
     const uint16_t *q;               // row r, query head h: q + r * q_stride + h * 128
     const void *k_cache, *v_cache;
-    const float *k_scale, *v_scale;  // of a scaled cache: [num_pages, Hkv]
     const int *cu, *lens, *table;    // [n_seq + 1], [n_seq], [n_seq, table_width] (nullptr: identity)
     uint16_t *out;                   // prompt: [rows, Hq, 128] bf16
     float *lse;                      // prompt: [rows, Hq]
@@ -71,7 +70,7 @@ constexpr int kRowsSimpleWarps = 8;
 // One warp per (row, query head), lane owns four channels, fp32 online softmax over the positions in order.
 template <bool PREFIX, int KV>
 __global__ void __launch_bounds__(kRowsSimpleWarps * 32)
-rows_simple_kernel(RowsArgs A, DevParams P)
+rows_simple_kernel(RowsArgs A, DevParams P, KvScales<KV> scales)
 {
     const int Hq = P.num_q_heads, lane = threadIdx.x & 31;
     const long long unit = (long long)blockIdx.x * kRowsSimpleWarps + (threadIdx.x >> 5);
@@ -105,7 +104,8 @@ rows_simple_kernel(RowsArgs A, DevParams P)
         }
         const size_t off = kv_row_offset(P, phys, c, i & 15) + lane * 4;
         const float4 k4 = load_channels<KV>(A.k_cache, off), v4 = load_channels<KV>(A.v_cache, off);
-        const float ks = KV == kKvBf16 ? 1.f : A.k_scale[phys * P.num_kv_heads + c], vs = KV == kKvBf16 ? 1.f : A.v_scale[phys * P.num_kv_heads + c];
+        float ks = 1.f, vs = 1.f;
+        if constexpr (KV != kKvBf16) { ks = scales.k[phys * P.num_kv_heads + c]; vs = scales.v[phys * P.num_kv_heads + c]; }
         float d = bf16lo_to_f32(qw.x) * k4.x;
         d = fmaf(bf16hi_to_f32(qw.x), k4.y, d);
         d = fmaf(bf16lo_to_f32(qw.y), k4.z, d);

@@ -69,15 +69,15 @@ int launch_sweep_scaled(const void *q, const void *k, const void *v, const Scale
                                                   ev1, msg, msg_len, launches, skip_finish);
 }
 
-int launch_rows_scaled(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *p, int kind, char *ws, int sms, cudaStream_t st)
+int launch_rows_scaled(const qf::RowsArgs &A, const qf::DevParams &P, const qf_params *p, const ScaledKv &s, char *ws, int sms, cudaStream_t st)
 {
-    const bool e4m3 = kind == qf::kKvE4m3;
+    const bool e4m3 = s.kind == qf::kKvE4m3;
     if (p->flags & QF_FLAG_SIMPLE_KERNEL) {
         const long long units = (long long)A.total_rows * P.num_q_heads;
         const long long blocks = (units + qf::kRowsSimpleWarps - 1) / qf::kRowsSimpleWarps;
         if (blocks > 0x7fffffffll) return QF_ERR_UNSUPPORTED;
-        if (e4m3) qf::rows_simple_kernel<false, qf::kKvE4m3><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
-        else qf::rows_simple_kernel<false, qf::kKvInt8><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P);
+        if (e4m3) qf::rows_simple_kernel<false, qf::kKvE4m3><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P, {s.k_scale, s.v_scale});
+        else qf::rows_simple_kernel<false, qf::kKvInt8><<<(unsigned)blocks, qf::kRowsSimpleWarps * 32, 0, st>>>(A, P, {s.k_scale, s.v_scale});
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return cuda_fail(e, "rows_simple_kernel launch");
         set_launches(1);
@@ -87,8 +87,8 @@ int launch_rows_scaled(const qf::RowsArgs &A, const qf::DevParams &P, const qf_p
     size_t len;
     char *msg = cuda_msg(&len);
     if (qf::make_rows_maps(&maps, A, P, true, msg, len)) return QF_ERR_CUDA;
-    const cudaError_t e = e4m3 ? qf::launch_rows_kernels<false, qf::kKvE4m3>(maps, A, P, ws, sms, st)
-                               : qf::launch_rows_kernels<false, qf::kKvInt8>(maps, A, P, ws, sms, st);
+    const cudaError_t e = e4m3 ? qf::launch_rows_kernels<false, qf::kKvE4m3>(maps, A, P, {s.k_scale, s.v_scale}, ws, sms, st)
+                               : qf::launch_rows_kernels<false, qf::kKvInt8>(maps, A, P, {s.k_scale, s.v_scale}, ws, sms, st);
     if (e != cudaSuccess) return cuda_fail(e, "rows_kernel launch");
     set_launches(2);
     return QF_OK;
@@ -108,14 +108,15 @@ int qf_rope_append_scaled(const void *q, const void *k, const void *v, void *q_o
     if ((k_cache || v_cache) && (!k_scale || !v_scale)) return refuse(p, QF_ERR_NULL);
     if (misaligned(k_scale, 4) || misaligned(v_scale, 4)) return refuse(p, QF_ERR_BAD_SHAPE);
     qf::RopeArgs A = {};
+    qf::RopeAxes X = {};
     int sms = 0;
-    const int rc = qf_host::rope_args(&A, q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base, positions,
+    const int rc = qf_host::rope_args(&A, &X, q, k, v, q_out, k_out, k_cache, v_cache, block_table, cu_tokens, seq_lens, pos_base, positions,
                                       pair_axis, num_axes, q_gain, k_gain, inv_freq, p, r, &sms);
     if (rc != QF_OK) return rc;
     const qf::DevParams P = qf_host::dev_params(p);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    const cudaError_t e = kv_type == QF_KV_E4M3 ? qf::launch_place_scaled<qf::kKvE4m3>(A, k_scale, v_scale, P, sms, st)
-                                                : qf::launch_place_scaled<qf::kKvInt8>(A, k_scale, v_scale, P, sms, st);
+    const cudaError_t e = kv_type == QF_KV_E4M3 ? qf::launch_place_scaled<qf::kKvE4m3>(A, X, k_scale, v_scale, P, sms, st)
+                                                : qf::launch_place_scaled<qf::kKvInt8>(A, X, k_scale, v_scale, P, sms, st);
     if (e != cudaSuccess) return qf_host::cuda_fail(e, "place_scaled_kernel launch");
     qf_host::set_launches(1);
     return QF_OK;

@@ -262,9 +262,7 @@ template <int KV> struct SweepScaled {
     int merge_entry, merge_head, merge_slot, merge_info;      // the range in red_acc: info = segments of its unit << 8 | round of heads
 };
 template <> struct SweepScaled<kKvBf16> {};
-template <int KV> struct SweepScales { const float *k, *v; };      // [num_pages, Hkv]
-template <> struct SweepScales<kKvBf16> {};
-static_assert(sizeof(SweepScaled<kKvBf16>) == 1 && sizeof(SweepScales<kKvBf16>) == 1, "empty for bf16");
+static_assert(sizeof(SweepScaled<kKvBf16>) == 1 && sizeof(KvScales<kKvBf16>) == 1, "empty for bf16");
 
 template <int G, int KV>
 struct SweepSmem {
@@ -294,7 +292,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
              float *__restrict__ o_part, float *__restrict__ m_part, float *__restrict__ lse_part,
              unsigned long long *__restrict__ header, const int *__restrict__ global_prefix,
              int4 *__restrict__ piece_info, float *__restrict__ seg, int seg_stride,
-             unsigned long long host_epoch, DevParams P, SweepScales<KV> scales)
+             unsigned long long host_epoch, DevParams P, KvScales<KV> scales)
 {
     constexpr int kPages = kPagesPerStage<KV>;
     extern __shared__ uint8_t smem_raw[];
@@ -921,7 +919,7 @@ inline unsigned long long next_epoch()
 }
 
 template <int G, int KV>
-int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, SweepScales<KV> scales, const void *q, const int32_t *bt,
+int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, KvScales<KV> scales, const void *q, const int32_t *bt,
                    const int32_t *sl, const int32_t *sr, float *o, float *m, float *l, const DevParams &P,
                    char *ws, const WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st,
                    cudaEvent_t ev0, cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish)
@@ -975,7 +973,7 @@ int launch_sweep_g(const CUtensorMap &kmap, const CUtensorMap &vmap, SweepScales
 
 // The kernel of the batch's group size, over either kind of cache.
 template <int KV, int G = 8>
-int launch_sweep_kv(const CUtensorMap &kmap, const CUtensorMap &vmap, SweepScales<KV> scales, const void *q,
+int launch_sweep_kv(const CUtensorMap &kmap, const CUtensorMap &vmap, KvScales<KV> scales, const void *q,
                     const int32_t *bt, const int32_t *sl, const int32_t *sr, float *o, float *m, float *l, const DevParams &P,
                     char *ws, const WorkspaceLayout &wsl, int n_ctas, unsigned long long epoch, cudaStream_t st,
                     cudaEvent_t ev0, cudaEvent_t ev1, char *msg, size_t msg_len, int *launches, bool skip_finish)
