@@ -252,7 +252,8 @@ int sweep(const void *q, const void *k_cache, const void *v_cache, const ScaledK
     // the request's shards (qf_merge_small.cuh) instead of the finish kernel and the merge kernel.
     const int n_ctas = sms < qf::kMaxSweepCtas ? sms : qf::kMaxSweepCtas;
     const bool small = step_out && step_lse && !(p->flags & QF_FLAG_NO_SMALL_MERGE) && p->out_shards == 0 &&
-                       qf::sweep_is_small(P, n_ctas, scaled ? qf::kPagesPerStage<qf::kKvE4m3> : qf::kPagesPerStage<qf::kKvBf16>);
+                       (scaled ? qf::sweep_is_small(P, n_ctas, qf::kPagesPerStage<qf::kKvE4m3>, qf::kSegmentCost<qf::kKvE4m3>)
+                               : qf::sweep_is_small(P, n_ctas, qf::kPagesPerStage<qf::kKvBf16>, qf::kSegmentCost<qf::kKvBf16>));
     int launches = 0;
     rc = scaled ? launch_sweep_scaled(q, k_cache, v_cache, *scaled, block_table, seq_lens, shard_ranges, o_part, m_part, lse_part,
                                       P, (char *)workspace, wsl, n_ctas, epoch, st, g_prof_start, g_prof_stop, g_cuda_msg,
