@@ -571,13 +571,15 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
         return;
     }
 
+    // A wait of the warps below ran out: nobody else may wait for this one's work (a merged state, a stage's copies) and see it missing.
+    [[maybe_unused]] auto give_up = [&]() { if (lane == 0) { sm.abort_flag = 1; epoch_or(header + kHdrStatus, epoch, kStatusTimeout); } };
     if constexpr (kMergers<G, KV> > 0) {
         const float kLn2 = 0.6931471805599453f;
         if (warp == kConsumerWarps + 1 + kIssuers<KV>) {
             // ============================ merging warp (scaled cache) ============================
             constexpr int RG = SweepSmem<G, KV>::kRoundHeads;
             for (uint32_t ph = 0;; ph ^= 1) {
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.scaled.merge_full), ph, abort_flag))) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.scaled.merge_full), ph, abort_flag))) { give_up(); break; }
                 if (sm.scaled.merge_entry < 0) break;
                 const int hr = sm.scaled.merge_info & 0xff, nseg = sm.scaled.merge_info >> 8;
                 const size_t out_row = out_entry(P, sm.scaled.merge_entry) * Hq + (size_t)sm.scaled.merge_head * G;
@@ -631,7 +633,7 @@ sweep_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ 
             const CUtensorMap *map = part ? &v_map : &k_map;
             const unsigned long long kv_policy = l2_evict_first_policy();
             for (int stage = 0, phase = 0;;) {
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.scaled.issue_bar[stage]), (uint32_t)phase, abort_flag))) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.scaled.issue_bar[stage]), (uint32_t)phase, abort_flag))) { give_up(); break; }
                 if (sm.meta[stage].entry < 0) break;
                 if (elect_one()) {      // one thread, with operands that are the same for the warp
                     const int np = sm.meta[stage].npages, y = P.kv_nhd ? sm.meta[stage].kv_head : 0;
