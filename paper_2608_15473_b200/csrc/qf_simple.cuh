@@ -66,8 +66,9 @@ sweep_simple_kernel(const uint16_t *__restrict__ q, const void *__restrict__ k_c
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
             const float sc = d * P.sm_scale * ks;
+            if (sc == neg_inf()) continue;           // weight 0 against any other score, and no maximum to begin with
             const float mn = max_nan(m[g], sc);      // NaN from the first NaN score on
-            const float alpha = __expf(m[g] - mn);   // m = -inf on the first token: e^{-inf} = 0
+            const float alpha = __expf(m[g] - mn);   // m = -inf until the first such score: e^{-inf} = 0
             const float p = __expf(sc - mn);
             l[g] = l[g] * alpha + p;
             const float pv = p * vs;

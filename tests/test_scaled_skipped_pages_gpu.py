@@ -84,3 +84,27 @@ def test_pages_whose_scores_are_minus_infinity(kind, flags, group, hkv, gone):
     ks[pg.table[:, bad].long().flatten().cuda()] = float("inf")
     got = run(pg, group, flags, pools=(kc, vc, ks, vs))
     check(pg, group, got, torch.tensor([i for i in range(pages * PAGE) if i // PAGE not in bad]))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("flags", KERNELS)
+@pytest.mark.parametrize("group,hkv", [(4, 2), (7, 2)])
+@pytest.mark.parametrize("gone", [[0], [0, 1, 2, 3], list(range(16))])
+def test_a_sweep_that_begins_with_scores_of_minus_infinity(kind, flags, group, hkv, gone):
+    pg = far_below(20, hkv, kind, B=40)
+    kc, vc, ks, vs = pg.device()
+    ks[pg.table[:, gone].long().flatten().cuda()] = float("inf")
+    got = run(pg, group, flags, pools=(kc, vc, ks, vs))
+    check(pg, group, got, torch.tensor([i for i in range(20 * PAGE) if i // PAGE not in gone]))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("flags", KERNELS)
+@pytest.mark.parametrize("group,hkv", [(4, 2), (7, 2)])
+def test_a_shard_whose_every_score_is_minus_infinity_is_empty(kind, flags, group, hkv):
+    pg = far_below(20, hkv, kind, B=3)
+    kc, vc, ks, vs = pg.device()
+    ks[:] = float("inf")
+    got = run(pg, group, flags, pools=(kc, vc, ks, vs))
+    assert (got["o"] == 0).all() and (got["out"] == 0).all()
+    assert all(torch.isneginf(got[n]).all() for n in ("m", "l", "lse"))
