@@ -22,8 +22,8 @@
 //
 // Bound: memory, with issue slots close behind.  Per page (4 KB) 290 warp instructions of all roles in e4m3 and 370 in int8,
 // counted over 32 requests of 16,384 tokens with four heads per group, where 6.5 TB/s leave an SM about 680 issue slots for
-// it.  Such a batch takes 167 us in e4m3 (6.4 TB/s) and 174 in int8; with one page per step, and one thread for all
-// copies, it took 237 and 253.
+// it.  Such a batch takes 167 to 181 us in e4m3 (6.4 to 5.9 TB/s) and 174 to 187 in int8 in short runs, 185 to 190 and 198 to 205 for
+// seconds on end, with one pool or several; with one page per step, and one thread for all copies, 237 and 253 (short runs).
 #pragma once
 
 #include "qf_common.cuh"

@@ -70,7 +70,8 @@ constexpr int kTilePages = kRowTile / kPageSize;
 constexpr int kUnit = 64;                        // positions of one product S = Q K^T and of one softmax pass
 // A scaled cache has four more warps, which expand tiles of codes to bf16 on their way into the ring, and two tiles of codes in
 // flight in the place of one in the ring.
-// (512 threads leave 128 registers each, enough for the softmax loop; moving registers to its warps with setmaxnreg cost time: the
+// (512 threads leave 128 registers each, where the bf16 kernel takes 158: the softmax loop fits, at 32 bytes of spill stores and 52 of
+// loads in all; moving registers to its warps with setmaxnreg cost time: the
 // bf16 form with 512 threads 1.90 ms without and 2.11 with it.)
 template <int KV> constexpr int kRowsThreads = (KV == kKvBf16 ? 12 : 16) * 32;
 template <int KV> constexpr int kRowsRing = KV == kKvBf16 ? 5 : 4;      // K and V tiles in flight or in use
@@ -83,6 +84,8 @@ constexpr int kRowsMaxCtas = 160;                // one per SM
 // tile of two row tiles 3,100 cycles and of one 2,100 to 2,600 (it reads as much K and V: HBM is what it waits for), and
 // what a block costs beside its tiles 5,800 and 3,700.  (7,500 and 5,000 when the units were chosen; 8, 5, 14 and 9, which
 // would fit better now, balance no better.)  A cut is not charged the second prologue and end that it causes.
+// All this is the bf16 kernel.  Over a scaled cache the same units are used, not measured again: expanding a tile costs there what
+// it costs whatever the rows, so a narrow tile is probably nearer to a wide one than 6 to 8.
 constexpr int kWideTileCost = 8, kNarrowTileCost = 6, kWideBlockCost = 18, kNarrowBlockCost = 12;
 constexpr int kMinSlice = 12;                    // less per CTA is not worth a merge
 constexpr int kWideSnap = 18, kNarrowSnap = 6;   // a cut this close to a block's border moves there

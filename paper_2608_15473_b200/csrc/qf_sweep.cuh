@@ -53,7 +53,7 @@ constexpr int kConsumerThreads = kConsumerWarps * 32;
 template <int KV> constexpr int kPagesPerStage = KV == kKvBf16 ? kConsumerWarps : 2 * kConsumerWarps;
 // A scaled cache's pages are half as long, so there are twice as many copies per byte, and one thread cannot issue them fast
 // enough: one more warp issues the copies of K, one those of V, from the places that the producer leaves in shared memory.
-// (The copies issued by a lane each: 248 us for 32 requests of 16,384 tokens, where this form takes 167.)
+// (The copies issued by a lane each: 248 us for 32 requests of 16,384 tokens, where this form took 167 in the same short runs.)
 template <int KV> constexpr int kIssuers = KV == kKvBf16 ? 0 : 2;
 // With up to four heads per group (one round of red_acc) one more warp merges the consumer warps' states at the end of a range, while
 // they go on with the next (256 requests of 500 tokens 76 -> 73 us; with two rounds the second waits for the first, 63 -> 65 us).
@@ -252,7 +252,7 @@ enum { kSegFirst = 1, kSegLast = 2 };
 
 // What only a scaled cache needs beside the rest.  Nothing for bf16, whose kernel is to be what it would be without these: with
 // the members in its shared memory, the scales among its parameters and the page's addresses formed before its rows, sweeps took
-// 0.15 to 0.3 % longer (one million tokens 606.5 us against 604.8); as it stands there is no difference to be seen (604.65 and 604.6).
+// 0.15 to 0.3 % longer (one million tokens 606.6 us against 604.9); as it stands there is no difference to be seen (604.65 and 604.6).
 template <int KV> struct SweepScaled {
     // of the stages' pages: scales, and where the issuing warps find them
     alignas(16) float scales[kStages][2][kPagesPerStage<KV>];
