@@ -389,7 +389,8 @@ int qf_rope_pair_axes(int32_t *pair_axis_host, int rotary_dim, const int32_t *se
  * [num_pages, Hkv].  Block tables, lengths, shards, states and statuses are what they are for the bf16 cache.
  *   QF_KV_E4M3   a code is an 8-bit float: 4 exponent bits, 3 mantissa bits, magnitudes up to 448, 0x7f and 0xff NaN
  *   QF_KV_INT8   a code is an integer, -128 to 127
- * The calls that read take any scale.  A NaN scale (or code) makes what it stands for NaN.  Pages with a table entry
+ * The calls that read take any finite scale, below zero too.  A NaN scale (or code) makes what it stands for NaN; an infinite scale
+ * stands for no numbers (scores and values under it come out infinite or NaN), and the call that writes never leaves one.  Pages with a table entry
  * outside [0, num_pages) are always skipped (their scales could not be read); QF_FLAG_CHECK_BOUNDS reports them.
  */
 enum { QF_KV_E4M3 = 1, QF_KV_INT8 = 2 };
